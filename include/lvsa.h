@@ -299,6 +299,107 @@ typedef struct lvsa_tensor {
   int64_t stride_token;
 } lvsa_tensor;
 
+/* ------------------------------------------------ rotary positions ---- */
+
+/* Element types of the calls below that take more than bf16. */
+#define LVSA_BF16 0
+#define LVSA_F16 1
+#define LVSA_F32 2
+
+/* Rotary positions over a latent grid: token i of the sequence (frame-major,
+ * i = (t * height + y) * width + x) has position (t, y, x), and the 64 pairs of
+ * a 128-element row are shared out among the axes: pairs 0 .. pairs[0]-1 turn
+ * with the frame t, the next pairs[1] with the row y, the next pairs[2] with the
+ * column x, any left over not at all.  Pair j, (a, b), becomes
+ *   (a cos - b sin, a sin + b cos)
+ * with the (cos, sin) that the table holds for the pair at its axis position.
+ * Tokens at or past frames*height*width (text tokens after the video) are not
+ * rotated.
+ *   layout PAIRS   pair j is elements (2j, 2j + 1)
+ *          HALVES  pair j is elements (j, j + 64)
+ *   table  device, 8-byte aligned, (cos, sin) in fp32:
+ *          [frames][pairs[0]], then [height][pairs[1]], then [width][pairs[2]];
+ *          any table works (lvsa_rope_table's, or a caller's own frequencies).
+ * frames, height, width >= 1, frames*height*width < 2^31, pairs >= 0 with
+ * 1 <= sum <= 64. */
+#define LVSA_ROPE_PAIRS 0
+#define LVSA_ROPE_HALVES 1
+typedef struct lvsa_rope {
+  int32_t frames;
+  int32_t height;
+  int32_t width;
+  int32_t pairs[3];
+  int32_t layout;
+  const float* table;
+} lvsa_rope;
+
+/* Entries (pairs of floats) of the table of *r, whose table pointer is not read:
+ * frames*pairs[0] + height*pairs[1] + width*pairs[2].  Errors: EINVAL. */
+lvsa_status lvsa_rope_table_size(const lvsa_rope* r, int64_t* entries);
+
+/* Fills host memory table[2 * capacity] (capacity in entries) with the usual
+ * frequencies: pair m of an axis with n pairs turns by pos * theta^(-m/n) at
+ * position pos.  Angles, cosines and sines are taken in fp64 and rounded once.
+ * r->table is not read.  Errors: EINVAL (ranges, nulls, theta not a positive
+ * finite number, capacity too small). */
+lvsa_status lvsa_rope_table(const lvsa_rope* r, double theta, float* table,
+                            int64_t capacity);
+
+/* ---------------------------------------------------- 8-bit K/V cache ---- */
+
+/* Keys and values of a sequence in device memory, held in 8 bits: a value is an
+ * e4m3 number (OCP FP8: 4 exponent bits, 3 mantissa bits, largest 448, no
+ * infinities) times the scale of its head and block of `block` tokens.  A
+ * scale is a power of two, the least 2^e with e >= -117 for which the largest
+ * finite magnitude of the block is at most 448 * 2^e, so that every held value
+ * is exactly a bf16 (and fp32) number; keys and values have scales of their own.
+ * e is at most 119: magnitudes above 448 * 2^119 (2.98e38) are held as that.
+ * What is not finite is held as NaN.
+ *   k        e4m3 [heads][capacity][128]
+ *   v        e4m3 [heads][capacity/64][128][64]: tiles of 64 tokens, transposed,
+ *            token 16a + 4b + r of a tile (a, b, r < 4) at place 16b + 4a + r
+ *   k_scale, v_scale   fp32 [heads][capacity/block]
+ * All contiguous, k and v 16-byte aligned.  Tokens 0 .. n_tokens-1 are held;
+ * what lies behind them is never used, whatever it is.  capacity is a multiple
+ * of 128, at most LVSA_MAX_CACHE_TOKENS; block is 64 or 128; heads <= 65535.
+ * The struct and the buffers are the caller's; a caller may lower n_tokens to
+ * drop the last tokens. */
+#define LVSA_MAX_CACHE_TOKENS (1 << 24)
+typedef struct lvsa_kv_cache {
+  int32_t heads;
+  int32_t capacity;
+  int32_t block;
+  int32_t n_tokens;
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+} lvsa_kv_cache;
+
+/* Quantises keys and values into tokens start .. start + n - 1 of the cache
+ * (n = k->n_tokens; 0 <= start <= cache->n_tokens, start + n <= capacity) and
+ * sets cache->n_tokens = max(cache->n_tokens, start + n).  k and v are
+ * [cache->heads, n, 128] of `dtype`.  rope (or NULL) rotates the keys on the
+ * way, token start + i at its grid position: the rotation is taken in fp64 and
+ * rounded to fp32 before the scale and the 8 bits.
+ * Blocks that the new tokens touch are written whole: their other held tokens
+ * keep the values they had, rounded again where the block's scale has grown;
+ * places behind the last token become zeros.  Blocks that they do not touch are
+ * left as they are.
+ * Errors: EINVAL (nulls, ranges, shapes), EUNSUPPORTED (layout, head_dim,
+ * capacity), EDEVICE (launch; n_tokens is then unchanged). */
+lvsa_status lvsa_kv_write(lvsa_kv_cache* cache, const lvsa_tensor* k,
+                          const lvsa_tensor* v, int32_t dtype, int32_t start,
+                          const lvsa_rope* rope, void* stream);
+
+/* Reads tokens start .. start + n - 1 (n = k->n_tokens, start + n <=
+ * cache->n_tokens) of keys and values back into k and v, [cache->heads, n, 128]
+ * of `dtype`; bf16 and fp32 hold every value exactly, fp16 rounds to nearest.
+ * Either of k, v may be NULL.  Errors as for lvsa_kv_write. */
+lvsa_status lvsa_kv_read(const lvsa_kv_cache* cache, int32_t start,
+                         lvsa_tensor* k, lvsa_tensor* v, int32_t dtype,
+                         void* stream);
+
 /* Tile counters.  The attention kernels run one persistent workgroup per
  * compute unit; workgroups take tiles (256 query rows of a head, or parts of
  * that) through atomic counters, eight per launch (one per XCD), so XCDs that
@@ -371,6 +472,51 @@ lvsa_status lvsa_attention_exact(const lvsa_tensor* q, const lvsa_tensor* k,
 lvsa_status lvsa_dense_attention(const lvsa_tensor* q, const lvsa_tensor* k,
                                  const lvsa_tensor* v, int32_t block,
                                  lvsa_tensor* out, void* stream);
+
+/* Rotates x [heads, n, 128] of `dtype`, whose token i is token start + i of the
+ * sequence (start >= 0), into out of the same shape and type.  fp32 arithmetic,
+ * one rounding.  out may be x itself (same strides), else must not overlap it.
+ * Errors: EINVAL (nulls, ranges, shapes), EUNSUPPORTED (layout, head_dim),
+ * EDEVICE (launch). */
+lvsa_status lvsa_rope_forward(const lvsa_tensor* x, int32_t dtype, int32_t start,
+                              const lvsa_rope* rope, lvsa_tensor* out,
+                              void* stream);
+
+/* Gradient of lvsa_rope_forward: the gradient of its output, grad_out, into that
+ * of its input, grad_in (the rotation by the opposite angles; the table is data).
+ * Arguments and errors as for lvsa_rope_forward. */
+lvsa_status lvsa_rope_backward(const lvsa_tensor* grad_out, int32_t dtype,
+                               int32_t start, const lvsa_rope* rope,
+                               lvsa_tensor* grad_in, void* stream);
+
+/* Attention of n query tokens (n = q->n_tokens >= 1) over the cache's tokens:
+ *   out[h, i] = sum_j softmax_j(q[h,i] . k[h/G,j] / sqrt(128)) v[h/G,j]
+ * with G = q->heads / cache->heads (a whole number: shared key heads), j over
+ * every held token (mask NULL) or, with a block CSR over the cache's tokens
+ * (mask->n_tokens = cache->n_tokens, mask->block 64 or 128 whatever the
+ * cache's block, at most 8000 blocks), over the held tokens of the key blocks
+ * kept for the query block (q_start + i) / mask->block: query i is then token
+ * q_start + i of the sequence, 0 <= q_start, q_start + n <= n_tokens.  Without
+ * a mask q_start is not used.  bf16 q and out; fp32 products and softmax;
+ * probabilities in bf16.  A query with no key gets zeros (an empty row, or an
+ * empty cache); keys and values that a query does not keep never reach it,
+ * whatever they are.  The mask's rules are lvsa_block_mask's.
+ * workspace: device memory, 16-byte aligned, of at least the bytes that
+ * lvsa_attention_cache_workspace gives for the same arguments (0: may be NULL);
+ * any content; written by the call, so calls that may overlap in time (two
+ * streams, two graphs) need one each.
+ * The result is deterministic for given shapes, mask and device.
+ * Errors: EINVAL (nulls, ranges, shape mismatch, workspace too small),
+ * EUNSUPPORTED (head_dim, block, alignment, strides, sizes), EDEVICE (launch). */
+lvsa_status lvsa_attention_cache(const lvsa_tensor* q, int32_t q_start,
+                                 const lvsa_kv_cache* cache,
+                                 const lvsa_block_mask* mask, lvsa_tensor* out,
+                                 void* workspace, int64_t workspace_bytes,
+                                 void* stream);
+lvsa_status lvsa_attention_cache_workspace(const lvsa_tensor* q, int32_t q_start,
+                                           const lvsa_kv_cache* cache,
+                                           const lvsa_block_mask* mask,
+                                           int64_t* bytes);
 
 #ifdef __cplusplus
 }

@@ -16,6 +16,11 @@ fallback.
     lvsa.attention_exact(q, k, v, ex.exact_mask(), out)  # Eq. 2 token for token
     m = lvsa.csr_mask(row_ptr, col_idx, n_tokens, block)  # any block CSR on the device
     lvsa.attention(q, k, v, m, out)
+    r = lvsa.Rope(121, 30, 52)                            # positions of a 121 x 30 x 52 grid
+    cache = lvsa.KvCache(heads=12, capacity=121 * 1560)   # 8-bit keys and values
+    q = lvsa.rope(q, r, start=n0)                         # new tokens n0, n0 + 1, ..
+    lvsa.kv_write(cache, k, v, start=n0, rope=r)          # keys rotated on the way
+    lvsa.attention_cache(q, cache)                        # over every token so far
 """
 import ctypes
 import os
@@ -26,7 +31,8 @@ __all__ = [
     "build_exact_mask_device", "csr_mask", "attention", "attention_noalloc",
     "attention_exact",
     "dense_attention", "WINDOW_BASIC", "WINDOW_ADAPTIVE", "WINDOW_EXPANDED",
-    "MAX_FRAMES",
+    "MAX_FRAMES", "Rope", "rope", "rope_backward", "KvCache", "kv_write", "kv_read",
+    "attention_cache", "ROPE_PAIRS", "ROPE_HALVES",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -34,6 +40,7 @@ LIB_PATH = os.path.join(_HERE, "liblvsa.so")
 
 WINDOW_BASIC, WINDOW_ADAPTIVE, WINDOW_EXPANDED = 0, 1, 2
 MAX_FRAMES = 4096
+ROPE_PAIRS, ROPE_HALVES = 0, 1
 OK, EINVAL, ENOMEM, EDEVICE, EUNSUPPORTED = 0, -1, -2, -3, -4
 
 _i32 = ctypes.c_int32
@@ -81,6 +88,16 @@ class _Tensor(ctypes.Structure):
     _fields_ = [("data", _p), ("heads", _i32), ("n_tokens", _i32),
                 ("head_dim", _i32), ("stride_head", _i64),
                 ("stride_token", _i64)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("frames", _i32), ("height", _i32), ("width", _i32), ("pairs", _i32 * 3),
+                ("layout", _i32), ("table", _p)]
+
+
+class _KvCache(ctypes.Structure):
+    _fields_ = [("heads", _i32), ("capacity", _i32), ("block", _i32), ("n_tokens", _i32),
+                ("k", _p), ("v", _p), ("k_scale", _p), ("v_scale", _p)]
 
 
 _LIB = None
@@ -132,6 +149,25 @@ def lib():
                                         _p]),
             "lvsa_dense_attention": (_i32, [ctypes.POINTER(_Tensor)] * 3 +
                                      [_i32, ctypes.POINTER(_Tensor), _p]),
+            "lvsa_rope_table_size": (_i32, [ctypes.POINTER(_Rope), ctypes.POINTER(_i64)]),
+            "lvsa_rope_table": (_i32, [ctypes.POINTER(_Rope), ctypes.c_double, _p, _i64]),
+            "lvsa_rope_forward": (_i32, [ctypes.POINTER(_Tensor), _i32, _i32,
+                                         ctypes.POINTER(_Rope), ctypes.POINTER(_Tensor), _p]),
+            "lvsa_rope_backward": (_i32, [ctypes.POINTER(_Tensor), _i32, _i32,
+                                          ctypes.POINTER(_Rope), ctypes.POINTER(_Tensor), _p]),
+            "lvsa_kv_write": (_i32, [ctypes.POINTER(_KvCache), ctypes.POINTER(_Tensor),
+                                     ctypes.POINTER(_Tensor), _i32, _i32,
+                                     ctypes.POINTER(_Rope), _p]),
+            "lvsa_kv_read": (_i32, [ctypes.POINTER(_KvCache), _i32, ctypes.POINTER(_Tensor),
+                                    ctypes.POINTER(_Tensor), _i32, _p]),
+            "lvsa_attention_cache": (_i32, [ctypes.POINTER(_Tensor), _i32,
+                                            ctypes.POINTER(_KvCache),
+                                            ctypes.POINTER(BlockMask),
+                                            ctypes.POINTER(_Tensor), _p, _i64, _p]),
+            "lvsa_attention_cache_workspace": (_i32, [ctypes.POINTER(_Tensor), _i32,
+                                                      ctypes.POINTER(_KvCache),
+                                                      ctypes.POINTER(BlockMask),
+                                                      ctypes.POINTER(_i64)]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -392,4 +428,218 @@ def dense_attention(q, k, v, block=128, out=None, stream=None):
     _check(lib().lvsa_dense_attention(ctypes.byref(tq), ctypes.byref(tk),
                                       ctypes.byref(tv), block, ctypes.byref(to),
                                       _stream_ptr(stream)), "lvsa_dense_attention")
+    return out
+
+
+# ------------------------------------------- rotary positions, 8-bit cache
+
+def _dtype_code(dtype):
+    import torch
+    codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    if dtype not in codes:
+        raise ValueError("expected bfloat16, float16 or float32")
+    return codes[dtype]
+
+
+def _on_device(t):
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError("expected a tensor on the current device")
+    return t
+
+
+def _rows(t):
+    """A [heads, n_tokens, head_dim] tensor on the current device; the strides of
+    axes of one element are put right, torch leaves them open."""
+    if t.dim() != 3:
+        raise ValueError("expected a [heads, n_tokens, head_dim] tensor")
+    if t.stride(2) != 1:
+        raise ValueError("head_dim must be contiguous")
+    _on_device(t)
+    H, n, d = t.shape
+    token = t.stride(1) if n > 1 else d
+    return _Tensor(t.data_ptr(), H, n, d, t.stride(0) if H > 1 else n * token, token)
+
+
+def _same_type(first, *others):
+    if any(t.dtype != first.dtype for t in others):
+        raise ValueError("expected tensors of one type")
+    return _dtype_code(first.dtype)
+
+
+def _on(stream):
+    """The context in which torch allocates for work on ``stream``."""
+    import contextlib
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
+class Rope:
+    """Rotary positions over a latent grid of ``frames`` x ``height`` x ``width``
+    tokens (lvsa_rope): ``pairs`` of the 64 pairs of a row turn with the frame,
+    the row and the column.  ``table``: a float32 device tensor [entries, 2] of
+    (cos, sin), frames first, then rows, then columns; built from ``theta``
+    (lvsa_rope_table) and put on ``device`` if not given."""
+
+    def __init__(self, frames, height, width, pairs=(22, 21, 21), theta=10000.0,
+                 layout=ROPE_PAIRS, table=None, device="cuda"):
+        import torch
+        self._c = _Rope(frames, height, width, (_i32 * 3)(*pairs), layout, None)
+        n = _i64()
+        _check(lib().lvsa_rope_table_size(ctypes.byref(self._c), ctypes.byref(n)),
+               "lvsa_rope_table_size")
+        if table is None:
+            host = torch.empty(n.value, 2, dtype=torch.float32)
+            _check(lib().lvsa_rope_table(ctypes.byref(self._c), theta, _p(host.data_ptr()),
+                                         n.value), "lvsa_rope_table")
+            table = host.to(device)
+        if (table.dtype != torch.float32 or not table.is_contiguous()
+                or table.numel() != 2 * n.value):
+            raise ValueError(f"expected a contiguous float32 table of {n.value} (cos, sin)")
+        self.table = table
+        self._c.table = table.data_ptr()
+
+
+def _rope_ref(r):
+    if r is None:
+        return None
+    _on_device(r.table)
+    return ctypes.byref(r._c)
+
+
+def _rotate(fn, x, r, start, out, stream):
+    import torch
+    with _on(stream):
+        if out is None:
+            out = torch.empty_like(x)
+        tx, to = _rows(x), _rows(out)
+        _check(getattr(lib(), fn)(ctypes.byref(tx), _same_type(x, out), start, _rope_ref(r),
+                                  ctypes.byref(to), _stream_ptr(stream)), fn)
+    return out
+
+
+def rope(x, r, start=0, out=None, stream=None):
+    """x [heads, n, 128] (bfloat16, float16, float32), token i of which is token
+    start + i of the grid, rotated by ``r`` (lvsa_rope_forward); out may be x."""
+    return _rotate("lvsa_rope_forward", x, r, start, out, stream)
+
+
+def rope_backward(grad, r, start=0, out=None, stream=None):
+    """Gradient of ``rope``: of its input, from that of its output
+    (lvsa_rope_backward); out may be grad."""
+    return _rotate("lvsa_rope_backward", grad, r, start, out, stream)
+
+
+class KvCache:
+    """Keys and values of a sequence held in 8 bits (lvsa_kv_cache): room for
+    ``capacity`` tokens (rounded up to 128) of ``heads`` key heads, one scale a
+    head and ``block`` tokens.  ``n_tokens`` are held; setting it lower drops the
+    last ones.  ``buffers``: the caller's own (k, v, k_scale, v_scale), as
+    lvsa_kv_cache lays them out; allocated if not given."""
+
+    def __init__(self, heads, capacity, block=128, n_tokens=0, buffers=None, device="cuda"):
+        import torch
+        capacity = -(-capacity // 128) * 128
+        f8, f32 = torch.float8_e4m3fn, torch.float32
+        shapes = [((heads, capacity, 128), f8), ((heads, capacity // 64, 128, 64), f8),
+                  ((heads, capacity // block), f32), ((heads, capacity // block), f32)]
+        if buffers is None:
+            buffers = [torch.empty(s, dtype=t, device=device) for s, t in shapes]
+        for b, (s, t) in zip(buffers, shapes, strict=True):
+            if tuple(b.shape) != s or b.dtype != t or not b.is_contiguous():
+                raise ValueError(f"expected a contiguous {t} buffer of shape {s}")
+        self.k, self.v, self.k_scale, self.v_scale = buffers
+        self._c = _KvCache(heads, capacity, block, 0, *(b.data_ptr() for b in buffers))
+        self.n_tokens = n_tokens
+
+    @property
+    def heads(self):
+        return self._c.heads
+
+    @property
+    def capacity(self):
+        return self._c.capacity
+
+    @property
+    def block(self):
+        return self._c.block
+
+    @property
+    def n_tokens(self):
+        return self._c.n_tokens
+
+    @n_tokens.setter
+    def n_tokens(self, n):
+        if not 0 <= n <= self._c.capacity:
+            raise ValueError(f"n_tokens must lie in 0 .. {self._c.capacity}")
+        self._c.n_tokens = n
+
+
+def _cache_ref(c):
+    for b in (c.k, c.v, c.k_scale, c.v_scale):
+        _on_device(b)
+    return ctypes.byref(c._c)
+
+
+def kv_write(cache, k, v, start=None, rope=None, stream=None):
+    """Quantises k and v [heads, n, 128] (bfloat16, float16, float32) into tokens
+    start, start + 1, .. of the cache (by default behind its last), the keys
+    rotated by ``rope`` on the way (lvsa_kv_write); returns the cache."""
+    tk, tv = _rows(k), _rows(v)
+    _check(lib().lvsa_kv_write(_cache_ref(cache), ctypes.byref(tk), ctypes.byref(tv),
+                               _same_type(k, v), cache.n_tokens if start is None else start,
+                               _rope_ref(rope), _stream_ptr(stream)), "lvsa_kv_write")
+    return cache
+
+
+def kv_read(cache, start=0, n=None, dtype=None, out=None, stream=None):
+    """Keys and values [heads, n, 128] of tokens start .. start + n - 1 (by default
+    to the last) in ``dtype`` (bfloat16 by default), or into ``out`` = (k, v)
+    (lvsa_kv_read); returns (k, v)."""
+    import torch
+    with _on(stream):
+        if out is None:
+            n = cache.n_tokens - start if n is None else n
+            if n < 1:
+                raise LvsaError(EINVAL, f"{n} tokens to read")
+            out = tuple(torch.empty(cache.heads, n, 128, dtype=dtype or torch.bfloat16,
+                                    device=cache.k.device) for _ in range(2))
+        k, v = out
+        tk, tv = _rows(k), _rows(v)
+        if tv.n_tokens != tk.n_tokens or (n is not None and tk.n_tokens != n):
+            raise ValueError("expected out tensors of n tokens")
+        if dtype is not None and k.dtype != dtype:
+            raise ValueError("expected out tensors of the given type")
+        _check(lib().lvsa_kv_read(_cache_ref(cache), start, ctypes.byref(tk), ctypes.byref(tv),
+                                  _same_type(k, v), _stream_ptr(stream)), "lvsa_kv_read")
+    return out
+
+
+def attention_cache(q, cache, mask=None, q_start=0, out=None, stream=None):
+    """Attention of q [heads, n, 128] (bfloat16; heads a multiple of the cache's)
+    over every held token, or over the blocks that ``mask`` (a BlockMask over the
+    cache's tokens) keeps for queries q_start, q_start + 1, ..
+    (lvsa_attention_cache); returns out."""
+    import torch
+    with _on(stream):
+        if out is None:
+            out = torch.empty_like(q)
+        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
+            raise ValueError("expected bfloat16 tensors")
+        tq, to = _rows(q), _rows(out)
+        c = _cache_ref(cache)
+        m = None if mask is None else ctypes.byref(mask)
+        need = _i64()
+        _check(lib().lvsa_attention_cache_workspace(ctypes.byref(tq), q_start, c, m,
+                                                    ctypes.byref(need)),
+               "lvsa_attention_cache_workspace")
+        work = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
+        _check(lib().lvsa_attention_cache(ctypes.byref(tq), q_start, c, m, ctypes.byref(to),
+                                          _p(work.data_ptr()) if need.value else None,
+                                          need.value, _stream_ptr(stream)),
+               "lvsa_attention_cache")
     return out

@@ -16,7 +16,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "liblvsa.so")
-SOURCES = ["api.cpp", "mask_host.cpp", "mask_device.hip", "attention.hip"]
+SOURCES = ["api.cpp", "api_cache.cpp", "mask_host.cpp", "mask_device.hip", "attention.hip",
+           "rope.hip", "kv_cache.hip", "attention_cache.hip"]
 ARCH = "gfx950"
 
 CFLAGS = [

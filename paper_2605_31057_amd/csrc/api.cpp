@@ -56,6 +56,16 @@ lvsa_status check_mask_shape(int32_t T, int32_t P, int32_t B, int32_t L) {
   return LVSA_OK;
 }
 
+lvsa_status check_tensor(const lvsa_tensor* t, int32_t heads, int32_t n) {
+  if (!t || !t->data) return LVSA_EINVAL;
+  if (t->heads != heads || t->n_tokens != n) return LVSA_EINVAL;
+  if (t->head_dim != 128) return LVSA_EUNSUPPORTED;
+  if (((uintptr_t)t->data) % 16 != 0) return LVSA_EUNSUPPORTED;
+  if (t->stride_token < 1 || t->stride_token % 8 != 0) return LVSA_EUNSUPPORTED;
+  if (t->stride_head < 0 || t->stride_head % 8 != 0) return LVSA_EUNSUPPORTED;
+  return LVSA_OK;
+}
+
 // Tile-counter pool (lvsa.h, "Tile counters").  Per device: sets of
 // kTileCounters 64-bit words in chunks of device memory.  An eager launch
 // takes a set whose event (recorded behind the set's last launch) has
@@ -534,16 +544,6 @@ lvsa_status lvsa_build_exact_mask_device(int32_t T, int32_t P, int32_t B,
 }
 
 namespace {
-
-lvsa_status check_tensor(const lvsa_tensor* t, int32_t heads, int32_t n) {
-  if (!t || !t->data) return LVSA_EINVAL;
-  if (t->heads != heads || t->n_tokens != n) return LVSA_EINVAL;
-  if (t->head_dim != 128) return LVSA_EUNSUPPORTED;
-  if (((uintptr_t)t->data) % 16 != 0) return LVSA_EUNSUPPORTED;
-  if (t->stride_token < 1 || t->stride_token % 8 != 0) return LVSA_EUNSUPPORTED;
-  if (t->stride_head < 0 || t->stride_head % 8 != 0) return LVSA_EUNSUPPORTED;
-  return LVSA_OK;
-}
 
 // Checks the tensors against (N, B, nb) and fills the launch arguments
 // except the mask and the counters.

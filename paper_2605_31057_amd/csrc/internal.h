@@ -88,4 +88,44 @@ struct CounterLease {
 lvsa_status acquire_counters(hipStream_t stream, CounterLease* lease);
 void release_counters(const CounterLease& lease, hipStream_t stream);
 
+// Checks one attention tensor: [heads, n, 128], 16-byte aligned rows.
+lvsa_status check_tensor(const lvsa_tensor* t, int32_t heads, int32_t n);
+
+// Rotary positions (rope.hip): x and y are [heads, n, 128] of `dtype`, strides in
+// elements; sign +1 forward, -1 for the gradient.
+struct RopeArgs;
+hipError_t launch_rope(const RopeArgs& r, const lvsa_tensor& x, const lvsa_tensor& y,
+                       int32_t dtype, int32_t start, float sign, hipStream_t stream);
+
+// Cache write and read (kv_cache.hip).  `rope.table` null: keys as they are.  `held`:
+// the tokens held before the write.
+hipError_t launch_kv_write(const lvsa_kv_cache& c, int32_t held, const lvsa_tensor& k,
+                           const lvsa_tensor& v, int32_t dtype, int32_t start,
+                           const RopeArgs& rope, hipStream_t stream);
+hipError_t launch_kv_read(const lvsa_kv_cache& c, int32_t start, const lvsa_tensor* k,
+                          const lvsa_tensor* v, int32_t n, int32_t dtype, hipStream_t stream);
+
+// Attention over the cache (attention_cache.hip).  Strides in elements; row_ptr
+// null: every held token.
+struct CacheAttnArgs {
+  const void* q;
+  void* o;
+  int64_t q_sh, q_st, o_sh, o_st;
+  int32_t heads, group;           // key heads, query heads of each
+  int32_t n, q_start;             // query tokens, and the first one's place
+  int32_t n_tokens, capacity;     // held tokens, places of a head
+  int32_t scale_shift;            // log2 of the cache's block
+  const uint8_t* k;
+  const uint8_t* v;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* row_ptr;
+  const int32_t* col_idx;
+  int32_t mask_block, mask_blocks;
+  float* workspace;
+};
+// Bytes of workspace of that launch on a device of `cus` compute units.
+int64_t cache_attention_workspace(const CacheAttnArgs& a, int32_t cus);
+hipError_t launch_cache_attention(const CacheAttnArgs& a, int32_t cus, hipStream_t stream);
+
 }  // namespace lvsa

@@ -1,0 +1,276 @@
+// kv_cache.hip -- writing keys and values into the 8-bit cache, and reading them back.
+//
+// A block of B tokens of a head holds x as e4m3(x / 2^e) with one e (lvsa.h).
+// Dividing by a power of two is exact, so the only rounding is the one to e4m3, a
+// held value is exact in bf16, and raising e rounds again only what falls below
+// e4m3's normal range.  V is held transposed in tiles of 64 tokens: the attention
+// product P V then takes 16 bytes of consecutive k-slots a lane (lvsa.h's order of
+// places is that of the accumulator registers that hold P).
+//
+// Bound: memory; 2 * sizeof(T) bytes read and 2 written per element pair.
+// One workgroup a block, head and tensor (K or V): the block's values stay in
+// registers between the maximum and the rounding, so they are read once.
+#include "values.h"
+
+namespace lvsa {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int ROWS = THREADS / 8;   // rows a pass: eight threads a row (values.h)
+constexpr int LDS_ROW = 136;        // bytes of a token's row in LDS, 8 more than its 128
+
+struct WriteArgs {
+  lvsa_kv_cache c;                  // n_tokens: held before
+  const void* k;
+  const void* v;
+  int64_t k_sh, k_st, v_sh, v_st;
+  int32_t start, n, first_block;
+};
+
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a < __builtin_inff() ? a : 0.f;   // NaN compares false
+}
+
+// Largest of x over the workgroup.
+__device__ __forceinline__ float block_max(float x, float* lds) {
+#pragma unroll
+  for (int off = 32; off > 0; off /= 2) x = fmaxf(x, __shfl_xor(x, off));
+  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
+  __syncthreads();
+  return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+}
+
+template <typename T, int B>
+__global__ __launch_bounds__(THREADS) void write_kernel(WriteArgs a, RopeArgs r) {
+  constexpr int PASSES = B / ROWS;
+  __shared__ float most_lds[4];
+  __shared__ __attribute__((aligned(16))) uint8_t bytes[B * LDS_ROW];
+  const int block = a.first_block + blockIdx.x;
+  const int64_t head = blockIdx.y;
+  const bool is_v = blockIdx.z != 0;
+  const int row = threadIdx.x / 8, c = threadIdx.x % 8;
+  const lvsa_kv_cache& m = a.c;
+  const int64_t base = head * m.capacity;              // the head's first place
+  float* const scale = (is_v ? m.v_scale : m.k_scale) + base / B + block;
+  const float old_scale = *scale;
+  const T* const src = is_v ? (const T*)a.v + head * a.v_sh : (const T*)a.k + head * a.k_sh;
+  const int64_t st = is_v ? a.v_st : a.k_st;
+
+  // The block's values: new tokens, held ones, zeros behind the last.
+  float lo[PASSES][8], hi[PASSES][8];
+  float most = 0.f;
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int32_t token = block * B + p * ROWS + row;
+    const int32_t i = token - a.start;
+    if (i >= 0 && i < a.n) {
+      load8(src + i * st + 8 * c, lo[p]);
+      load8(src + i * st + 64 + 8 * c, hi[p]);
+      if (!is_v && r.table) {
+        f32x2 cs[8];
+        load_turns(r, token, c, cs);
+        rotate16<double>(lo[p], hi[p], cs, r.halves, 1.f);
+      }
+    } else if (token < m.n_tokens) {
+      uint32_t w[4];
+      if (!is_v) {
+        const uint8_t* k = (const uint8_t*)m.k + (base + token) * 128 + 8 * c;
+        w[0] = *(const uint32_t*)k, w[1] = *(const uint32_t*)(k + 4);
+        w[2] = *(const uint32_t*)(k + 64), w[3] = *(const uint32_t*)(k + 68);
+      } else {
+        const uint8_t* v = (const uint8_t*)m.v + (base / 64 + token / 64) * 8192 +
+                           (8 * c) * 64 + v_place(token % 64);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint8_t* e = v + ((j & 1) * 4 + (j >> 1) * 64) * 64;
+          w[j] = e[0] | e[64] << 8 | e[128] << 16 | (uint32_t)e[192] << 24;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float x[4];
+        from_e4m3(w[j], x);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) (j < 2 ? lo[p] : hi[p])[4 * (j & 1) + b] = x[b] * old_scale;
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < 8; ++b) lo[p][b] = hi[p][b] = 0.f;
+    }
+#pragma unroll
+    for (int b = 0; b < 8; ++b)
+      most = fmaxf(most, fmaxf(finite_abs(lo[p][b]), finite_abs(hi[p][b])));
+  }
+  // Every held value has been read when the first one is overwritten: the barrier of
+  // the maximum comes between.
+  const int e = scale_exponent(block_max(most, most_lds));
+  const float inv = pow2(-e);
+  if (threadIdx.x == 0) *scale = pow2(e);
+  auto word = [&](const float (&x)[8], int j) {
+    float y[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const float z = x[4 * j + b];
+      const float in = __builtin_amdgcn_fmed3f(z * inv, -448.f, 448.f);   // e = 119 only
+      y[b] = fabsf(z) < __builtin_inff() ? in : __builtin_nanf("");
+    }
+    return to_e4m3(y[0], y[1], y[2], y[3]);
+  };
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const u32x2 wl = {word(lo[p], 0), word(lo[p], 1)}, wh = {word(hi[p], 0), word(hi[p], 1)};
+    if (is_v) {
+      uint8_t* const to = bytes + (p * ROWS + row) * LDS_ROW + 8 * c;
+      *(u32x2*)to = wl;
+      *(u32x2*)(to + 64) = wh;
+    } else {
+      uint8_t* const to = (uint8_t*)m.k + (base + block * B + p * ROWS + row) * 128 + 8 * c;
+      *(u32x2*)to = wl;
+      *(u32x2*)(to + 64) = wh;
+    }
+  }
+  if (!is_v) return;
+  __syncthreads();
+  // V: four elements d and 16 tokens a thread, transposed four bytes by four.
+  for (int at = threadIdx.x; at < B / 64 * 128; at += THREADS) {
+    const int tile = at / 128, dq = at % 128 / 4, g = at % 4;
+    u32x4 out[4];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        w[j] = *(const uint32_t*)(bytes + (tile * 64 + 16 * kt + 4 * g + j) * LDS_ROW + 4 * dq);
+      transpose4(w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[j][kt] = w[j];
+    }
+    uint8_t* const to = (uint8_t*)m.v + (base / 64 + block * (B / 64) + tile) * 8192 +
+                        4 * dq * 64 + 16 * g;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *(u32x4*)(to + 64 * j) = out[j];
+  }
+}
+
+struct ReadArgs {
+  lvsa_kv_cache c;
+  void* k;
+  void* v;
+  int64_t k_sh, k_st, v_sh, v_st;
+  int32_t start, n, first_tile;
+};
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float (&x)[4]) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  t4 a;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = (T)x[i];
+  *(t4*)p = a;
+}
+
+// One workgroup a tile of 64 tokens, head and tensor.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void read_kernel(ReadArgs a) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const int tile = a.first_tile + blockIdx.x;
+  const int64_t head = blockIdx.y;
+  const lvsa_kv_cache& m = a.c;
+  const int64_t base = head * m.capacity;
+  const bool is_v = a.k == nullptr || blockIdx.z != 0;
+  const float scale =
+      (is_v ? m.v_scale : m.k_scale)[base / m.block + (int64_t)tile * 64 / m.block];
+  if (!is_v) {
+    T* const out = (T*)a.k + head * a.k_sh;
+    for (int at = threadIdx.x; at < 64 * 32; at += THREADS) {
+      const int token = tile * 64 + at / 32, i = token - a.start;
+      if (i < 0 || i >= a.n) continue;
+      float x[4];
+      from_e4m3(*(const uint32_t*)((const uint8_t*)m.k + (base + token) * 128 + at % 32 * 4), x);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) x[b] *= scale;
+      store4(out + i * a.k_st + at % 32 * 4, x);
+    }
+    return;
+  }
+  // V: four elements d and 16 tokens a thread.
+  T* const out = (T*)a.v + head * a.v_sh;
+  if (threadIdx.x >= 128) return;
+  const int dq = threadIdx.x % 32, g = threadIdx.x / 32;
+  const uint8_t* const from =
+      (const uint8_t*)m.v + (base / 64 + tile) * 8192 + 4 * dq * 64 + 16 * g;
+  u32x4 in[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) in[j] = *(const u32x4*)(from + 64 * j);
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt) {
+    uint32_t w[4] = {in[0][kt], in[1][kt], in[2][kt], in[3][kt]};
+    transpose4(w);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = tile * 64 + 16 * kt + 4 * g + j - a.start;
+      if (i < 0 || i >= a.n) continue;
+      float x[4];
+      from_e4m3(w[j], x);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) x[b] *= scale;
+      store4(out + i * a.v_st + 4 * dq, x);
+    }
+  }
+}
+
+template <typename T>
+void start_write(const WriteArgs& a, const RopeArgs& r, dim3 grid, hipStream_t s) {
+  if (a.c.block == 64)
+    write_kernel<T, 64><<<grid, THREADS, 0, s>>>(a, r);
+  else
+    write_kernel<T, 128><<<grid, THREADS, 0, s>>>(a, r);
+}
+
+}  // namespace
+
+hipError_t launch_kv_write(const lvsa_kv_cache& c, int32_t held, const lvsa_tensor& k,
+                           const lvsa_tensor& v, int32_t dtype, int32_t start,
+                           const RopeArgs& rope, hipStream_t stream) {
+  WriteArgs a;
+  a.c = c;
+  a.c.n_tokens = held;
+  a.k = k.data, a.v = v.data;
+  a.k_sh = k.stride_head, a.k_st = k.stride_token;
+  a.v_sh = v.stride_head, a.v_st = v.stride_token;
+  a.start = start, a.n = k.n_tokens;
+  a.first_block = start / c.block;
+  const int32_t last = (start + k.n_tokens - 1) / c.block;
+  const dim3 grid((uint32_t)(last - a.first_block + 1), (uint32_t)c.heads, 2);
+  if (dtype == LVSA_BF16)
+    start_write<__bf16>(a, rope, grid, stream);
+  else if (dtype == LVSA_F16)
+    start_write<_Float16>(a, rope, grid, stream);
+  else
+    start_write<float>(a, rope, grid, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const lvsa_kv_cache& c, int32_t start, const lvsa_tensor* k,
+                          const lvsa_tensor* v, int32_t n, int32_t dtype, hipStream_t stream) {
+  ReadArgs a = {};
+  a.c = c;
+  if (k) a.k = k->data, a.k_sh = k->stride_head, a.k_st = k->stride_token;
+  if (v) a.v = v->data, a.v_sh = v->stride_head, a.v_st = v->stride_token;
+  a.start = start, a.n = n;
+  a.first_tile = start / 64;
+  const int32_t last = (start + n - 1) / 64;
+  const dim3 grid((uint32_t)(last - a.first_tile + 1), (uint32_t)c.heads, k && v ? 2 : 1);
+  if (dtype == LVSA_BF16)
+    read_kernel<__bf16><<<grid, THREADS, 0, stream>>>(a);
+  else if (dtype == LVSA_F16)
+    read_kernel<_Float16><<<grid, THREADS, 0, stream>>>(a);
+  else
+    read_kernel<float><<<grid, THREADS, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace lvsa

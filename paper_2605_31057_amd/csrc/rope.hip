@@ -1,0 +1,72 @@
+// rope.hip -- rotary positions over a latent grid, and their gradient.
+//
+// y = R x with R a 2x2 rotation per pair of elements (lvsa.h); the gradient of x is
+// R^T times that of y, the same kernel with the angles' signs turned.
+//
+// Bound: memory, 2 * 128 * sizeof(T) bytes a row against 3 operations an element.
+// Eight threads work a row (values.h) and keep the (cos, sin) of their eight pairs in
+// registers over several heads, so the table, 64 bytes a thread, is read once
+// for all of them and not once a row, where it would be as many bytes as the rows.
+#include "values.h"
+
+namespace lvsa {
+namespace {
+
+constexpr int THREADS = 256;
+
+struct RopeTensors {
+  const void* x;
+  void* y;
+  int64_t x_sh, x_st, y_sh, y_st;
+  int32_t heads, n, start, per;   // per: heads a thread works
+  float sign;
+};
+
+template <typename T>
+__global__ __launch_bounds__(THREADS) void rope_kernel(RopeTensors t, RopeArgs r) {
+  const int64_t id = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  const int64_t i = id / 8;
+  const int c = (int)(id % 8);
+  if (i >= t.n) return;
+  f32x2 cs[8];
+  load_turns(r, t.start + (int32_t)i, c, cs);
+  const int h0 = blockIdx.y * t.per, h1 = min(h0 + t.per, t.heads);
+  for (int h = h0; h < h1; ++h) {
+    const T* x = (const T*)t.x + h * t.x_sh + i * t.x_st + 8 * c;
+    T* y = (T*)t.y + h * t.y_sh + i * t.y_st + 8 * c;
+    float lo[8], hi[8];
+    load8(x, lo);
+    load8(x + 64, hi);
+    rotate16<float>(lo, hi, cs, r.halves, t.sign);
+    store8(y, lo);
+    store8(y + 64, hi);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs& r, const lvsa_tensor& x, const lvsa_tensor& y,
+                       int32_t dtype, int32_t start, float sign, hipStream_t stream) {
+  RopeTensors t;
+  t.x = x.data;
+  t.y = y.data;
+  t.x_sh = x.stride_head, t.x_st = x.stride_token;
+  t.y_sh = y.stride_head, t.y_st = y.stride_token;
+  t.heads = x.heads, t.n = x.n_tokens, t.start = start, t.sign = sign;
+  // Heads a thread: all of them where the tokens alone fill the chip (2048 threads on
+  // each of 256 compute units), one where they are few.
+  const int64_t threads = (int64_t)x.n_tokens * 8;
+  const int64_t groups = (2048 * 256 + threads - 1) / threads;
+  t.per = groups >= x.heads ? 1 : (int32_t)((x.heads + groups - 1) / groups);
+  const dim3 grid((uint32_t)((threads + THREADS - 1) / THREADS),
+                  (uint32_t)((x.heads + t.per - 1) / t.per));
+  if (dtype == LVSA_BF16)
+    rope_kernel<__bf16><<<grid, THREADS, 0, stream>>>(t, r);
+  else if (dtype == LVSA_F16)
+    rope_kernel<_Float16><<<grid, THREADS, 0, stream>>>(t, r);
+  else
+    rope_kernel<float><<<grid, THREADS, 0, stream>>>(t, r);
+  return hipGetLastError();
+}
+
+}  // namespace lvsa

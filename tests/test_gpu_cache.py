@@ -1,0 +1,632 @@
+"""Rotary positions, the 8-bit K/V cache and the attention over it on the GPU,
+against their plain forms in 64 bits (oracle/cache.py)."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_31057_amd as L
+from oracle import cache as OC
+from oracle import mask as M
+
+pytestmark = pytest.mark.gpu
+
+BF, HF, SF = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    L.lib()
+
+
+def _say(*a):
+    print("[cache]", *a, flush=True)
+    sys.stdout.flush()
+
+
+def _randn(shape, seed, dtype=BF, layout="hnd", scale=1.0):
+    """[heads, n, 128] on the GPU; nhd: a view of one [n, 3, heads, 128] buffer."""
+    g = torch.Generator().manual_seed(seed)
+    H, n, _ = shape
+    if layout == "nhd":
+        x = torch.randn(n, 3, H, 128, generator=g) * scale
+        return x.to(dtype).cuda()[:, 1].transpose(0, 1)
+    return (torch.randn(H, n, 128, generator=g) * scale).to(dtype).cuda()
+
+
+def _wide(t):
+    return t.detach().cpu().double().numpy()
+
+
+# ------------------------------------------------------------- rotary
+
+def _turns(r, grid, pairs, start, n):
+    return OC.token_turns(grid, pairs, _wide(r.table.view(-1, 2)), range(start, start + n))
+
+
+def _assert_rotated(got, x, cos, sin, halves):
+    """fp32: the smaller product is rounded, then their sum; then the type's own
+    rounding, half a step (and half its subnormal step for fp16)."""
+    want = OC.rotate(x, cos, sin, halves)
+    inner = OC.rotate(np.abs(x), cos * 0, np.abs(sin), halves)      # |b s|
+    inner = np.maximum(np.abs(inner), np.abs(OC.rotate(np.abs(x), np.abs(cos), sin * 0, halves)))
+    step = torch.finfo(got.dtype).eps / 2
+    tol = (np.abs(want) + inner) * (2.0 ** -23 + step * 2.0 ** -20) + np.abs(want) * step
+    tol += 2.0 ** -25 if got.dtype == HF else 2.0 ** -149
+    err = np.abs(_wide(got) - want)
+    assert (err <= tol).all(), (err / tol).max()
+
+
+ROPES = [
+    # H, n, (T, h, w), pairs, start, halves, dtype, layout
+    (1, 1, (1, 1, 1), (22, 21, 21), 0, False, BF, "hnd"),
+    (3, 1, (5, 4, 7), (22, 21, 21), 139, True, SF, "nhd"),
+    (2, 33, (5, 4, 7), (22, 21, 21), 100, False, HF, "hnd"),    # past the grid's 140 tokens
+    (2, 70, (3, 5, 9), (16, 24, 24), 120, True, BF, "nhd"),
+    (4, 257, (2, 16, 16), (8, 12, 12), 250, False, SF, "hnd"),  # 32 pairs: half unrotated
+    (1, 300, (300, 1, 1), (64, 0, 0), 0, True, HF, "hnd"),      # one axis
+    (40, 31, (7, 3, 2), (0, 40, 24), 4, False, BF, "hnd"),
+    (2, 9, (4096, 30, 52), (22, 21, 21), 4096 * 1560 - 5, False, SF, "hnd"),
+]
+
+
+@pytest.mark.parametrize("case", ROPES)
+def test_rope_and_its_gradient(case):
+    H, n, grid, pairs, start, halves, dtype, layout = case
+    _say("rope", case)
+    r = L.Rope(*grid, pairs=pairs, layout=L.ROPE_HALVES if halves else L.ROPE_PAIRS)
+    x = _randn((H, n, 128), 5, dtype, layout)
+    cos, sin = _turns(r, grid, pairs, start, n)
+    _assert_rotated(L.rope(x, r, start=start), _wide(x), cos, sin, halves)
+    _assert_rotated(L.rope_backward(x, r, start=start), _wide(x), cos, -sin, halves)
+    # in place, and into rows of a wider buffer
+    y = x.clone()
+    wide = torch.full((n, H, 160), 3.0, dtype=dtype, device="cuda")
+    out = wide[:, :, :128].transpose(0, 1)
+    want = L.rope(x, r, start=start)
+    assert L.rope(y, r, start=start, out=y) is y
+    L.rope(x, r, start=start, out=out)
+    assert torch.equal(y, want) and torch.equal(out, want)
+    assert (wide[:, :, 128:] == 3.0).all()
+
+
+@pytest.mark.parametrize("halves", [False, True])
+def test_rope_gradient_against_differences(halves):
+    """L(x) = <w, rope(x)>: (L(x + d) - L(x - d)) / 2 = <rope_backward(w), d>, the map
+    being linear; fp32 roundings of every term bound the difference."""
+    H, n, grid = 2, 50, (4, 3, 5)
+    r = L.Rope(*grid, layout=L.ROPE_HALVES if halves else L.ROPE_PAIRS)
+    x, w, d = (_randn((H, n, 128), s, SF) for s in (1, 2, 3))
+    hi, lo = (_wide(L.rope(y, r, start=20)) for y in (x + d, x - d))
+    num = (_wide(w) * (hi - lo)).sum() / 2
+    ana = (_wide(L.rope_backward(w, r, start=20)) * _wide(d)).sum()
+    size = (np.abs(_wide(w)) * (np.abs(hi) + np.abs(lo) + 3 * np.abs(_wide(x)) +
+                                3 * np.abs(_wide(d)))).sum()
+    assert abs(num - ana) <= size * 2.0 ** -21
+    # and back again: the rotation by the opposite angle
+    y = L.rope_backward(L.rope(x, r, start=7), r, start=7)
+    assert np.abs(_wide(y) - _wide(x)).max() <= 4 * 2.0 ** -23 * np.abs(_wide(x)).max() * 2
+
+
+# -------------------------------------------------------------- cache
+
+def _held(c):
+    """(k, v) of the held tokens as float64, from the buffers by the documented
+    layout."""
+    n, B = c.n_tokens, c.block
+    k = c.k.float().cpu().double().numpy()
+    tok = np.arange(c.capacity) % 64
+    place = (tok // 4 % 4) * 16 + tok // 16 * 4 + tok % 4
+    tiles = c.v.float().cpu().double().numpy()
+    v = tiles[:, np.arange(c.capacity) // 64, :, place].transpose(1, 0, 2)
+    ks, vs = (np.repeat(_wide(s), B, 1)[..., None] for s in (c.k_scale, c.v_scale))
+    return (k * ks)[:, :n], (v * vs)[:, :n]
+
+
+def _assert_held(c, o):
+    assert c.n_tokens == o.n
+    k, v = _held(c)
+    assert np.array_equal(k, o.k[:, : o.n], equal_nan=True)
+    assert np.array_equal(v, o.v[:, : o.n], equal_nan=True)
+    nb = -(-o.n // c.block)
+    assert np.array_equal(_wide(c.k_scale)[:, :nb], o.k_scale[:, :nb])
+    assert np.array_equal(_wide(c.v_scale)[:, :nb], o.v_scale[:, :nb])
+    for dtype in (BF, SF, HF):
+        for got, held in zip(L.kv_read(c, dtype=dtype), (o.k, o.v)):
+            with np.errstate(over="ignore"):
+                want = torch.from_numpy(held[:, : o.n]).to(dtype)   # bf16, fp32: exact
+            assert torch.equal(got.cpu().nan_to_num(7.0, 9.0, 11.0),
+                               want.nan_to_num(7.0, 9.0, 11.0))
+
+
+# block, heads, [(start or None, n, scale, dtype, layout)]
+WRITES = [
+    (128, 1, [(None, 1, 1.0, BF, "hnd")]),
+    (64, 2, [(None, 1, 1.0, BF, "hnd"), (None, 1, 30.0, BF, "nhd"), (None, 1, 1e-3, HF, "hnd")]),
+    (128, 3, [(None, 200, 1.0, BF, "nhd"), (None, 100, 40.0, BF, "hnd"),
+              (None, 57, 0.01, SF, "nhd")]),
+    # a denoising loop writes its chunk again: larger, then smaller than before
+    (128, 2, [(None, 150, 1.0, SF, "hnd"), (150, 90, 500.0, SF, "hnd"), (150, 90, 1.0, SF, "hnd"),
+              (150, 90, 2e-4, HF, "hnd")]),
+    # into the middle, tokens behind it kept; within one block; over several
+    (64, 2, [(None, 300, 1.0, BF, "hnd"), (70, 5, 9.0, BF, "hnd"), (63, 130, 0.2, BF, "nhd"),
+             (0, 300, 3.0, HF, "hnd")]),
+    (128, 1, [(None, 384, 1.0, BF, "hnd"), (127, 2, 3.0, SF, "hnd"), (128, 128, 1.0, BF, "hnd"),
+              (383, 1, 100.0, BF, "hnd")]),
+    (128, 2, [(None, 130, 1e-38, SF, "hnd"), (None, 20, 1e36, SF, "hnd")]),
+]
+
+
+@pytest.mark.parametrize("case", WRITES)
+def test_writes_bit_for_bit(case):
+    B, H, steps = case
+    c, o = L.KvCache(H, 384, B), OC.Cache(H, 384, B)
+    for b in (c.k, c.v):
+        b.view(torch.uint8).fill_(0x7F)      # NaN everywhere: none may stay or come in
+    for s, (start, n, scale, dtype, layout) in enumerate(steps):
+        _say("write", B, H, start, n, scale, dtype, layout)
+        k, v = (_randn((H, n, 128), 10 * s + j, dtype, layout, scale) for j in (0, 1))
+        at = c.n_tokens if start is None else start
+        assert L.kv_write(c, k, v, start=start) is c
+        o.write(_wide(k), _wide(v), at)
+        _assert_held(c, o)
+
+
+def test_write_leaves_other_blocks():
+    for B in (64, 128):
+        c = L.KvCache(2, 512, B)
+        k, v = _randn((2, 512, 128), 1), _randn((2, 512, 128), 2)
+        L.kv_write(c, k, v)
+        before = [b.view(torch.uint8).clone() if b.dtype != SF else b.clone()
+                  for b in (c.k, c.v, c.k_scale, c.v_scale)]
+        L.kv_write(c, k[:, :100] * 8, v[:, :100] * 8, start=200)
+        lo, hi = 200 // B * B, -(-300 // B) * B
+        after = [b.view(torch.uint8) if b.dtype != SF else b
+                 for b in (c.k, c.v, c.k_scale, c.v_scale)]
+        for (x, y), per in zip(zip(before, after), (1, 64, B, B)):
+            a, z = lo // per, hi // per
+            assert torch.equal(x[:, :a], y[:, :a]) and torch.equal(x[:, z:], y[:, z:])
+            assert not torch.equal(x[:, a:z], y[:, a:z])
+        c.n_tokens = 250
+        L.kv_write(c, k[:, :10], v[:, :10])           # tokens behind the last: zeros
+        _, vv = L.kv_read(c, 250, 10)
+        assert torch.isfinite(vv).all()
+        end = -(-260 // B) * B
+        assert (c.k.view(torch.uint8)[:, 260:end] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, SF])
+def test_write_special_values(dtype):
+    """NaN and infinities are held as NaN and leave the scale alone; zeros, the
+    type's largest and smallest magnitudes."""
+    big = torch.finfo(dtype).max
+    x = torch.randn(1, 128, 128, generator=torch.Generator().manual_seed(3)).to(dtype)
+    x[0, 3, 5], x[0, 4, 6], x[0, 5, 7] = float("nan"), float("inf"), -float("inf")
+    y = torch.zeros(1, 128, 128, dtype=dtype)
+    y[0, 0, 0] = torch.finfo(dtype).tiny / 4          # subnormal
+    z = torch.full((1, 128, 128), big, dtype=dtype)
+    z[0, 1] = -big
+    z[0, 2] = 1.0
+    c, o = L.KvCache(1, 384, 128), OC.Cache(1, 384, 128)
+    for k, v in ((x, y), (y * 0, z), (z, x)):
+        _say("special", dtype)
+        o.write(_wide(k), _wide(v), o.n)
+        L.kv_write(c, k.cuda(), v.cuda())
+        _assert_held(c, o)
+
+
+@pytest.mark.parametrize("halves,dtype", [(False, BF), (True, BF), (False, SF), (True, HF)])
+def test_write_with_rope_bit_for_bit(halves, dtype):
+    """Keys rotated in 64 bits, rounded to 32, then to the cache: the same bits as
+    numpy's."""
+    grid, pairs = (4, 5, 13), (22, 21, 21)            # 260 tokens, text from there
+    r = L.Rope(*grid, pairs=pairs, layout=L.ROPE_HALVES if halves else L.ROPE_PAIRS)
+    c, o = L.KvCache(2, 384, 128), OC.Cache(2, 384, 128)
+    for s, n in enumerate((65, 64, 1, 150, 20)):
+        _say("write rope", halves, dtype, n)
+        k, v = (_randn((2, n, 128), 10 * s + j, dtype) for j in (0, 1))
+        cos, sin = _turns(r, grid, pairs, c.n_tokens, n)
+        turned = OC.rotate(_wide(k), cos, sin, halves).astype(np.float32).astype(np.float64)
+        o.write(turned, _wide(v), o.n)
+        L.kv_write(c, k, v, rope=r)
+        _assert_held(c, o)
+
+
+def test_reads_of_parts():
+    c = L.KvCache(3, 640, 64)
+    L.kv_write(c, _randn((3, 600, 128), 1), _randn((3, 600, 128), 2))
+    k, v = L.kv_read(c)
+    assert k.shape == (3, 600, 128) and k.dtype == BF
+    for start, n in ((0, 1), (599, 1), (63, 2), (64, 64), (5, 321), (599 - 64, 65)):
+        for dtype in (BF, HF, SF):
+            a, b = L.kv_read(c, start, n, dtype=dtype)
+            assert torch.equal(a, k[:, start: start + n].to(dtype))
+            assert torch.equal(b, v[:, start: start + n].to(dtype))
+    wide = torch.full((602, 2, 3, 128), 5.0, dtype=BF, device="cuda")
+    out = (wide[1:601, 0].transpose(0, 1), wide[1:601, 1].transpose(0, 1))
+    assert L.kv_read(c, out=out) is out
+    assert torch.equal(out[0], k) and torch.equal(out[1], v)
+    assert (wide[0] == 5.0).all() and (wide[601] == 5.0).all()
+    with pytest.raises(L.LvsaError):
+        L.kv_read(c, 0, 601)
+    with pytest.raises(L.LvsaError):
+        L.kv_read(c, 600)
+
+
+# ---------------------------------------------------------- attention
+
+def _filled(H, N, B, seed=0, capacity=None, scale=1.0):
+    c = L.KvCache(H, capacity or max(N, 1), B)
+    for b in (c.k, c.v):
+        b.view(torch.uint8).fill_(0x7F)
+    if N:
+        g = torch.Generator().manual_seed(seed + 77)
+        spread = torch.exp(0.5 * torch.randn(H, 1, 1, generator=g)).cuda()
+        L.kv_write(c, (_randn((H, N, 128), seed + 1, SF) * spread * scale).to(BF),
+                   (_randn((H, N, 128), seed + 2, SF) * spread).to(BF))
+    return c
+
+
+def _assert_attended(got, q, c, keep=None):
+    """Bounds per element.  Each weight is off by half a bf16 step (2^-8) and by what
+    its score is off: fp32 sums of 128 products (2^-24 each, at most 2^-17 of
+    sum |q k|) and q's smallest elements against its largest, at most 2^-20 of
+    max |q| sum |k|, in all below 2^-16 of `reach`; sums over N keys in fp32; the
+    output's half step.  A row's weights are divided by their own sum, so a weight's
+    error counts by how far its v lies from the output."""
+    k, v = _held(c)
+    out, spread, size, reach = OC.attend(_wide(q), k, v, keep)
+    w = 2.0 ** -8 * 1.02 + 2.0 ** -16 * reach[..., None]
+    tol = (np.abs(out) + w * spread) * 2.0 ** -8 + w * spread
+    tol += size * k.shape[1] * 2.0 ** -24 * 2 + 1e-37
+    err = np.abs(_wide(got) - out)
+    assert np.isfinite(_wide(got)).all()
+    assert (err <= tol).all(), (float((err / tol).max()), np.argwhere(err > tol)[:4].tolist())
+
+
+# heads, group, queries, tokens, cache block
+DENSE = [
+    (1, 1, 1, 1, 128), (1, 1, 1, 63, 64), (2, 1, 1, 64, 128), (3, 1, 1, 65, 64),
+    (1, 1, 1, 1000, 128), (2, 4, 1, 129, 128), (1, 17, 1, 300, 64), (2, 5, 7, 513, 128),
+    (2, 1, 16, 128, 128), (1, 1, 17, 640, 64), (1, 1, 33, 127, 128), (2, 1, 100, 1, 128),
+    (1, 2, 64, 200, 64), (1, 1, 129, 257, 128), (2, 1, 256, 384, 64), (1, 3, 100, 1100, 128),
+    (1, 1, 300, 3000, 64), (40, 1, 1, 70, 128), (1, 1, 513, 65, 128), (5, 2, 130, 192, 64),
+]
+
+
+@pytest.mark.parametrize("case", DENSE)
+def test_attention_over_every_token(case):
+    H, G, n, N, B = case
+    _say("attend", case)
+    c = _filled(H, N, B, seed=N)
+    for layout in ("hnd", "nhd"):
+        q = _randn((H * G, n, 128), N + n, BF, layout)
+        out = torch.full((n, H * G, 136), 3.0, dtype=BF, device="cuda")
+        got = out[:, :, :128].transpose(0, 1)
+        assert L.attention_cache(q, c, out=got) is got
+        _assert_attended(got, q, c)
+        assert (out[:, :, 128:] == 3.0).all()
+        assert torch.equal(L.attention_cache(q, c), got)     # the same bits again
+
+
+def test_attention_over_an_empty_cache():
+    c = _filled(2, 0, 128, capacity=256)
+    for n in (1, 40, 300):
+        got = L.attention_cache(_randn((4, n, 128), 1), c)
+        assert (got == 0).all()
+
+
+def test_attention_of_dropped_tokens():
+    """Tokens behind the last, NaN among them, have no part in it."""
+    c = _filled(2, 200, 64, capacity=384)
+    k = _randn((2, 180, 128), 5)
+    k[:, 40:] = float("nan")
+    L.kv_write(c, k, k, start=200)
+    for keep, n in ((70, 1), (101, 40), (230, 300), (64, 1), (128, 2)):
+        c.n_tokens = keep
+        q = _randn((2, n, 128), keep)
+        _say("dropped", keep, n)
+        _assert_attended(L.attention_cache(q, c), q, c)
+
+
+def _random_csr(nb, seed, share, hole=()):
+    rng = np.random.default_rng(seed)
+    rows = [sorted(np.nonzero(rng.random(nb) < share)[0].tolist()) if r not in hole else []
+            for r in range(nb)]
+    rp = np.concatenate([[0], np.cumsum([len(r) for r in rows])]).astype(np.int32)
+    ci = np.array([c for r in rows for c in r] or [0], dtype=np.int32)
+    return rp, ci
+
+
+# heads, group, tokens, first query, queries, mask block, cache block, share, rows without a key
+MASKED = [
+    (1, 1, 1000, 999, 1, 128, 128, 0.5, ()), (2, 3, 1000, 0, 1, 64, 128, 0.3, ()),
+    (1, 1, 1000, 700, 300, 128, 64, 0.4, (6,)), (2, 1, 1000, 0, 1000, 64, 64, 0.3, (0, 15)),
+    (1, 2, 777, 333, 250, 64, 128, 0.5, (5, 6)), (1, 1, 640, 130, 120, 128, 128, 0.0, ()),
+    (2, 1, 1500, 511, 515, 128, 128, 0.9, (7,)), (1, 4, 500, 60, 10, 64, 64, 0.6, (0,)),
+    (1, 1, 130, 0, 130, 128, 128, 1.0, ()), (3, 1, 2000, 1024, 512, 64, 128, 0.2, ()),
+]
+
+
+@pytest.mark.parametrize("case", MASKED)
+def test_attention_over_a_block_csr(case):
+    H, G, N, start, n, B, cb, share, hole = case
+    _say("masked", case)
+    c = _filled(H, N, cb, seed=N)
+    rp, ci = _random_csr(-(-N // B), N + n, share, hole)
+    mask = L.csr_mask(torch.from_numpy(rp).cuda(), torch.from_numpy(ci).cuda(), N, B)
+    q = _randn((H * G, n, 128), 4, BF, "nhd")
+    got = L.attention_cache(q, c, mask=mask, q_start=start)
+    keep = OC.block_keep(rp, ci, B, N, start, n)
+    _assert_attended(got, q, c, keep)
+    none = ~keep.any(1)
+    assert (got[:, torch.from_numpy(none).cuda()] == 0).all()
+    assert torch.equal(L.attention_cache(q, c, mask=mask, q_start=start), got)
+
+
+@pytest.mark.parametrize("n", [1, 40, 600])
+def test_unkept_blocks_never_reach_a_query(n):
+    """NaN in every block that no query keeps, and in blocks that only some keep."""
+    H, N, B = 2, 900, 64
+    c = _filled(H, N, B, seed=3)
+    nb = -(-N // B)
+    rp, ci = _random_csr(nb, 9, 0.4)
+    rows = [list(ci[rp[r]: rp[r + 1]]) for r in range(nb)]
+    start = 200
+    poison = 5
+    bad = torch.full((H, 30, 128), float("nan"), dtype=BF, device="cuda")
+    L.kv_write(c, bad, bad, start=poison * B + 10)
+    mask = L.csr_mask(torch.from_numpy(rp).cuda(), torch.from_numpy(ci).cuda(), N, B)
+    q = _randn((H, n, 128), 4)
+    got = L.attention_cache(q, c, mask=mask, q_start=start)
+    hit = np.array([poison in rows[(start + i) // B] for i in range(n)])
+    keep = OC.block_keep(rp, ci, B, N, start, n)
+    if (~hit).any():
+        ok = torch.from_numpy(~hit)
+        _assert_attended(got[:, ok.cuda()], q[:, ok.cuda()], c, keep[~hit])
+    if hit.any():
+        assert torch.isnan(got[:, torch.from_numpy(hit).cuda()]).all()
+
+
+def test_columns_outside_the_mask_are_skipped():
+    N, B = 700, 64
+    c = _filled(1, N, B)
+    nb = -(-N // B)
+    good = _random_csr(nb, 2, 0.5)
+    rows = [[-3] + list(good[1][good[0][r]: good[0][r + 1]]) + [nb, nb + 7] for r in range(nb)]
+    rp = np.concatenate([[0], np.cumsum([len(r) for r in rows])]).astype(np.int32)
+    ci = np.array([x for r in rows for x in r], dtype=np.int32)
+    q = _randn((1, N, 128), 4)
+    a, b = (L.attention_cache(q, c, mask=L.csr_mask(torch.from_numpy(x).cuda(),
+                                                    torch.from_numpy(y).cuda(), N, B))
+            for x, y in (good, (rp, ci)))
+    keep = OC.block_keep(good[0], good[1], B, N, 0, N)
+    _assert_attended(a, q, c, keep)
+    _assert_attended(b, q, c, keep)
+
+
+@pytest.mark.parametrize("n", [1, 50, 300])
+@pytest.mark.parametrize("scale", [4.0, 30.0, 1e-3])
+def test_wide_and_narrow_logits(n, scale):
+    c = _filled(2, 1100, 128, seed=6, scale=scale)
+    q = _randn((2, n, 128), 8)
+    q[0, 0, :120] *= 2.0 ** -13            # a row of very different magnitudes
+    _assert_attended(L.attention_cache(q, c), q, c)
+
+
+@pytest.mark.parametrize("n", [1, 300])
+def test_rising_scores(n):
+    """Keys ordered so that every block's scores exceed the last one's."""
+    H, N = 1, 2000
+    c = L.KvCache(H, N, 128)
+    k = _randn((H, N, 128), 1) * 0.05
+    k[..., 0] += torch.arange(N, device="cuda") / 25
+    L.kv_write(c, k, _randn((H, N, 128), 2))
+    q = _randn((H, n, 128), 3)
+    q[..., 0] = 4.0
+    _assert_attended(L.attention_cache(q, c), q, c)
+
+
+def test_weights_add_up_to_one():
+    """Equal values everywhere come back as they are."""
+    for n, N in ((1, 5000), (70, 1000), (500, 3000)):
+        c = L.KvCache(2, N, 128)
+        v = torch.full((2, N, 128), 1.375, dtype=BF, device="cuda")
+        L.kv_write(c, _randn((2, N, 128), 1), v)
+        got = L.attention_cache(_randn((2, n, 128), 2), c)
+        assert (got == 1.375).all()
+
+
+def test_places_past_32_bits():
+    """64 heads of 2^20 places: a head's tokens begin past 2^32 bytes; and one head
+    of 2^24 places, its last token past 2^30 elements."""
+    c = L.KvCache(64, 1 << 20, 128)
+    k, v = _randn((64, 300, 128), 1), _randn((64, 300, 128), 2)
+    L.kv_write(c, k, v)
+    a, b = L.kv_read(c, 10, 290)
+    small = L.KvCache(64, 384, 128)
+    L.kv_write(small, k, v)
+    x, y = L.kv_read(small, 10, 290)
+    assert torch.equal(a, x) and torch.equal(b, y)
+    q = _randn((64, 3, 128), 3)
+    assert torch.equal(L.attention_cache(q, c), L.attention_cache(q, small))
+    q = _randn((64, 300, 128), 3)
+    assert torch.equal(L.attention_cache(q, c), L.attention_cache(q, small))
+    del c, small
+    N = 1 << 24
+    c = L.KvCache(1, N, 64)
+    for b in (c.k, c.v):
+        b.view(torch.uint8).zero_()
+    c.k_scale.fill_(1.0)
+    c.v_scale.fill_(1.0)
+    c.n_tokens = N - 100
+    k, v = torch.zeros(1, 100, 128, dtype=BF, device="cuda"), _randn((1, 100, 128), 2)
+    k[0, 99, 0] = 400.0
+    L.kv_write(c, k, v)
+    want = L.kv_read(c, N - 1, 1)[1]
+    q = torch.zeros(1, 300, 128, dtype=BF, device="cuda")
+    q[..., 0] = 4.0                        # the last key's score: 141 above the others'
+    assert torch.equal(L.attention_cache(q[:, :1], c), want)
+    assert torch.equal(L.attention_cache(q, c), want.expand(1, 300, 128))
+
+
+# -------------------------------------------------- together, as used
+
+def _chunk(s, H, n, dtype=BF):
+    return tuple(_randn((H, n, 128), 100 * s + j, dtype) for j in range(3))
+
+
+def test_generation_chunk_by_chunk():
+    """Frames arrive in chunks, each denoised in two passes that write the chunk's
+    tokens again, under an LVSA mask over the frames so far: against the plain
+    forms, and the whole at the end against the library's attention over the keys
+    and values read back."""
+    h, w, H, B = 7, 19, 2, 64                 # 133 tokens a frame: blocks straddle frames
+    P = h * w
+    p = L.Params(budget_frames=5, window=1)
+    T = 6
+    r = L.Rope(T, h, w)
+    c, o = L.KvCache(H, T * P, B), OC.Cache(H, -(-T * P // 128) * 128, B)
+    nb = -(-T * P // B)
+    rp = torch.empty(nb + 1, dtype=torch.int32, device="cuda")
+    ci = torch.empty(nb * nb, dtype=torch.int32, device="cuda")
+    frames, queries = 0, []
+    for s, more in enumerate((2, 1, 3)):
+        start, n = frames * P, more * P
+        frames += more
+        for step in range(2):
+            _say("chunk", s, step)
+            q, k, v = _chunk(10 * s + step, H, n)
+            mask = L.build_mask_device(frames, P, B, step, rp, ci, params=p)
+            qr = L.rope(q, r, start=start)
+            L.kv_write(c, k, v, start=start, rope=r)
+            got = L.attention_cache(qr, c, mask=mask, q_start=start)
+            cos, sin = _turns(r, (T, h, w), (22, 21, 21), start, n)
+            o.write(OC.rotate(_wide(k), cos, sin, False).astype(np.float32).astype(np.float64),
+                    _wide(v), start)
+            _assert_held(c, o)
+            row_ptr, cols = M.build_mask(frames, P, B, step, C=5, W=1)
+            _assert_attended(got, qr, c, OC.block_keep(row_ptr, cols, B, frames * P, start, n))
+        queries.append(qr)
+    q = torch.cat(queries, 1)
+    a = L.attention_cache(q, c, mask=mask)
+    k, v = L.kv_read(c)
+    b = L.attention(q, k, v, mask)
+    # both are within bf16's steps of the same values
+    assert (a.float() - b.float()).abs().max() <= 2e-2
+    assert (a.float() - b.float()).abs().mean() <= 2e-3
+
+
+def test_on_another_stream():
+    c = L.KvCache(2, 1000, 128)
+    r = L.Rope(10, 10, 10)
+    q, k, v = _chunk(1, 2, 700)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        c.n_tokens = 0
+        L.kv_write(c, k, v, rope=r, stream=s)
+        got = L.attention_cache(L.rope(q, r, stream=s), c, stream=s)
+        one = L.attention_cache(q[:, :1], c, stream=s)
+        back = L.kv_read(c, stream=s)
+    s.synchronize()
+    d = L.KvCache(2, 1000, 128)
+    L.kv_write(d, k, v, rope=r)
+    assert torch.equal(got, L.attention_cache(L.rope(q, r), d))
+    assert torch.equal(one, L.attention_cache(q[:, :1], d))
+    assert all(torch.equal(x, y) for x, y in zip(back, L.kv_read(d)))
+
+
+def test_two_streams_at_once():
+    """Calls over one cache in flight together: a workspace each."""
+    c = _filled(4, 4000, 128)
+    qs = [_randn((4, n, 128), n) for n in (1, 8, 200, 400)]
+    want = [L.attention_cache(q, c) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(10):
+        for q in qs:
+            for s in streams:
+                got.append((L.attention_cache(q, c, stream=s), q))
+    torch.cuda.synchronize()
+    for g, q in got:
+        assert torch.equal(g, want[[x is q for x in qs].index(True)])
+
+
+def test_graphs_replayed_among_eager_calls():
+    """Two captured steps (positions, write, attention of a frame and of one token)
+    over caches of their own, replayed in turn with new inputs among eager calls."""
+    H, P, N = 2, 160, 1500
+    r = L.Rope(10, 10, 16)
+    caches = [_filled(H, N, 128, seed=s, capacity=2048) for s in (1, 2)]
+    mirror = [_filled(H, N, 128, seed=s, capacity=2048) for s in (1, 2)]
+    ins = [_chunk(s, H, P) for s in (1, 2)]
+
+    def step(c, x):
+        q, k, v = x
+        L.kv_write(c, k, v, start=N - 50, rope=r)
+        qr = L.rope(q, r, start=N - 50)
+        return (L.attention_cache(qr, c), L.attention_cache(qr[:, :1], c),
+                *L.kv_read(c, N - 60, 100))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for c, x in zip(caches, ins):
+            step(c, x)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for c, m in zip(caches, mirror):
+        for a, b in zip((c.k, c.v), (m.k, m.v)):
+            b.view(torch.uint8).copy_(a.view(torch.uint8))
+        m.k_scale.copy_(c.k_scale)
+        m.v_scale.copy_(c.v_scale)
+        m.n_tokens = c.n_tokens
+    graphs, outs = [], []
+    for c, x in zip(caches, ins):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(c, x))
+        graphs.append(g)
+    for rep in range(4):
+        for j in (0, 1):
+            for t, new in zip(ins[j], _chunk(50 + 10 * rep + j, H, P)):
+                t.copy_(new)
+            for t in outs[j]:
+                t.fill_(float("nan"))
+        graphs[rep % 2].replay()
+        eager = [step(m, x) for m, x in zip(mirror, ins)]
+        graphs[1 - rep % 2].replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert all(torch.equal(x, y) for x, y in zip(a, b)), rep
+
+
+def test_workspace_is_checked():
+    import ctypes
+    c = _filled(1, 20000, 128)
+    q = _randn((1, 1, 128), 1)
+    out = torch.full_like(q, 7.0)
+    tq, to, need = L._rows(q), L._rows(out), ctypes.c_int64()
+    ref = ctypes.byref
+    assert L.lib().lvsa_attention_cache_workspace(ref(tq), 0, ref(c._c), None, ref(need)) == L.OK
+    assert need.value > 0
+    work = torch.empty(need.value + 16, dtype=torch.uint8, device="cuda")
+    call = L.lib().lvsa_attention_cache
+
+    def run(ptr, size):
+        return call(ref(tq), 0, ref(c._c), None, ref(to), ptr, size, L._stream_ptr(None))
+
+    assert run(None, need.value) == L.EINVAL
+    assert run(work.data_ptr(), need.value - 1) == L.EINVAL
+    assert run(work.data_ptr() + 8, need.value) == L.EUNSUPPORTED
+    torch.cuda.synchronize()
+    assert (out == 7.0).all()
+    work.fill_(0xFF)                          # any content
+    assert run(work.data_ptr(), need.value) == L.OK
+    assert torch.equal(out, L.attention_cache(q, c))
+    assert (work[need.value:] == 0xFF).all()
