@@ -29,12 +29,18 @@ constexpr int D = 128;
 constexpr int UNIT = 64;              // keys of a unit
 constexpr int WAVES = 4;
 constexpr int THREADS = 64 * WAVES;
+constexpr int TILE_ROWS = 256;
 
-// How a launch is cut (the same for workspace and kernels).
+// How a launch is cut (the same for workspace and kernels).  Rows form: an item's rows
+// share a key head and, with a mask, a query block.  Tile form: 256 rows; with a
+// mask of one query head and 256 / mask_block query blocks, else of a key head's
+// queries.
 struct Plan {
-  int32_t rt;          // 16-row tiles of an item
-  int32_t blocks;      // query blocks (1 without a mask)
-  int32_t tiles;       // items of a key head and query block
+  bool tile;
+  int32_t item_rows;   // rows of an item
+  int32_t blocks;      // rows form: query blocks (1 without a mask)
+  int32_t tiles;       // items of a key head and query block (of a head, tile form)
+  int32_t heads;       // tile form with a mask: query heads; else key heads
   int32_t splits;
 };
 
@@ -44,35 +50,54 @@ struct KernelArgs {
   float scale_log2;
 };
 
-// The query rows of an item.
+// The rows of an item.  Row r is row row0 + r of `rows`, which are the tokens first ..
+// first + len - 1 of the query heads head0, head0 + 1, .. one head after the other.
 struct Item {
-  int32_t kvh;         // key head
-  int32_t first, len;  // query tokens of its query block: first .. first + len - 1
-  int32_t row0;        // first row
-  int32_t walk, units; // CSR entry of its first unit, units
+  int32_t kvh, head0;
+  int32_t first, len, rows, row0;
+  int32_t block0, blocks;   // query blocks of the mask
 };
 
-__device__ __forceinline__ Item item_of(const KernelArgs& k, int32_t id) {
+__device__ __forceinline__ Item item_of(const KernelArgs& k, int32_t tile, int32_t rest) {
   const CacheAttnArgs& a = k.a;
   Item it;
-  const int32_t tile = id % k.p.tiles, rest = id / k.p.tiles;
+  it.row0 = tile * k.p.item_rows;
+  it.block0 = 0;
+  it.blocks = 0;
+  it.first = 0;
+  it.len = a.n;
+  if (k.p.tile && a.row_ptr) {
+    const int32_t per = TILE_ROWS / a.mask_block, from = a.q_start / a.mask_block;
+    it.kvh = rest / a.group;
+    it.head0 = rest;
+    it.block0 = from + tile * per;
+    it.blocks = min(per, (a.q_start + a.n - 1) / a.mask_block + 1 - it.block0);
+    it.first = it.block0 * a.mask_block - a.q_start;
+    it.len = it.rows = TILE_ROWS;
+    it.row0 = 0;
+    return it;
+  }
   const int32_t qb = rest % k.p.blocks;
   it.kvh = rest / k.p.blocks;
-  it.row0 = tile * k.p.rt * 16;
-  if (!a.row_ptr) {
-    it.first = 0;
-    it.len = a.n;
-    it.walk = 0;
-    it.units = (a.n_tokens + UNIT - 1) / UNIT;
-  } else {
-    const int32_t block = a.q_start / a.mask_block + qb;
-    const int32_t lo = max(block * a.mask_block, a.q_start) - a.q_start;
-    it.first = lo;
-    it.len = min((block + 1) * a.mask_block - a.q_start, a.n) - lo;
-    it.walk = a.row_ptr[block];
-    it.units = min(max(a.row_ptr[block + 1] - it.walk, 0), a.mask_blocks) * (a.mask_block / UNIT);
+  it.head0 = it.kvh * a.group;
+  if (a.row_ptr) {
+    it.block0 = a.q_start / a.mask_block + qb;
+    it.blocks = 1;
+    it.first = max(it.block0 * a.mask_block - a.q_start, 0);
+    it.len = min((it.block0 + 1) * a.mask_block - a.q_start, a.n) - it.first;
   }
+  it.rows = it.len * a.group;
   return it;
+}
+
+// Query head and token of row r of an item; false (and 0, 0) where there is none.
+__device__ __forceinline__ bool row_of(const Item& it, const CacheAttnArgs& a, int32_t r,
+                                       int32_t& head, int32_t& token) {
+  const int32_t row = it.row0 + r, h = row / it.len, t = it.first + row - h * it.len;
+  const bool ok = row < it.rows && (uint32_t)t < (uint32_t)a.n;
+  head = ok ? it.head0 + h : 0;
+  token = ok ? t : 0;
+  return ok;
 }
 
 __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1, float scale) {
@@ -107,21 +132,26 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
   const int g = lane / 16, i = lane % 16;
   const int32_t split = blockIdx.x % ka.p.splits, id = blockIdx.x / ka.p.splits;
-  const Item it = item_of(ka, id);
-  const int32_t rows = it.len * a.group;
-  if (it.row0 >= rows) return;
-  const int32_t u0 = (int32_t)((int64_t)it.units * split / ka.p.splits);
-  const int32_t u1 = (int32_t)((int64_t)it.units * (split + 1) / ka.p.splits);
+  const Item it = item_of(ka, id % ka.p.tiles, id / ka.p.tiles);
+  if (it.row0 >= it.rows) return;
+  // Its units: the first `units` of the walk, or with a mask of the row's entries.
+  const int32_t per = a.row_ptr ? a.mask_block / UNIT : 1;
+  int32_t walk = 0, units = (a.n_tokens + UNIT - 1) / UNIT;
+  if (a.row_ptr) {
+    walk = a.row_ptr[it.block0];
+    units = min(max(a.row_ptr[it.block0 + 1] - walk, 0), a.mask_blocks) * per;
+  }
+  const int32_t u0 = (int32_t)((int64_t)units * split / ka.p.splits);
+  const int32_t u1 = (int32_t)((int64_t)units * (split + 1) / ka.p.splits);
 
   // Q fragments: row 16rt + i, elements in the order of K's.
   bf16x8 qf[RT][4];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int32_t row = it.row0 + 16 * rt + i;
-    const bool ok = row < rows;
-    const int32_t h = ok ? row / it.len : 0, t = ok ? row - h * it.len : 0;
-    const __bf16* q = (const __bf16*)a.q + (int64_t)(it.kvh * a.group + h) * a.q_sh +
-                      (int64_t)(it.first + t) * a.q_st + 16 * g;
+    int32_t h, t;
+    const bool ok = row_of(it, a, 16 * rt + i, h, t);
+    const __bf16* q =
+        (const __bf16*)a.q + (int64_t)h * a.q_sh + (int64_t)t * a.q_st + 16 * g;
 #pragma unroll
     for (int s = 0; s < 4; ++s)
       qf[rt][s] = ok ? *(const bf16x8*)(q + (s / 2) * 64 + (s % 2) * 8) : bf16x8{};
@@ -132,13 +162,12 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
   const uint8_t* const vb = a.v + base * D + i * UNIT + 16 * g;
   const float* const ks = a.k_scale + (base >> a.scale_shift);
   const float* const vs = a.v_scale + (base >> a.scale_shift);
-  const int32_t per = a.row_ptr ? a.mask_block / UNIT : 1;
   auto load = [&](int32_t u, UnitData& d) {
     d.key0 = a.n_tokens;
     if (u >= u1) return;
     int32_t unit = u;
     if (a.row_ptr) {
-      const int32_t kblock = a.col_idx[it.walk + u / per];
+      const int32_t kblock = a.col_idx[walk + u / per];
       if ((uint32_t)kblock >= (uint32_t)a.mask_blocks) return;
       unit = kblock * per + u % per;
     }
@@ -264,8 +293,8 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
   __syncthreads();
   for (int at = threadIdx.x; at < ROWS * (D / 4); at += THREADS) {
     const int r = at / (D / 4), c = at % (D / 4) * 4;
-    const int32_t row = it.row0 + r;
-    if (row >= rows) break;
+    int32_t h, t;
+    if (!row_of(it, a, r, h, t)) break;
     float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) top = fmaxf(top, lds_m[w][r]);
@@ -278,9 +307,7 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
       acc += f * *(const f32x4*)&lds_o[w][r][c];
     }
     if (ka.p.splits == 1) {
-      const int32_t h = row / it.len, t = row - h * it.len;
-      __bf16* out = (__bf16*)a.o + (int64_t)(it.kvh * a.group + h) * a.o_sh +
-                    (int64_t)(it.first + t) * a.o_st + c;
+      __bf16* out = (__bf16*)a.o + (int64_t)h * a.o_sh + (int64_t)t * a.o_st + c;
       const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
       bf16x4 b;
 #pragma unroll
@@ -298,14 +325,649 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
   }
 }
 
-// Combines the splits of a row, in their order: 32 threads a row.
-__global__ __launch_bounds__(THREADS) void combine_kernel(KernelArgs ka, int32_t rows_item) {
+// ------------------------------------------------------------------- tiles
+//
+// Many query rows: an item is 256 rows of one query head, eight waves of 32, which walk
+// the union of its query blocks' key lists 128 keys (two units) a step, sharing
+// every K and V byte through LDS.
+//
+//   S^T = K Q^T     fp8 MFMA 16x16x128, K as its e4m3 bytes with the block's scale as
+//                   the instruction's, Q as the sum of two e4m3 numbers (q_split)
+//   O^T += V^T P^T  bf16 MFMA 16x16x32, V converted to bf16 on its way into LDS
+//
+// Two fp8 MFMAs of 128 elements take the matrix core as long as four bf16 ones of
+// 32, but K's bytes are half the LDS reads and need no conversion.  V is converted
+// once a workgroup, 32 elements a thread and step.  P needs its eight bits: e4m3
+// pairs as for Q would cost two VALU operations an element more than they save.
+//
+// Schedule: waves w and w + 4 share a SIMD and run half a step apart, one in its
+// matrix phase while the other is in its softmax phase; a barrier ends each half
+// step.  Half steps 2j and 2j + 1: the leaders (waves 0-3) are in matrix phase j, then
+// softmax j + 1; the others in softmax j, then matrix phase j.  K(j+1) and V(j) stay
+// in LDS through both; K(j+2) and V(j+1) go into the other two stages, by every wave
+// in its softmax phase: K straight from memory to LDS, V from registers that the
+// wave's matrix phase before loaded.
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+
+constexpr int TILE_THREADS = 512;
+constexpr int K_STAGE = 2 * UNIT * D;        // 128 rows of 128 bytes
+constexpr int V_STAGE = 2 * UNIT * D * 2;    // 128 rows (d) of 256 bytes (keys)
+constexpr int V_AT = 2 * K_STAGE;
+constexpr int LIST_AT = V_AT + 2 * V_STAGE;
+constexpr int LIST_WORDS = kMaxSparseBlocks;
+constexpr int BITMAP_WORDS = 256;
+static_assert(BITMAP_WORDS * 32 >= LIST_WORDS, "a bit a block");
+constexpr int TILE_LDS = LIST_AT + LIST_WORDS * 4 + 64;
+
+// Distance (log2) of a row's reference above the largest score it was set from.
+constexpr float HEADROOM = 7.f;
+constexpr float WIDE_HEADROOM = 39.f;
+
+// LDS layouts.  K stage: row = key, 8 chunks of 16 bytes, chunk c at place c ^ (row/2 % 8).
+// V stage: row = d, 16 chunks of 8 keys in bf16, chunk c at place c ^ (row % 16); chunk
+// 4u + g holds the keys that lane group g's P registers hold of the 32-key group u
+// (tokens 32u + 4g + r and 32u + 16 + 4g + r).  Both spread the 16 rows that a read takes
+// at one chunk over all banks.
+
+// One wave load (1 KiB) from memory into LDS.  Inline assembly, so that the compiler
+// puts no wait for it between here and the half step's end, where tile_sync waits.
+// The nop is the wait state between a write of M0 and the load.
+__device__ __forceinline__ void load_to_lds(uint32_t dst, __amdgpu_buffer_rsrc_t rsrc,
+                                            uint32_t voff, uint32_t soff) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %1, %2, %3 offen lds"
+      :
+      : "s"(dst), "v"(voff), "s"(rsrc), "s"(soff)
+      : "memory", "m0");
+}
+__device__ __forceinline__ void tile_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+// The same, with the wave's loads into LDS done.
+__device__ __forceinline__ void tile_sync() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, bytes, 0x00020000);
+}
+
+// The lane's index, made anew where a rare branch needs it: what is derived from it
+// there is not kept in registers through the loop.
+__device__ __forceinline__ int fresh_lane() {
+  int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
+// One step's units.
+struct Step {
+  int32_t unit[2];   // 0 where there is none
+  int32_t left[2];   // held tokens from the unit's first on; 0: none, or not kept by any
+  int32_t keep;      // bit u: this wave's query block keeps unit u
+};
+
+// Q of a wave: two 16-row tiles, each the sum of two e4m3 operands.  With 2^a the least
+// power of two that keeps the row within 448 * 2^a: hi = e4m3(q / 2^a), low =
+// e4m3(16 (q / 2^a - hi)).  A bf16 number has 8 significant bits, hi takes its first
+// 4 and low the rest exactly, down to 2^-14 of the row's largest; below, hi + low is
+// within 2^-22 of the largest.
+struct QSplit {
+  i32x8 hi[2], low[2];
+  int32_t scale[2];   // exponent bytes: byte 0 of hi, byte 1 of low
+};
+
+template <int QT>
+__device__ __forceinline__ void q_split(QSplit& q, const __bf16* row, bool ok) {
+  float x[4][8];
+  float most = 0.f;
+  bool bad = false;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    if (ok) {
+      load8(row + (s / 2) * 64 + (s % 2) * 8, x[s]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      bad |= !(fabsf(x[s][e]) < __builtin_inff());
+      most = fmaxf(most, fabsf(x[s][e]));
+    }
+  }
+  most = row_max(most < __builtin_inff() ? most : 0.f);
+  const int a = scale_exponent(most);
+  const float inv = pow2(-a);
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      float y[4], h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = __builtin_amdgcn_fmed3f(x[s][4 * w + e] * inv, -448.f, 448.f);
+        y[e] = bad ? __builtin_nanf("") : z;   // a row that is not finite becomes NaN
+      }
+      const uint32_t hi = to_e4m3(y[0], y[1], y[2], y[3]);
+      from_e4m3(hi, h);
+      q.hi[QT][2 * s + w] = (int)hi;
+      q.low[QT][2 * s + w] = (int)to_e4m3(16.f * (y[0] - h[0]), 16.f * (y[1] - h[1]),
+                                          16.f * (y[2] - h[2]), 16.f * (y[3] - h[3]));
+    }
+  q.scale[QT] = (a + 127) | (a - 4 + 127) << 8;
+}
+
+struct TileState {
+  f32x4 o[8][2];   // O^T [d tile][query tile]
+  f32x4 l[2];      // row sums, in register 0
+  float m[2];      // references (log2)
+  int flags;       // READY: every row has a finite m; WIDE: a step was redone
+};
+constexpr int READY = 1, WIDE = 2;
+
+struct Scores {
+  f32x4 s[8][2];   // [16-key tile][query tile]
+};
+struct Probs {
+  bf16x8 p[4][2];  // [32-key group][query tile]
+};
+
+// Per-lane LDS offsets of the fragments.
+struct FragAt {
+  uint32_t k;        // K row i, chunk g (chunk 4 + g at ^ 64)
+  uint32_t v[4];     // V row i, chunk 4u + g
+};
+
+__device__ __forceinline__ i32x8 k_frag(const char* k, const FragAt& f, int kt) {
+  const i32x4 a = *(const i32x4*)(k + f.k + kt * 16 * D);
+  const i32x4 b = *(const i32x4*)(k + (f.k ^ 64u) + kt * 16 * D);
+  return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+__device__ __forceinline__ bf16x8 v_frag(const char* v, const FragAt& f, int dt, int u) {
+  return *(const bf16x8*)(v + f.v[u] + dt * 16 * 256);
+}
+template <int KT>
+__device__ __forceinline__ void score_tile(Scores& sc, const i32x8& f, const QSplit& q,
+                                           int k_scale) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int qt = t ^ (KT & 1);
+    f32x4 c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+        f, q.hi[qt], f32x4{}, 0, 0, KT / 4, k_scale, 0, q.scale[qt]);
+    sc.s[KT][qt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+        f, q.low[qt], c, 0, 0, KT / 4, k_scale, 1, q.scale[qt]);
+  }
+}
+template <int KT>
+__device__ __forceinline__ void score_from(Scores& sc, const char* k, const FragAt& f,
+                                           const QSplit& q, int k_scale) {
+  if constexpr (KT < 8) {
+    score_tile<KT>(sc, k_frag(k, f, KT), q, k_scale);
+    score_from<KT + 1>(sc, k, f, q, k_scale);
+  }
+}
+
+// Scores of keys that do not exist or that the wave's query block does not keep: -inf.
+__device__ __forceinline__ void mask_scores(Scores& sc, const Step& st) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int left = (st.keep >> u) & 1 ? st.left[u] : 0;
+    if (left >= UNIT) continue;
+    const int lim = left - 4 * (fresh_lane() / 16);
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (r % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+        const bool ok = 16 * kt + r < lim;
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt)
+          sc.s[4 * u + kt][qt][r] = ok ? sc.s[4 * u + kt][qt][r] : -__builtin_inff();
+      }
+  }
+}
+
+// Raises the reference of rows whose largest score lies above it to `head` above that
+// score, the others by `lift`, and rescales O and l.
+__device__ __forceinline__ void raise(const Scores& sc, TileState& st, float scale, float head,
+                                      float lift) {
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int kt = 0; kt < 8; ++kt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, sc.s[kt][qt][r]);
+    top = row_max(top) * scale;
+    const float m = top > st.m[qt] ? top + head : st.m[qt] + lift;
+    const float f = m == st.m[qt] ? 1.f : __builtin_amdgcn_exp2f(st.m[qt] - m);
+    st.m[qt] = m;
+    st.l[qt][0] *= f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) st.o[dt][qt] *= f;
+  }
+  const bool ready = __builtin_amdgcn_ballot_w64(st.m[0] == -__builtin_inff() ||
+                                                 st.m[1] == -__builtin_inff()) == 0;
+  st.flags = (st.flags & ~READY) | (ready ? READY : 0);
+}
+
+// P = 2^(s * scale - m); returns the bits of all probabilities or-ed together.
+__device__ __forceinline__ uint32_t weights(const Scores& sc, Probs& pr, const float (&m)[2],
+                                            float scale) {
+  uint32_t bits = 0u;
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) {
+          const float a =
+              __builtin_amdgcn_exp2f(__builtin_fmaf(sc.s[2 * u + t][qt][r], scale, -m[qt]));
+          const float b =
+              __builtin_amdgcn_exp2f(__builtin_fmaf(sc.s[2 * u + t][qt][r + 1], scale, -m[qt]));
+          const bf16x2 pk = {(__bf16)a, (__bf16)b};
+          bits |= __builtin_bit_cast(uint32_t, pk);
+          pr.p[u][qt][4 * t + r] = pk[0];
+          pr.p[u][qt][4 * t + r + 1] = pk[1];
+        }
+    }
+  return bits;
+}
+
+// Scores to weights against the rows' references as they stand, HEADROOM above the
+// score they were set from: a step takes a row maximum only when some weight reaches 2
+// (the top exponent bit of its bf16), and is then done again with the reference
+// raised.  Exact either way: O and l always use the same reference.  The sums l are
+// taken of the rounded weights, so a row's weights add up to 1.
+__device__ __forceinline__ void softmax_phase(const Scores& sc, TileState& st, Probs& pr,
+                                              float scale) {
+  const int flags = __builtin_amdgcn_readfirstlane(st.flags);
+  const bool first = !(flags & READY);
+  if (first) raise(sc, st, scale, (flags & WIDE) ? WIDE_HEADROOM : HEADROOM, 0.f);
+  float m[2];
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) m[qt] = st.m[qt] == -__builtin_inff() ? 0.f : st.m[qt];
+  const uint32_t bits = weights(sc, pr, m, scale);
+  if (__builtin_amdgcn_ballot_w64((bits & 0x40004000u) != 0u) && !first) {
+    st.flags |= WIDE;
+    raise(sc, st, scale, WIDE_HEADROOM, (flags & WIDE) ? 0.f : WIDE_HEADROOM - HEADROOM);
+    weights(sc, pr, st.m, scale);
+  }
+}
+
+// l += row sums of P, O += P V, S = K Q^T of the next step.  V of a unit that the wave's
+// query block does not keep is left out: what it holds never reaches the block.
+__device__ __forceinline__ void matrix_phase(const char* k, const char* v, const QSplit& q,
+                                             Scores& sc, const Probs& pr, TileState& st,
+                                             const FragAt& f, const bf16x8& ones, int keep,
+                                             int k_scale) {
+  if (keep != 3) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (!((keep >> (u / 2)) & 1)) continue;
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt)
+        st.l[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pr.p[u][qt], st.l[qt], 0, 0, 0);
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        const bf16x8 x = v_frag(v, f, dt, u);
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt)
+          st.o[dt][qt] =
+              __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pr.p[u][qt], st.o[dt][qt], 0, 0, 0);
+      }
+    }
+    score_from<0>(sc, k, f, q, k_scale);
+    return;
+  }
+  constexpr int AHEAD = 8;
+  bf16x8 fr[32];
+  i32x8 kf[8];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fr[i] = v_frag(v, f, i / 4, i % 4);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      st.l[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pr.p[u][qt], st.l[qt], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  // Chains of four MFMAs into one accumulator; consecutive chains share an operand.
+#pragma unroll
+  for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = 8 * dt + 4 * t + i;
+        const int u = t ? 3 - i : i, qt = t ^ (dt & 1);
+        if (at % 2 == 0) {
+          const int n = at / 2 + AHEAD;
+          if (n < 32) fr[n] = v_frag(v, f, n / 4, n % 4);
+          else if ((n - 32) % 4 == 0) kf[(n - 32) / 4] = k_frag(k, f, (n - 32) / 4);
+        }
+        st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[4 * dt + u], pr.p[u][qt],
+                                                               st.o[dt][qt], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#define SCORE_TILE(KT)                                       \
+  if (KT + 2 < 8) kf[KT + 2] = k_frag(k, f, KT + 2);         \
+  score_tile<KT>(sc, kf[KT], q, k_scale);                    \
+  __builtin_amdgcn_sched_barrier(0);
+  SCORE_TILE(0)
+  SCORE_TILE(1)
+  SCORE_TILE(2)
+  SCORE_TILE(3)
+  SCORE_TILE(4)
+  SCORE_TILE(5)
+  if (true) { score_tile<6>(sc, kf[6], q, k_scale); __builtin_amdgcn_sched_barrier(0); }
+  score_tile<7>(sc, kf[7], q, k_scale);
+#undef SCORE_TILE
+}
+
+// V bytes of a step that a thread converts: 16 places of one d in each unit.
+struct VHold {
+  u32x4 w[2];
+};
+
+// The union of the CSR rows block0 .. block0 + count - 1 (at most four) as words in
+// `list`, ascending: key block in bits 0..27, bit 28 + r set when row r keeps it.
+// `bm`: LDS for four bitmaps.  Columns outside [0, nb) are skipped and at most nb entries
+// of a row are read.  Returns the number of words.
+__device__ __forceinline__ int32_t union_list(uint32_t* list, uint32_t* bm, int32_t* sums,
+                                              const int32_t* __restrict__ row_ptr,
+                                              const int32_t* __restrict__ col_idx, int block0,
+                                              int count, int nb) {
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  for (int t = tid; t < 4 * BITMAP_WORDS; t += TILE_THREADS) bm[t] = 0u;
+  __syncthreads();
+  for (int r = 0; r < count; ++r) {
+    const int32_t lo = row_ptr[block0 + r], hi = min(row_ptr[block0 + r + 1], lo + nb);
+    for (int t = lo + tid; t < hi; t += TILE_THREADS) {
+      const uint32_t kb = (uint32_t)col_idx[t];
+      if (kb < (uint32_t)nb) atomicOr(&bm[r * BITMAP_WORDS + kb / 32], 1u << (kb % 32));
+    }
+  }
+  __syncthreads();
+  uint32_t row[4] = {}, all = 0u;
+  int32_t incl = 0;
+  if (tid < BITMAP_WORDS) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) all |= row[r] = bm[r * BITMAP_WORDS + tid];
+    incl = __popc(all);
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int32_t y = __shfl_up(incl, off);
+      if (lane >= off) incl += y;
+    }
+    if (lane == 63) sums[wave] = incl;
+  }
+  __syncthreads();
+  int32_t total = 0, before = 0;
+#pragma unroll
+  for (int w = 0; w < BITMAP_WORDS / 64; ++w) {
+    if (w < wave) before += sums[w];
+    total += sums[w];
+  }
+  int32_t at = before + incl - __popc(all);
+  for (uint32_t rest = all; rest; rest &= rest - 1u) {
+    const int b = __ffs(rest) - 1;
+    uint32_t word = (uint32_t)(32 * tid + b);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) word |= ((row[r] >> b) & 1u) << (28 + r);
+    list[at++] = word;
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(total);
+}
+
+// MB: the mask's block, 0 without a mask.
+template <int MB>
+__global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
+  __shared__ __attribute__((aligned(1024))) char lds[MB ? TILE_LDS : LIST_AT];
   const CacheAttnArgs& a = ka.a;
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int g = lane / 16, i = lane % 16;
+  // Workgroups go round the eight XCDs; each takes a run of consecutive items, tiles
+  // of one head first, which share keys in its L2.
+  const uint32_t total = gridDim.x;
+  const uint32_t xcd = blockIdx.x % 8, nth = blockIdx.x / 8;
+  const uint32_t id = xcd * (total / 8) + min(xcd, total % 8) + nth;
+  const int32_t tile = id % ka.p.tiles;
+  const int32_t split = id / ka.p.tiles % ka.p.splits;
+  const Item it = item_of(ka, tile, id / ka.p.tiles / ka.p.splits);
+
+  // Steps of the split.
+  uint32_t* const list = (uint32_t*)(lds + LIST_AT);
+  int32_t words, n, s0 = 0;
+  if constexpr (MB == 0) {
+    words = (a.n_tokens + UNIT - 1) / UNIT;
+    n = (words + 1) / 2;
+  } else {
+    words = union_list(list, (uint32_t*)(lds + V_AT), (int32_t*)(lds + TILE_LDS - 64), a.row_ptr,
+                       a.col_idx, it.block0, it.blocks, a.mask_blocks);
+    n = MB == 128 ? words : (words + 1) / 2;
+  }
+  s0 = (int32_t)((int64_t)n * split / ka.p.splits);
+  n = (int32_t)((int64_t)n * (split + 1) / ka.p.splits) - s0;
+  const int my_block = MB ? 32 * wave / (MB ? MB : 1) : 0;
+  auto step_at = [&](int j) {
+    Step st;
+    if constexpr (MB == 0) {
+      st.unit[0] = 2 * (s0 + j);
+      st.unit[1] = 2 * (s0 + j) + 1;
+      st.keep = 3;
+    } else if constexpr (MB == 128) {
+      const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)list[s0 + j]);
+      st.unit[0] = 2 * (int)(w & 0x0FFFFFFFu);
+      st.unit[1] = st.unit[0] + 1;
+      st.keep = ((w >> (28 + my_block)) & 1u) * 3;
+    } else {
+      const int at = 2 * (s0 + j);
+      const uint32_t w0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)list[at]);
+      const uint32_t w1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)list[min(at + 1, words - 1)]);
+      st.unit[0] = (int)(w0 & 0x0FFFFFFFu);
+      st.unit[1] = (int)(w1 & 0x0FFFFFFFu);
+      st.keep = ((w0 >> (28 + my_block)) & 1u) |
+                (at + 1 < words ? ((w1 >> (28 + my_block)) & 1u) << 1 : 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) st.left[u] = a.n_tokens - st.unit[u] * UNIT;
+    return st;
+  };
+
+  // The wave's rows.
+  QSplit q;
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    int32_t head, token;
+    const bool ok = row_of(it, a, 32 * wave + 16 * qt + i, head, token);
+    const __bf16* row =
+        (const __bf16*)a.q + (int64_t)head * a.q_sh + (int64_t)token * a.q_st + 16 * g;
+    if (qt == 0) q_split<0>(q, row, ok); else q_split<1>(q, row, ok);
+  }
+  TileState ts;
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) ts.o[dt][qt] = f32x4{};
+    ts.l[qt] = f32x4{};
+    ts.m[qt] = -__builtin_inff();
+  }
+  ts.flags = 0;
+  bf16x8 ones;   // rows 0, 4, 8, 12 of the row sums' A operand: register 0 of every lane
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = lane % 4 == 0 ? (__bf16)1.f : (__bf16)0.f;
+
+  if (n > 0) {
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_void*)lds;
+    const int64_t base = (int64_t)it.kvh * a.capacity;
+    const uint32_t bytes = (uint32_t)a.capacity * D;
+    const __amdgpu_buffer_rsrc_t rk = rsrc_of(a.k + base * D, bytes);
+    const __amdgpu_buffer_rsrc_t rv = rsrc_of(a.v + base * D, bytes);
+    const float* const ks = a.k_scale + (base >> a.scale_shift);
+    const float* const vs = a.v_scale + (base >> a.scale_shift);
+    // K loads: a wave brings in 16 rows (of unit wave / 4), two loads of eight rows.
+    const int my_unit = wave / 4;
+    const uint32_t k_off = (uint32_t)((16 * (wave % 4) + lane / 8) * D +
+                                      ((lane % 8) ^ (lane / 16)) * 16);
+    const uint32_t k_dst = lds_base + (uint32_t)wave * 2048u;
+    auto load_k = [&](const Step& st, int stage) {
+      const uint32_t so = (uint32_t)(my_unit ? st.unit[1] : st.unit[0]) * (UNIT * D);
+      const uint32_t dst = k_dst + (uint32_t)stage * K_STAGE;
+      load_to_lds(dst, rk, k_off, so);
+      load_to_lds(dst + 1024u, rk, (k_off + 1024u) ^ 64u, so);
+    };
+    // V: the thread's 16 bytes (place 16 (tid % 4) of d = tid / 4) of each unit.
+    auto load_v = [&](const Step& st, VHold& h) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        h.w[u] = __builtin_amdgcn_raw_buffer_load_b128(rv, tid * 16, st.unit[u] * (UNIT * D), 0);
+    };
+    const int vd = tid / 4, vg = tid % 4;
+    auto scale_at = [&](const float* s, int unit) {
+      return s[(unit * UNIT) >> a.scale_shift];
+    };
+    auto store_v = [&](const Step& st, VHold& h, int stage) {
+      char* const to = lds + V_AT + stage * V_STAGE + vd * 256;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float scale = scale_at(vs, st.unit[u]);
+        if (st.left[u] < UNIT) {   // bytes of tokens that are not held: zeros
+          if (st.left[u] <= 0) scale = 1.f;   // a scale that no write has set
+          const int from = 4 * (fresh_lane() % 4);
+#pragma unroll
+          for (int kt = 0; kt < 4; ++kt) {
+            uint32_t keep = 0u;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              keep |= 16 * kt + from + r < st.left[u] ? 0xFFu << (8 * r) : 0u;
+            h.w[u][kt] &= keep;
+          }
+        }
+        *(bf16x8*)(to + (((8 * u + vg) ^ (vd % 16)) * 16)) = to_bf16(h.w[u][0], h.w[u][1], scale);
+        *(bf16x8*)(to + (((8 * u + 4 + vg) ^ (vd % 16)) * 16)) =
+            to_bf16(h.w[u][2], h.w[u][3], scale);
+      }
+    };
+    auto k_scales = [&](const Step& st) {
+      return (int)((__float_as_uint(scale_at(ks, st.unit[0])) >> 23) |
+                   (__float_as_uint(scale_at(ks, st.unit[1])) >> 23) << 8);
+    };
+    FragAt f;
+    f.k = (uint32_t)(i * D + ((g ^ (i / 2)) * 16));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) f.v[u] = (uint32_t)(i * 256 + (((4 * u + g) ^ i) * 16));
+
+    int lead_v = wave < 4;
+    asm("" : "+v"(lead_v));   // not known to be uniform: one loop, not one for each side
+    const bool lead = lead_v != 0;
+    const float scale = ka.scale_log2;
+    VHold hold;
+    Step cur = step_at(0), w1 = step_at(min(1, n - 1)), w2 = step_at(min(2, n - 1));
+    load_v(cur, hold);
+    load_k(cur, 0);
+    load_k(w1, 1);
+    store_v(cur, hold, 0);
+    if (!lead) load_v(w1, hold);
+    tile_sync();
+    Scores sc;
+    Probs pr;
+    score_from<0>(sc, lds, f, q, k_scales(cur));
+    mask_scores(sc, cur);
+    int keep = cur.keep;
+    if (lead) softmax_phase(sc, ts, pr, scale);
+    int ksc = k_scales(w1);
+    tile_barrier();
+    for (int j = 0; j < n; ++j) {
+      const int even = j & 1;
+      const char* const kj = lds + (even ^ 1) * K_STAGE;              // K(j+1)
+      const char* const vj = lds + V_AT + even * V_STAGE;             // V(j)
+      const Step w3 = step_at(min(j + 3, n - 1));
+      const int next_ksc = k_scales(w2);
+      if (lead) {
+        load_v(w1, hold);
+        matrix_phase(kj, vj, q, sc, pr, ts, f, ones, keep, ksc);
+        keep = w1.keep;
+        mask_scores(sc, w1);
+        tile_barrier();
+        asm volatile("" : "+v"(hold.w[0]), "+v"(hold.w[1]));   // V has arrived
+        load_k(w2, even);
+        store_v(w1, hold, even ^ 1);
+        softmax_phase(sc, ts, pr, scale);
+      } else {
+        asm volatile("" : "+v"(hold.w[0]), "+v"(hold.w[1]));
+        load_k(w2, even);
+        store_v(w1, hold, even ^ 1);
+        softmax_phase(sc, ts, pr, scale);
+        tile_barrier();
+        load_v(w2, hold);
+        matrix_phase(kj, vj, q, sc, pr, ts, f, ones, keep, ksc);
+        keep = w1.keep;
+        mask_scores(sc, w1);
+      }
+      tile_sync();
+      ksc = next_ksc;
+      w1 = w2;
+      w2 = w3;
+    }
+  }
+
+  // Every wave holds whole rows.
+  if (ka.p.splits == 1) {
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      int32_t head, token;
+      if (!row_of(it, a, 32 * wave + 16 * qt + i, head, token)) continue;
+      const float l = ts.l[qt][0];
+      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+      __bf16* const out =
+          (__bf16*)a.o + (int64_t)head * a.o_sh + (int64_t)token * a.o_st + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        bf16x4 b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = (__bf16)(ts.o[dt][qt][e] * inv);
+        *(bf16x4*)(out + 16 * dt) = b;
+      }
+    }
+    return;
+  }
+  const int64_t item = (int64_t)(id / ka.p.tiles / ka.p.splits) * ka.p.tiles + tile;
+  const int64_t slots = (int64_t)total * TILE_ROWS;
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const int64_t slot = (item * ka.p.splits + split) * TILE_ROWS + 32 * wave + 16 * qt + i;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt)
+      *(f32x4*)(a.workspace + slot * D + 16 * dt + 4 * g) = ts.o[dt][qt];
+    if (g == 0) {
+      a.workspace[slots * D + 2 * slot] = ts.m[qt];
+      a.workspace[slots * D + 2 * slot + 1] = ts.l[qt][0];
+    }
+  }
+}
+
+// Combines the splits of a row, in their order: 32 threads a row.
+__global__ __launch_bounds__(THREADS) void combine_kernel(KernelArgs ka) {
+  const CacheAttnArgs& a = ka.a;
+  const int32_t rows_item = ka.p.item_rows;
   const int32_t id = blockIdx.x / (rows_item / 8);
   const int r = blockIdx.x % (rows_item / 8) * 8 + threadIdx.x / 32, c = threadIdx.x % 32 * 4;
-  const Item it = item_of(ka, id);
-  const int32_t row = it.row0 + r;
-  if (row >= it.len * a.group) return;
+  const Item it = item_of(ka, id % ka.p.tiles, id / ka.p.tiles);
+  int32_t h, t;
+  if (!row_of(it, a, r, h, t)) return;
   const int64_t items = gridDim.x / (rows_item / 8);
   const int64_t slots = items * ka.p.splits * rows_item;
   const int64_t slot0 = (int64_t)id * ka.p.splits * rows_item + r;
@@ -322,28 +984,60 @@ __global__ __launch_bounds__(THREADS) void combine_kernel(KernelArgs ka, int32_t
     acc += f * *(const f32x4*)(a.workspace + slot * D + c);
   }
   const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-  const int32_t h = row / it.len, t = row - h * it.len;
   bf16x4 b;
 #pragma unroll
   for (int e = 0; e < 4; ++e) b[e] = (__bf16)(acc[e] * inv);
-  *(bf16x4*)((__bf16*)a.o + (int64_t)(it.kvh * a.group + h) * a.o_sh +
-             (int64_t)(it.first + t) * a.o_st + c) = b;
+  *(bf16x4*)((__bf16*)a.o + (int64_t)h * a.o_sh + (int64_t)t * a.o_st + c) = b;
 }
+
+// Items of a launch, without the splits.
+int64_t items_of(const Plan& p) { return (int64_t)p.heads * p.blocks * p.tiles; }
+
+// Tiles from this many rows a key head (with a mask, a query block and key head) on.
+constexpr int64_t TILE_FROM = 65;
 
 Plan plan_of(const CacheAttnArgs& a, int32_t cus) {
   Plan p;
   p.blocks = 1;
+  p.heads = a.heads;
   int64_t rows = (int64_t)a.n * a.group;
-  int64_t units = (a.n_tokens + UNIT - 1) / UNIT;
+  const int64_t units = (a.n_tokens + UNIT - 1) / UNIT;
+  int32_t blocks = 1;
   if (a.row_ptr) {
-    p.blocks = (a.q_start + a.n - 1) / a.mask_block - a.q_start / a.mask_block + 1;
+    blocks = (a.q_start + a.n - 1) / a.mask_block - a.q_start / a.mask_block + 1;
     rows = (int64_t)(a.n < a.mask_block ? a.n : a.mask_block) * a.group;
   }
-  p.rt = rows > 16 ? 2 : 1;
-  p.tiles = (int32_t)((rows + 16 * p.rt - 1) / (16 * p.rt));
+  p.tile = rows >= TILE_FROM;
+  if (p.tile) {
+    p.item_rows = TILE_ROWS;
+    if (a.row_ptr) {
+      const int32_t per = TILE_ROWS / a.mask_block;
+      p.heads = a.heads * a.group;
+      p.tiles = (blocks + per - 1) / per;
+    } else {
+      p.tiles = (int32_t)((rows + TILE_ROWS - 1) / TILE_ROWS);
+    }
+    // One workgroup a compute unit: the number of splits that ends first, in steps
+    // (a round of the grid takes its splits' steps and about TILE_FIXED more).
+    constexpr int64_t TILE_FIXED = 6;
+    const int64_t steps = (units + 1) / 2, items = items_of(p);
+    int64_t best = 0;
+    p.splits = 1;
+    for (int64_t s = 1; s <= 64 && (s == 1 || s <= steps / 2); ++s) {
+      const int64_t time = (items * s + cus - 1) / cus * ((steps + s - 1) / s + TILE_FIXED) +
+                           (s > 1 ? TILE_FIXED : 0);
+      if (s == 1 || time < best) {
+        best = time;
+        p.splits = (int32_t)s;
+      }
+    }
+    return p;
+  }
+  p.blocks = blocks;
+  p.item_rows = rows > 16 ? 32 : 16;
+  p.tiles = (int32_t)((rows + p.item_rows - 1) / p.item_rows);
   // Two workgroups a compute unit; a wave's share is at least two units.
-  const int64_t items = (int64_t)a.heads * p.blocks * p.tiles;
-  int64_t splits = 2 * cus / items;
+  int64_t splits = 2 * cus / items_of(p);
   if (splits > units / (2 * WAVES)) splits = units / (2 * WAVES);
   p.splits = splits < 1 ? 1 : (int32_t)splits;
   return p;
@@ -353,8 +1047,7 @@ Plan plan_of(const CacheAttnArgs& a, int32_t cus) {
 
 int64_t cache_attention_workspace(const CacheAttnArgs& a, int32_t cus) {
   const Plan p = plan_of(a, cus);
-  if (p.splits == 1) return 0;
-  return (int64_t)a.heads * p.blocks * p.tiles * p.splits * 16 * p.rt * (D + 2) * 4;
+  return p.splits == 1 ? 0 : items_of(p) * p.splits * p.item_rows * (D + 2) * 4;
 }
 
 hipError_t launch_cache_attention(const CacheAttnArgs& a, int32_t cus, hipStream_t stream) {
@@ -362,14 +1055,22 @@ hipError_t launch_cache_attention(const CacheAttnArgs& a, int32_t cus, hipStream
   k.a = a;
   k.p = plan_of(a, cus);
   k.scale_log2 = 1.4426950408889634f / 11.313708498984761f;   // log2(e) / sqrt(128)
-  const int64_t items = (int64_t)a.heads * k.p.blocks * k.p.tiles;
+  const int64_t items = items_of(k.p);
   const dim3 grid((uint32_t)(items * k.p.splits));
-  if (k.p.rt == 1)
+  if (k.p.tile) {
+    if (!a.row_ptr)
+      tile_kernel<0><<<grid, TILE_THREADS, 0, stream>>>(k);
+    else if (a.mask_block == 64)
+      tile_kernel<64><<<grid, TILE_THREADS, 0, stream>>>(k);
+    else
+      tile_kernel<128><<<grid, TILE_THREADS, 0, stream>>>(k);
+  } else if (k.p.item_rows == 16) {
     rows_kernel<1><<<grid, THREADS, 0, stream>>>(k);
-  else
+  } else {
     rows_kernel<2><<<grid, THREADS, 0, stream>>>(k);
+  }
   if (hipError_t e = hipGetLastError(); e != hipSuccess || k.p.splits == 1) return e;
-  combine_kernel<<<dim3((uint32_t)(items * (k.p.rt * 2))), THREADS, 0, stream>>>(k, 16 * k.p.rt);
+  combine_kernel<<<dim3((uint32_t)(items * (k.p.item_rows / 8))), THREADS, 0, stream>>>(k);
   return hipGetLastError();
 }
 
