@@ -14,6 +14,8 @@
 // unit ahead: nothing is shared between waves but the final combination.  With
 // splits > 1 partial results (fp32 O, reference m and row sum l) go to the
 // workspace and a second kernel combines them in the order of the splits.
+#include <type_traits>
+
 #include "values.h"
 
 namespace lvsa {
@@ -345,8 +347,10 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
 // step.  Half steps 2j and 2j + 1: the leaders (waves 0-3) are in matrix phase j, then
 // softmax j + 1; the others in softmax j, then matrix phase j.  K(j+1) and V(j) stay
 // in LDS through both; K(j+2) and V(j+1) go into the other two stages, by every wave
-// in its softmax phase: K straight from memory to LDS, V from registers that the
-// wave's matrix phase before loaded.
+// in its softmax phase.  Both come straight from memory into LDS; V's bytes into a
+// place of each wave's own, from which the wave takes them a step later, converts
+// them and writes them into the stage (held in registers meanwhile, 8 of them, they
+// made the compiler spill).
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -356,7 +360,8 @@ constexpr int TILE_THREADS = 512;
 constexpr int K_STAGE = 2 * UNIT * D;        // 128 rows of 128 bytes
 constexpr int V_STAGE = 2 * UNIT * D * 2;    // 128 rows (d) of 256 bytes (keys)
 constexpr int V_AT = 2 * K_STAGE;
-constexpr int LIST_AT = V_AT + 2 * V_STAGE;
+constexpr int RAW_AT = V_AT + 2 * V_STAGE;   // V's bytes of a step
+constexpr int LIST_AT = RAW_AT + K_STAGE;
 constexpr int LIST_WORDS = kMaxSparseBlocks;
 constexpr int BITMAP_WORDS = 256;
 static_assert(BITMAP_WORDS * 32 >= LIST_WORDS, "a bit a block");
@@ -366,11 +371,15 @@ constexpr int TILE_LDS = LIST_AT + LIST_WORDS * 4 + 64;
 constexpr float HEADROOM = 7.f;
 constexpr float WIDE_HEADROOM = 39.f;
 
-// LDS layouts.  K stage: row = key, 8 chunks of 16 bytes, chunk c at place c ^ (row/2 % 8).
-// V stage: row = d, 16 chunks of 8 keys in bf16, chunk c at place c ^ (row % 16); chunk
-// 4u + g holds the keys that lane group g's P registers hold of the 32-key group u
-// (tokens 32u + 4g + r and 32u + 16 + 4g + r).  Both spread the 16 rows that a read takes
-// at one chunk over all banks.
+// LDS layout: slabs of rows of 64 bytes (four chunks of 16), chunk c of row r at place
+// c ^ x(r), x(r) = -(r/4) mod 4.  The 64 lanes of a fragment read 16 rows whole, chunk g
+// of row i for lane (g, i); a read is served 16 lanes at a time, four rows' worth of
+// banks, and x puts the four lanes that share a row's banks at four chunks.
+//   K stage: slab h (elements 64h .. 64h+63), row = key, 128 rows
+//   V stage: slab u (keys of the 32-key group u), row = d, 128 rows; chunk g holds the
+//   keys that lane group g's P registers hold: tokens 32u + 4g + r, 32u + 16 + 4g + r
+constexpr int SLAB = 128 * 64;
+__device__ __forceinline__ int xsw(int row) { return -(row >> 2) & 3; }
 
 // One wave load (1 KiB) from memory into LDS.  Inline assembly, so that the compiler
 // puts no wait for it between here and the half step's end, where tile_sync waits.
@@ -465,7 +474,7 @@ __device__ __forceinline__ void q_split(QSplit& q, const __bf16* row, bool ok) {
 
 struct TileState {
   f32x4 o[8][2];   // O^T [d tile][query tile]
-  f32x4 l[2];      // row sums, in register 0
+  f32x4 l;         // row sums: register 0 of query tile 0, register 1 of query tile 1
   float m[2];      // references (log2)
   int flags;       // READY: every row has a finite m; WIDE: a step was redone
 };
@@ -478,19 +487,14 @@ struct Probs {
   bf16x8 p[4][2];  // [32-key group][query tile]
 };
 
-// Per-lane LDS offsets of the fragments.
-struct FragAt {
-  uint32_t k;        // K row i, chunk g (chunk 4 + g at ^ 64)
-  uint32_t v[4];     // V row i, chunk 4u + g
-};
-
-__device__ __forceinline__ i32x8 k_frag(const char* k, const FragAt& f, int kt) {
-  const i32x4 a = *(const i32x4*)(k + f.k + kt * 16 * D);
-  const i32x4 b = *(const i32x4*)(k + (f.k ^ 64u) + kt * 16 * D);
+// Fragments: `at` is the lane's offset in a slab's first 16 rows.
+__device__ __forceinline__ i32x8 k_frag(const char* k, uint32_t at, int kt) {
+  const i32x4 a = *(const i32x4*)(k + at + kt * 1024);
+  const i32x4 b = *(const i32x4*)(k + at + kt * 1024 + SLAB);
   return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
-__device__ __forceinline__ bf16x8 v_frag(const char* v, const FragAt& f, int dt, int u) {
-  return *(const bf16x8*)(v + f.v[u] + dt * 16 * 256);
+__device__ __forceinline__ bf16x8 v_frag(const char* v, uint32_t at, int dt, int u) {
+  return *(const bf16x8*)(v + at + dt * 1024 + u * SLAB);
 }
 template <int KT>
 __device__ __forceinline__ void score_tile(Scores& sc, const i32x8& f, const QSplit& q,
@@ -505,10 +509,11 @@ __device__ __forceinline__ void score_tile(Scores& sc, const i32x8& f, const QSp
   }
 }
 template <int KT>
-__device__ __forceinline__ void score_from(Scores& sc, const char* k, const FragAt& f,
+__device__ __forceinline__ void score_from(Scores& sc, const char* k, uint32_t f,
                                            const QSplit& q, int k_scale) {
   if constexpr (KT < 8) {
     score_tile<KT>(sc, k_frag(k, f, KT), q, k_scale);
+    __builtin_amdgcn_sched_barrier(0);
     score_from<KT + 1>(sc, k, f, q, k_scale);
   }
 }
@@ -548,7 +553,7 @@ __device__ __forceinline__ void raise(const Scores& sc, TileState& st, float sca
     const float m = top > st.m[qt] ? top + head : st.m[qt] + lift;
     const float f = m == st.m[qt] ? 1.f : __builtin_amdgcn_exp2f(st.m[qt] - m);
     st.m[qt] = m;
-    st.l[qt][0] *= f;
+    st.l[qt] *= f;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) st.o[dt][qt] *= f;
   }
@@ -604,19 +609,29 @@ __device__ __forceinline__ void softmax_phase(const Scores& sc, TileState& st, P
   }
 }
 
+// A operand of the row sums of query tile qt: ones in rows qt, 4 + qt, 8 + qt, 12 + qt,
+// which are register qt of every lane of the result.  Made anew each time: kept, it
+// would hold eight registers.
+__device__ __forceinline__ bf16x8 sum_rows(int qt) {
+  const uint32_t w = fresh_lane() % 4 == qt ? 0x3F803F80u : 0u;
+  return __builtin_bit_cast(bf16x8, u32x4{w, w, w, w});
+}
+
 // l += row sums of P, O += P V, S = K Q^T of the next step.  V of a unit that the wave's
-// query block does not keep is left out: what it holds never reaches the block.
+// query block does not keep is left out: what it holds never reaches the block.  UNITS:
+// the units that a block keeps or not as one (2: the step whole), 0: it keeps all.
+template <int UNITS>
 __device__ __forceinline__ void matrix_phase(const char* k, const char* v, const QSplit& q,
                                              Scores& sc, const Probs& pr, TileState& st,
-                                             const FragAt& f, const bf16x8& ones, int keep,
+                                             uint32_t f, int keep,
                                              int k_scale) {
-  if (keep != 3) {
+  if (UNITS && keep != 3) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      if (!((keep >> (u / 2)) & 1)) continue;
+      if (UNITS == 2 || !((keep >> (u / 2)) & 1)) continue;
 #pragma unroll
       for (int qt = 0; qt < 2; ++qt)
-        st.l[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pr.p[u][qt], st.l[qt], 0, 0, 0);
+        st.l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sum_rows(qt), pr.p[u][qt], st.l, 0, 0, 0);
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) {
         const bf16x8 x = v_frag(v, f, dt, u);
@@ -624,6 +639,7 @@ __device__ __forceinline__ void matrix_phase(const char* k, const char* v, const
         for (int qt = 0; qt < 2; ++qt)
           st.o[dt][qt] =
               __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pr.p[u][qt], st.o[dt][qt], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     score_from<0>(sc, k, f, q, k_scale);
@@ -636,12 +652,14 @@ __device__ __forceinline__ void matrix_phase(const char* k, const char* v, const
   for (int i = 0; i < AHEAD; ++i) fr[i] = v_frag(v, f, i / 4, i % 4);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int qt = 0; qt < 2; ++qt)
+  for (int qt = 0; qt < 2; ++qt) {
+    const bf16x8 ones = sum_rows(qt);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      st.l[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pr.p[u][qt], st.l[qt], 0, 0, 0);
+      st.l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pr.p[u][qt], st.l, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
+  }
   // Chains of four MFMAs into one accumulator; consecutive chains share an operand.
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt)
@@ -674,11 +692,6 @@ __device__ __forceinline__ void matrix_phase(const char* k, const char* v, const
   score_tile<7>(sc, kf[7], q, k_scale);
 #undef SCORE_TILE
 }
-
-// V bytes of a step that a thread converts: 16 places of one d in each unit.
-struct VHold {
-  u32x4 w[2];
-};
 
 // The union of the CSR rows block0 .. block0 + count - 1 (at most four) as words in
 // `list`, ascending: key block in bits 0..27, bit 28 + r set when row r keeps it.
@@ -802,13 +815,10 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
   for (int qt = 0; qt < 2; ++qt) {
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) ts.o[dt][qt] = f32x4{};
-    ts.l[qt] = f32x4{};
     ts.m[qt] = -__builtin_inff();
   }
+  ts.l = f32x4{};
   ts.flags = 0;
-  bf16x8 ones;   // rows 0, 4, 8, 12 of the row sums' A operand: register 0 of every lane
-#pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = lane % 4 == 0 ? (__bf16)1.f : (__bf16)0.f;
 
   if (n > 0) {
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_void*)lds;
@@ -818,29 +828,38 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     const __amdgpu_buffer_rsrc_t rv = rsrc_of(a.v + base * D, bytes);
     const float* const ks = a.k_scale + (base >> a.scale_shift);
     const float* const vs = a.v_scale + (base >> a.scale_shift);
-    // K loads: a wave brings in 16 rows (of unit wave / 4), two loads of eight rows.
-    const int my_unit = wave / 4;
-    const uint32_t k_off = (uint32_t)((16 * (wave % 4) + lane / 8) * D +
-                                      ((lane % 8) ^ (lane / 16)) * 16);
-    const uint32_t k_dst = lds_base + (uint32_t)wave * 2048u;
+    // Loads into LDS, 1 KiB each.  K: a wave brings in 16 keys, both slabs, of unit
+    // wave / 4.  V: 16 columns d of each unit, as they lie.
+    const uint32_t k_off = (uint32_t)((16 * (wave % 4) + lane / 4) * D +
+                                      ((lane % 4) ^ xsw(lane / 4)) * 16);
+    const uint32_t dst0 = lds_base + (uint32_t)wave * 1024u;
     auto load_k = [&](const Step& st, int stage) {
-      const uint32_t so = (uint32_t)(my_unit ? st.unit[1] : st.unit[0]) * (UNIT * D);
-      const uint32_t dst = k_dst + (uint32_t)stage * K_STAGE;
+      const uint32_t so = (uint32_t)(wave / 4 ? st.unit[1] : st.unit[0]) * (UNIT * D);
+      const uint32_t dst = dst0 + (uint32_t)stage * K_STAGE;
       load_to_lds(dst, rk, k_off, so);
-      load_to_lds(dst + 1024u, rk, (k_off + 1024u) ^ 64u, so);
+      load_to_lds(dst + SLAB, rk, k_off, so + 64u);
     };
-    // V: the thread's 16 bytes (place 16 (tid % 4) of d = tid / 4) of each unit.
-    auto load_v = [&](const Step& st, VHold& h) {
+    auto load_v = [&](const Step& st) {
+      const uint32_t so = (uint32_t)wave * 1024u;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        h.w[u] = __builtin_amdgcn_raw_buffer_load_b128(rv, tid * 16, st.unit[u] * (UNIT * D), 0);
+        load_to_lds(dst0 + RAW_AT + u * SLAB, rv, (uint32_t)lane * 16u,
+                    (uint32_t)st.unit[u] * (UNIT * D) + so);
     };
-    const int vd = tid / 4, vg = tid % 4;
     auto scale_at = [&](const float* s, int unit) {
       return s[(unit * UNIT) >> a.scale_shift];
     };
-    auto store_v = [&](const Step& st, VHold& h, int stage) {
-      char* const to = lds + V_AT + stage * V_STAGE + vd * 256;
+    // The thread's 16 places (16 (tid % 4) .. of d = tid / 4) of each unit, taken from the
+    // wave's raw bytes, and converted into the stage.
+    const char* const raw = lds + RAW_AT + tid * 16;
+    char* const v_to = lds + V_AT + (tid / 4) * 64 + ((tid % 4) ^ xsw(tid / 4)) * 16;
+    auto take_v = [&](u32x4 (&w)[2]) {
+      w[0] = *(const u32x4*)raw;
+      w[1] = *(const u32x4*)(raw + SLAB);
+      // Read before the next loads into the same place are issued.
+      asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(w[0]), "+v"(w[1]) : : "memory");
+    };
+    auto store_v = [&](const Step& st, u32x4 (&w)[2], int stage) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         float scale = scale_at(vs, st.unit[u]);
@@ -853,75 +872,79 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
               keep |= 16 * kt + from + r < st.left[u] ? 0xFFu << (8 * r) : 0u;
-            h.w[u][kt] &= keep;
+            w[u][kt] &= keep;
           }
         }
-        *(bf16x8*)(to + (((8 * u + vg) ^ (vd % 16)) * 16)) = to_bf16(h.w[u][0], h.w[u][1], scale);
-        *(bf16x8*)(to + (((8 * u + 4 + vg) ^ (vd % 16)) * 16)) =
-            to_bf16(h.w[u][2], h.w[u][3], scale);
+        *(bf16x8*)(v_to + stage * V_STAGE + (2 * u) * SLAB) = to_bf16(w[u][0], w[u][1], scale);
+        *(bf16x8*)(v_to + stage * V_STAGE + (2 * u + 1) * SLAB) =
+            to_bf16(w[u][2], w[u][3], scale);
       }
     };
     auto k_scales = [&](const Step& st) {
       return (int)((__float_as_uint(scale_at(ks, st.unit[0])) >> 23) |
                    (__float_as_uint(scale_at(ks, st.unit[1])) >> 23) << 8);
     };
-    FragAt f;
-    f.k = (uint32_t)(i * D + ((g ^ (i / 2)) * 16));
-#pragma unroll
-    for (int u = 0; u < 4; ++u) f.v[u] = (uint32_t)(i * 256 + (((4 * u + g) ^ i) * 16));
+    const uint32_t f = (uint32_t)(i * 64 + (g ^ xsw(i)) * 16);
 
-    int lead_v = wave < 4;
-    asm("" : "+v"(lead_v));   // not known to be uniform: one loop, not one for each side
-    const bool lead = lead_v != 0;
+    const bool lead = wave < 4;
     const float scale = ka.scale_log2;
-    VHold hold;
-    Step cur = step_at(0), w1 = step_at(min(1, n - 1)), w2 = step_at(min(2, n - 1));
-    load_v(cur, hold);
-    load_k(cur, 0);
-    load_k(w1, 1);
-    store_v(cur, hold, 0);
-    if (!lead) load_v(w1, hold);
-    tile_sync();
+    Step w1 = step_at(min(1, n - 1)), w2 = step_at(min(2, n - 1));
     Scores sc;
     Probs pr;
-    score_from<0>(sc, lds, f, q, k_scales(cur));
-    mask_scores(sc, cur);
-    int keep = cur.keep;
-    if (lead) softmax_phase(sc, ts, pr, scale);
-    int ksc = k_scales(w1);
-    tile_barrier();
-    for (int j = 0; j < n; ++j) {
-      const int even = j & 1;
-      const char* const kj = lds + (even ^ 1) * K_STAGE;              // K(j+1)
-      const char* const vj = lds + V_AT + even * V_STAGE;             // V(j)
-      const Step w3 = step_at(min(j + 3, n - 1));
-      const int next_ksc = k_scales(w2);
-      if (lead) {
-        load_v(w1, hold);
-        matrix_phase(kj, vj, q, sc, pr, ts, f, ones, keep, ksc);
-        keep = w1.keep;
-        mask_scores(sc, w1);
-        tile_barrier();
-        asm volatile("" : "+v"(hold.w[0]), "+v"(hold.w[1]));   // V has arrived
-        load_k(w2, even);
-        store_v(w1, hold, even ^ 1);
-        softmax_phase(sc, ts, pr, scale);
-      } else {
-        asm volatile("" : "+v"(hold.w[0]), "+v"(hold.w[1]));
-        load_k(w2, even);
-        store_v(w1, hold, even ^ 1);
-        softmax_phase(sc, ts, pr, scale);
-        tile_barrier();
-        load_v(w2, hold);
-        matrix_phase(kj, vj, q, sc, pr, ts, f, ones, keep, ksc);
-        keep = w1.keep;
-        mask_scores(sc, w1);
-      }
+    int keep;
+    {
+      const Step w0 = step_at(0);
+      u32x4 w[2];
+      load_v(w0);
+      load_k(w0, 0);
+      load_k(w1, 1);
       tile_sync();
-      ksc = next_ksc;
-      w1 = w2;
-      w2 = w3;
+      take_v(w);
+      load_v(w1);
+      store_v(w0, w, 0);
+      score_from<0>(sc, lds, f, q, k_scales(w0));
+      keep = w0.keep;
+      mask_scores(sc, w0);
+      if (lead) softmax_phase(sc, ts, pr, scale);
     }
+    int ksc = k_scales(w1);
+    tile_sync();
+    auto walk = [&](auto leading) {
+      constexpr bool LEAD = decltype(leading)::value;
+      for (int j = 0; j < n; ++j) {
+        const int even = j & 1;
+        const char* const kj = lds + (even ^ 1) * K_STAGE;              // K(j+1)
+        const char* const vj = lds + V_AT + even * V_STAGE;             // V(j)
+        const Step w3 = step_at(min(j + 3, n - 1));
+        const int next_ksc = k_scales(w2);
+        if (LEAD) {
+          matrix_phase<MB / UNIT>(kj, vj, q, sc, pr, ts, f, keep, ksc);
+          keep = w1.keep;
+          mask_scores(sc, w1);
+          tile_barrier();
+        }
+        u32x4 w[2];
+        take_v(w);
+        load_k(w2, even);
+        load_v(w2);
+        store_v(w1, w, even ^ 1);
+        softmax_phase(sc, ts, pr, scale);
+        if (!LEAD) {
+          tile_barrier();
+          matrix_phase<MB / UNIT>(kj, vj, q, sc, pr, ts, f, keep, ksc);
+          keep = w1.keep;
+          mask_scores(sc, w1);
+        }
+        tile_sync();
+        ksc = next_ksc;
+        w1 = w2;
+        w2 = w3;
+      }
+    };
+    if (lead)
+      walk(std::true_type{});
+    else
+      walk(std::false_type{});
   }
 
   // Every wave holds whole rows.
@@ -930,7 +953,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     for (int qt = 0; qt < 2; ++qt) {
       int32_t head, token;
       if (!row_of(it, a, 32 * wave + 16 * qt + i, head, token)) continue;
-      const float l = ts.l[qt][0];
+      const float l = ts.l[qt];
       const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
       __bf16* const out =
           (__bf16*)a.o + (int64_t)head * a.o_sh + (int64_t)token * a.o_st + 4 * g;
@@ -954,7 +977,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
       *(f32x4*)(a.workspace + slot * D + 16 * dt + 4 * g) = ts.o[dt][qt];
     if (g == 0) {
       a.workspace[slots * D + 2 * slot] = ts.m[qt];
-      a.workspace[slots * D + 2 * slot + 1] = ts.l[qt][0];
+      a.workspace[slots * D + 2 * slot + 1] = ts.l[qt];
     }
   }
 }
