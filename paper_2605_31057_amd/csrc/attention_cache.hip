@@ -115,23 +115,22 @@ __device__ __forceinline__ float row_max(float x) {
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
-// One unit's K and V bytes of a lane (group g = lane/16, i = lane%16).  K: rows
-// 16kt + i, elements 16g .. +15 and 64 + 16g .. +15.  V: columns d = 16dt + i,
-// places 16g .. +15, tokens 16kt + 4g + r of the unit in the order (kt, r).
-struct UnitData {
-  u32x4 k[4][2];
-  u32x4 v[8];
-  float k_scale, v_scale;
-  int32_t key0;        // first token; at or past n_tokens: nothing to do
-};
-
+// RT: 16-row tiles of the item, each K and V fragment is used for all of them.  A wave
+// holds one unit's bytes: K's of the next unit are loaded when this one's scores are
+// done, V's when its products are, so both are on their way for most of a unit, and
+// with two waves a SIMD (one from 33 rows on, for the registers) a compute unit has
+// some 64 KB in flight.
+//
+// A lane (group g = lane/16, i = lane%16) takes K rows 16kt + i, elements 16g .. +15 and
+// 64 + 16g .. +15, and V columns d = 16dt + i, places 16g .. +15, which are tokens 16kt + 4g
+// + r of the unit in the order (kt, r): what its score registers hold.
 template <int RT>
 __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelArgs ka) {
   constexpr int ROWS = 16 * RT;
   const CacheAttnArgs& a = ka.a;
   __shared__ __attribute__((aligned(16))) float lds_o[WAVES][ROWS][D + 4];
   __shared__ float lds_m[WAVES][ROWS], lds_l[WAVES][ROWS];
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int g = lane / 16, i = lane % 16;
   const int32_t split = blockIdx.x % ka.p.splits, id = blockIdx.x / ka.p.splits;
   const Item it = item_of(ka, id % ka.p.tiles, id / ka.p.tiles);
@@ -160,32 +159,32 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
   }
 
   const int64_t base = (int64_t)it.kvh * a.capacity;
-  const uint8_t* const kb = a.k + (base + i) * D + 16 * g;
-  const uint8_t* const vb = a.v + base * D + i * UNIT + 16 * g;
+  const uint8_t* const kb = a.k + base * D;
+  const uint8_t* const vb = a.v + base * D;
+  const uint32_t k_lane = i * D + 16 * g, v_lane = i * UNIT + 16 * g;
   const float* const ks = a.k_scale + (base >> a.scale_shift);
   const float* const vs = a.v_scale + (base >> a.scale_shift);
-  auto load = [&](int32_t u, UnitData& d) {
-    d.key0 = a.n_tokens;
-    if (u >= u1) return;
-    int32_t unit = u;
-    if (a.row_ptr) {
-      const int32_t kblock = a.col_idx[walk + u / per];
-      if ((uint32_t)kblock >= (uint32_t)a.mask_blocks) return;
-      unit = kblock * per + u % per;
-    }
-    const int32_t key0 = __builtin_amdgcn_readfirstlane(unit * UNIT);
-    d.key0 = key0;
-    if (key0 >= a.n_tokens) return;
+  // First token of the walk's unit u; n_tokens where there is none.
+  auto key_of = [&](int32_t u) -> int32_t {
+    if (u >= u1) return a.n_tokens;
+    if (!a.row_ptr) return u * UNIT;
+    const int32_t block = __builtin_amdgcn_readfirstlane(a.col_idx[walk + u / per]);
+    if ((uint32_t)block >= (uint32_t)a.mask_blocks) return a.n_tokens;
+    return min((block * per + u % per) * UNIT, a.n_tokens);
+  };
+  u32x4 k[4][2], v[8];
+  auto load_k = [&](int32_t key0) {
+    const uint8_t* const at = kb + (int64_t)key0 * D;
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
       for (int half = 0; half < 2; ++half)
-        d.k[kt][half] = *(const u32x4*)(kb + (int64_t)(key0 + 16 * kt) * D + 64 * half);
+        k[kt][half] = *(const u32x4*)(at + k_lane + kt * 16 * D + 64 * half);
+  };
+  auto load_v = [&](int32_t key0) {
+    const uint8_t* const at = vb + (int64_t)key0 * D;
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt)
-      d.v[dt] = *(const u32x4*)(vb + (int64_t)key0 * D + dt * 16 * UNIT);
-    d.k_scale = ks[key0 >> a.scale_shift];
-    d.v_scale = vs[key0 >> a.scale_shift];
+    for (int dt = 0; dt < 8; ++dt) v[dt] = *(const u32x4*)(at + v_lane + dt * 16 * UNIT);
   };
 
   f32x4 o[8][RT];
@@ -197,8 +196,25 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) o[dt][rt] = f32x4{};
   }
-  auto work = [&](UnitData& d) {
-    if (d.key0 >= a.n_tokens) return;
+  // Units of the wave: u0 + wave, then every fourth.  Columns outside the mask are
+  // passed over (their place holds no tokens).
+  int32_t u = u0 + wave;
+  auto next_unit = [&]() -> int32_t {
+    int32_t key = a.n_tokens;
+    while (u < u1 && key >= a.n_tokens) {
+      key = key_of(u);
+      u += WAVES;
+    }
+    return key;
+  };
+  int32_t key0 = next_unit();
+  if (key0 < a.n_tokens) {
+    load_k(key0);
+    load_v(key0);
+  }
+  while (key0 < a.n_tokens) {
+    const int32_t key1 = next_unit();
+    const float k_scale = ks[key0 >> a.scale_shift], v_scale = vs[key0 >> a.scale_shift];
     f32x4 s[4][RT];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
@@ -206,15 +222,18 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
       for (int rt = 0; rt < RT; ++rt) s[kt][rt] = f32x4{};
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
-        const u32x4 w = d.k[kt][st / 2];
-        const bf16x8 f = to_bf16(w[(st % 2) * 2], w[(st % 2) * 2 + 1], d.k_scale);
+        const u32x4 w = k[kt][st / 2];
+        const bf16x8 f = to_bf16(w[(st % 2) * 2], w[(st % 2) * 2 + 1], k_scale);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
           s[kt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[rt][st], s[kt][rt], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (key1 < a.n_tokens) load_k(key1);
+    __builtin_amdgcn_sched_barrier(0);
     // Keys at or past n_tokens: no weight, and V bytes of zero whatever they hold.
-    const int32_t left = a.n_tokens - d.key0;
+    const int32_t left = a.n_tokens - key0;
     if (left < UNIT) {
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
@@ -227,7 +246,7 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
           for (int rt = 0; rt < RT; ++rt) s[kt][rt][r] = ok ? s[kt][rt][r] : -__builtin_inff();
         }
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) d.v[dt][kt] &= keep;
+        for (int dt = 0; dt < 8; ++dt) v[dt][kt] &= keep;
       }
     }
     bf16x8 p[RT][2];
@@ -263,20 +282,14 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
     for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const bf16x8 f = to_bf16(d.v[dt][2 * half], d.v[dt][2 * half + 1], d.v_scale);
+        const bf16x8 f = to_bf16(v[dt][2 * half], v[dt][2 * half + 1], v_scale);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
           o[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, p[rt][half], o[dt][rt], 0, 0, 0);
       }
-  };
-
-  UnitData d0, d1;
-  load(u0 + wave, d0);
-  for (int32_t u = u0 + wave; u < u1; u += 2 * WAVES) {
-    load(u + WAVES, d1);
-    work(d0);
-    load(u + 2 * WAVES, d0);
-    work(d1);
+    __builtin_amdgcn_sched_barrier(0);
+    if (key1 < a.n_tokens) load_v(key1);
+    key0 = key1;
   }
 
   // The waves' parts, combined in LDS in the waves' order.
@@ -982,29 +995,59 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
   }
 }
 
-// Combines the splits of a row, in their order: 32 threads a row.
+// Combines the splits of the rows.  GROUPS * 32 threads a row, each taking every
+// GROUPS-th split of four elements, then the groups in their order: with many splits
+// their loads are on their way together (42 splits of 12 rows: 25 us one split after the
+// other, 4 so).
+template <int GROUPS>
 __global__ __launch_bounds__(THREADS) void combine_kernel(KernelArgs ka) {
+  constexpr int BLOCK_ROWS = 8 / GROUPS;
+  __shared__ f32x4 part[GROUPS > 1 ? GROUPS : 1][32];
+  __shared__ float part_l[GROUPS > 1 ? GROUPS : 1];
   const CacheAttnArgs& a = ka.a;
-  const int32_t rows_item = ka.p.item_rows;
-  const int32_t id = blockIdx.x / (rows_item / 8);
-  const int r = blockIdx.x % (rows_item / 8) * 8 + threadIdx.x / 32, c = threadIdx.x % 32 * 4;
+  const int32_t rows_item = ka.p.item_rows, splits = ka.p.splits;
+  const int32_t blocks = rows_item / BLOCK_ROWS;      // of an item
+  const int32_t id = blockIdx.x / blocks;
+  const int grp = GROUPS > 1 ? threadIdx.x / 32 : 0, c = threadIdx.x % 32 * 4;
+  const int r = blockIdx.x % blocks * BLOCK_ROWS + (GROUPS > 1 ? 0 : threadIdx.x / 32);
   const Item it = item_of(ka, id % ka.p.tiles, id / ka.p.tiles);
   int32_t h, t;
   if (!row_of(it, a, r, h, t)) return;
-  const int64_t items = gridDim.x / (rows_item / 8);
-  const int64_t slots = items * ka.p.splits * rows_item;
-  const int64_t slot0 = (int64_t)id * ka.p.splits * rows_item + r;
-  const float* ml = a.workspace + slots * D;
-  float top = -__builtin_inff(), sum = 0.f;
-  for (int s = 0; s < ka.p.splits; ++s)
-    top = fmaxf(top, ml[2 * (slot0 + (int64_t)s * rows_item)]);
+  const int64_t slots = (int64_t)(gridDim.x / blocks) * splits * rows_item;
+  const int64_t slot0 = (int64_t)id * splits * rows_item + r;
+  const float* const ml = a.workspace + slots * D;
+  float top = -__builtin_inff();
+  if (GROUPS > 1) {
+    for (int s = threadIdx.x % 64; s < splits; s += 64)
+      top = fmaxf(top, ml[2 * (slot0 + (int64_t)s * rows_item)]);
+#pragma unroll
+    for (int off = 32; off > 0; off /= 2) top = fmaxf(top, __shfl_xor(top, off));
+  } else {
+    for (int s = 0; s < splits; ++s)
+      top = fmaxf(top, ml[2 * (slot0 + (int64_t)s * rows_item)]);
+  }
   f32x4 acc = {};
-  for (int s = 0; s < ka.p.splits; ++s) {
+  float sum = 0.f;
+#pragma unroll 4
+  for (int s = grp; s < splits; s += GROUPS) {
     const int64_t slot = slot0 + (int64_t)s * rows_item;
-    const float ms = ml[2 * slot];
+    const float ms = ml[2 * slot], ls = ml[2 * slot + 1];
+    const f32x4 os = *(const f32x4*)(a.workspace + slot * D + c);
     const float f = ms == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ms - top);
-    sum += f * ml[2 * slot + 1];
-    acc += f * *(const f32x4*)(a.workspace + slot * D + c);
+    sum += f * ls;
+    acc += f * os;
+  }
+  if (GROUPS > 1) {
+    part[grp][threadIdx.x % 32] = acc;
+    if (c == 0) part_l[grp] = sum;
+    __syncthreads();
+    if (grp > 0) return;
+    sum = part_l[0];
+#pragma unroll
+    for (int p = 1; p < GROUPS; ++p) {
+      acc += part[p][threadIdx.x];
+      sum += part_l[p];
+    }
   }
   const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
   bf16x4 b;
@@ -1057,10 +1100,10 @@ Plan plan_of(const CacheAttnArgs& a, int32_t cus) {
     return p;
   }
   p.blocks = blocks;
-  p.item_rows = rows > 16 ? 32 : 16;
+  p.item_rows = rows > 32 ? 64 : rows > 16 ? 32 : 16;
   p.tiles = (int32_t)((rows + p.item_rows - 1) / p.item_rows);
   // Two workgroups a compute unit; a wave's share is at least two units.
-  int64_t splits = 2 * cus / items_of(p);
+  int64_t splits = (p.item_rows > 32 ? 1 : 2) * (int64_t)cus / items_of(p);
   if (splits > units / (2 * WAVES)) splits = units / (2 * WAVES);
   p.splits = splits < 1 ? 1 : (int32_t)splits;
   return p;
@@ -1089,11 +1132,16 @@ hipError_t launch_cache_attention(const CacheAttnArgs& a, int32_t cus, hipStream
       tile_kernel<128><<<grid, TILE_THREADS, 0, stream>>>(k);
   } else if (k.p.item_rows == 16) {
     rows_kernel<1><<<grid, THREADS, 0, stream>>>(k);
-  } else {
+  } else if (k.p.item_rows == 32) {
     rows_kernel<2><<<grid, THREADS, 0, stream>>>(k);
+  } else {
+    rows_kernel<4><<<grid, THREADS, 0, stream>>>(k);
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess || k.p.splits == 1) return e;
-  combine_kernel<<<dim3((uint32_t)(items * (k.p.item_rows / 8))), THREADS, 0, stream>>>(k);
+  if (k.p.splits > 4)
+    combine_kernel<8><<<dim3((uint32_t)(items * k.p.item_rows)), THREADS, 0, stream>>>(k);
+  else
+    combine_kernel<1><<<dim3((uint32_t)(items * (k.p.item_rows / 8))), THREADS, 0, stream>>>(k);
   return hipGetLastError();
 }
 
