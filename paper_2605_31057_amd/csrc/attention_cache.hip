@@ -14,8 +14,6 @@
 // unit ahead: nothing is shared between waves but the final combination.  With
 // splits > 1 partial results (fp32 O, reference m and row sum l) go to the
 // workspace and a second kernel combines them in the order of the splits.
-#include <type_traits>
-
 #include "values.h"
 
 namespace lvsa {
@@ -110,6 +108,15 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1, float scale)
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// A value that the launch only reads, at an index that is the same in the whole wave:
+// by a scalar load, which no wait for the wave's vector loads holds up (they are
+// counted in order, so a vector load behind K's and V's would wait for those).
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T* p, int32_t at) {
+  typedef const __attribute__((address_space(4))) T* constant;
+  return *((constant)(uintptr_t)p + __builtin_amdgcn_readfirstlane(at));
+}
+
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
@@ -168,7 +175,7 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
   auto key_of = [&](int32_t u) -> int32_t {
     if (u >= u1) return a.n_tokens;
     if (!a.row_ptr) return u * UNIT;
-    const int32_t block = __builtin_amdgcn_readfirstlane(a.col_idx[walk + u / per]);
+    const int32_t block = uniform_load(a.col_idx, walk + u / per);
     if ((uint32_t)block >= (uint32_t)a.mask_blocks) return a.n_tokens;
     return min((block * per + u % per) * UNIT, a.n_tokens);
   };
@@ -214,7 +221,8 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
   }
   while (key0 < a.n_tokens) {
     const int32_t key1 = next_unit();
-    const float k_scale = ks[key0 >> a.scale_shift], v_scale = vs[key0 >> a.scale_shift];
+    const float k_scale = uniform_load(ks, key0 >> a.scale_shift);
+    const float v_scale = uniform_load(vs, key0 >> a.scale_shift);
     f32x4 s[4][RT];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
@@ -397,14 +405,15 @@ __device__ __forceinline__ int xsw(int row) { return -(row >> 2) & 3; }
 // One wave load (1 KiB) from memory into LDS.  Inline assembly, so that the compiler
 // puts no wait for it between here and the half step's end, where tile_sync waits.
 // The nop is the wait state between a write of M0 and the load.
-__device__ __forceinline__ void load_to_lds(uint32_t dst, __amdgpu_buffer_rsrc_t rsrc,
-                                            uint32_t voff, uint32_t soff) {
+__device__ __forceinline__ void load_to_lds(uint32_t dst, const u32x4& rsrc, uint32_t voff,
+                                            uint32_t soff) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
       "s_nop 0\n\t"
       "buffer_load_dwordx4 %1, %2, %3 offen lds"
       :
-      : "s"(dst), "v"(voff), "s"(rsrc), "s"(soff)
+      : "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(voff), "s"(rsrc),
+        "s"(__builtin_amdgcn_readfirstlane(soff))
       : "memory", "m0");
 }
 __device__ __forceinline__ void tile_barrier() {
@@ -415,8 +424,12 @@ __device__ __forceinline__ void tile_sync() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, bytes, 0x00020000);
+// Buffer resource of `bytes` bytes from p on, in scalar registers.
+__device__ __forceinline__ u32x4 rsrc_of(const void* p, uint32_t bytes) {
+  const uint64_t at = (uint64_t)p;
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xFFFF),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
 
 // The lane's index, made anew where a rare branch needs it: what is derived from it
@@ -433,6 +446,17 @@ struct Step {
   int32_t left[2];   // held tokens from the unit's first on; 0: none, or not kept by any
   int32_t keep;      // bit u: this wave's query block keeps unit u
 };
+// One of two by value: a reference to either would put both into memory.
+__device__ __forceinline__ Step pick(bool first, const Step& a, const Step& b) {
+  Step s;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    s.unit[u] = first ? a.unit[u] : b.unit[u];
+    s.left[u] = first ? a.left[u] : b.left[u];
+  }
+  s.keep = first ? a.keep : b.keep;
+  return s;
+}
 
 // Q of a wave: two 16-row tiles, each the sum of two e4m3 operands.  With 2^a the least
 // power of two that keeps the row within 448 * 2^a: hi = e4m3(q / 2^a), low =
@@ -837,8 +861,8 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_void*)lds;
     const int64_t base = (int64_t)it.kvh * a.capacity;
     const uint32_t bytes = (uint32_t)a.capacity * D;
-    const __amdgpu_buffer_rsrc_t rk = rsrc_of(a.k + base * D, bytes);
-    const __amdgpu_buffer_rsrc_t rv = rsrc_of(a.v + base * D, bytes);
+    const uint8_t* const k_head = a.k + base * D;
+    const uint8_t* const v_head = a.v + base * D;
     const float* const ks = a.k_scale + (base >> a.scale_shift);
     const float* const vs = a.v_scale + (base >> a.scale_shift);
     // Loads into LDS, 1 KiB each.  K: a wave brings in 16 keys, both slabs, of unit
@@ -849,18 +873,20 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     auto load_k = [&](const Step& st, int stage) {
       const uint32_t so = (uint32_t)(wave / 4 ? st.unit[1] : st.unit[0]) * (UNIT * D);
       const uint32_t dst = dst0 + (uint32_t)stage * K_STAGE;
+      const u32x4 rk = rsrc_of(k_head, bytes);
       load_to_lds(dst, rk, k_off, so);
       load_to_lds(dst + SLAB, rk, k_off, so + 64u);
     };
     auto load_v = [&](const Step& st) {
       const uint32_t so = (uint32_t)wave * 1024u;
+      const u32x4 rv = rsrc_of(v_head, bytes);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
         load_to_lds(dst0 + RAW_AT + u * SLAB, rv, (uint32_t)lane * 16u,
                     (uint32_t)st.unit[u] * (UNIT * D) + so);
     };
     auto scale_at = [&](const float* s, int unit) {
-      return s[(unit * UNIT) >> a.scale_shift];
+      return uniform_load(s, (unit * UNIT) >> a.scale_shift);
     };
     // The thread's 16 places (16 (tid % 4) .. of d = tid / 4) of each unit, taken from the
     // wave's raw bytes, and converted into the stage.
@@ -901,75 +927,80 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
 
     const bool lead = wave < 4;
     const float scale = ka.scale_log2;
-    Step w1 = step_at(min(1, n - 1)), w2 = step_at(min(2, n - 1));
+    // Steps j + 1, j + 2, j + 3.
+    Step s1 = step_at(min(1, n - 1)), s2 = step_at(min(2, n - 1)), s3 = step_at(min(3, n - 1));
     Scores sc;
     Probs pr;
+    // A softmax phase: V of step a is converted into stage 1 - stage, K of step b and its
+    // V bytes are loaded.
+    auto soft = [&](const Step& sa, const Step& sb, int stage) {
+      u32x4 w[2];
+      take_v(w);
+      load_k(sb, stage);
+      load_v(sb);
+      store_v(sa, w, stage ^ 1);
+      softmax_phase(sc, ts, pr, scale);
+    };
     int keep;
     {
-      const Step w0 = step_at(0);
+      const Step s0 = step_at(0);
       u32x4 w[2];
-      load_v(w0);
-      load_k(w0, 0);
-      load_k(w1, 1);
+      load_v(s0);
+      load_k(s0, 0);
+      load_k(s1, 1);
       tile_sync();
       take_v(w);
-      load_v(w1);
-      store_v(w0, w, 0);
-      score_from<0>(sc, lds, f, q, k_scales(w0));
-      keep = w0.keep;
-      mask_scores(sc, w0);
-      if (lead) softmax_phase(sc, ts, pr, scale);
-    }
-    int ksc = k_scales(w1);
-    tile_sync();
-    auto walk = [&](auto leading) {
-      constexpr bool LEAD = decltype(leading)::value;
-      for (int j = 0; j < n; ++j) {
-        const int even = j & 1;
-        const char* const kj = lds + (even ^ 1) * K_STAGE;              // K(j+1)
-        const char* const vj = lds + V_AT + even * V_STAGE;             // V(j)
-        const Step w3 = step_at(min(j + 3, n - 1));
-        const int next_ksc = k_scales(w2);
-        if (LEAD) {
-          matrix_phase<MB / UNIT>(kj, vj, q, sc, pr, ts, f, keep, ksc);
-          keep = w1.keep;
-          mask_scores(sc, w1);
-          tile_barrier();
-        }
-        u32x4 w[2];
-        take_v(w);
-        load_k(w2, even);
-        load_v(w2);
-        store_v(w1, w, even ^ 1);
+      load_v(s1);
+      store_v(s0, w, 0);
+      score_from<0>(sc, lds, f, q, k_scales(s0));
+      keep = s0.keep;
+      mask_scores(sc, s0);
+      tile_sync();
+      // Half step 0: the others' softmax 0 and their share of V(1), K(2); the leaders
+      // begin with their matrix phase 0, so they have taken softmax 0 before.
+      if (lead) {
         softmax_phase(sc, ts, pr, scale);
-        if (!LEAD) {
-          tile_barrier();
-          matrix_phase<MB / UNIT>(kj, vj, q, sc, pr, ts, f, keep, ksc);
-          keep = w1.keep;
-          mask_scores(sc, w1);
-        }
-        tile_sync();
-        ksc = next_ksc;
-        w1 = w2;
-        w2 = w3;
+      } else {
+        soft(s1, s2, 0);
+        tile_barrier();
       }
-    };
-    if (lead)
-      walk(std::true_type{});
-    else
-      walk(std::false_type{});
+    }
+    int ksc = k_scales(s1);
+    // Both sides run the same loop: matrix phase j, then a softmax phase, the leaders'
+    // of the same step (loads of j + 2), the others' of the next one (loads of j + 3).
+    for (int j = 0; j < n; ++j) {
+      const int even = j & 1;
+      const Step s4 = step_at(min(j + 4, n - 1));
+      const int next_ksc = k_scales(s2);
+      matrix_phase<MB / UNIT>(lds + (even ^ 1) * K_STAGE, lds + V_AT + even * V_STAGE, q, sc, pr,
+                              ts, f, keep, ksc);
+      keep = s1.keep;
+      mask_scores(sc, s1);
+      tile_sync();   // the others' loads; a leader has none under way here
+      if (j + 1 < n) soft(pick(lead, s1, s2), pick(lead, s2, s3), lead ? even : even ^ 1);
+      if (lead)
+        tile_sync();
+      else if (j + 1 < n)
+        tile_barrier();
+      ksc = next_ksc;
+      s1 = s2;
+      s2 = s3;
+      s3 = s4;
+    }
   }
 
-  // Every wave holds whole rows.
+  // Every wave holds whole rows.  (The lane anew: rows and addresses are not kept from
+  // the start.)
+  const int lane2 = fresh_lane(), g2 = lane2 / 16, i2 = lane2 % 16;
   if (ka.p.splits == 1) {
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
       int32_t head, token;
-      if (!row_of(it, a, 32 * wave + 16 * qt + i, head, token)) continue;
+      if (!row_of(it, a, 32 * wave + 16 * qt + i2, head, token)) continue;
       const float l = ts.l[qt];
       const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
       __bf16* const out =
-          (__bf16*)a.o + (int64_t)head * a.o_sh + (int64_t)token * a.o_st + 4 * g;
+          (__bf16*)a.o + (int64_t)head * a.o_sh + (int64_t)token * a.o_st + 4 * g2;
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) {
         bf16x4 b;
@@ -984,11 +1015,11 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
   const int64_t slots = (int64_t)total * TILE_ROWS;
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
-    const int64_t slot = (item * ka.p.splits + split) * TILE_ROWS + 32 * wave + 16 * qt + i;
+    const int64_t slot = (item * ka.p.splits + split) * TILE_ROWS + 32 * wave + 16 * qt + i2;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt)
-      *(f32x4*)(a.workspace + slot * D + 16 * dt + 4 * g) = ts.o[dt][qt];
-    if (g == 0) {
+      *(f32x4*)(a.workspace + slot * D + 16 * dt + 4 * g2) = ts.o[dt][qt];
+    if (g2 == 0) {
       a.workspace[slots * D + 2 * slot] = ts.m[qt];
       a.workspace[slots * D + 2 * slot + 1] = ts.l[qt];
     }
