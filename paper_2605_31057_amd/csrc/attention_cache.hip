@@ -14,6 +14,8 @@
 // unit ahead: nothing is shared between waves but the final combination.  With
 // splits > 1 partial results (fp32 O, reference m and row sum l) go to the
 // workspace and a second kernel combines them in the order of the splits.
+#include <type_traits>
+
 #include "values.h"
 
 namespace lvsa {
@@ -215,14 +217,17 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
     return key;
   };
   int32_t key0 = next_unit();
+  float k_scale = 1.f, v_scale = 1.f;
   if (key0 < a.n_tokens) {
     load_k(key0);
     load_v(key0);
+    k_scale = uniform_load(ks, key0 >> a.scale_shift);
+    v_scale = uniform_load(vs, key0 >> a.scale_shift);
   }
   while (key0 < a.n_tokens) {
     const int32_t key1 = next_unit();
-    const float k_scale = uniform_load(ks, key0 >> a.scale_shift);
-    const float v_scale = uniform_load(vs, key0 >> a.scale_shift);
+    const int32_t scale1 = min(key1, a.n_tokens - 1) >> a.scale_shift;
+    const float k_scale1 = uniform_load(ks, scale1), v_scale1 = uniform_load(vs, scale1);
     f32x4 s[4][RT];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
@@ -298,6 +303,8 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
     __builtin_amdgcn_sched_barrier(0);
     if (key1 < a.n_tokens) load_v(key1);
     key0 = key1;
+    k_scale = k_scale1;
+    v_scale = v_scale1;
   }
 
   // The waves' parts, combined in LDS in the waves' order.
@@ -382,7 +389,8 @@ constexpr int K_STAGE = 2 * UNIT * D;        // 128 rows of 128 bytes
 constexpr int V_STAGE = 2 * UNIT * D * 2;    // 128 rows (d) of 256 bytes (keys)
 constexpr int V_AT = 2 * K_STAGE;
 constexpr int RAW_AT = V_AT + 2 * V_STAGE;   // V's bytes of a step
-constexpr int LIST_AT = RAW_AT + K_STAGE;
+constexpr int ZERO_AT = RAW_AT + K_STAGE;    // with a mask: two slabs of zeros, the list
+constexpr int LIST_AT = ZERO_AT + V_STAGE / 2;
 constexpr int LIST_WORDS = kMaxSparseBlocks;
 constexpr int BITMAP_WORDS = 256;
 static_assert(BITMAP_WORDS * 32 >= LIST_WORDS, "a bit a block");
@@ -445,6 +453,7 @@ struct Step {
   int32_t unit[2];   // 0 where there is none
   int32_t left[2];   // held tokens from the unit's first on; 0: none, or not kept by any
   int32_t keep;      // bit u: this wave's query block keeps unit u
+  int32_t scales;    // exponent bytes: K of unit 0, of unit 1, V of unit 0, of unit 1
 };
 // One of two by value: a reference to either would put both into memory.
 __device__ __forceinline__ Step pick(bool first, const Step& a, const Step& b) {
@@ -455,6 +464,7 @@ __device__ __forceinline__ Step pick(bool first, const Step& a, const Step& b) {
     s.left[u] = first ? a.left[u] : b.left[u];
   }
   s.keep = first ? a.keep : b.keep;
+  s.scales = first ? a.scales : b.scales;
   return s;
 }
 
@@ -530,9 +540,6 @@ __device__ __forceinline__ i32x8 k_frag(const char* k, uint32_t at, int kt) {
   const i32x4 b = *(const i32x4*)(k + at + kt * 1024 + SLAB);
   return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
-__device__ __forceinline__ bf16x8 v_frag(const char* v, uint32_t at, int dt, int u) {
-  return *(const bf16x8*)(v + at + dt * 1024 + u * SLAB);
-}
 template <int KT>
 __device__ __forceinline__ void score_tile(Scores& sc, const i32x8& f, const QSplit& q,
                                            int k_scale) {
@@ -559,6 +566,7 @@ __device__ __forceinline__ void score_from(Scores& sc, const char* k, uint32_t f
 __device__ __forceinline__ void mask_scores(Scores& sc, const Step& st) {
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
+    if (st.keep == 0) break;   // its weights are zeros (weigh)
     const int left = (st.keep >> u) & 1 ? st.left[u] : 0;
     if (left >= UNIT) continue;
     const int lim = left - 4 * (fresh_lane() / 16);
@@ -646,6 +654,21 @@ __device__ __forceinline__ void softmax_phase(const Scores& sc, TileState& st, P
   }
 }
 
+// Weights of a step: zeros where the wave's query block keeps none of it (rows without a
+// key have no reference, and would look for one every step).
+template <bool MASKED>
+__device__ __forceinline__ void weigh(const Scores& sc, TileState& st, Probs& pr, float scale,
+                                      int keep) {
+  if (MASKED && keep == 0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) pr.p[u][qt] = bf16x8{};
+    return;
+  }
+  softmax_phase(sc, st, pr, scale);
+}
+
 // A operand of the row sums of query tile qt: ones in rows qt, 4 + qt, 8 + qt, 12 + qt,
 // which are register qt of every lane of the result.  Made anew each time: kept, it
 // would hold eight registers.
@@ -654,39 +677,31 @@ __device__ __forceinline__ bf16x8 sum_rows(int qt) {
   return __builtin_bit_cast(bf16x8, u32x4{w, w, w, w});
 }
 
-// l += row sums of P, O += P V, S = K Q^T of the next step.  V of a unit that the wave's
-// query block does not keep is left out: what it holds never reaches the block.  UNITS:
-// the units that a block keeps or not as one (2: the step whole), 0: it keeps all.
-template <int UNITS>
-__device__ __forceinline__ void matrix_phase(const char* k, const char* v, const QSplit& q,
+// Matrix phase: l += row sums of P, O += P V, S = K Q^T of the next step.  MASKED: the
+// wave's query block may keep a unit or not (`keep`); V of one that it does not is read
+// from slabs of zeros, so that what the unit holds (NaN) never reaches the block.  (A
+// branch around the products made the compiler spill; its weights are zeros and the
+// workgroup's other waves take the time anyway.)
+template <bool MASKED>
+__device__ __forceinline__ void matrix_phase(const char* lds, int k_at, int v_at, const QSplit& q,
                                              Scores& sc, const Probs& pr, TileState& st,
-                                             uint32_t f, int keep,
-                                             int k_scale) {
-  if (UNITS && keep != 3) {
+                                             uint32_t f, int keep, int k_scale) {
+  // Fragments read ahead.  4,680 queries of 40 heads over 63,960 tokens: 4.63 ms with 8,
+  // 4.60 with 10, 4.54 with 12, 4.55 with 14; one frame of 12 heads over the 121-frame mask:
+  // 306 us with 4, 249 with 6, 235, 220, 238 and 226 with 8 to 14.
+  constexpr int AHEAD = MASKED ? 10 : 12;
+  const char* const k = lds + k_at;
+  uint32_t from[2];   // the slabs of V's units
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (UNITS == 2 || !((keep >> (u / 2)) & 1)) continue;
-#pragma unroll
-      for (int qt = 0; qt < 2; ++qt)
-        st.l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sum_rows(qt), pr.p[u][qt], st.l, 0, 0, 0);
-#pragma unroll
-      for (int dt = 0; dt < 8; ++dt) {
-        const bf16x8 x = v_frag(v, f, dt, u);
-#pragma unroll
-        for (int qt = 0; qt < 2; ++qt)
-          st.o[dt][qt] =
-              __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pr.p[u][qt], st.o[dt][qt], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    score_from<0>(sc, k, f, q, k_scale);
-    return;
-  }
-  constexpr int AHEAD = 8;
+  for (int u = 0; u < 2; ++u)
+    from[u] = f + (uint32_t)(MASKED && !((keep >> u) & 1) ? ZERO_AT : v_at + u * 2 * SLAB);
+  auto frag = [&](int i) {
+    return *(const bf16x8*)(lds + from[i % 4 / 2] + i % 2 * SLAB + i / 4 * 1024);
+  };
   bf16x8 fr[32];
   i32x8 kf[8];
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fr[i] = v_frag(v, f, i / 4, i % 4);
+  for (int i = 0; i < AHEAD; ++i) fr[i] = frag(i);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
@@ -708,26 +723,27 @@ __device__ __forceinline__ void matrix_phase(const char* k, const char* v, const
         const int u = t ? 3 - i : i, qt = t ^ (dt & 1);
         if (at % 2 == 0) {
           const int n = at / 2 + AHEAD;
-          if (n < 32) fr[n] = v_frag(v, f, n / 4, n % 4);
+          if (n < 32) fr[n] = frag(n);
           else if ((n - 32) % 4 == 0) kf[(n - 32) / 4] = k_frag(k, f, (n - 32) / 4);
         }
         st.o[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[4 * dt + u], pr.p[u][qt],
                                                                st.o[dt][qt], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
-#define SCORE_TILE(KT)                                       \
-  if (KT + 2 < 8) kf[KT + 2] = k_frag(k, f, KT + 2);         \
-  score_tile<KT>(sc, kf[KT], q, k_scale);                    \
-  __builtin_amdgcn_sched_barrier(0);
-  SCORE_TILE(0)
-  SCORE_TILE(1)
-  SCORE_TILE(2)
-  SCORE_TILE(3)
-  SCORE_TILE(4)
-  SCORE_TILE(5)
-  if (true) { score_tile<6>(sc, kf[6], q, k_scale); __builtin_amdgcn_sched_barrier(0); }
-  score_tile<7>(sc, kf[7], q, k_scale);
-#undef SCORE_TILE
+  auto score = [&](auto kt) {
+    constexpr int KT = decltype(kt)::value;
+    if constexpr (KT + 2 < 8) kf[KT + 2] = k_frag(k, f, KT + 2);
+    score_tile<KT>(sc, kf[KT], q, k_scale);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  score(std::integral_constant<int, 0>{});
+  score(std::integral_constant<int, 1>{});
+  score(std::integral_constant<int, 2>{});
+  score(std::integral_constant<int, 3>{});
+  score(std::integral_constant<int, 4>{});
+  score(std::integral_constant<int, 5>{});
+  score(std::integral_constant<int, 6>{});
+  score(std::integral_constant<int, 7>{});
 }
 
 // The union of the CSR rows block0 .. block0 + count - 1 (at most four) as words in
@@ -784,7 +800,7 @@ __device__ __forceinline__ int32_t union_list(uint32_t* list, uint32_t* bm, int3
 // MB: the mask's block, 0 without a mask.
 template <int MB>
 __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
-  __shared__ __attribute__((aligned(1024))) char lds[MB ? TILE_LDS : LIST_AT];
+  __shared__ __attribute__((aligned(1024))) char lds[MB ? TILE_LDS : ZERO_AT];
   const CacheAttnArgs& a = ka.a;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -799,38 +815,70 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
   const Item it = item_of(ka, tile, id / ka.p.tiles / ka.p.splits);
 
   // Steps of the split.
-  uint32_t* const list = (uint32_t*)(lds + LIST_AT);
+  const uint32_t* const list = (const uint32_t*)(lds + LIST_AT);
   int32_t words, n, s0 = 0;
   if constexpr (MB == 0) {
     words = (a.n_tokens + UNIT - 1) / UNIT;
     n = (words + 1) / 2;
   } else {
-    words = union_list(list, (uint32_t*)(lds + V_AT), (int32_t*)(lds + TILE_LDS - 64), a.row_ptr,
+    words = union_list((uint32_t*)(lds + LIST_AT), (uint32_t*)(lds + V_AT), (int32_t*)(lds + TILE_LDS - 64), a.row_ptr,
                        a.col_idx, it.block0, it.blocks, a.mask_blocks);
     n = MB == 128 ? words : (words + 1) / 2;
+    for (int at = tid * 16; at < V_STAGE / 2; at += TILE_THREADS * 16)
+      *(u32x4*)(lds + ZERO_AT + at) = u32x4{};   // read after the next barriers
   }
   s0 = (int32_t)((int64_t)n * split / ka.p.splits);
   n = (int32_t)((int64_t)n * (split + 1) / ka.p.splits) - s0;
   const int my_block = MB ? 32 * wave / (MB ? MB : 1) : 0;
+  // Units and scales of 64 steps, a step a lane, from which a step's are read by lane:
+  // memory or LDS reads in the loop would be counted together with the fragments' reads
+  // (scalar loads come back in any order, so the next wait is for all of them).
+  const int64_t base = (int64_t)it.kvh * a.capacity;
+  const float* const ks = a.k_scale + (base >> a.scale_shift);
+  const float* const vs = a.v_scale + (base >> a.scale_shift);
+  uint32_t win_w[2] = {}, win_s = 0;   // words (two with 64-token blocks), scales
+  auto fill_window = [&](int first) {
+    const int j = s0 + min(first + fresh_lane(), n - 1);
+    int32_t unit[2] = {2 * j, 2 * j + 1};
+    if constexpr (MB == 128) {
+      win_w[0] = list[j];
+      unit[0] = 2 * (int)(win_w[0] & 0x0FFFFFFFu);
+      unit[1] = unit[0] + 1;
+    } else if constexpr (MB == 64) {
+      win_w[0] = list[2 * j];
+      win_w[1] = 2 * j + 1 < words ? list[2 * j + 1] : 0u;   // no row keeps it
+      unit[0] = (int)(win_w[0] & 0x0FFFFFFFu);
+      unit[1] = (int)(win_w[1] & 0x0FFFFFFFu);
+    }
+    win_s = 0u;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int32_t at = (unit[u] * UNIT) >> a.scale_shift;
+      const bool held = unit[u] * UNIT < a.n_tokens;   // else no write may have set them
+      const uint32_t k = held ? __float_as_uint(ks[at]) >> 23 & 0xFFu : 127u;
+      const uint32_t v = held ? __float_as_uint(vs[at]) >> 23 & 0xFFu : 127u;
+      win_s |= k << (8 * u) | v << (16 + 8 * u);
+    }
+  };
   auto step_at = [&](int j) {
     Step st;
+    const int in = j % 64;
+    st.scales = __builtin_amdgcn_readlane((int)win_s, in);
     if constexpr (MB == 0) {
       st.unit[0] = 2 * (s0 + j);
       st.unit[1] = 2 * (s0 + j) + 1;
       st.keep = 3;
     } else if constexpr (MB == 128) {
-      const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)list[s0 + j]);
+      const uint32_t w = (uint32_t)__builtin_amdgcn_readlane((int)win_w[0], in);
       st.unit[0] = 2 * (int)(w & 0x0FFFFFFFu);
       st.unit[1] = st.unit[0] + 1;
       st.keep = ((w >> (28 + my_block)) & 1u) * 3;
     } else {
-      const int at = 2 * (s0 + j);
-      const uint32_t w0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)list[at]);
-      const uint32_t w1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)list[min(at + 1, words - 1)]);
+      const uint32_t w0 = (uint32_t)__builtin_amdgcn_readlane((int)win_w[0], in);
+      const uint32_t w1 = (uint32_t)__builtin_amdgcn_readlane((int)win_w[1], in);
       st.unit[0] = (int)(w0 & 0x0FFFFFFFu);
       st.unit[1] = (int)(w1 & 0x0FFFFFFFu);
-      st.keep = ((w0 >> (28 + my_block)) & 1u) |
-                (at + 1 < words ? ((w1 >> (28 + my_block)) & 1u) << 1 : 0u);
+      st.keep = ((w0 >> (28 + my_block)) & 1u) | ((w1 >> (28 + my_block)) & 1u) << 1;
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) st.left[u] = a.n_tokens - st.unit[u] * UNIT;
@@ -859,12 +907,9 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
 
   if (n > 0) {
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_void*)lds;
-    const int64_t base = (int64_t)it.kvh * a.capacity;
     const uint32_t bytes = (uint32_t)a.capacity * D;
     const uint8_t* const k_head = a.k + base * D;
     const uint8_t* const v_head = a.v + base * D;
-    const float* const ks = a.k_scale + (base >> a.scale_shift);
-    const float* const vs = a.v_scale + (base >> a.scale_shift);
     // Loads into LDS, 1 KiB each.  K: a wave brings in 16 keys, both slabs, of unit
     // wave / 4.  V: 16 columns d of each unit, as they lie.
     const uint32_t k_off = (uint32_t)((16 * (wave % 4) + lane / 4) * D +
@@ -885,9 +930,6 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
         load_to_lds(dst0 + RAW_AT + u * SLAB, rv, (uint32_t)lane * 16u,
                     (uint32_t)st.unit[u] * (UNIT * D) + so);
     };
-    auto scale_at = [&](const float* s, int unit) {
-      return uniform_load(s, (unit * UNIT) >> a.scale_shift);
-    };
     // The thread's 16 places (16 (tid % 4) .. of d = tid / 4) of each unit, taken from the
     // wave's raw bytes, and converted into the stage.
     const char* const raw = lds + RAW_AT + tid * 16;
@@ -901,9 +943,9 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     auto store_v = [&](const Step& st, u32x4 (&w)[2], int stage) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        float scale = scale_at(vs, st.unit[u]);
+        const float scale =
+            __uint_as_float((((uint32_t)st.scales >> (16 + 8 * u)) & 0xFFu) << 23);
         if (st.left[u] < UNIT) {   // bytes of tokens that are not held: zeros
-          if (st.left[u] <= 0) scale = 1.f;   // a scale that no write has set
           const int from = 4 * (fresh_lane() % 4);
 #pragma unroll
           for (int kt = 0; kt < 4; ++kt) {
@@ -919,18 +961,16 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
             to_bf16(w[u][2], w[u][3], scale);
       }
     };
-    auto k_scales = [&](const Step& st) {
-      return (int)((__float_as_uint(scale_at(ks, st.unit[0])) >> 23) |
-                   (__float_as_uint(scale_at(ks, st.unit[1])) >> 23) << 8);
-    };
     const uint32_t f = (uint32_t)(i * 64 + (g ^ xsw(i)) * 16);
 
     const bool lead = wave < 4;
     const float scale = ka.scale_log2;
     // Steps j + 1, j + 2, j + 3.
+    fill_window(0);
     Step s1 = step_at(min(1, n - 1)), s2 = step_at(min(2, n - 1)), s3 = step_at(min(3, n - 1));
     Scores sc;
     Probs pr;
+    int keep;   // of the step whose scores are at hand
     // A softmax phase: V of step a is converted into stage 1 - stage, K of step b and its
     // V bytes are loaded.
     auto soft = [&](const Step& sa, const Step& sb, int stage) {
@@ -939,9 +979,8 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
       load_k(sb, stage);
       load_v(sb);
       store_v(sa, w, stage ^ 1);
-      softmax_phase(sc, ts, pr, scale);
+      weigh<MB != 0>(sc, ts, pr, scale, keep);
     };
-    int keep;
     {
       const Step s0 = step_at(0);
       u32x4 w[2];
@@ -952,28 +991,27 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
       take_v(w);
       load_v(s1);
       store_v(s0, w, 0);
-      score_from<0>(sc, lds, f, q, k_scales(s0));
+      score_from<0>(sc, lds, f, q, s0.scales);
       keep = s0.keep;
       mask_scores(sc, s0);
       tile_sync();
       // Half step 0: the others' softmax 0 and their share of V(1), K(2); the leaders
       // begin with their matrix phase 0, so they have taken softmax 0 before.
       if (lead) {
-        softmax_phase(sc, ts, pr, scale);
+        weigh<MB != 0>(sc, ts, pr, scale, keep);
       } else {
         soft(s1, s2, 0);
         tile_barrier();
       }
     }
-    int ksc = k_scales(s1);
     // Both sides run the same loop: matrix phase j, then a softmax phase, the leaders'
     // of the same step (loads of j + 2), the others' of the next one (loads of j + 3).
     for (int j = 0; j < n; ++j) {
       const int even = j & 1;
+      if ((j + 4) % 64 == 0 && j + 4 < n) fill_window(j + 4);
       const Step s4 = step_at(min(j + 4, n - 1));
-      const int next_ksc = k_scales(s2);
-      matrix_phase<MB / UNIT>(lds + (even ^ 1) * K_STAGE, lds + V_AT + even * V_STAGE, q, sc, pr,
-                              ts, f, keep, ksc);
+      matrix_phase<MB != 0>(lds, (even ^ 1) * K_STAGE, V_AT + even * V_STAGE, q, sc, pr, ts, f,
+                            keep, s1.scales);
       keep = s1.keep;
       mask_scores(sc, s1);
       tile_sync();   // the others' loads; a leader has none under way here
@@ -982,7 +1020,6 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
         tile_sync();
       else if (j + 1 < n)
         tile_barrier();
-      ksc = next_ksc;
       s1 = s2;
       s2 = s3;
       s3 = s4;
@@ -1090,7 +1127,8 @@ __global__ __launch_bounds__(THREADS) void combine_kernel(KernelArgs ka) {
 // Items of a launch, without the splits.
 int64_t items_of(const Plan& p) { return (int64_t)p.heads * p.blocks * p.tiles; }
 
-// Tiles from this many rows a key head (with a mask, a query block and key head) on.
+// Tiles from this many rows a key head (with a mask, which keeps a tile within one
+// query head, from this many queries) on.
 constexpr int64_t TILE_FROM = 65;
 
 Plan plan_of(const CacheAttnArgs& a, int32_t cus) {
@@ -1104,7 +1142,7 @@ Plan plan_of(const CacheAttnArgs& a, int32_t cus) {
     blocks = (a.q_start + a.n - 1) / a.mask_block - a.q_start / a.mask_block + 1;
     rows = (int64_t)(a.n < a.mask_block ? a.n : a.mask_block) * a.group;
   }
-  p.tile = rows >= TILE_FROM;
+  p.tile = (a.row_ptr ? a.n : rows) >= TILE_FROM;
   if (p.tile) {
     p.item_rows = TILE_ROWS;
     if (a.row_ptr) {
