@@ -433,49 +433,62 @@ def dense_attention(q, k, v, block=128, out=None, stream=None):
 
 # ------------------------------------------- rotary positions, 8-bit cache
 
-def _dtype_code(dtype):
-    import torch
-    codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-    if dtype not in codes:
-        raise ValueError("expected bfloat16, float16 or float32")
-    return codes[dtype]
+# A call of one of these on a few tokens takes a few microseconds on the GPU, so the
+# marshalling keeps to what it needs: plain integers, no context managers without a
+# stream, nothing looked up twice.
+
+_TORCH = None
+_CODES = {}
 
 
-def _on_device(t):
-    import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError("expected a tensor on the current device")
-    return t
+def _torch():
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _CODES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
+        _TORCH = torch
+    return _TORCH
 
 
-def _rows(t):
-    """A [heads, n_tokens, head_dim] tensor on the current device; the strides of
-    axes of one element are put right, torch leaves them open."""
-    if t.dim() != 3:
+def _rows(t, device):
+    """A [heads, n_tokens, head_dim] tensor on device number ``device``; the strides
+    of axes of one element are put right, torch leaves them open."""
+    shape = t.shape
+    if len(shape) != 3:
         raise ValueError("expected a [heads, n_tokens, head_dim] tensor")
-    if t.stride(2) != 1:
+    sh, st, sd = t.stride()
+    if sd != 1:
         raise ValueError("head_dim must be contiguous")
-    _on_device(t)
-    H, n, d = t.shape
-    token = t.stride(1) if n > 1 else d
-    return _Tensor(t.data_ptr(), H, n, d, t.stride(0) if H > 1 else n * token, token)
+    if t.get_device() != device:
+        raise ValueError("expected a tensor on the current device")
+    H, n, d = shape
+    if n <= 1:
+        st = d
+    return _Tensor(t.data_ptr(), H, n, d, sh if H > 1 else n * st, st)
 
 
-def _same_type(first, *others):
-    if any(t.dtype != first.dtype for t in others):
+def _type_code(first, second):
+    if first.dtype != second.dtype:
         raise ValueError("expected tensors of one type")
-    return _dtype_code(first.dtype)
+    code = _CODES.get(first.dtype)
+    if code is None:
+        raise ValueError("expected bfloat16, float16 or float32")
+    return code
 
 
-def _on(stream):
-    """The context in which torch allocates for work on ``stream``."""
-    import contextlib
-    import torch
-    if stream is None:
-        return contextlib.nullcontext()
+def _raw_stream(device):
+    """The current stream of ``device``, as an address."""
+    raw = getattr(_TORCH._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw else _TORCH.cuda.current_stream(device).cuda_stream
+
+
+def _with_stream(fn, stream, *args):
+    """fn(*args) with ``stream`` current: torch allocates for it then."""
+    torch = _torch()
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-    return torch.cuda.stream(stream)
+    with torch.cuda.stream(stream):
+        return fn(*args)
 
 
 class Rope:
@@ -487,7 +500,7 @@ class Rope:
 
     def __init__(self, frames, height, width, pairs=(22, 21, 21), theta=10000.0,
                  layout=ROPE_PAIRS, table=None, device="cuda"):
-        import torch
+        torch = _torch()
         self._c = _Rope(frames, height, width, (_i32 * 3)(*pairs), layout, None)
         n = _i64()
         _check(lib().lvsa_rope_table_size(ctypes.byref(self._c), ctypes.byref(n)),
@@ -504,34 +517,39 @@ class Rope:
         self._c.table = table.data_ptr()
 
 
-def _rope_ref(r):
+def _rope_ref(r, device):
     if r is None:
         return None
-    _on_device(r.table)
+    if r.table.get_device() != device:
+        raise ValueError("expected a table on the current device")
     return ctypes.byref(r._c)
 
 
-def _rotate(fn, x, r, start, out, stream):
-    import torch
-    with _on(stream):
-        if out is None:
-            out = torch.empty_like(x)
-        tx, to = _rows(x), _rows(out)
-        _check(getattr(lib(), fn)(ctypes.byref(tx), _same_type(x, out), start, _rope_ref(r),
-                                  ctypes.byref(to), _stream_ptr(stream)), fn)
+def _rotate(name, x, r, start, out):
+    torch = _torch()
+    dev = torch.cuda.current_device()
+    if out is None:
+        out = torch.empty_like(x)
+    _check(getattr(lib(), name)(ctypes.byref(_rows(x, dev)), _type_code(x, out), start,
+                                _rope_ref(r, dev), ctypes.byref(_rows(out, dev)),
+                                _raw_stream(dev)), name)
     return out
 
 
 def rope(x, r, start=0, out=None, stream=None):
     """x [heads, n, 128] (bfloat16, float16, float32), token i of which is token
     start + i of the grid, rotated by ``r`` (lvsa_rope_forward); out may be x."""
-    return _rotate("lvsa_rope_forward", x, r, start, out, stream)
+    if stream is not None:
+        return _with_stream(rope, stream, x, r, start, out)
+    return _rotate("lvsa_rope_forward", x, r, start, out)
 
 
 def rope_backward(grad, r, start=0, out=None, stream=None):
     """Gradient of ``rope``: of its input, from that of its output
     (lvsa_rope_backward); out may be grad."""
-    return _rotate("lvsa_rope_backward", grad, r, start, out, stream)
+    if stream is not None:
+        return _with_stream(rope_backward, stream, grad, r, start, out)
+    return _rotate("lvsa_rope_backward", grad, r, start, out)
 
 
 class KvCache:
@@ -542,7 +560,7 @@ class KvCache:
     lvsa_kv_cache lays them out; allocated if not given."""
 
     def __init__(self, heads, capacity, block=128, n_tokens=0, buffers=None, device="cuda"):
-        import torch
+        torch = _torch()
         capacity = -(-capacity // 128) * 128
         f8, f32 = torch.float8_e4m3fn, torch.float32
         shapes = [((heads, capacity, 128), f8), ((heads, capacity // 64, 128, 64), f8),
@@ -579,9 +597,9 @@ class KvCache:
         self._c.n_tokens = n
 
 
-def _cache_ref(c):
-    for b in (c.k, c.v, c.k_scale, c.v_scale):
-        _on_device(b)
+def _cache_ref(c, device):
+    if c.k.get_device() != device:
+        raise ValueError("expected a cache on the current device")
     return ctypes.byref(c._c)
 
 
@@ -589,10 +607,13 @@ def kv_write(cache, k, v, start=None, rope=None, stream=None):
     """Quantises k and v [heads, n, 128] (bfloat16, float16, float32) into tokens
     start, start + 1, .. of the cache (by default behind its last), the keys
     rotated by ``rope`` on the way (lvsa_kv_write); returns the cache."""
-    tk, tv = _rows(k), _rows(v)
-    _check(lib().lvsa_kv_write(_cache_ref(cache), ctypes.byref(tk), ctypes.byref(tv),
-                               _same_type(k, v), cache.n_tokens if start is None else start,
-                               _rope_ref(rope), _stream_ptr(stream)), "lvsa_kv_write")
+    if stream is not None:
+        return _with_stream(kv_write, stream, cache, k, v, start, rope)
+    dev = _torch().cuda.current_device()
+    _check(lib().lvsa_kv_write(_cache_ref(cache, dev), ctypes.byref(_rows(k, dev)),
+                               ctypes.byref(_rows(v, dev)), _type_code(k, v),
+                               cache._c.n_tokens if start is None else start,
+                               _rope_ref(rope, dev), _raw_stream(dev)), "lvsa_kv_write")
     return cache
 
 
@@ -600,22 +621,24 @@ def kv_read(cache, start=0, n=None, dtype=None, out=None, stream=None):
     """Keys and values [heads, n, 128] of tokens start .. start + n - 1 (by default
     to the last) in ``dtype`` (bfloat16 by default), or into ``out`` = (k, v)
     (lvsa_kv_read); returns (k, v)."""
-    import torch
-    with _on(stream):
-        if out is None:
-            n = cache.n_tokens - start if n is None else n
-            if n < 1:
-                raise LvsaError(EINVAL, f"{n} tokens to read")
-            out = tuple(torch.empty(cache.heads, n, 128, dtype=dtype or torch.bfloat16,
-                                    device=cache.k.device) for _ in range(2))
-        k, v = out
-        tk, tv = _rows(k), _rows(v)
-        if tv.n_tokens != tk.n_tokens or (n is not None and tk.n_tokens != n):
-            raise ValueError("expected out tensors of n tokens")
-        if dtype is not None and k.dtype != dtype:
-            raise ValueError("expected out tensors of the given type")
-        _check(lib().lvsa_kv_read(_cache_ref(cache), start, ctypes.byref(tk), ctypes.byref(tv),
-                                  _same_type(k, v), _stream_ptr(stream)), "lvsa_kv_read")
+    if stream is not None:
+        return _with_stream(kv_read, stream, cache, start, n, dtype, out)
+    torch = _torch()
+    dev = torch.cuda.current_device()
+    if out is None:
+        n = cache.n_tokens - start if n is None else n
+        if n < 1:
+            raise LvsaError(EINVAL, f"{n} tokens to read")
+        out = torch.empty(2, cache._c.heads, n, 128, dtype=dtype or torch.bfloat16,
+                          device=cache.k.device).unbind(0)
+    k, v = out
+    tk, tv = _rows(k, dev), _rows(v, dev)
+    if tv.n_tokens != tk.n_tokens or (n is not None and tk.n_tokens != n):
+        raise ValueError("expected out tensors of n tokens")
+    if dtype is not None and k.dtype != dtype:
+        raise ValueError("expected out tensors of the given type")
+    _check(lib().lvsa_kv_read(_cache_ref(cache, dev), start, ctypes.byref(tk), ctypes.byref(tv),
+                              _type_code(k, v), _raw_stream(dev)), "lvsa_kv_read")
     return out
 
 
@@ -624,22 +647,24 @@ def attention_cache(q, cache, mask=None, q_start=0, out=None, stream=None):
     over every held token, or over the blocks that ``mask`` (a BlockMask over the
     cache's tokens) keeps for queries q_start, q_start + 1, ..
     (lvsa_attention_cache); returns out."""
-    import torch
-    with _on(stream):
-        if out is None:
-            out = torch.empty_like(q)
-        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
-            raise ValueError("expected bfloat16 tensors")
-        tq, to = _rows(q), _rows(out)
-        c = _cache_ref(cache)
-        m = None if mask is None else ctypes.byref(mask)
-        need = _i64()
-        _check(lib().lvsa_attention_cache_workspace(ctypes.byref(tq), q_start, c, m,
-                                                    ctypes.byref(need)),
-               "lvsa_attention_cache_workspace")
-        work = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
-        _check(lib().lvsa_attention_cache(ctypes.byref(tq), q_start, c, m, ctypes.byref(to),
-                                          _p(work.data_ptr()) if need.value else None,
-                                          need.value, _stream_ptr(stream)),
-               "lvsa_attention_cache")
+    if stream is not None:
+        return _with_stream(attention_cache, stream, q, cache, mask, q_start, out)
+    torch = _torch()
+    dev = torch.cuda.current_device()
+    if out is None:
+        out = torch.empty_like(q)
+    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
+        raise ValueError("expected bfloat16 tensors")
+    L = lib()
+    tq, to = ctypes.byref(_rows(q, dev)), ctypes.byref(_rows(out, dev))
+    c = _cache_ref(cache, dev)
+    m = None if mask is None else ctypes.byref(mask)
+    need = _i64()
+    _check(L.lvsa_attention_cache_workspace(tq, q_start, c, m, ctypes.byref(need)),
+           "lvsa_attention_cache_workspace")
+    size, work = need.value, None
+    if size:
+        work = torch.empty(size, dtype=torch.uint8, device=q.device)
+    _check(L.lvsa_attention_cache(tq, q_start, c, m, to, work.data_ptr() if size else None, size,
+                                  _raw_stream(dev)), "lvsa_attention_cache")
     return out

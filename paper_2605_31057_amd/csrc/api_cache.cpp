@@ -1,5 +1,6 @@
 // api_cache.cpp -- the C ABI of the rotary positions, the 8-bit K/V cache and the
 // attention over it (lvsa.h): argument checks and dispatch.
+#include <atomic>
 #include <climits>
 #include <cmath>
 
@@ -146,11 +147,19 @@ lvsa_status cache_attention_args(const lvsa_tensor* q, int32_t q_start,
   return LVSA_OK;
 }
 
+// Compute units of the current device (asked for once per device).
 lvsa_status compute_units(int32_t* cus) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices];
   int dev = 0, n = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1)
-    return LVSA_EDEVICE;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return LVSA_EDEVICE;
+  if (dev < kDevices) n = known[dev].load(std::memory_order_relaxed);
+  if (n < 1) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+        n < 1)
+      return LVSA_EDEVICE;
+    if (dev < kDevices) known[dev].store(n, std::memory_order_relaxed);
+  }
   *cus = n;
   return LVSA_OK;
 }

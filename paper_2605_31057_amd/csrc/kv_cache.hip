@@ -15,9 +15,10 @@
 namespace lvsa {
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int ROWS = THREADS / 8;   // rows a pass: eight threads a row (values.h)
 constexpr int LDS_ROW = 136;        // bytes of a token's row in LDS, 8 more than its 128
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct WriteArgs {
   lvsa_kv_cache c;                  // n_tokens: held before
@@ -32,19 +33,58 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a < __builtin_inff() ? a : 0.f;   // NaN compares false
 }
 
-// Largest of x over the workgroup.
-__device__ __forceinline__ float block_max(float x, float* lds) {
+// The V tiles of a block (64 tokens each, at `tiles`) from or to token rows in LDS, four
+// elements and 16 tokens a thread, transposed four bytes by four.
+template <int B, int THREADS>
+__device__ __forceinline__ void tiles_to_rows(const uint8_t* tiles, uint8_t* rows) {
 #pragma unroll
-  for (int off = 32; off > 0; off /= 2) x = fmaxf(x, __shfl_xor(x, off));
-  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
-  __syncthreads();
-  return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+  for (int at = threadIdx.x; at < B / 64 * 128; at += THREADS) {
+    const int tile = at / 128, dq = at % 128 / 4, g = at % 4;
+    u32x4 in[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      in[j] = *(const u32x4*)(tiles + tile * 8192 + (4 * dq + j) * 64 + 16 * g);
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      uint32_t w[4] = {in[0][kt], in[1][kt], in[2][kt], in[3][kt]};
+      transpose4(w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *(uint32_t*)(rows + (tile * 64 + 16 * kt + 4 * g + j) * LDS_ROW + 4 * dq) = w[j];
+    }
+  }
+}
+template <int B, int THREADS>
+__device__ __forceinline__ void rows_to_tiles(const uint8_t* rows, uint8_t* tiles) {
+#pragma unroll
+  for (int at = threadIdx.x; at < B / 64 * 128; at += THREADS) {
+    const int tile = at / 128, dq = at % 128 / 4, g = at % 4;
+    u32x4 out[4];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        w[j] = *(const uint32_t*)(rows + (tile * 64 + 16 * kt + 4 * g + j) * LDS_ROW + 4 * dq);
+      transpose4(w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[j][kt] = w[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(u32x4*)(tiles + tile * 8192 + (4 * dq + j) * 64 + 16 * g) = out[j];
+  }
 }
 
+// Eight threads a row (values.h), two rows a thread.  Every load is issued before the
+// first value is used and none depends on a lane's token: rows of the source are
+// clamped to those that exist and chosen afterwards, so a block of a few new tokens
+// waits for memory once (a branch a row: 8.8 us for one token into a held block,
+// 10.2 us for a frame of 12 heads).
 template <typename T, int B>
-__global__ __launch_bounds__(THREADS) void write_kernel(WriteArgs a, RopeArgs r) {
-  constexpr int PASSES = B / ROWS;
-  __shared__ float most_lds[4];
+__global__ __launch_bounds__(4 * B) void write_kernel(WriteArgs a, RopeArgs r) {
+  constexpr int THREADS = 4 * B, ROWS = B / 2;
+  __shared__ float most_lds[THREADS / 64];
   __shared__ __attribute__((aligned(16))) uint8_t bytes[B * LDS_ROW];
   const int block = a.first_block + blockIdx.x;
   const int64_t head = blockIdx.y;
@@ -52,59 +92,85 @@ __global__ __launch_bounds__(THREADS) void write_kernel(WriteArgs a, RopeArgs r)
   const int row = threadIdx.x / 8, c = threadIdx.x % 8;
   const lvsa_kv_cache& m = a.c;
   const int64_t base = head * m.capacity;              // the head's first place
+  const int32_t token0 = block * B, end = a.start + a.n;
   float* const scale = (is_v ? m.v_scale : m.k_scale) + base / B + block;
-  const float old_scale = *scale;
+  uint8_t* const k_rows = (uint8_t*)m.k + (base + token0) * 128;
+  uint8_t* const v_tiles = (uint8_t*)m.v + (base + token0) / 64 * 8192;
   const T* const src = is_v ? (const T*)a.v + head * a.v_sh : (const T*)a.k + head * a.k_sh;
   const int64_t st = is_v ? a.v_st : a.k_st;
+  const bool turn = !is_v && r.table;
+  // Whether the block holds tokens that stay.
+  const bool stays = token0 < min(a.start, m.n_tokens) || end < min(token0 + B, m.n_tokens);
 
+  float lo[2][8], hi[2][8];
+  f32x2 cs[2][8];
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const int32_t token = token0 + p * ROWS + row;
+    const int32_t i = min(max(token - a.start, 0), a.n - 1);
+    load8(src + i * st + 8 * c, lo[p]);
+    load8(src + i * st + 64 + 8 * c, hi[p]);
+    if (turn) load_turns(r, token, c, cs[p]);
+  }
+  u32x2 old[2][2];
+  float old_scale = 0.f;
+  if (stays) {
+    old_scale = *scale;
+    if (is_v) {
+      tiles_to_rows<B, THREADS>(v_tiles, bytes);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = p * ROWS + row, d = 64 * h + 8 * c;
+        if (is_v)
+          old[p][h] = *(const u32x2*)(bytes + at * LDS_ROW + d);
+        else
+          old[p][h] = *(const u32x2*)(k_rows + at * 128 + d);
+      }
+  }
   // The block's values: new tokens, held ones, zeros behind the last.
-  float lo[PASSES][8], hi[PASSES][8];
   float most = 0.f;
 #pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int32_t token = block * B + p * ROWS + row;
-    const int32_t i = token - a.start;
-    if (i >= 0 && i < a.n) {
-      load8(src + i * st + 8 * c, lo[p]);
-      load8(src + i * st + 64 + 8 * c, hi[p]);
-      if (!is_v && r.table) {
-        f32x2 cs[8];
-        load_turns(r, token, c, cs);
-        rotate16<double>(lo[p], hi[p], cs, r.halves, 1.f);
-      }
-    } else if (token < m.n_tokens) {
-      uint32_t w[4];
-      if (!is_v) {
-        const uint8_t* k = (const uint8_t*)m.k + (base + token) * 128 + 8 * c;
-        w[0] = *(const uint32_t*)k, w[1] = *(const uint32_t*)(k + 4);
-        w[2] = *(const uint32_t*)(k + 64), w[3] = *(const uint32_t*)(k + 68);
-      } else {
-        const uint8_t* v = (const uint8_t*)m.v + (base / 64 + token / 64) * 8192 +
-                           (8 * c) * 64 + v_place(token % 64);
+  for (int p = 0; p < 2; ++p) {
+    const int32_t token = token0 + p * ROWS + row;
+    const bool fresh = token >= a.start && token < end;
+    if (turn) rotate16<double>(lo[p], hi[p], cs[p], r.halves, 1.f);
+    if (stays) {
+      const bool held = token < m.n_tokens;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint8_t* e = v + ((j & 1) * 4 + (j >> 1) * 64) * 64;
-          w[j] = e[0] | e[64] << 8 | e[128] << 16 | (uint32_t)e[192] << 24;
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          float x[4];
+          from_e4m3(old[p][h][q], x);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            float& y = (h ? hi : lo)[p][4 * q + b];
+            y = fresh ? y : held ? x[b] * old_scale : 0.f;
+          }
         }
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float x[4];
-        from_e4m3(w[j], x);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) (j < 2 ? lo[p] : hi[p])[4 * (j & 1) + b] = x[b] * old_scale;
-      }
     } else {
 #pragma unroll
-      for (int b = 0; b < 8; ++b) lo[p][b] = hi[p][b] = 0.f;
+      for (int b = 0; b < 8; ++b) {
+        lo[p][b] = fresh ? lo[p][b] : 0.f;
+        hi[p][b] = fresh ? hi[p][b] : 0.f;
+      }
     }
 #pragma unroll
     for (int b = 0; b < 8; ++b)
       most = fmaxf(most, fmaxf(finite_abs(lo[p][b]), finite_abs(hi[p][b])));
   }
-  // Every held value has been read when the first one is overwritten: the barrier of
-  // the maximum comes between.
-  const int e = scale_exponent(block_max(most, most_lds));
+#pragma unroll
+  for (int off = 32; off > 0; off /= 2) most = fmaxf(most, __shfl_xor(most, off));
+  if (threadIdx.x % 64 == 0) most_lds[threadIdx.x / 64] = most;
+  // Every held value has been read when the first one is overwritten.
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) most = fmaxf(most, most_lds[w]);
+  const int e = scale_exponent(most);
   const float inv = pow2(-e);
   if (threadIdx.x == 0) *scale = pow2(e);
   auto word = [&](const float (&x)[8], int j) {
@@ -117,43 +183,24 @@ __global__ __launch_bounds__(THREADS) void write_kernel(WriteArgs a, RopeArgs r)
     }
     return to_e4m3(y[0], y[1], y[2], y[3]);
   };
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
+  for (int p = 0; p < 2; ++p) {
     const u32x2 wl = {word(lo[p], 0), word(lo[p], 1)}, wh = {word(hi[p], 0), word(hi[p], 1)};
+    const int at = p * ROWS + row;
     if (is_v) {
-      uint8_t* const to = bytes + (p * ROWS + row) * LDS_ROW + 8 * c;
-      *(u32x2*)to = wl;
-      *(u32x2*)(to + 64) = wh;
+      *(u32x2*)(bytes + at * LDS_ROW + 8 * c) = wl;
+      *(u32x2*)(bytes + at * LDS_ROW + 64 + 8 * c) = wh;
     } else {
-      uint8_t* const to = (uint8_t*)m.k + (base + block * B + p * ROWS + row) * 128 + 8 * c;
-      *(u32x2*)to = wl;
-      *(u32x2*)(to + 64) = wh;
+      *(u32x2*)(k_rows + at * 128 + 8 * c) = wl;
+      *(u32x2*)(k_rows + at * 128 + 64 + 8 * c) = wh;
     }
   }
   if (!is_v) return;
   __syncthreads();
-  // V: four elements d and 16 tokens a thread, transposed four bytes by four.
-  for (int at = threadIdx.x; at < B / 64 * 128; at += THREADS) {
-    const int tile = at / 128, dq = at % 128 / 4, g = at % 4;
-    u32x4 out[4];
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt) {
-      uint32_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        w[j] = *(const uint32_t*)(bytes + (tile * 64 + 16 * kt + 4 * g + j) * LDS_ROW + 4 * dq);
-      transpose4(w);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) out[j][kt] = w[j];
-    }
-    uint8_t* const to = (uint8_t*)m.v + (base / 64 + block * (B / 64) + tile) * 8192 +
-                        4 * dq * 64 + 16 * g;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) *(u32x4*)(to + 64 * j) = out[j];
-  }
+  rows_to_tiles<B, THREADS>(bytes, v_tiles);
 }
+
+constexpr int THREADS = 256;        // of a read
 
 struct ReadArgs {
   lvsa_kv_cache c;
@@ -175,7 +222,6 @@ __device__ __forceinline__ void store4(T* p, const float (&x)[4]) {
 // One workgroup a tile of 64 tokens, head and tensor.
 template <typename T>
 __global__ __launch_bounds__(THREADS) void read_kernel(ReadArgs a) {
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   const int tile = a.first_tile + blockIdx.x;
   const int64_t head = blockIdx.y;
   const lvsa_kv_cache& m = a.c;
@@ -225,9 +271,9 @@ __global__ __launch_bounds__(THREADS) void read_kernel(ReadArgs a) {
 template <typename T>
 void start_write(const WriteArgs& a, const RopeArgs& r, dim3 grid, hipStream_t s) {
   if (a.c.block == 64)
-    write_kernel<T, 64><<<grid, THREADS, 0, s>>>(a, r);
+    write_kernel<T, 64><<<grid, 256, 0, s>>>(a, r);
   else
-    write_kernel<T, 128><<<grid, THREADS, 0, s>>>(a, r);
+    write_kernel<T, 128><<<grid, 512, 0, s>>>(a, r);
 }
 
 }  // namespace

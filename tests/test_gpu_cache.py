@@ -611,7 +611,7 @@ def test_workspace_is_checked():
     c = _filled(1, 20000, 128)
     q = _randn((1, 1, 128), 1)
     out = torch.full_like(q, 7.0)
-    tq, to, need = L._rows(q), L._rows(out), ctypes.c_int64()
+    tq, to, need = L._rows(q, 0), L._rows(out, 0), ctypes.c_int64()
     ref = ctypes.byref
     assert L.lib().lvsa_attention_cache_workspace(ref(tq), 0, ref(c._c), None, ref(need)) == L.OK
     assert need.value > 0
