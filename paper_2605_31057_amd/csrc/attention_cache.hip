@@ -971,15 +971,14 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     Scores sc;
     Probs pr;
     int keep;   // of the step whose scores are at hand
-    // A softmax phase: V of step a is converted into stage 1 - stage, K of step b and its
-    // V bytes are loaded.
-    auto soft = [&](const Step& sa, const Step& sb, int stage) {
+    // A softmax phase's loads: V of step a is converted into stage 1 - stage, K of step b
+    // and its V bytes are loaded.
+    auto bring = [&](const Step& sa, const Step& sb, int stage) {
       u32x4 w[2];
       take_v(w);
       load_k(sb, stage);
       load_v(sb);
       store_v(sa, w, stage ^ 1);
-      weigh<MB != 0>(sc, ts, pr, scale, keep);
     };
     {
       const Step s0 = step_at(0);
@@ -997,32 +996,46 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
       tile_sync();
       // Half step 0: the others' softmax 0 and their share of V(1), K(2); the leaders
       // begin with their matrix phase 0, so they have taken softmax 0 before.
-      if (lead) {
-        weigh<MB != 0>(sc, ts, pr, scale, keep);
-      } else {
-        soft(s1, s2, 0);
-        tile_barrier();
+      if (!lead) bring(s1, s2, 0);
+      weigh<MB != 0>(sc, ts, pr, scale, keep);
+      if (!lead) tile_barrier();
+    }
+    // Step j + 1, j + 2 and j + 3 become j + 2, j + 3 and j + 4.
+    auto advance = [&](int j) {
+      if ((j + 4) % 64 == 0 && j + 4 < n) fill_window(j + 4);
+      s1 = s2;
+      s2 = s3;
+      s3 = step_at(min(j + 4, n - 1));
+    };
+    // A wave without a row only brings its share of the bytes in.
+    int32_t head, token;
+    if (!__builtin_amdgcn_ballot_w64(row_of(it, a, 32 * wave + lane % 32, head, token))) {
+      for (int j = 0; j < n; ++j) {
+        tile_sync();
+        if (j + 1 < n) bring(pick(lead, s1, s2), pick(lead, s2, s3), (j & 1) ^ (lead ? 0 : 1));
+        if (lead || j + 1 < n) tile_sync();
+        advance(j);
       }
+      return;
     }
     // Both sides run the same loop: matrix phase j, then a softmax phase, the leaders'
     // of the same step (loads of j + 2), the others' of the next one (loads of j + 3).
     for (int j = 0; j < n; ++j) {
       const int even = j & 1;
-      if ((j + 4) % 64 == 0 && j + 4 < n) fill_window(j + 4);
-      const Step s4 = step_at(min(j + 4, n - 1));
       matrix_phase<MB != 0>(lds, (even ^ 1) * K_STAGE, V_AT + even * V_STAGE, q, sc, pr, ts, f,
                             keep, s1.scales);
       keep = s1.keep;
       mask_scores(sc, s1);
       tile_sync();   // the others' loads; a leader has none under way here
-      if (j + 1 < n) soft(pick(lead, s1, s2), pick(lead, s2, s3), lead ? even : even ^ 1);
+      if (j + 1 < n) {
+        bring(pick(lead, s1, s2), pick(lead, s2, s3), lead ? even : even ^ 1);
+        weigh<MB != 0>(sc, ts, pr, scale, keep);
+      }
       if (lead)
         tile_sync();
       else if (j + 1 < n)
         tile_barrier();
-      s1 = s2;
-      s2 = s3;
-      s3 = s4;
+      advance(j);
     }
   }
 
@@ -1052,6 +1065,8 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
   const int64_t slots = (int64_t)total * TILE_ROWS;
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
+    int32_t head, token;
+    if (!row_of(it, a, 32 * wave + 16 * qt + i2, head, token)) continue;
     const int64_t slot = (item * ka.p.splits + split) * TILE_ROWS + 32 * wave + 16 * qt + i2;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt)
