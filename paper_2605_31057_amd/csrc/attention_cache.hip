@@ -521,7 +521,8 @@ __device__ __forceinline__ void q_split(QSplit& q, const __bf16* row, bool ok) {
 
 struct TileState {
   f32x4 o[8][2];   // O^T [d tile][query tile]
-  f32x4 l;         // row sums: register 0 of query tile 0, register 1 of query tile 1
+  f32x4 l[2];      // row sums, the same in every register (an accumulator each: a row that
+                   // is NaN would spoil the other tile's row of the same lane)
   float m[2];      // references (log2)
   int flags;       // READY: every row has a finite m; WIDE: a step was redone
 };
@@ -598,7 +599,7 @@ __device__ __forceinline__ void raise(const Scores& sc, TileState& st, float sca
     const float m = top > st.m[qt] ? top + head : st.m[qt] + lift;
     const float f = m == st.m[qt] ? 1.f : __builtin_amdgcn_exp2f(st.m[qt] - m);
     st.m[qt] = m;
-    st.l[qt] *= f;
+    st.l[qt][0] *= f;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) st.o[dt][qt] *= f;
   }
@@ -669,14 +670,6 @@ __device__ __forceinline__ void weigh(const Scores& sc, TileState& st, Probs& pr
   softmax_phase(sc, st, pr, scale);
 }
 
-// A operand of the row sums of query tile qt: ones in rows qt, 4 + qt, 8 + qt, 12 + qt,
-// which are register qt of every lane of the result.  Made anew each time: kept, it
-// would hold eight registers.
-__device__ __forceinline__ bf16x8 sum_rows(int qt) {
-  const uint32_t w = fresh_lane() % 4 == qt ? 0x3F803F80u : 0u;
-  return __builtin_bit_cast(bf16x8, u32x4{w, w, w, w});
-}
-
 // Matrix phase: l += row sums of P, O += P V, S = K Q^T of the next step.  MASKED: the
 // wave's query block may keep a unit or not (`keep`); V of one that it does not is read
 // from slabs of zeros, so that what the unit holds (NaN) never reaches the block.  (A
@@ -698,20 +691,22 @@ __device__ __forceinline__ void matrix_phase(const char* lds, int k_at, int v_at
   auto frag = [&](int i) {
     return *(const bf16x8*)(lds + from[i % 4 / 2] + i % 2 * SLAB + i / 4 * 1024);
   };
+  // Made anew each time: kept, they would hold four registers.
+  uint32_t one = 0x3F803F80u;
+  asm volatile("" : "+v"(one));
+  const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{one, one, one, one});
   bf16x8 fr[32];
   i32x8 kf[8];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) fr[i] = frag(i);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int qt = 0; qt < 2; ++qt) {
-    const bf16x8 ones = sum_rows(qt);
+  for (int qt = 0; qt < 2; ++qt)
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      st.l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pr.p[u][qt], st.l, 0, 0, 0);
+      st.l[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pr.p[u][qt], st.l[qt], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
-  }
   // Chains of four MFMAs into one accumulator; consecutive chains share an operand.
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt)
@@ -902,7 +897,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     for (int dt = 0; dt < 8; ++dt) ts.o[dt][qt] = f32x4{};
     ts.m[qt] = -__builtin_inff();
   }
-  ts.l = f32x4{};
+  ts.l[0] = ts.l[1] = f32x4{};
   ts.flags = 0;
 
   if (n > 0) {
@@ -1047,7 +1042,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     for (int qt = 0; qt < 2; ++qt) {
       int32_t head, token;
       if (!row_of(it, a, 32 * wave + 16 * qt + i2, head, token)) continue;
-      const float l = ts.l[qt];
+      const float l = ts.l[qt][0];
       const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
       __bf16* const out =
           (__bf16*)a.o + (int64_t)head * a.o_sh + (int64_t)token * a.o_st + 4 * g2;
@@ -1073,7 +1068,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
       *(f32x4*)(a.workspace + slot * D + 16 * dt + 4 * g2) = ts.o[dt][qt];
     if (g2 == 0) {
       a.workspace[slots * D + 2 * slot] = ts.m[qt];
-      a.workspace[slots * D + 2 * slot + 1] = ts.l[qt];
+      a.workspace[slots * D + 2 * slot + 1] = ts.l[qt][0];
     }
   }
 }

@@ -93,6 +93,19 @@ def test_rope_and_its_gradient(case):
     assert (wide[:, :, 128:] == 3.0).all()
 
 
+def test_rope_of_many_tokens():
+    """Enough tokens that a thread works several heads: the same bits as in pieces."""
+    H, n = 5, 70001
+    r = L.Rope(45, 40, 40)
+    x = torch.randn(n, H, 128, device="cuda").bfloat16().transpose(0, 1)
+    got = L.rope(x, r, start=999)
+    back = L.rope_backward(x, r, start=999)
+    for a in range(0, n, 9000):
+        piece = x[:, a: a + 9000]
+        assert torch.equal(got[:, a: a + 9000], L.rope(piece, r, start=999 + a))
+        assert torch.equal(back[:, a: a + 9000], L.rope_backward(piece, r, start=999 + a))
+
+
 @pytest.mark.parametrize("halves", [False, True])
 def test_rope_gradient_against_differences(halves):
     """L(x) = <w, rope(x)>: (L(x + d) - L(x - d)) / 2 = <rope_backward(w), d>, the map
@@ -235,6 +248,26 @@ def test_write_with_rope_bit_for_bit(halves, dtype):
         _assert_held(c, o)
 
 
+@pytest.mark.parametrize("B", [64, 128])
+def test_long_write_equals_pieces(B):
+    """A clip at once, and block by block: the same bytes."""
+    H, n = 6, 20000
+    r = L.Rope(20, 25, 39)
+    k, v = _randn((H, n, 128), 1, BF, "nhd"), _randn((H, n, 128), 2, HF).to(BF)
+    a, b = L.KvCache(H, n, B), L.KvCache(H, n, B)
+    for c in (a, b):
+        for t in (c.k, c.v):
+            t.view(torch.uint8).zero_()
+    L.kv_write(a, k, v, rope=r)
+    for at in range(0, n, 5 * B):
+        L.kv_write(b, k[:, at: at + 5 * B], v[:, at: at + 5 * B], rope=r)
+    for s, t in ((a.k, b.k), (a.v, b.v)):
+        assert torch.equal(s.view(torch.uint8), t.view(torch.uint8))
+    nb = -(-n // B)
+    assert torch.equal(a.k_scale[:, :nb], b.k_scale[:, :nb])
+    assert torch.equal(a.v_scale[:, :nb], b.v_scale[:, :nb])
+
+
 def test_reads_of_parts():
     c = L.KvCache(3, 640, 64)
     L.kv_write(c, _randn((3, 600, 128), 1), _randn((3, 600, 128), 2))
@@ -293,7 +326,7 @@ DENSE = [
     (1, 1, 1, 1000, 128), (2, 4, 1, 129, 128), (1, 17, 1, 300, 64), (2, 5, 7, 513, 128),
     (2, 1, 16, 128, 128), (1, 1, 17, 640, 64), (1, 1, 33, 127, 128), (2, 1, 100, 1, 128),
     (1, 2, 64, 200, 64), (1, 1, 129, 257, 128), (2, 1, 256, 384, 64), (1, 3, 100, 1100, 128),
-    (1, 1, 300, 3000, 64), (40, 1, 1, 70, 128), (1, 1, 513, 65, 128), (5, 2, 130, 192, 64),
+    (1, 1, 300, 2900, 64), (40, 1, 1, 70, 128), (1, 1, 513, 65, 128), (5, 2, 130, 192, 64),
 ]
 
 
@@ -417,6 +450,21 @@ def test_wide_and_narrow_logits(n, scale):
     _assert_attended(L.attention_cache(q, c), q, c)
 
 
+@pytest.mark.parametrize("n", [3, 60, 300])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_a_query_that_is_not_finite(n, bad):
+    """It becomes NaN, the others do not notice."""
+    c = _filled(2, 700, 64, seed=1)
+    q = _randn((2, n, 128), 2)
+    want = L.attention_cache(q, c)
+    q[1, 2, 77] = bad
+    got = L.attention_cache(q, c)
+    assert torch.isnan(got[1, 2]).all()
+    got[1, 2] = want[1, 2]
+    _assert_attended(got[:, :2], q[:, :2], c)
+    assert (got.float() - want.float()).abs().max() <= 2e-2
+
+
 @pytest.mark.parametrize("n", [1, 300])
 def test_rising_scores(n):
     """Keys ordered so that every block's scores exceed the last one's."""
@@ -432,7 +480,7 @@ def test_rising_scores(n):
 
 def test_weights_add_up_to_one():
     """Equal values everywhere come back as they are."""
-    for n, N in ((1, 5000), (70, 1000), (500, 3000)):
+    for n, N in ((1, 5000), (70, 1000), (500, 2900)):
         c = L.KvCache(2, N, 128)
         v = torch.full((2, N, 128), 1.375, dtype=BF, device="cuda")
         L.kv_write(c, _randn((2, N, 128), 1), v)
@@ -555,6 +603,36 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for g, q in got:
         assert torch.equal(g, want[[x is q for x in qs].index(True)])
+
+
+def test_two_threads_at_once():
+    """Host calls of two threads, each on a stream and a cache of its own."""
+    import threading
+    r = L.Rope(10, 10, 20)
+    ins = [_chunk(s, 3, 400) for s in (1, 2)]
+
+    def work(x, stream, out):
+        with torch.cuda.stream(stream):
+            c = L.KvCache(3, 2000, 128)
+            for at in (0, 400, 800, 700):
+                L.kv_write(c, x[1], x[2], start=at, rope=r)
+                q = L.rope(x[0], r, start=at)
+                out.append((L.attention_cache(q, c), L.attention_cache(q[:, :2], c)))
+            stream.synchronize()
+
+    torch.cuda.synchronize()
+    got, want = [[], []], [[], []]
+    for j in (0, 1):
+        work(ins[j], torch.cuda.Stream(), want[j])
+    threads = [threading.Thread(target=work, args=(ins[j], torch.cuda.Stream(), got[j]))
+               for j in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for a, b in zip(got, want):
+        assert len(a) == len(b) == 4
+        assert all(torch.equal(x, y) for p, q in zip(a, b) for x, y in zip(p, q))
 
 
 def test_graphs_replayed_among_eager_calls():
