@@ -427,9 +427,11 @@ __device__ __forceinline__ void load_to_lds(uint32_t dst, const u32x4& rsrc, uin
 __device__ __forceinline__ void tile_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
-// The same, with the wave's loads into LDS done.
+// The same, with the wave's loads into LDS done but for the last LEFT (other loads
+// among them only make the wait longer).
+template <int LEFT>
 __device__ __forceinline__ void tile_sync() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(LEFT) : "memory");
 }
 
 // Buffer resource of `bytes` bytes from p on, in scalar registers.
@@ -930,6 +932,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     const char* const raw = lds + RAW_AT + tid * 16;
     char* const v_to = lds + V_AT + (tid / 4) * 64 + ((tid % 4) ^ xsw(tid / 4)) * 16;
     auto take_v = [&](u32x4 (&w)[2]) {
+      asm volatile("s_waitcnt vmcnt(2)" ::: "memory");   // all but K's loads, later ones
       w[0] = *(const u32x4*)raw;
       w[1] = *(const u32x4*)(raw + SLAB);
       // Read before the next loads into the same place are issued.
@@ -966,12 +969,10 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     Scores sc;
     Probs pr;
     int keep;   // of the step whose scores are at hand
-    // A softmax phase's loads: V of step a is converted into stage 1 - stage, K of step b
-    // and its V bytes are loaded.
-    auto bring = [&](const Step& sa, const Step& sb, int stage) {
+    // V of step a is converted into stage 1 - stage, the bytes of step b are loaded.
+    auto bring_v = [&](const Step& sa, const Step& sb, int stage) {
       u32x4 w[2];
       take_v(w);
-      load_k(sb, stage);
       load_v(sb);
       store_v(sa, w, stage ^ 1);
     };
@@ -981,19 +982,22 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
       load_v(s0);
       load_k(s0, 0);
       load_k(s1, 1);
-      tile_sync();
+      tile_sync<0>();
       take_v(w);
       load_v(s1);
       store_v(s0, w, 0);
       score_from<0>(sc, lds, f, q, s0.scales);
       keep = s0.keep;
       mask_scores(sc, s0);
-      tile_sync();
+      tile_sync<0>();
       // Half step 0: the others' softmax 0 and their share of V(1), K(2); the leaders
       // begin with their matrix phase 0, so they have taken softmax 0 before.
-      if (!lead) bring(s1, s2, 0);
+      if (!lead) load_k(s2, 0);
       weigh<MB != 0>(sc, ts, pr, scale, keep);
-      if (!lead) tile_barrier();
+      if (!lead) {
+        bring_v(s1, s2, 0);
+        tile_barrier();
+      }
     }
     // Step j + 1, j + 2 and j + 3 become j + 2, j + 3 and j + 4.
     auto advance = [&](int j) {
@@ -1006,11 +1010,16 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     int32_t head, token;
     if (!__builtin_amdgcn_ballot_w64(row_of(it, a, 32 * wave + lane % 32, head, token))) {
       for (int j = 0; j < n; ++j) {
-        tile_sync();
-        if (j + 1 < n) bring(pick(lead, s1, s2), pick(lead, s2, s3), (j & 1) ^ (lead ? 0 : 1));
-        if (lead || j + 1 < n) tile_sync();
+        tile_sync<2>();
+        if (j + 1 < n) {
+          const int stage = (j & 1) ^ (lead ? 0 : 1);
+          load_k(pick(lead, s2, s3), stage);
+          bring_v(pick(lead, s1, s2), pick(lead, s2, s3), stage);
+        }
+        if (lead || j + 1 < n) tile_sync<2>();
         advance(j);
       }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       return;
     }
     // Both sides run the same loop: matrix phase j, then a softmax phase, the leaders'
@@ -1021,17 +1030,21 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
                             keep, s1.scales);
       keep = s1.keep;
       mask_scores(sc, s1);
-      tile_sync();   // the others' loads; a leader has none under way here
+      tile_sync<2>();   // K's loads; V's have until the bytes are taken
       if (j + 1 < n) {
-        bring(pick(lead, s1, s2), pick(lead, s2, s3), lead ? even : even ^ 1);
+        const int stage = lead ? even : even ^ 1;
+        load_k(pick(lead, s2, s3), stage);
         weigh<MB != 0>(sc, ts, pr, scale, keep);
+        bring_v(pick(lead, s1, s2), pick(lead, s2, s3), stage);
       }
       if (lead)
-        tile_sync();
+        tile_sync<2>();
       else if (j + 1 < n)
         tile_barrier();
       advance(j);
     }
+    // No load may land in LDS that is another workgroup's by then.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 
   // Every wave holds whole rows.  (The lane anew: rows and addresses are not kept from
