@@ -378,14 +378,15 @@ typedef struct lvsa_kv_cache {
 
 /* Quantises keys and values into tokens start .. start + n - 1 of the cache
  * (n = k->n_tokens; 0 <= start <= cache->n_tokens, start + n <= capacity) and
- * sets cache->n_tokens = max(cache->n_tokens, start + n).  k and v are
- * [cache->heads, n, 128] of `dtype`.  rope (or NULL) rotates the keys on the
+ * sets cache->n_tokens = max(cache->n_tokens, start + n), at the call (a write that
+ * is captured into a graph sets it once, not when the graph is replayed).  k and v
+ * are [cache->heads, n, 128] of `dtype`.  rope (or NULL) rotates the keys on the
  * way, token start + i at its grid position: the rotation is taken in fp64 and
  * rounded to fp32 before the scale and the 8 bits.
  * Blocks that the new tokens touch are written whole: their other held tokens
  * keep the values they had, rounded again where the block's scale has grown;
  * places behind the last token become zeros.  Blocks that they do not touch are
- * left as they are.
+ * left as they are.  Writes that touch the same block have to be ordered.
  * Errors: EINVAL (nulls, ranges, shapes), EUNSUPPORTED (layout, head_dim,
  * capacity), EDEVICE (launch; n_tokens is then unchanged). */
 lvsa_status lvsa_kv_write(lvsa_kv_cache* cache, const lvsa_tensor* k,
@@ -505,7 +506,10 @@ lvsa_status lvsa_rope_backward(const lvsa_tensor* grad_out, int32_t dtype,
  * lvsa_attention_cache_workspace gives for the same arguments (0: may be NULL);
  * any content; written by the call, so calls that may overlap in time (two
  * streams, two graphs) need one each.
- * The result is deterministic for given shapes, mask and device.
+ * out must not overlap q or the cache.  The result is deterministic for given
+ * shapes, mask and device.  With 65 or more queries, v of magnitudes below 2^-100
+ * loses precision where a row's scores exceed those of the keys taken first by more
+ * than 5 (natural logarithm).
  * Errors: EINVAL (nulls, ranges, shape mismatch, workspace too small),
  * EUNSUPPORTED (head_dim, block, alignment, strides, sizes), EDEVICE (launch). */
 lvsa_status lvsa_attention_cache(const lvsa_tensor* q, int32_t q_start,

@@ -476,6 +476,14 @@ def _type_code(first, second):
     return code
 
 
+def _place(at):
+    """A token's place, within what the library's 32-bit arguments hold (ctypes would
+    cut it down without a word)."""
+    if not 0 <= at < 2 ** 31:
+        raise LvsaError(EINVAL, f"token {at}")
+    return at
+
+
 def _raw_stream(device):
     """The current stream of ``device``, as an address."""
     raw = getattr(_TORCH._C, "_cuda_getCurrentRawStream", None)
@@ -501,6 +509,8 @@ class Rope:
     def __init__(self, frames, height, width, pairs=(22, 21, 21), theta=10000.0,
                  layout=ROPE_PAIRS, table=None, device="cuda"):
         torch = _torch()
+        if not all(0 <= n < 2 ** 31 for n in (frames, height, width, *pairs)):
+            raise LvsaError(EINVAL, "Rope")
         self._c = _Rope(frames, height, width, (_i32 * 3)(*pairs), layout, None)
         n = _i64()
         _check(lib().lvsa_rope_table_size(ctypes.byref(self._c), ctypes.byref(n)),
@@ -530,8 +540,8 @@ def _rotate(name, x, r, start, out):
     dev = torch.cuda.current_device()
     if out is None:
         out = torch.empty_like(x)
-    _check(getattr(lib(), name)(ctypes.byref(_rows(x, dev)), _type_code(x, out), start,
-                                _rope_ref(r, dev), ctypes.byref(_rows(out, dev)),
+    _check(getattr(lib(), name)(ctypes.byref(_rows(x, dev)), _type_code(x, out),
+                                _place(start), _rope_ref(r, dev), ctypes.byref(_rows(out, dev)),
                                 _raw_stream(dev)), name)
     return out
 
@@ -562,6 +572,9 @@ class KvCache:
     def __init__(self, heads, capacity, block=128, n_tokens=0, buffers=None, device="cuda"):
         torch = _torch()
         capacity = -(-capacity // 128) * 128
+        if block not in (64, 128) or not 0 < capacity <= 1 << 24 or not 0 < heads < 65536:
+            raise LvsaError(EUNSUPPORTED, f"KvCache of {heads} heads, {capacity} tokens, "
+                            f"blocks of {block}")
         f8, f32 = torch.float8_e4m3fn, torch.float32
         shapes = [((heads, capacity, 128), f8), ((heads, capacity // 64, 128, 64), f8),
                   ((heads, capacity // block), f32), ((heads, capacity // block), f32)]
@@ -570,6 +583,8 @@ class KvCache:
         for b, (s, t) in zip(buffers, shapes, strict=True):
             if tuple(b.shape) != s or b.dtype != t or not b.is_contiguous():
                 raise ValueError(f"expected a contiguous {t} buffer of shape {s}")
+            if b.device != buffers[0].device:
+                raise ValueError("expected buffers on one device")
         self.k, self.v, self.k_scale, self.v_scale = buffers
         self._c = _KvCache(heads, capacity, block, 0, *(b.data_ptr() for b in buffers))
         self.n_tokens = n_tokens
@@ -612,7 +627,7 @@ def kv_write(cache, k, v, start=None, rope=None, stream=None):
     dev = _torch().cuda.current_device()
     _check(lib().lvsa_kv_write(_cache_ref(cache, dev), ctypes.byref(_rows(k, dev)),
                                ctypes.byref(_rows(v, dev)), _type_code(k, v),
-                               cache._c.n_tokens if start is None else start,
+                               cache._c.n_tokens if start is None else _place(start),
                                _rope_ref(rope, dev), _raw_stream(dev)), "lvsa_kv_write")
     return cache
 
@@ -637,7 +652,7 @@ def kv_read(cache, start=0, n=None, dtype=None, out=None, stream=None):
         raise ValueError("expected out tensors of n tokens")
     if dtype is not None and k.dtype != dtype:
         raise ValueError("expected out tensors of the given type")
-    _check(lib().lvsa_kv_read(_cache_ref(cache, dev), start, ctypes.byref(tk), ctypes.byref(tv),
+    _check(lib().lvsa_kv_read(_cache_ref(cache, dev), _place(start), ctypes.byref(tk), ctypes.byref(tv),
                               _type_code(k, v), _raw_stream(dev)), "lvsa_kv_read")
     return out
 
@@ -656,6 +671,7 @@ def attention_cache(q, cache, mask=None, q_start=0, out=None, stream=None):
     if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
         raise ValueError("expected bfloat16 tensors")
     L = lib()
+    q_start = _place(q_start)
     tq, to = ctypes.byref(_rows(q, dev)), ctypes.byref(_rows(out, dev))
     c = _cache_ref(cache, dev)
     m = None if mask is None else ctypes.byref(mask)

@@ -211,6 +211,15 @@ def test_python_refusals():
         L.Rope(3, 4, 5, table=torch.zeros(7, 2), device="cpu")
     with pytest.raises(ValueError):
         L.KvCache(2, 256, n_tokens=257, device="cpu")
+    for bad in (dict(frames=2 ** 32 + 3), dict(pairs=(2 ** 32, 21, 21)), dict(height=-1)):
+        with pytest.raises(L.LvsaError):
+            L.Rope(**{**dict(frames=3, height=4, width=5, device="cpu"), **bad})
+    for bad in ((2, 256, 32), (2, 0, 64), (2, (1 << 24) + 1, 64), (0, 128, 64), (65536, 128, 64)):
+        with pytest.raises(L.LvsaError):
+            L.KvCache(*bad, device="cpu")
+    for at in (-1, 2 ** 31, 2 ** 32):      # ctypes would take 2^32 for 0
+        with pytest.raises(L.LvsaError):
+            L._place(at)
     c = L.KvCache(2, 200, 64, device="cpu")
     assert (c.heads, c.capacity, c.block, c.n_tokens) == (2, 256, 64, 0)
     with pytest.raises(ValueError):

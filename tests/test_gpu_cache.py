@@ -424,6 +424,37 @@ def test_unkept_blocks_never_reach_a_query(n):
         assert torch.isnan(got[:, torch.from_numpy(hit).cuda()]).all()
 
 
+def test_places_past_32_bits_are_refused():
+    c = _filled(1, 200, 64)
+    x, r = _randn((1, 2, 128), 1), L.Rope(3, 4, 5)
+    for at in (2 ** 32, -1):
+        for f in (lambda: L.rope(x, r, start=at), lambda: L.kv_write(c, x, x, start=at),
+                  lambda: L.kv_read(c, at, 1), lambda: L.attention_cache(x, c, q_start=at)):
+            with pytest.raises(L.LvsaError):
+                f()
+    assert c.n_tokens == 200
+
+
+@pytest.mark.parametrize("n", [1, 70, 260])
+def test_masks_of_8000_blocks(n):
+    """The most that a mask may have; the last query block's row is full, the others
+    hold a few blocks, first and last among them."""
+    B, nb = 64, 8000
+    N = nb * B - 5
+    c = _filled(1, N, 128)
+    rng = np.random.default_rng(n)
+    rows = [sorted({0, nb - 1, *rng.integers(0, nb, 20).tolist()}) for _ in range(nb - 1)]
+    rows.append(list(range(nb)))
+    rp = np.concatenate([[0], np.cumsum([len(r) for r in rows])]).astype(np.int32)
+    ci = np.array([x for r in rows for x in r], dtype=np.int32)
+    mask = L.csr_mask(torch.from_numpy(rp).cuda(), torch.from_numpy(ci).cuda(), N, B)
+    q = _randn((1, n, 128), 4)
+    got = L.attention_cache(q, c, mask=mask, q_start=N - n)
+    some = [0, n // 2, n - 1]
+    keep = OC.block_keep(rp, ci, B, N, N - n, n)
+    _assert_attended(got[:, some], q[:, some], c, keep[some])
+
+
 def test_columns_outside_the_mask_are_skipped():
     N, B = 700, 64
     c = _filled(1, N, B)
