@@ -2,18 +2,17 @@
 //
 //   out = softmax(q K^T / sqrt(128)) V, K and V from e4m3 bytes times a power of two.
 //
-// e4m3 * 2^e is exact in bf16, so K and V fragments are converted on their way to
-// the bf16 matrix instructions (cvt_scalef32, the scale at no cost) and the only
-// roundings are those of P to bf16 and of the output.
+// e4m3 * 2^e is exact in bf16: bytes become bf16 matrix operands by one conversion
+// (cvt_scalef32, the scale at no cost), and the only roundings are those of P to bf16
+// and of the output, besides fp32 sums (and the fp8 products of the tiles, below).
 //
-// Work: an item is up to ROWS query rows that share a key head and, with a mask, a
-// query block (row = query head of the group times the block's tokens + token, so
-// shared key heads are read once for the whole group).  Its keys, units of 64
-// tokens, are split over `splits` workgroups, and a workgroup's over its four
-// waves.  A wave takes K and V fragments from memory straight into registers, one
-// unit ahead: nothing is shared between waves but the final combination.  With
-// splits > 1 partial results (fp32 O, reference m and row sum l) go to the
-// workspace and a second kernel combines them in the order of the splits.
+// Work: an item is some query rows of one key head; its keys, units of 64 tokens, are
+// split over `splits` workgroups.  With splits > 1 partial results (fp32 O, reference
+// m and row sum l) go to the workspace and combine_kernel adds them in the order of
+// the splits.  Two forms, by the rows that can share an item (plan_of): up to 64 rows
+// the keys' bytes bound the call and rows_kernel streams them, from there on the
+// products do and tile_kernel works 256 rows at a time.  12 heads over 32,768 tokens, 32,
+// 64, 100 and 200 queries: 27, 36, 48 and 60 us.
 #include <type_traits>
 
 #include "values.h"
@@ -124,6 +123,13 @@ __device__ __forceinline__ float row_max(float x) {
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
+// Few query rows: an item is up to 16 RT rows that share a key head and, with a mask, a
+// query block (row = query head of the group times the block's tokens + token, so
+// shared key heads are read once for the whole group).  Four waves take every fourth
+// unit and share nothing until their results are combined in LDS.  One query of 12
+// heads over 32,760 tokens: 19 us, 5.3 TB/s of keys and values; 40 rows of 8 key heads
+// over 131,071 tokens 59 us, 4.6 TB/s (and the combining launch, 4 to 5 us).
+//
 // RT: 16-row tiles of the item, each K and V fragment is used for all of them.  A wave
 // holds one unit's bytes: K's of the next unit are loaded when this one's scores are
 // done, V's when its products are, so both are on their way for most of a unit, and
@@ -357,28 +363,37 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
 
 // ------------------------------------------------------------------- tiles
 //
-// Many query rows: an item is 256 rows of one query head, eight waves of 32, which walk
-// the union of its query blocks' key lists 128 keys (two units) a step, sharing
-// every K and V byte through LDS.
+// Many query rows: an item is 256 rows, eight waves of 32, which walk the union of its
+// query blocks' key lists 128 keys (two units) a step, sharing every K and V byte
+// through LDS.
 //
 //   S^T = K Q^T     fp8 MFMA 16x16x128, K as its e4m3 bytes with the block's scale as
 //                   the instruction's, Q as the sum of two e4m3 numbers (q_split)
 //   O^T += V^T P^T  bf16 MFMA 16x16x32, V converted to bf16 on its way into LDS
 //
 // Two fp8 MFMAs of 128 elements take the matrix core as long as four bf16 ones of
-// 32, but K's bytes are half the LDS reads and need no conversion.  V is converted
-// once a workgroup, 32 elements a thread and step.  P needs its eight bits: e4m3
-// pairs as for Q would cost two VALU operations an element more than they save.
+// 32 (4.0 and 2.1 PFLOP/s under load), but K's bytes are half the LDS reads and need no
+// conversion.  The instruction adds its 128 products less exactly than fp32: 1.3e-5 of
+// the result on N(0, 1) data, 2^-13 of sum |q k| at worst (measured), far below P's
+// rounding.  V is converted once a workgroup, 32 elements a thread and step.  P needs
+// its eight bits: e4m3 pairs as for Q would cost two VALU operations an element more
+// than they save.
+//
+// What bounds it: board power, and the matrix phase.  4,680 queries of 40 heads over
+// 63,960 tokens take 4.45 ms (1.38 PFLOP/s; a large bf16 matrix product 1.6), the matrix
+// cores busy 63% of the cycles at 2.0 GHz.  Without exponentials it takes the same time,
+// without the softmax's arithmetic 6% less, without loads and conversions 4% less, with
+// half the fp8 products 15% less.
 //
 // Schedule: waves w and w + 4 share a SIMD and run half a step apart, one in its
 // matrix phase while the other is in its softmax phase; a barrier ends each half
 // step.  Half steps 2j and 2j + 1: the leaders (waves 0-3) are in matrix phase j, then
 // softmax j + 1; the others in softmax j, then matrix phase j.  K(j+1) and V(j) stay
 // in LDS through both; K(j+2) and V(j+1) go into the other two stages, by every wave
-// in its softmax phase.  Both come straight from memory into LDS; V's bytes into a
-// place of each wave's own, from which the wave takes them a step later, converts
-// them and writes them into the stage (held in registers meanwhile, 8 of them, they
-// made the compiler spill).
+// in its softmax phase: K's loads before the weights; after them V's bytes, loaded a step
+// ago into a place of the wave's own, are converted and written into the stage, and
+// the next step's loaded (held in registers meanwhile, 8 of them, they made the compiler
+// spill).  All loads go from memory into LDS.
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -452,8 +467,8 @@ __device__ __forceinline__ int fresh_lane() {
 
 // One step's units.
 struct Step {
-  int32_t unit[2];   // 0 where there is none
-  int32_t left[2];   // held tokens from the unit's first on; 0: none, or not kept by any
+  int32_t unit[2];
+  int32_t left[2];   // held tokens from the unit's first on, at most 0: none
   int32_t keep;      // bit u: this wave's query block keeps unit u
   int32_t scales;    // exponent bytes: K of unit 0, of unit 1, V of unit 0, of unit 1
 };
@@ -681,10 +696,10 @@ template <bool MASKED>
 __device__ __forceinline__ void matrix_phase(const char* lds, int k_at, int v_at, const QSplit& q,
                                              Scores& sc, const Probs& pr, TileState& st,
                                              uint32_t f, int keep, int k_scale) {
-  // Fragments read ahead.  4,680 queries of 40 heads over 63,960 tokens: 4.63 ms with 8,
-  // 4.60 with 10, 4.54 with 12, 4.55 with 14; one frame of 12 heads over the 121-frame mask:
-  // 306 us with 4, 249 with 6, 235, 220, 238 and 226 with 8 to 14.
-  constexpr int AHEAD = MASKED ? 10 : 12;
+  // Fragments read ahead, 6, 8, 10, 12 and 14.  4,680 queries of 40 heads over 63,960
+  // tokens: 4.61, 4.46, 4.49, 4.42 and 4.47 ms; one frame of 12 heads over the 121-frame
+  // mask: 220, 217, 211, 213 and 213 us, with 64-token blocks 209, 206, 215, 213 and 213.
+  constexpr int AHEAD = 12;
   const char* const k = lds + k_at;
   uint32_t from[2];   // the slabs of V's units
 #pragma unroll
@@ -818,15 +833,16 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     words = (a.n_tokens + UNIT - 1) / UNIT;
     n = (words + 1) / 2;
   } else {
-    words = union_list((uint32_t*)(lds + LIST_AT), (uint32_t*)(lds + V_AT), (int32_t*)(lds + TILE_LDS - 64), a.row_ptr,
-                       a.col_idx, it.block0, it.blocks, a.mask_blocks);
+    words = union_list((uint32_t*)(lds + LIST_AT), (uint32_t*)(lds + V_AT),
+                       (int32_t*)(lds + TILE_LDS - 64), a.row_ptr, a.col_idx, it.block0,
+                       it.blocks, a.mask_blocks);
     n = MB == 128 ? words : (words + 1) / 2;
     for (int at = tid * 16; at < V_STAGE / 2; at += TILE_THREADS * 16)
       *(u32x4*)(lds + ZERO_AT + at) = u32x4{};   // read after the next barriers
   }
   s0 = (int32_t)((int64_t)n * split / ka.p.splits);
   n = (int32_t)((int64_t)n * (split + 1) / ka.p.splits) - s0;
-  const int my_block = MB ? 32 * wave / (MB ? MB : 1) : 0;
+  const int my_block = MB ? 32 * wave / (MB ? MB : 1) : 0;   // of the item's query blocks
   // Units and scales of 64 steps, a step a lane, from which a step's are read by lane:
   // memory or LDS reads in the loop would be counted together with the fragments' reads
   // (scalar loads come back in any order, so the next wait is for all of them).
