@@ -47,6 +47,7 @@ _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
 _p = ctypes.c_void_p
 _pi32 = ctypes.POINTER(ctypes.c_int32)
+_byref = ctypes.byref
 
 
 class LvsaError(RuntimeError):
@@ -435,19 +436,36 @@ def dense_attention(q, k, v, block=128, out=None, stream=None):
 
 # A call of one of these on a few tokens takes a few microseconds on the GPU, so the
 # marshalling keeps to what it needs: plain integers, no context managers without a
-# stream, nothing looked up twice.
+# stream, and nothing looked up twice (``_fast``).
 
-_TORCH = None
-_CODES = {}
+_FAST = None
 
 
-def _torch():
-    global _TORCH
-    if _TORCH is None:
+class _Fast:
+    """What the calls below use of torch and the library."""
+
+    def __init__(self):
         import torch
-        _CODES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
-        _TORCH = torch
-    return _TORCH
+        L = lib()
+        self.torch = torch
+        self.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+        self.bf16 = torch.bfloat16
+        self.empty, self.empty_like = torch.empty, torch.empty_like
+        self.device = torch.cuda.current_device
+        # The current stream of a device, as an address.
+        self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+        self.forward, self.backward = L.lvsa_rope_forward, L.lvsa_rope_backward
+        self.write, self.read = L.lvsa_kv_write, L.lvsa_kv_read
+        self.attend = L.lvsa_attention_cache
+        self.attend_workspace = L.lvsa_attention_cache_workspace
+
+
+def _fast():
+    global _FAST
+    if _FAST is None:
+        _FAST = _Fast()
+    return _FAST
 
 
 def _rows(t, device):
@@ -464,13 +482,13 @@ def _rows(t, device):
     H, n, d = shape
     if n <= 1:
         st = d
-    return _Tensor(t.data_ptr(), H, n, d, sh if H > 1 else n * st, st)
+    return _byref(_Tensor(t.data_ptr(), H, n, d, sh if H > 1 else n * st, st))
 
 
 def _type_code(first, second):
     if first.dtype != second.dtype:
         raise ValueError("expected tensors of one type")
-    code = _CODES.get(first.dtype)
+    code = _FAST.codes.get(first.dtype)
     if code is None:
         raise ValueError("expected bfloat16, float16 or float32")
     return code
@@ -484,15 +502,9 @@ def _place(at):
     return at
 
 
-def _raw_stream(device):
-    """The current stream of ``device``, as an address."""
-    raw = getattr(_TORCH._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw else _TORCH.cuda.current_stream(device).cuda_stream
-
-
 def _with_stream(fn, stream, *args):
     """fn(*args) with ``stream`` current: torch allocates for it then."""
-    torch = _torch()
+    torch = _fast().torch
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     with torch.cuda.stream(stream):
@@ -508,7 +520,7 @@ class Rope:
 
     def __init__(self, frames, height, width, pairs=(22, 21, 21), theta=10000.0,
                  layout=ROPE_PAIRS, table=None, device="cuda"):
-        torch = _torch()
+        import torch
         if not all(0 <= n < 2 ** 31 for n in (frames, height, width, *pairs)):
             raise LvsaError(EINVAL, "Rope")
         self._c = _Rope(frames, height, width, (_i32 * 3)(*pairs), layout, None)
@@ -525,24 +537,26 @@ class Rope:
             raise ValueError(f"expected a contiguous float32 table of {n.value} (cos, sin)")
         self.table = table
         self._c.table = table.data_ptr()
+        self._device, self._ref = table.get_device(), ctypes.byref(self._c)
 
 
 def _rope_ref(r, device):
     if r is None:
         return None
-    if r.table.get_device() != device:
+    if r._device != device:
         raise ValueError("expected a table on the current device")
-    return ctypes.byref(r._c)
+    return r._ref
 
 
-def _rotate(name, x, r, start, out):
-    torch = _torch()
-    dev = torch.cuda.current_device()
+def _rotate(call, name, x, r, start, out):
+    f = _FAST
+    dev = f.device()
     if out is None:
-        out = torch.empty_like(x)
-    _check(getattr(lib(), name)(ctypes.byref(_rows(x, dev)), _type_code(x, out),
-                                _place(start), _rope_ref(r, dev), ctypes.byref(_rows(out, dev)),
-                                _raw_stream(dev)), name)
+        out = f.empty_like(x)
+    status = call(_rows(x, dev), _type_code(x, out), _place(start), _rope_ref(r, dev),
+                  _rows(out, dev), f.stream(dev))
+    if status:
+        raise LvsaError(status, name)
     return out
 
 
@@ -551,7 +565,7 @@ def rope(x, r, start=0, out=None, stream=None):
     start + i of the grid, rotated by ``r`` (lvsa_rope_forward); out may be x."""
     if stream is not None:
         return _with_stream(rope, stream, x, r, start, out)
-    return _rotate("lvsa_rope_forward", x, r, start, out)
+    return _rotate(_fast().forward, "lvsa_rope_forward", x, r, start, out)
 
 
 def rope_backward(grad, r, start=0, out=None, stream=None):
@@ -559,7 +573,7 @@ def rope_backward(grad, r, start=0, out=None, stream=None):
     (lvsa_rope_backward); out may be grad."""
     if stream is not None:
         return _with_stream(rope_backward, stream, grad, r, start, out)
-    return _rotate("lvsa_rope_backward", grad, r, start, out)
+    return _rotate(_fast().backward, "lvsa_rope_backward", grad, r, start, out)
 
 
 class KvCache:
@@ -570,7 +584,7 @@ class KvCache:
     lvsa_kv_cache lays them out; allocated if not given."""
 
     def __init__(self, heads, capacity, block=128, n_tokens=0, buffers=None, device="cuda"):
-        torch = _torch()
+        import torch
         capacity = -(-capacity // 128) * 128
         if block not in (64, 128) or not 0 < capacity <= 1 << 24 or not 0 < heads < 65536:
             raise LvsaError(EUNSUPPORTED, f"KvCache of {heads} heads, {capacity} tokens, "
@@ -587,6 +601,7 @@ class KvCache:
                 raise ValueError("expected buffers on one device")
         self.k, self.v, self.k_scale, self.v_scale = buffers
         self._c = _KvCache(heads, capacity, block, 0, *(b.data_ptr() for b in buffers))
+        self._device, self._ref = self.k.get_device(), ctypes.byref(self._c)
         self.n_tokens = n_tokens
 
     @property
@@ -613,9 +628,9 @@ class KvCache:
 
 
 def _cache_ref(c, device):
-    if c.k.get_device() != device:
+    if c._device != device:
         raise ValueError("expected a cache on the current device")
-    return ctypes.byref(c._c)
+    return c._ref
 
 
 def kv_write(cache, k, v, start=None, rope=None, stream=None):
@@ -624,11 +639,11 @@ def kv_write(cache, k, v, start=None, rope=None, stream=None):
     rotated by ``rope`` on the way (lvsa_kv_write); returns the cache."""
     if stream is not None:
         return _with_stream(kv_write, stream, cache, k, v, start, rope)
-    dev = _torch().cuda.current_device()
-    _check(lib().lvsa_kv_write(_cache_ref(cache, dev), ctypes.byref(_rows(k, dev)),
-                               ctypes.byref(_rows(v, dev)), _type_code(k, v),
-                               cache._c.n_tokens if start is None else _place(start),
-                               _rope_ref(rope, dev), _raw_stream(dev)), "lvsa_kv_write")
+    f = _fast()
+    dev = f.device()
+    _check(f.write(_cache_ref(cache, dev), _rows(k, dev), _rows(v, dev), _type_code(k, v),
+                   cache._c.n_tokens if start is None else _place(start),
+                   _rope_ref(rope, dev), f.stream(dev)), "lvsa_kv_write")
     return cache
 
 
@@ -638,22 +653,24 @@ def kv_read(cache, start=0, n=None, dtype=None, out=None, stream=None):
     (lvsa_kv_read); returns (k, v)."""
     if stream is not None:
         return _with_stream(kv_read, stream, cache, start, n, dtype, out)
-    torch = _torch()
-    dev = torch.cuda.current_device()
+    f = _fast()
+    dev = f.device()
+    _place(start)
     if out is None:
         n = cache.n_tokens - start if n is None else n
         if n < 1:
             raise LvsaError(EINVAL, f"{n} tokens to read")
-        out = torch.empty(2, cache._c.heads, n, 128, dtype=dtype or torch.bfloat16,
-                          device=cache.k.device).unbind(0)
+        if start + n > cache.n_tokens:
+            raise LvsaError(EINVAL, f"tokens {start} .. {start + n - 1} of {cache.n_tokens}")
+        out = f.empty((2, cache._c.heads, n, 128), dtype=dtype or f.bf16,
+                      device=cache.k.device).unbind(0)
     k, v = out
-    tk, tv = _rows(k, dev), _rows(v, dev)
-    if tv.n_tokens != tk.n_tokens or (n is not None and tk.n_tokens != n):
+    if v.shape != k.shape or (n is not None and k.shape[1] != n):
         raise ValueError("expected out tensors of n tokens")
     if dtype is not None and k.dtype != dtype:
         raise ValueError("expected out tensors of the given type")
-    _check(lib().lvsa_kv_read(_cache_ref(cache, dev), _place(start), ctypes.byref(tk), ctypes.byref(tv),
-                              _type_code(k, v), _raw_stream(dev)), "lvsa_kv_read")
+    _check(f.read(_cache_ref(cache, dev), start, _rows(k, dev), _rows(v, dev), _type_code(k, v),
+                  f.stream(dev)), "lvsa_kv_read")
     return out
 
 
@@ -664,23 +681,20 @@ def attention_cache(q, cache, mask=None, q_start=0, out=None, stream=None):
     (lvsa_attention_cache); returns out."""
     if stream is not None:
         return _with_stream(attention_cache, stream, q, cache, mask, q_start, out)
-    torch = _torch()
-    dev = torch.cuda.current_device()
+    f = _fast()
+    dev = f.device()
     if out is None:
-        out = torch.empty_like(q)
-    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
+        out = f.empty_like(q)
+    if q.dtype != f.bf16 or out.dtype != f.bf16:
         raise ValueError("expected bfloat16 tensors")
-    L = lib()
-    q_start = _place(q_start)
-    tq, to = ctypes.byref(_rows(q, dev)), ctypes.byref(_rows(out, dev))
-    c = _cache_ref(cache, dev)
-    m = None if mask is None else ctypes.byref(mask)
+    tq, to, c = _rows(q, dev), _rows(out, dev), _cache_ref(cache, dev)
+    m = None if mask is None else _byref(mask)
+    _place(q_start)
     need = _i64()
-    _check(L.lvsa_attention_cache_workspace(tq, q_start, c, m, ctypes.byref(need)),
-           "lvsa_attention_cache_workspace")
+    _check(f.attend_workspace(tq, q_start, c, m, _byref(need)), "lvsa_attention_cache_workspace")
     size, work = need.value, None
     if size:
-        work = torch.empty(size, dtype=torch.uint8, device=q.device)
-    _check(L.lvsa_attention_cache(tq, q_start, c, m, to, work.data_ptr() if size else None, size,
-                                  _raw_stream(dev)), "lvsa_attention_cache")
+        work = f.empty(size, dtype=f.torch.uint8, device=q.device)
+    _check(f.attend(tq, q_start, c, m, to, work.data_ptr() if size else None, size,
+                    f.stream(dev)), "lvsa_attention_cache")
     return out

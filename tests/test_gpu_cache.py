@@ -722,13 +722,13 @@ def test_workspace_is_checked():
     out = torch.full_like(q, 7.0)
     tq, to, need = L._rows(q, 0), L._rows(out, 0), ctypes.c_int64()
     ref = ctypes.byref
-    assert L.lib().lvsa_attention_cache_workspace(ref(tq), 0, ref(c._c), None, ref(need)) == L.OK
+    assert L.lib().lvsa_attention_cache_workspace(tq, 0, ref(c._c), None, ref(need)) == L.OK
     assert need.value > 0
     work = torch.empty(need.value + 16, dtype=torch.uint8, device="cuda")
     call = L.lib().lvsa_attention_cache
 
     def run(ptr, size):
-        return call(ref(tq), 0, ref(c._c), None, ref(to), ptr, size, L._stream_ptr(None))
+        return call(tq, 0, ref(c._c), None, to, ptr, size, L._stream_ptr(None))
 
     assert run(None, need.value) == L.EINVAL
     assert run(work.data_ptr(), need.value - 1) == L.EINVAL
