@@ -380,7 +380,7 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
 // than they save.
 //
 // What bounds it: board power, and the matrix phase.  4,680 queries of 40 heads over
-// 63,960 tokens take 4.45 ms (1.38 PFLOP/s; a large bf16 matrix product 1.6), the matrix
+// 63,960 tokens take 4.43 ms (1.38 PFLOP/s; a large bf16 matrix product 1.6), the matrix
 // cores busy 63% of the cycles at 2.0 GHz.  Without exponentials it takes the same time,
 // without the softmax's arithmetic 6% less, without loads and conversions 4% less, with
 // half the fp8 products 15% less.
@@ -570,16 +570,6 @@ __device__ __forceinline__ void score_tile(Scores& sc, const i32x8& f, const QSp
         f, q.low[qt], c, 0, 0, KT / 4, k_scale, 1, q.scale[qt]);
   }
 }
-template <int KT>
-__device__ __forceinline__ void score_from(Scores& sc, const char* k, uint32_t f,
-                                           const QSplit& q, int k_scale) {
-  if constexpr (KT < 8) {
-    score_tile<KT>(sc, k_frag(k, f, KT), q, k_scale);
-    __builtin_amdgcn_sched_barrier(0);
-    score_from<KT + 1>(sc, k, f, q, k_scale);
-  }
-}
-
 // Scores of keys that do not exist or that the wave's query block does not keep: -inf.
 __device__ __forceinline__ void mask_scores(Scores& sc, const Step& st) {
 #pragma unroll
@@ -979,12 +969,6 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
 
     const bool lead = wave < 4;
     const float scale = ka.scale_log2;
-    // Steps j + 1, j + 2, j + 3.
-    fill_window(0);
-    Step s1 = step_at(min(1, n - 1)), s2 = step_at(min(2, n - 1)), s3 = step_at(min(3, n - 1));
-    Scores sc;
-    Probs pr;
-    int keep;   // of the step whose scores are at hand
     // V of step a is converted into stage 1 - stage, the bytes of step b are loaded.
     auto bring_v = [&](const Step& sa, const Step& sb, int stage) {
       u32x4 w[2];
@@ -992,30 +976,32 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
       load_v(sb);
       store_v(sa, w, stage ^ 1);
     };
-    {
-      const Step s0 = step_at(0);
-      u32x4 w[2];
-      load_v(s0);
-      load_k(s0, 0);
-      load_k(s1, 1);
-      tile_sync<0>();
-      take_v(w);
-      load_v(s1);
-      store_v(s0, w, 0);
-      score_from<0>(sc, lds, f, q, s0.scales);
-      keep = s0.keep;
-      mask_scores(sc, s0);
-      tile_sync<0>();
-      // Half step 0: the others' softmax 0 and their share of V(1), K(2); the leaders
-      // begin with their matrix phase 0, so they have taken softmax 0 before.
-      if (!lead) load_k(s2, 0);
-      weigh<MB != 0>(sc, ts, pr, scale, keep);
-      if (!lead) {
-        bring_v(s1, s2, 0);
-        tile_barrier();
-      }
+    // The loop begins with matrix phase -1, which has no weights and zeros for V and gives
+    // the scores of step 0.  With code of its own for these scores and their softmax, 4,680
+    // queries of 40 heads over 63,960 tokens took 4.48 ms instead of 4.43, 256 queries of
+    // 256 heads over 32,768 tokens 910 us instead of 903; one frame over a mask the same.
+    fill_window(0);
+    Step s1 = step_at(0), s2 = step_at(min(1, n - 1)), s3 = step_at(min(2, n - 1));   // j + 1 ..
+    load_v(s1);
+    load_k(s1, 0);
+    if (MB == 0)
+      for (int at = tid * 16; at < V_STAGE; at += TILE_THREADS * 16)
+        *(u32x4*)(lds + V_AT + V_STAGE + at) = u32x4{};
+    Scores sc;
+    Probs pr;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) pr.p[u][qt] = bf16x8{};
+    int keep = 0;   // of the step whose weights are at hand
+    tile_sync<0>();
+    // The others begin half a step later, with their share of V(0) and K(1).
+    if (!lead) {
+      load_k(s2, 1);
+      bring_v(s1, s2, 1);
+      tile_barrier();
     }
-    // Step j + 1, j + 2 and j + 3 become j + 2, j + 3 and j + 4.
+    // Steps j + 1, j + 2 and j + 3 become j + 2, j + 3 and j + 4.
     auto advance = [&](int j) {
       if ((j + 4) % 64 == 0 && j + 4 < n) fill_window(j + 4);
       s1 = s2;
@@ -1025,7 +1011,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     // A wave without a row only brings its share of the bytes in.
     int32_t head, token;
     if (!__builtin_amdgcn_ballot_w64(row_of(it, a, 32 * wave + lane % 32, head, token))) {
-      for (int j = 0; j < n; ++j) {
+      for (int j = -1; j < n; ++j) {
         tile_sync<2>();
         if (j + 1 < n) {
           const int stage = (j & 1) ^ (lead ? 0 : 1);
@@ -1040,7 +1026,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     }
     // Both sides run the same loop: matrix phase j, then a softmax phase, the leaders'
     // of the same step (loads of j + 2), the others' of the next one (loads of j + 3).
-    for (int j = 0; j < n; ++j) {
+    for (int j = -1; j < n; ++j) {
       const int even = j & 1;
       matrix_phase<MB != 0>(lds, (even ^ 1) * K_STAGE, V_AT + even * V_STAGE, q, sc, pr, ts, f,
                             keep, s1.scales);
