@@ -381,7 +381,7 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
 //
 // What bounds it: board power, and the matrix phase.  4,680 queries of 40 heads over
 // 63,960 tokens take 4.43 ms (1.38 PFLOP/s; a large bf16 matrix product 1.6), the matrix
-// cores busy 63% of the cycles at 2.0 GHz.  Without exponentials it takes the same time,
+// cores busy 64% of the cycles at 2.0 GHz.  Without exponentials it takes the same time,
 // without the softmax's arithmetic 6% less, without loads and conversions 4% less, with
 // half the fp8 products 15% less.
 //
