@@ -4,7 +4,7 @@
 //
 // e4m3 * 2^e is exact in bf16: bytes become bf16 matrix operands by one conversion
 // (cvt_scalef32, the scale at no cost), and the only roundings are those of P to bf16
-// and of the output, besides fp32 sums (and the fp8 products of the tiles, below).
+// and of the output, besides fp32 sums.
 //
 // Work: an item is some query rows of one key head; its keys, units of 64 tokens, are
 // split over `splits` workgroups.  With splits > 1 partial results (fp32 O, reference
@@ -13,8 +13,6 @@
 // the keys' bytes bound the call and rows_kernel streams them, from there on the
 // products do and tile_kernel works 256 rows at a time.  12 heads over 32,768 tokens, 32,
 // 64, 100 and 200 queries: 27, 36, 48 and 60 us.
-#include <type_traits>
-
 #include "values.h"
 
 namespace lvsa {
@@ -107,6 +105,23 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1, float scale)
   const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false);
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// A lane's part of a query row: an element that is not finite makes it (one element of
+// it, which is enough) NaN, so that the row becomes NaN whatever signs its keys have.
+// Adding 2^7 to a half's magnitude carries into its sign bit from the exponent of
+// infinity on.
+__device__ __forceinline__ void spoil_if_not_finite(bf16x8 (&q)[4]) {
+  uint32_t over = 0u;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const u32x4 w = __builtin_bit_cast(u32x4, q[s]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) over |= (w[e] & 0x7FFF7FFFu) + 0x00800080u;
+  }
+  u32x4 w = __builtin_bit_cast(u32x4, q[0]);
+  w[0] |= over & 0x80008000u ? 0x7FC0u : 0u;
+  q[0] = __builtin_bit_cast(bf16x8, w);
 }
 
 // A value that the launch only reads, at an index that is the same in the whole wave:
@@ -367,23 +382,22 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
 // query blocks' key lists 128 keys (two units) a step, sharing every K and V byte
 // through LDS.
 //
-//   S^T = K Q^T     fp8 MFMA 16x16x128, K as its e4m3 bytes with the block's scale as
-//                   the instruction's, Q as the sum of two e4m3 numbers (q_split)
+//   S^T = K Q^T     bf16 MFMA 16x16x32, K as bytes in LDS, converted in registers
 //   O^T += V^T P^T  bf16 MFMA 16x16x32, V converted to bf16 on its way into LDS
 //
-// Two fp8 MFMAs of 128 elements take the matrix core as long as four bf16 ones of
-// 32 (4.0 and 2.1 PFLOP/s under load), but K's bytes are half the LDS reads and need no
-// conversion.  The instruction adds its 128 products less exactly than fp32: 1.3e-5 of
-// the result on N(0, 1) data, 2^-13 of sum |q k| at worst (measured), far below P's
-// rounding.  V is converted once a workgroup, 32 elements a thread and step.  P needs
-// its eight bits: e4m3 pairs as for Q would cost two VALU operations an element more
-// than they save.
+// Scores take bf16 products and fp32 sums, as the other form's do.  The fp8 matrix
+// instructions would take K's bytes as they are (Q as the sum of two e4m3 numbers), but
+// add 128 products with an error of up to 2^-13 of sum |q k|: where one channel of q
+// and k is 32 (128) and the others N(0, 1), the result was off by 1.4e-2 (0.15) of its
+// norm, and is by 2.2e-3 now, as without such a channel (2 heads, 128 queries, 4,096
+// tokens).  They were 10% faster (40 heads of 4,680 queries over 63,960 tokens 4.33 and
+// 4.79 ms, one frame of 12 heads over the 121-frame mask 210 and 231 us).  V is converted
+// once a workgroup, 32 elements a thread and step; K by every wave, 128 conversions of
+// two elements: once a workgroup, through LDS, took 3% longer (twice K's LDS reads, and
+// registers that the compiler spilled).
 //
 // What bounds it: board power, and the matrix phase.  4,680 queries of 40 heads over
-// 63,960 tokens take 4.43 ms (1.38 PFLOP/s; a large bf16 matrix product 1.6), the matrix
-// cores busy 64% of the cycles at 2.0 GHz.  Without exponentials it takes the same time,
-// without the softmax's arithmetic 6% less, without loads and conversions 4% less, with
-// half the fp8 products 15% less.
+// 63,960 tokens take 4.79 ms (1.28 PFLOP/s; a large bf16 matrix product 1.6).
 //
 // Schedule: waves w and w + 4 share a SIMD and run half a step apart, one in its
 // matrix phase while the other is in its softmax phase; a barrier ends each half
@@ -457,6 +471,11 @@ __device__ __forceinline__ u32x4 rsrc_of(const void* p, uint32_t bytes) {
                (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
 
+// The scale of exponent byte `at` of a step's.
+__device__ __forceinline__ float scale_of(int32_t scales, int at) {
+  return __uint_as_float((((uint32_t)scales >> (8 * at)) & 0xFFu) << 23);
+}
+
 // The lane's index, made anew where a rare branch needs it: what is derived from it
 // there is not kept in registers through the loop.
 __device__ __forceinline__ int fresh_lane() {
@@ -485,61 +504,16 @@ __device__ __forceinline__ Step pick(bool first, const Step& a, const Step& b) {
   return s;
 }
 
-// Q of a wave: two 16-row tiles, each the sum of two e4m3 operands.  With 2^a the least
-// power of two that keeps the row within 448 * 2^a: hi = e4m3(q / 2^a), low =
-// e4m3(16 (q / 2^a - hi)).  A bf16 number has 8 significant bits, hi takes its first
-// 4 and low the rest exactly, down to 2^-14 of the row's largest; below, hi + low is
-// within 2^-22 of the largest.
-struct QSplit {
-  i32x8 hi[2], low[2];
-  int32_t scale[2];   // exponent bytes: byte 0 of hi, byte 1 of low
+// Q of a wave: two 16-row tiles, elements in the order of K's fragments.
+struct QTiles {
+  bf16x8 f[2][4];
 };
-
-template <int QT>
-__device__ __forceinline__ void q_split(QSplit& q, const __bf16* row, bool ok) {
-  float x[4][8];
-  float most = 0.f;
-  bool bad = false;
-#pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    if (ok) {
-      load8(row + (s / 2) * 64 + (s % 2) * 8, x[s]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      bad |= !(fabsf(x[s][e]) < __builtin_inff());
-      most = fmaxf(most, fabsf(x[s][e]));
-    }
-  }
-  most = row_max(most < __builtin_inff() ? most : 0.f);
-  const int a = scale_exponent(most);
-  const float inv = pow2(-a);
-#pragma unroll
-  for (int s = 0; s < 4; ++s)
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      float y[4], h[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float z = __builtin_amdgcn_fmed3f(x[s][4 * w + e] * inv, -448.f, 448.f);
-        y[e] = bad ? __builtin_nanf("") : z;   // a row that is not finite becomes NaN
-      }
-      const uint32_t hi = to_e4m3(y[0], y[1], y[2], y[3]);
-      from_e4m3(hi, h);
-      q.hi[QT][2 * s + w] = (int)hi;
-      q.low[QT][2 * s + w] = (int)to_e4m3(16.f * (y[0] - h[0]), 16.f * (y[1] - h[1]),
-                                          16.f * (y[2] - h[2]), 16.f * (y[3] - h[3]));
-    }
-  q.scale[QT] = (a + 127) | (a - 4 + 127) << 8;
-}
 
 struct TileState {
   f32x4 o[8][2];   // O^T [d tile][query tile]
-  f32x4 l[2];      // row sums, the same in every register (an accumulator each: a row that
-                   // is NaN would spoil the other tile's row of the same lane)
+  f32x4 l[2];      // row sums, in register 0 (the others add the same products, but are not
+                   // rescaled; an accumulator each: a row that is NaN would spoil the other
+                   // tile's row of the same lane)
   float m[2];      // references (log2)
   int flags;       // READY: every row has a finite m; WIDE: a step was redone
 };
@@ -557,18 +531,6 @@ __device__ __forceinline__ i32x8 k_frag(const char* k, uint32_t at, int kt) {
   const i32x4 a = *(const i32x4*)(k + at + kt * 1024);
   const i32x4 b = *(const i32x4*)(k + at + kt * 1024 + SLAB);
   return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-}
-template <int KT>
-__device__ __forceinline__ void score_tile(Scores& sc, const i32x8& f, const QSplit& q,
-                                           int k_scale) {
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int qt = t ^ (KT & 1);
-    f32x4 c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-        f, q.hi[qt], f32x4{}, 0, 0, KT / 4, k_scale, 0, q.scale[qt]);
-    sc.s[KT][qt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-        f, q.low[qt], c, 0, 0, KT / 4, k_scale, 1, q.scale[qt]);
-  }
 }
 // Scores of keys that do not exist or that the wave's query block does not keep: -inf.
 __device__ __forceinline__ void mask_scores(Scores& sc, const Step& st) {
@@ -683,13 +645,13 @@ __device__ __forceinline__ void weigh(const Scores& sc, TileState& st, Probs& pr
 // branch around the products made the compiler spill; its weights are zeros and the
 // workgroup's other waves take the time anyway.)
 template <bool MASKED>
-__device__ __forceinline__ void matrix_phase(const char* lds, int k_at, int v_at, const QSplit& q,
+__device__ __forceinline__ void matrix_phase(const char* lds, int k_at, int v_at, const QTiles& q,
                                              Scores& sc, const Probs& pr, TileState& st,
-                                             uint32_t f, int keep, int k_scale) {
-  // Fragments read ahead, 6, 8, 10, 12 and 14.  4,680 queries of 40 heads over 63,960
-  // tokens: 4.61, 4.46, 4.49, 4.42 and 4.47 ms; one frame of 12 heads over the 121-frame
-  // mask: 220, 217, 211, 213 and 213 us, with 64-token blocks 209, 206, 215, 213 and 213.
-  constexpr int AHEAD = 12;
+                                             uint32_t f, int keep, int k_scales) {
+  // Fragments read ahead, 8, 10 and 12.  4,680 queries of 40 heads over 63,960 tokens:
+  // 4.94, 4.83 and 4.80 ms; one frame of 12 heads over the 121-frame mask: 231, 237 and
+  // 236 us, with 64-token blocks 231, 238 and 233.
+  constexpr int AHEAD = MASKED ? 8 : 12;
   const char* const k = lds + k_at;
   uint32_t from[2];   // the slabs of V's units
 #pragma unroll
@@ -732,20 +694,31 @@ __device__ __forceinline__ void matrix_phase(const char* lds, int k_at, int v_at
                                                                st.o[dt][qt], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
-  auto score = [&](auto kt) {
-    constexpr int KT = decltype(kt)::value;
-    if constexpr (KT + 2 < 8) kf[KT + 2] = k_frag(k, f, KT + 2);
-    score_tile<KT>(sc, kf[KT], q, k_scale);
-    __builtin_amdgcn_sched_barrier(0);
+  // Scores, a K fragment's conversion ahead of its two MFMAs: two of its four conversions
+  // behind each MFMA of the fragment before, in its shadow.
+  // Scores, in such chains too: 16 keys' fragments are converted among the MFMAs of the
+  // 16 before, one behind every other.
+  const float scale[2] = {scale_of(k_scales, 0), scale_of(k_scales, 1)};
+  auto convert = [&](int kt, int c) {
+    return to_bf16(kf[kt][2 * c], kf[kt][2 * c + 1], scale[kt / 4]);
   };
-  score(std::integral_constant<int, 0>{});
-  score(std::integral_constant<int, 1>{});
-  score(std::integral_constant<int, 2>{});
-  score(std::integral_constant<int, 3>{});
-  score(std::integral_constant<int, 4>{});
-  score(std::integral_constant<int, 5>{});
-  score(std::integral_constant<int, 6>{});
-  score(std::integral_constant<int, 7>{});
+  bf16x8 fk[2][4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) fk[0][c] = convert(0, c);
+#pragma unroll
+  for (int kt = 0; kt < 8; ++kt) {
+    if (kt + 2 < 8) kf[kt + 2] = k_frag(k, f, kt + 2);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = t ? 3 - i : i, qt = t ^ (kt & 1);
+        sc.s[kt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            fk[kt % 2][c], q.f[qt][c], i ? sc.s[kt][qt] : f32x4{}, 0, 0, 0);
+        if (i % 2 && kt < 7) fk[(kt + 1) % 2][2 * t + i / 2] = convert(kt + 1, 2 * t + i / 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  }
 }
 
 // The union of the CSR rows block0 .. block0 + count - 1 (at most four) as words in
@@ -889,14 +862,17 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
   };
 
   // The wave's rows.
-  QSplit q;
+  QTiles q;
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
     int32_t head, token;
     const bool ok = row_of(it, a, 32 * wave + 16 * qt + i, head, token);
     const __bf16* row =
         (const __bf16*)a.q + (int64_t)head * a.q_sh + (int64_t)token * a.q_st + 16 * g;
-    if (qt == 0) q_split<0>(q, row, ok); else q_split<1>(q, row, ok);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      q.f[qt][s] = ok ? *(const bf16x8*)(row + (s / 2) * 64 + (s % 2) * 8) : bf16x8{};
+    spoil_if_not_finite(q.f[qt]);
   }
   TileState ts;
 #pragma unroll
@@ -947,8 +923,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
     auto store_v = [&](const Step& st, u32x4 (&w)[2], int stage) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float scale =
-            __uint_as_float((((uint32_t)st.scales >> (16 + 8 * u)) & 0xFFu) << 23);
+        const float scale = scale_of(st.scales, 2 + u);
         if (st.left[u] < UNIT) {   // bytes of tokens that are not held: zeros
           const int from = 4 * (fresh_lane() % 4);
 #pragma unroll
