@@ -104,14 +104,14 @@ __global__ __launch_bounds__(4 * B) void write_kernel(WriteArgs a, RopeArgs r) {
   const bool stays = token0 < min(a.start, m.n_tokens) || end < min(token0 + B, m.n_tokens);
 
   float lo[2][8], hi[2][8];
-  f32x2 cs[2][8];
+  Turns turns[2];
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     const int32_t token = token0 + p * ROWS + row;
     const int32_t i = min(max(token - a.start, 0), a.n - 1);
     load8(src + i * st + 8 * c, lo[p]);
     load8(src + i * st + 64 + 8 * c, hi[p]);
-    if (turn) load_turns(r, token, c, cs[p]);
+    if (turn) load_turns(r, token, c, turns[p]);
   }
   u32x2 old[2][2];
   float old_scale = 0.f;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(4 * B) void write_kernel(WriteArgs a, RopeArgs r) {
   for (int p = 0; p < 2; ++p) {
     const int32_t token = token0 + p * ROWS + row;
     const bool fresh = token >= a.start && token < end;
-    if (turn) rotate16<double>(lo[p], hi[p], cs[p], r.halves, 1.f);
+    if (turn) rotate16<double>(lo[p], hi[p], turns[p], r.halves, 1.f);
     if (stays) {
       const bool held = token < m.n_tokens;
 #pragma unroll

@@ -29,8 +29,8 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeTensors t, RopeArgs r
   const int64_t i = id / 8;
   const int c = (int)(id % 8);
   if (i >= t.n) return;
-  f32x2 cs[8];
-  load_turns(r, t.start + (int32_t)i, c, cs);
+  Turns turns;
+  load_turns(r, t.start + (int32_t)i, c, turns);
   const int h0 = blockIdx.y * t.per, h1 = min(h0 + t.per, t.heads);
   for (int h = h0; h < h1; ++h) {
     const T* x = (const T*)t.x + h * t.x_sh + i * t.x_st + 8 * c;
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeTensors t, RopeArgs r
     float lo[8], hi[8];
     load8(x, lo);
     load8(x + 64, hi);
-    rotate16<float>(lo, hi, cs, r.halves, t.sign);
+    rotate16<float>(lo, hi, turns, r.halves, t.sign);
     store8(y, lo);
     store8(y + 64, hi);
   }

@@ -65,26 +65,37 @@ __device__ __forceinline__ TokenTurn token_turn(const RopeArgs& r, int32_t token
   k.x = r.at_col + x * (r.p012 - r.p01) - r.p01;
   return k;
 }
-// (cos, sin) of pair j.
+// Whether pair j of the token turns.
+__device__ __forceinline__ bool pair_turns(const RopeArgs& r, const TokenTurn& k, int j) {
+  return k.turns && j < r.p012;
+}
+// (cos, sin) of a pair j that turns.
 __device__ __forceinline__ f32x2 turn_of(const RopeArgs& r, const TokenTurn& k, int j) {
-  if (!k.turns || j >= r.p012) return f32x2{1.f, 0.f};
   const int32_t e = j + (j < r.p0 ? k.t : j < r.p01 ? k.y : k.x);
   return *(const f32x2*)(r.table + 2 * (int64_t)e);
 }
 
 // A row is worked by eight threads: thread c holds elements 8c .. 8c+7 (lo) and
 // 64+8c .. 64+8c+7 (hi), which is whole pairs in either layout.  The (cos, sin) of
-// its eight pairs, and the rotation by them.
-__device__ __forceinline__ void load_turns(const RopeArgs& r, int32_t token, int c,
-                                           f32x2 (&cs)[8]) {
+// its eight pairs, and which of them turn: the others keep their values as they are (times
+// (1, 0) an infinity would make its partner NaN).
+struct Turns {
+  f32x2 cs[8];
+  bool on[8];
+};
+__device__ __forceinline__ void load_turns(const RopeArgs& r, int32_t token, int c, Turns& turns) {
   const TokenTurn k = token_turn(r, token);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    cs[i] = turn_of(r, k, r.halves ? 8 * c + i : i < 4 ? 4 * c + i : 32 + 4 * c + i - 4);
+  for (int i = 0; i < 8; ++i) {
+    const int j = r.halves ? 8 * c + i : i < 4 ? 4 * c + i : 32 + 4 * c + i - 4;
+    turns.on[i] = pair_turns(r, k, j);
+    turns.cs[i] = turns.on[i] ? turn_of(r, k, j) : f32x2{1.f, 0.f};
+  }
 }
 // F: the type of the arithmetic (float or double).  sign -1: the opposite angles.
 template <typename F>
-__device__ __forceinline__ void turn_pair(float& a, float& b, f32x2 cs, float sign) {
+__device__ __forceinline__ void turn_pair(float& a, float& b, f32x2 cs, bool on, float sign) {
+  if (!on) return;
   const F x = a, y = b, c = cs[0], s = sign * cs[1];
   if constexpr (sizeof(F) == 8) {
     a = (float)(x * c - y * s);
@@ -95,16 +106,16 @@ __device__ __forceinline__ void turn_pair(float& a, float& b, f32x2 cs, float si
   }
 }
 template <typename F>
-__device__ __forceinline__ void rotate16(float (&lo)[8], float (&hi)[8], const f32x2 (&cs)[8],
+__device__ __forceinline__ void rotate16(float (&lo)[8], float (&hi)[8], const Turns& t,
                                          bool halves, float sign) {
   if (halves) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn_pair<F>(lo[i], hi[i], cs[i], sign);
+    for (int i = 0; i < 8; ++i) turn_pair<F>(lo[i], hi[i], t.cs[i], t.on[i], sign);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      turn_pair<F>(lo[2 * i], lo[2 * i + 1], cs[i], sign);
-      turn_pair<F>(hi[2 * i], hi[2 * i + 1], cs[4 + i], sign);
+      turn_pair<F>(lo[2 * i], lo[2 * i + 1], t.cs[i], t.on[i], sign);
+      turn_pair<F>(hi[2 * i], hi[2 * i + 1], t.cs[4 + i], t.on[4 + i], sign);
     }
   }
 }
