@@ -396,7 +396,8 @@ lvsa_status lvsa_kv_write(lvsa_kv_cache* cache, const lvsa_tensor* k,
 /* Reads tokens start .. start + n - 1 (n = k->n_tokens, start + n <=
  * cache->n_tokens) of keys and values back into k and v, [cache->heads, n, 128]
  * of `dtype`; bf16 and fp32 hold every value exactly, fp16 rounds to nearest.
- * Either of k, v may be NULL.  Errors as for lvsa_kv_write. */
+ * Either of k, v may be NULL; they must not overlap, and rows of one that share
+ * elements are refused.  Errors as for lvsa_kv_write. */
 lvsa_status lvsa_kv_read(const lvsa_kv_cache* cache, int32_t start,
                          lvsa_tensor* k, lvsa_tensor* v, int32_t dtype,
                          void* stream);
@@ -476,7 +477,8 @@ lvsa_status lvsa_dense_attention(const lvsa_tensor* q, const lvsa_tensor* k,
 
 /* Rotates x [heads, n, 128] of `dtype`, whose token i is token start + i of the
  * sequence (start >= 0), into out of the same shape and type.  fp32 arithmetic,
- * one rounding.  out may be x itself (same strides), else must not overlap it.
+ * one rounding.  out may be x itself (same strides), else must not overlap it;
+ * rows of out that share elements are refused.
  * Errors: EINVAL (nulls, ranges, shapes), EUNSUPPORTED (layout, head_dim),
  * EDEVICE (launch). */
 lvsa_status lvsa_rope_forward(const lvsa_tensor* x, int32_t dtype, int32_t start,
@@ -506,7 +508,8 @@ lvsa_status lvsa_rope_backward(const lvsa_tensor* grad_out, int32_t dtype,
  * lvsa_attention_cache_workspace gives for the same arguments (0: may be NULL);
  * any content; written by the call, so calls that may overlap in time (two
  * streams, two graphs) need one each.
- * out must not overlap q or the cache.  The result is deterministic for given
+ * out must not overlap q or the cache, and rows of it that share elements are
+ * refused.  The result is deterministic for given
  * shapes, mask and device.  With more than 64 queries (times the query heads of a
  * key head), v of magnitudes below 2^-100 loses precision where a row's scores exceed
  * those of the keys taken first by more than 5 (natural logarithm).
