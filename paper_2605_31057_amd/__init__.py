@@ -480,6 +480,8 @@ def _rows(t, device):
     if t.get_device() != device:
         raise ValueError("expected a tensor on the current device")
     H, n, d = shape
+    if (H | n | d) >> 31:      # ctypes would cut them down without a word
+        raise LvsaError(EUNSUPPORTED, f"a tensor of shape {tuple(shape)}")
     if n <= 1:
         st = d
     return _byref(_Tensor(t.data_ptr(), H, n, d, sh if H > 1 else n * st, st))
@@ -521,7 +523,7 @@ class Rope:
     def __init__(self, frames, height, width, pairs=(22, 21, 21), theta=10000.0,
                  layout=ROPE_PAIRS, table=None, device="cuda"):
         import torch
-        if not all(0 <= n < 2 ** 31 for n in (frames, height, width, *pairs)):
+        if not all(0 <= n < 2 ** 31 for n in (frames, height, width, layout, *pairs)):
             raise LvsaError(EINVAL, "Rope")
         self._c = _Rope(frames, height, width, (_i32 * 3)(*pairs), layout, None)
         n = _i64()
