@@ -455,7 +455,11 @@ class _Fast:
         # The current stream of a device, as an address.
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
-        self.forward, self.backward = L.lvsa_rope_forward, L.lvsa_rope_backward
+        self.turns = ((L.lvsa_rope_forward, "lvsa_rope_forward"),
+                      (L.lvsa_rope_backward, "lvsa_rope_backward"))
+        self.grad_enabled = torch.is_grad_enabled
+        self.written = torch.autograd.graph.increment_version
+        self.turn = _turn_function(torch)
         self.write, self.read = L.lvsa_kv_write, L.lvsa_kv_read
         self.attend = L.lvsa_attention_cache
         self.attend_workspace = L.lvsa_attention_cache_workspace
@@ -550,11 +554,43 @@ def _rope_ref(r, device):
     return r._ref
 
 
-def _rotate(call, name, x, r, start, out):
+def _turn_function(torch):
+    class Turn(torch.autograd.Function):
+        """``rope`` (back False) or ``rope_backward`` (True): each is the other's
+        gradient."""
+
+        @staticmethod
+        def forward(ctx, x, out, r, start, back):
+            ctx.turn = r, start, back
+            if out is not None:
+                ctx.mark_dirty(out)
+            return _launch_turn(x, r, start, out, back)
+
+        @staticmethod
+        def backward(ctx, grad):
+            r, start, back = ctx.turn
+            return _rotate(_readable(grad), r, start, None, not back), None, None, None, None
+
+    return Turn
+
+
+def _readable(grad):
+    """A gradient as autograd hands it on (expanded, say) with rows that the library
+    takes."""
+    sh, st, sd = grad.stride()
+    H, n, _ = grad.shape
+    if (sd == 1 and (n == 1 or (st > 0 and st % 8 == 0)) and (H == 1 or sh % 8 == 0)
+            and grad.data_ptr() % 16 == 0):
+        return grad
+    return grad.clone(memory_format=_FAST.torch.contiguous_format)
+
+
+def _launch_turn(x, r, start, out, back):
     f = _FAST
     dev = f.device()
     if out is None:
         out = f.empty_like(x)
+    call, name = f.turns[back]
     status = call(_rows(x, dev), _type_code(x, out), _place(start), _rope_ref(r, dev),
                   _rows(out, dev), f.stream(dev))
     if status:
@@ -562,20 +598,33 @@ def _rotate(call, name, x, r, start, out):
     return out
 
 
+def _rotate(x, r, start, out, back):
+    f = _fast()
+    if (x.requires_grad or (out is not None and out.requires_grad)) and f.grad_enabled():
+        return f.turn.apply(x, out, r, start, back)
+    if out is None:
+        return _launch_turn(x, r, start, out, back)
+    _launch_turn(x, r, start, out, back)
+    f.written(out)       # a graph that has saved it notices
+    return out
+
+
 def rope(x, r, start=0, out=None, stream=None):
     """x [heads, n, 128] (bfloat16, float16, float32), token i of which is token
-    start + i of the grid, rotated by ``r`` (lvsa_rope_forward); out may be x."""
+    start + i of the grid, rotated by ``r`` (lvsa_rope_forward); out may be x.
+    Differentiable in x (the table is data)."""
     if stream is not None:
         return _with_stream(rope, stream, x, r, start, out)
-    return _rotate(_fast().forward, "lvsa_rope_forward", x, r, start, out)
+    return _rotate(x, r, start, out, False)
 
 
 def rope_backward(grad, r, start=0, out=None, stream=None):
     """Gradient of ``rope``: of its input, from that of its output
-    (lvsa_rope_backward); out may be grad."""
+    (lvsa_rope_backward); out may be grad.  What autograd calls, for programs that
+    have no graph."""
     if stream is not None:
         return _with_stream(rope_backward, stream, grad, r, start, out)
-    return _rotate(_fast().backward, "lvsa_rope_backward", grad, r, start, out)
+    return _rotate(grad, r, start, out, True)
 
 
 class KvCache:
@@ -638,7 +687,8 @@ def _cache_ref(c, device):
 def kv_write(cache, k, v, start=None, rope=None, stream=None):
     """Quantises k and v [heads, n, 128] (bfloat16, float16, float32) into tokens
     start, start + 1, .. of the cache (by default behind its last), the keys
-    rotated by ``rope`` on the way (lvsa_kv_write); returns the cache."""
+    rotated by ``rope`` on the way (lvsa_kv_write); returns the cache.  It has no
+    gradient."""
     if stream is not None:
         return _with_stream(kv_write, stream, cache, k, v, start, rope)
     f = _fast()
@@ -680,7 +730,7 @@ def attention_cache(q, cache, mask=None, q_start=0, out=None, stream=None):
     """Attention of q [heads, n, 128] (bfloat16; heads a multiple of the cache's)
     over every held token, or over the blocks that ``mask`` (a BlockMask over the
     cache's tokens) keeps for queries q_start, q_start + 1, ..
-    (lvsa_attention_cache); returns out."""
+    (lvsa_attention_cache); returns out.  It has no gradient."""
     if stream is not None:
         return _with_stream(attention_cache, stream, q, cache, mask, q_start, out)
     f = _fast()
