@@ -502,7 +502,8 @@ lvsa_status lvsa_rope_backward(const lvsa_tensor* grad_out, int32_t dtype,
  * q_start + i of the sequence, 0 <= q_start, q_start + n <= n_tokens.  Without
  * a mask q_start is not used.  bf16 q and out; exact products of q and the held
  * keys, fp32 sums and softmax; probabilities in bf16.  A query with no key gets
- * zeros (an empty row, or an empty cache); keys and values that a query does not keep never reach it,
+ * zeros (an empty row, or an empty cache); one with a key and an element that is
+ * not finite gets NaN; keys and values that a query does not keep never reach it,
  * whatever they are.  The mask's rules are lvsa_block_mask's.
  * workspace: device memory, 16-byte aligned, of at least the bytes that
  * lvsa_attention_cache_workspace gives for the same arguments (0: may be NULL);

@@ -107,11 +107,11 @@ __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1, float scale)
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A lane's part of a query row: an element that is not finite makes it (one element of
-// it, which is enough) NaN, so that the row becomes NaN whatever signs its keys have.
-// Adding 2^7 to a half's magnitude carries into its sign bit from the exponent of
-// infinity on.
-__device__ __forceinline__ void spoil_if_not_finite(bf16x8 (&q)[4]) {
+// Whether a lane's part of a query row holds an element that is not finite: adding 2^7
+// to a half's magnitude carries into its sign bit from the exponent of infinity on.
+// Such a row becomes NaN whatever signs its keys have (scores of -inf alone would look
+// like a row without keys).
+__device__ __forceinline__ bool not_finite(const bf16x8 (&q)[4]) {
   uint32_t over = 0u;
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
@@ -119,9 +119,7 @@ __device__ __forceinline__ void spoil_if_not_finite(bf16x8 (&q)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) over |= (w[e] & 0x7FFF7FFFu) + 0x00800080u;
   }
-  u32x4 w = __builtin_bit_cast(u32x4, q[0]);
-  w[0] |= over & 0x80008000u ? 0x7FC0u : 0u;
-  q[0] = __builtin_bit_cast(bf16x8, w);
+  return (over & 0x80008000u) != 0u;
 }
 
 // A value that the launch only reads, at an index that is the same in the whole wave:
@@ -245,6 +243,7 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
     k_scale = uniform_load(ks, key0 >> a.scale_shift);
     v_scale = uniform_load(vs, key0 >> a.scale_shift);
   }
+  const bool worked = key0 < a.n_tokens;
   while (key0 < a.n_tokens) {
     const int32_t key1 = next_unit();
     const int32_t scale1 = min(key1, a.n_tokens - 1) >> a.scale_shift;
@@ -331,7 +330,7 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
   // The waves' parts, combined in LDS in the waves' order.
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float sum = l[rt];
+    float sum = worked && not_finite(qf[rt]) ? __builtin_nanf("") : l[rt];
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (g == 0) {
@@ -872,7 +871,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tile_kernel(KernelArgs ka) {
 #pragma unroll
     for (int s = 0; s < 4; ++s)
       q.f[qt][s] = ok ? *(const bf16x8*)(row + (s / 2) * 64 + (s % 2) * 8) : bf16x8{};
-    spoil_if_not_finite(q.f[qt]);
+    if (not_finite(q.f[qt])) q.f[qt][0][0] = (__bf16)__builtin_nanf("");
   }
   TileState ts;
 #pragma unroll

@@ -106,3 +106,27 @@ def test_a_query_that_is_not_finite_over_keys_of_one_sign(n, bad):
     got = L.attention_cache(q, c)
     assert torch.isnan(got[0, 1]).all()
     assert torch.equal(got[0, 2:], want[0, 2:]) and torch.equal(got[0, 0], want[0, 0])
+
+
+@pytest.mark.parametrize("n", [1, 16, 17, 40, 64])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_the_same_with_few_rows(n, bad):
+    """An infinity times keys of one sign gives scores of -inf alone: NaN, not the zeros
+    of a query without keys, with and without a mask."""
+    N = 300
+    c = L.KvCache(1, N, 64)
+    g = torch.Generator().manual_seed(n)
+    k, v = (torch.randn(1, N, 128, generator=g) for _ in range(2))
+    k[..., 9] = -1.0
+    L.kv_write(c, k.to(BF).cuda(), v.to(BF).cuda())
+    q = torch.randn(1, n, 128, generator=g).to(BF).cuda()
+    for mask in (None, _full_mask(N, 64)):
+        want = L.attention_cache(q, c, mask=mask, q_start=0)
+        p = q.clone()
+        p[0, n // 2, 9] = bad
+        got = L.attention_cache(p, c, mask=mask, q_start=0)
+        assert torch.isnan(got[0, n // 2]).all()
+        others = [i for i in range(n) if i != n // 2]
+        assert torch.equal(got[0, others], want[0, others])
+    none = L.KvCache(1, 128)
+    assert (L.attention_cache(p, none) == 0).all()       # no key at all: still zeros
