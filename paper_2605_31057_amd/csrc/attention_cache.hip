@@ -9,10 +9,9 @@
 // Work: an item is some query rows of one key head; its keys, units of 64 tokens, are
 // split over `splits` workgroups.  With splits > 1 partial results (fp32 O, reference
 // m and row sum l) go to the workspace and combine_kernel adds them in the order of
-// the splits.  Two forms, by the rows that can share an item (plan_of): up to 64 rows
-// the keys' bytes bound the call and rows_kernel streams them, from there on the
-// products do and tile_kernel works 256 rows at a time.  12 heads over 32,768 tokens, 32,
-// 64, 100 and 200 queries: 27, 36, 48 and 60 us.
+// the splits.  Two forms (plan_of): up to 64 rows the keys' bytes bound the call and
+// rows_kernel streams them, from there on the products do and tile_kernel works 256 rows
+// at a time.
 #include "values.h"
 
 namespace lvsa {
@@ -389,14 +388,15 @@ __global__ __launch_bounds__(THREADS, RT <= 2 ? 2 : 1) void rows_kernel(KernelAr
 // add 128 products with an error of up to 2^-13 of sum |q k|: where one channel of q
 // and k is 32 (128) and the others N(0, 1), the result was off by 1.4e-2 (0.15) of its
 // norm, and is by 2.2e-3 now, as without such a channel (2 heads, 128 queries, 4,096
-// tokens).  They were 10% faster (40 heads of 4,680 queries over 63,960 tokens 4.33 and
-// 4.79 ms, one frame of 12 heads over the 121-frame mask 210 and 231 us).  V is converted
-// once a workgroup, 32 elements a thread and step; K by every wave, 128 conversions of
-// two elements: once a workgroup, through LDS, took 3% longer (twice K's LDS reads, and
-// registers that the compiler spilled).
+// tokens).  They were 8 to 11% faster (40 heads of 4,680 queries over 63,960 tokens 4.40
+// and 4.88 ms, one frame of 12 heads over the 121-frame mask 211 and 233 us).  V is
+// converted once a workgroup, 32 elements a thread and step; K by every wave, 128
+// conversions of two elements.  K converted once a workgroup, in place of its bytes in
+// LDS, takes twice the LDS reads and some spills: 4.90 ms, and 217 us with a mask.
 //
-// What bounds it: board power, and the matrix phase.  4,680 queries of 40 heads over
-// 63,960 tokens take 4.79 ms (1.28 PFLOP/s; a large bf16 matrix product 1.6).
+// What bounds it: the matrix phase, its issue slots shared with the other wave's softmax.
+// 4,680 queries of 40 heads over 63,960 tokens take 4.88 ms (1.26 PFLOP/s; a large bf16
+// matrix product 1.6), the matrix cores busy 55% of the cycles.
 //
 // Schedule: waves w and w + 4 share a SIMD and run half a step apart, one in its
 // matrix phase while the other is in its softmax phase; a barrier ends each half
@@ -1127,7 +1127,12 @@ __global__ __launch_bounds__(THREADS) void combine_kernel(KernelArgs ka) {
 int64_t items_of(const Plan& p) { return (int64_t)p.heads * p.blocks * p.tiles; }
 
 // Tiles from this many rows a key head (with a mask, which keeps a tile within one
-// query head, from this many queries) on.
+// query head, from this many queries) on.  Rows form and tiles, us, at 32, 64, 80, 128 and
+// 200 rows: 12 heads over 32,768 tokens 27/41, 36/43, 53/44, 53/47 and 91/61; 8 key
+// heads of 8 query heads 27/32 (64 rows), 37/33 (72) and 62/50 (256).  Under a mask of
+// 121 frames (18% of 188,760 tokens), at 32, 64, 65, 100 and 200 queries: 12 heads 25/40,
+// 31/42, 45/42, 73/51 and 75/58, with 64-token blocks 33/39, 44/41, 44/41, 59/49 and 75/56;
+// 8 key heads of 8 query heads 52/124, 86/128, 108/129, 276/160 and 278/176.
 constexpr int64_t TILE_FROM = 65;
 
 Plan plan_of(const CacheAttnArgs& a, int32_t cus) {
@@ -1151,8 +1156,11 @@ Plan plan_of(const CacheAttnArgs& a, int32_t cus) {
     } else {
       p.tiles = (int32_t)((rows + TILE_ROWS - 1) / TILE_ROWS);
     }
-    // One workgroup a compute unit: the number of splits that ends first, in steps
-    // (a round of the grid takes its splits' steps and about TILE_FIXED more).
+    // One workgroup a compute unit: the number of splits that ends first, in steps (a
+    // round of the grid takes its splits' steps and about TILE_FIXED more: 84 workgroups of
+    // 2, 4 and 8 steps take 19.4, 25.6 and 38 us, with a mask 4 and 8 steps 27.8 and 41 us,
+    // which is 3.1 to 3.4 us a step and 13 to 14 us; combining takes 8 to 9 us).  With a
+    // mask the steps are those of every block: what its rows keep is on the device.
     constexpr int64_t TILE_FIXED = 6;
     const int64_t steps = (units + 1) / 2, items = items_of(p);
     int64_t best = 0;

@@ -8,7 +8,7 @@
 // places is that of the accumulator registers that hold P).
 //
 // Bound: memory, sizeof(T) bytes read and one written an element: 40 heads of 32,760
-// tokens, keys rotated, 201 us (5.0 TB/s); 16 heads of 103,862 tokens back in bf16 233 us
+// tokens, keys rotated, 209 us (4.8 TB/s); 16 heads of 103,862 tokens back in bf16 233 us
 // (5.5 TB/s).  One workgroup a block, head and tensor (K or V): the block's values stay
 // in registers between the maximum and the rounding, so they are read once.
 #include "values.h"
@@ -80,8 +80,8 @@ __device__ __forceinline__ void rows_to_tiles(const uint8_t* rows, uint8_t* tile
 // Eight threads a row (values.h), two rows a thread.  Every load is issued before the
 // first value is used and none depends on a lane's token: rows of the source are
 // clamped to those that exist and chosen afterwards, so a block of a few new tokens
-// waits for memory once: 6.8 us for one token into a held block of 12 heads, 8.6 us for
-// 1,560 tokens (with a branch a row and four rows a thread 8.8 and 10.2 us).
+// waits for memory once: 7 us for one token into a held block of 12 heads, 8.8 us for
+// 1,560 tokens (a branch a row and four rows a thread took 2 us longer in both).
 template <typename T, int B>
 __global__ __launch_bounds__(4 * B) void write_kernel(WriteArgs a, RopeArgs r) {
   constexpr int THREADS = 4 * B, ROWS = B / 2;
