@@ -707,6 +707,7 @@ def kv_read(cache, start=0, n=None, dtype=None, out=None, stream=None):
         return _with_stream(kv_read, stream, cache, start, n, dtype, out)
     f = _fast()
     dev = f.device()
+    given = out is not None
     _place(start)
     if out is None:
         n = cache.n_tokens - start if n is None else n
@@ -723,6 +724,8 @@ def kv_read(cache, start=0, n=None, dtype=None, out=None, stream=None):
         raise ValueError("expected out tensors of the given type")
     _check(f.read(_cache_ref(cache, dev), start, _rows(k, dev), _rows(v, dev), _type_code(k, v),
                   f.stream(dev)), "lvsa_kv_read")
+    if given:
+        f.written([k, v])
     return out
 
 
@@ -735,6 +738,7 @@ def attention_cache(q, cache, mask=None, q_start=0, out=None, stream=None):
         return _with_stream(attention_cache, stream, q, cache, mask, q_start, out)
     f = _fast()
     dev = f.device()
+    given = out is not None
     if out is None:
         out = f.empty_like(q)
     if q.dtype != f.bf16 or out.dtype != f.bf16:
@@ -749,4 +753,6 @@ def attention_cache(q, cache, mask=None, q_start=0, out=None, stream=None):
         work = f.empty(size, dtype=f.torch.uint8, device=q.device)
     _check(f.attend(tq, q_start, c, m, to, work.data_ptr() if size else None, size,
                     f.stream(dev)), "lvsa_attention_cache")
+    if given:
+        f.written(out)
     return out

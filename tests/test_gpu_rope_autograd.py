@@ -152,3 +152,20 @@ def test_a_training_step():
     # sums of 50 products, a rounding of 2^-24 each, and those of the rotation
     size = torch.einsum("nk,ine,ne->ki", a.abs(), M.abs(), t.abs())
     assert ((W.grad.cpu() - want).abs() <= 60 * 2.0 ** -24 * size).all()
+
+
+def test_reads_and_attention_into_a_saved_tensor_are_noticed():
+    c = L.KvCache(2, 128)
+    k = torch.randn(2, 100, 128, device="cuda").bfloat16()
+    L.kv_write(c, k, k)
+    for write in (lambda t: L.attention_cache(k, c, out=t),
+                  lambda t: L.kv_read(c, out=(t, torch.empty_like(t))),
+                  lambda t: L.kv_read(c, out=(torch.empty_like(t), t))):
+        t = torch.ones_like(k)
+        w = torch.ones_like(k).requires_grad_()
+        y = (w * t).sum()
+        write(t)
+        with pytest.raises(RuntimeError):
+            y.backward()
+    with torch.inference_mode():
+        L.attention_cache(k, c, out=torch.empty_like(k))
