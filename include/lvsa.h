@@ -510,10 +510,11 @@ lvsa_status lvsa_rope_backward(const lvsa_tensor* grad_out, int32_t dtype,
  * any content; written by the call, so calls that may overlap in time (two
  * streams, two graphs) need one each.
  * out must not overlap q or the cache, and rows of it that share elements are
- * refused.  The result is deterministic for given
- * shapes, mask and device.  With more than 64 queries (times the query heads of a
- * key head), v of magnitudes below 2^-100 loses precision where a row's scores exceed
- * those of the keys taken first by more than 5 (natural logarithm).
+ * refused.  The result is deterministic for given shapes, mask and device.  Scores
+ * and sums of weights (up to 2 each) times v past fp32's range become infinite or
+ * NaN.  With more than 64 queries (times the query heads of a key head), v of
+ * magnitudes below 2^-100 loses precision where a row's scores exceed those of the
+ * keys taken first by more than 5 (natural logarithm).
  * Errors: EINVAL (nulls, ranges, shape mismatch, workspace too small),
  * EUNSUPPORTED (head_dim, block, alignment, strides, sizes), EDEVICE (launch). */
 lvsa_status lvsa_attention_cache(const lvsa_tensor* q, int32_t q_start,

@@ -693,8 +693,6 @@ __device__ __forceinline__ void matrix_phase(const char* lds, int k_at, int v_at
                                                                st.o[dt][qt], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
-  // Scores, a K fragment's conversion ahead of its two MFMAs: two of its four conversions
-  // behind each MFMA of the fragment before, in its shadow.
   // Scores, in such chains too: 16 keys' fragments are converted among the MFMAs of the
   // 16 before, one behind every other.
   const float scale[2] = {scale_of(k_scales, 0), scale_of(k_scales, 1)};
