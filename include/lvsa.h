@@ -500,11 +500,13 @@ lvsa_status lvsa_rope_backward(const lvsa_tensor* grad_out, int32_t dtype,
  * cache's block, at most 8000 blocks), over the held tokens of the key blocks
  * kept for the query block (q_start + i) / mask->block: query i is then token
  * q_start + i of the sequence, 0 <= q_start, q_start + n <= n_tokens.  Without
- * a mask q_start is not used.  bf16 q and out; exact products of q and the held
- * keys, fp32 sums and softmax; probabilities in bf16.  A query with no key gets
- * zeros (an empty row, or an empty cache); one with a key and an element that is
- * not finite gets NaN; keys and values that a query does not keep never reach it,
- * whatever they are.  The mask's rules are lvsa_block_mask's.
+ * a mask q_start is not used.  The tokens are those held at the call (a call that
+ * is captured into a graph attends to as many when it is replayed).  bf16 q and
+ * out; exact products of q and the held keys, fp32 sums and softmax; probabilities
+ * in bf16.  A query with no key gets zeros (an empty row, or an empty cache); one
+ * with a key and an element that is not finite gets NaN; keys and values that a
+ * query does not keep never reach it, whatever they are.  The mask's rules are
+ * lvsa_block_mask's.
  * workspace: device memory, 16-byte aligned, of at least the bytes that
  * lvsa_attention_cache_workspace gives for the same arguments (0: may be NULL);
  * any content; written by the call, so calls that may overlap in time (two

@@ -169,3 +169,35 @@ def test_reads_and_attention_into_a_saved_tensor_are_noticed():
             y.backward()
     with torch.inference_mode():
         L.attention_cache(k, c, out=torch.empty_like(k))
+
+
+def test_a_captured_gradient():
+    """Forward and gradient captured into a graph, replayed with new inputs among eager
+    calls."""
+    r = _rope()
+    x, w = _x(1).requires_grad_(), _x(2)
+
+    def step():
+        y = L.rope(x, r, **R)
+        return y.detach(), torch.autograd.grad(y, x, w)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, g = step()
+    for s in range(4):
+        with torch.no_grad():
+            x.copy_(_x(10 + s))
+            w.copy_(_x(20 + s))
+            y.fill_(0.0)
+            g.fill_(0.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, L.rope(_x(10 + s), r, **R))
+        assert torch.equal(g, L.rope_backward(_x(20 + s), r, **R))
