@@ -284,7 +284,8 @@ def _run_own(s):
         return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
     if c["op"] == "norm":
         if not c["y"]:
-            return {"h": lvsa.residual_norm(s["plan"], s["x"], **s["params"])}
+            return {"h": lvsa.residual_norm(s["plan"], s["x"], dtype=TYPES[c["block"]],
+                                            **s["params"])}
         r, h = lvsa.residual_norm(s["plan"], s["x"], s["y"], **s["params"])
         return {"r": r, "h": h}
     return lvsa.residual_norm_backward(s["plan"], s["grad_h"], s["grad_r"], s["r"], s.get("y"),
