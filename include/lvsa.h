@@ -402,6 +402,73 @@ lvsa_status lvsa_kv_read(const lvsa_kv_cache* cache, int32_t start,
                          lvsa_tensor* k, lvsa_tensor* v, int32_t dtype,
                          void* stream);
 
+/* ------------------------------------- residual step between blocks ---- */
+
+/* Rows [n][dim] in device memory: row i begins at data + i*stride (elements).  data is
+ * 16-byte aligned and stride a multiple of 8. */
+typedef struct lvsa_rows {
+  void* data;
+  int32_t n;
+  int64_t stride;
+} lvsa_rows;
+
+/* The step from one block of a transformer layer to the next on its residual stream:
+ *   r = residual * x + gate * u,      u = P(y) * post_weight
+ *   h = (N(r) * weight + bias) * (1 + scale) + shift
+ * x the stream before, y the block's output, r the stream behind it, h the next block's
+ * input.  N and P are norms over a row's `dim` columns:
+ *   NONE    N: there is no h;  P: u = y
+ *   LAYER   (x - mean(x)) / sqrt(var(x) + eps), var the mean of squared deviations
+ *   RMS     x / sqrt(mean(x^2) + eps)
+ * gate, scale and shift have a row for every `frame_tokens` rows of x, in order: row f
+ * is for rows f*frame_tokens .. (f+1)*frame_tokens - 1, ceil(n / frame_tokens) rows in
+ * all, at gate + f*gate_stride (frame_tokens 0: one row for all).  weight, bias and
+ * post_weight are one row [dim].  Each may be NULL: gate, weight and post_weight are
+ * then 1, bias 0, scale and shift 0 (scale and shift come together).
+ * x and r are of stream_type, y and h of block_type, gate .. post_weight of param_type
+ * (LVSA_BF16, LVSA_F16, LVSA_F32); stream_type is block_type or LVSA_F32.  Arithmetic
+ * and sums in fp32, one rounding of r and of h (h is taken from r before its rounding).
+ * dim is a multiple of 8, at most LVSA_MAX_NORM_DIM; strides are multiples of 8 and
+ * everything is 16-byte aligned. */
+#define LVSA_NORM_NONE 0
+#define LVSA_NORM_LAYER 1
+#define LVSA_NORM_RMS 2
+#define LVSA_MAX_NORM_DIM 32768
+typedef struct lvsa_residual_norm {
+  int32_t dim;
+  int32_t frame_tokens;
+  int32_t norm;            /* N */
+  int32_t post;            /* P */
+  float eps;
+  float residual;
+  int32_t stream_type;
+  int32_t block_type;
+  int32_t param_type;
+  const void* gate;
+  const void* scale;
+  const void* shift;
+  int64_t gate_stride;
+  int64_t scale_stride;
+  int64_t shift_stride;
+  const void* weight;
+  const void* bias;
+  const void* post_weight;
+} lvsa_residual_norm;
+
+/* Gradients that lvsa_residual_norm_backward writes; data or pointers NULL: not wanted.
+ * x is of stream_type, y of block_type, the others of param_type and contiguous: gate,
+ * scale, shift [ceil(n / frame_tokens)][dim], weight, bias, post_weight [dim]. */
+typedef struct lvsa_residual_norm_grads {
+  lvsa_rows x;
+  lvsa_rows y;
+  void* gate;
+  void* scale;
+  void* shift;
+  void* weight;
+  void* bias;
+  void* post_weight;
+} lvsa_residual_norm_grads;
+
 /* Tile counters.  The attention kernels run one persistent workgroup per
  * compute unit; workgroups take tiles (256 query rows of a head, or parts of
  * that) through atomic counters, eight per launch (one per XCD), so XCDs that
@@ -528,6 +595,74 @@ lvsa_status lvsa_attention_cache_workspace(const lvsa_tensor* q, int32_t q_start
                                            const lvsa_kv_cache* cache,
                                            const lvsa_block_mask* mask,
                                            int64_t* bytes);
+
+/* lvsa_attention, or lvsa_dense_attention of the mask's block for a mask without rows
+ * (row_ptr and col_idx NULL: every block) and of block 128 for mask NULL, that also gives
+ * what the gradients need: lse [heads][n_tokens] in fp32, contiguous,
+ *   lse[h, i] = log sum_j exp(q[h,i] . k[h,j] / sqrt(d))
+ * over the keys that query i attends (-inf without any), its sums in fp32.  out is bit
+ * for bit that of the call without lse.
+ * Errors as for lvsa_attention, and EUNSUPPORTED for lse not 4-byte aligned. */
+lvsa_status lvsa_attention_lse(const lvsa_tensor* q, const lvsa_tensor* k,
+                               const lvsa_tensor* v, const lvsa_block_mask* mask,
+                               lvsa_tensor* out, float* lse, void* stream);
+
+/* Gradients of lvsa_attention_lse's out: from grad_out those of q, k and v,
+ *   p = exp(s - lse), s = q k' / sqrt(d),    grad_v = p' grad_out,
+ *   e = p (grad_out v' - rowsum(grad_out out)),
+ *   grad_q = e k / sqrt(d),   grad_k = e' q / sqrt(d)
+ * over the pairs that the mask keeps (NULL: all), with q, k, v, out, lse and mask as they
+ * were for that call.  fp32 products and sums; p and e are rounded to bf16 where they
+ * enter products, the gradients once at the end.  A query without keys gets a zero
+ * gradient, and so does a key that no query keeps; blocks that the mask does not keep
+ * together never reach each other's gradients, whatever they hold.
+ * grad_q, grad_k and grad_v are [heads, n_tokens, 128] in bf16; they must not overlap
+ * each other or an input, and rows of one that share elements are refused.
+ * workspace: device memory, 16-byte aligned, of at least the bytes that
+ * lvsa_attention_backward_workspace gives for the same q and mask; any content; written
+ * by the call, so calls that may overlap in time need one each.
+ * No atomics on floats: the result is the same every time for given shapes, mask and
+ * device.  Shape limits are lvsa_attention's.
+ * Errors: EINVAL (nulls, shape mismatch, overlapping, workspace too small), EUNSUPPORTED
+ * (head_dim, block, alignment, strides, sizes), EDEVICE (launch). */
+lvsa_status lvsa_attention_backward(const lvsa_tensor* grad_out, const lvsa_tensor* q,
+                                    const lvsa_tensor* k, const lvsa_tensor* v,
+                                    const lvsa_tensor* out, const float* lse,
+                                    const lvsa_block_mask* mask, lvsa_tensor* grad_q,
+                                    lvsa_tensor* grad_k, lvsa_tensor* grad_v,
+                                    void* workspace, int64_t workspace_bytes, void* stream);
+lvsa_status lvsa_attention_backward_workspace(const lvsa_tensor* q,
+                                              const lvsa_block_mask* mask, int64_t* bytes);
+
+/* The residual step (lvsa_residual_norm): r and h from x and y.  Without a block's output
+ * (y NULL) r is x itself, residual has to be 1, gate, post and post_weight absent, and r
+ * NULL; h is NULL for norm NONE.  r may be x itself and h y itself (same type and
+ * strides), else they overlap neither each other nor an input.
+ * Errors: EINVAL (nulls, ranges, shapes, rows of r or h that share elements),
+ * EUNSUPPORTED (dim, types, alignment, strides), EDEVICE (launch). */
+lvsa_status lvsa_residual_norm_forward(const lvsa_residual_norm* p, const lvsa_rows* x,
+                                       const lvsa_rows* y, lvsa_rows* r, lvsa_rows* h,
+                                       void* stream);
+
+/* Its gradients, from those of h (grad_h, of block_type; NULL for norm NONE) and of r
+ * (grad_r, of stream_type; NULL: zero), at r and y as they were: what r holds is taken
+ * for the stream behind the block (without y: for x).  A gradient of y, gate or
+ * post_weight takes y; one of a parameter that the step does not have is refused.
+ * grads->x may be grad_r itself and grads->y grad_h itself (same type and strides), else
+ * the gradients overlap neither each other nor an input.  Sums over rows are in fp32 and
+ * in a fixed order.
+ * workspace: as for lvsa_attention_backward, by lvsa_residual_norm_workspace for the same
+ * p, n rows and grads (0 bytes: may be NULL).
+ * Errors as for lvsa_residual_norm_forward, and EINVAL for a workspace too small. */
+lvsa_status lvsa_residual_norm_backward(const lvsa_residual_norm* p, const lvsa_rows* grad_h,
+                                        const lvsa_rows* grad_r, const lvsa_rows* r,
+                                        const lvsa_rows* y,
+                                        const lvsa_residual_norm_grads* grads,
+                                        void* workspace, int64_t workspace_bytes,
+                                        void* stream);
+lvsa_status lvsa_residual_norm_workspace(const lvsa_residual_norm* p, int32_t n,
+                                         const lvsa_residual_norm_grads* grads,
+                                         int64_t* bytes);
 
 #ifdef __cplusplus
 }

@@ -21,6 +21,9 @@ fallback.
     q = lvsa.rope(q, r, start=n0)                         # new tokens n0, n0 + 1, ..
     lvsa.kv_write(cache, k, v, start=n0, rope=r)          # keys rotated on the way
     lvsa.attention_cache(q, cache)                        # over every token so far
+    step = lvsa.ResidualNorm(1536, frame_tokens=1560)     # gate and norm between two blocks
+    x, h = lvsa.residual_norm(step, x, y, gate=g, scale=s, shift=t)   # x + g y; its norm * (1 + s) + t
+    lvsa.attention(q, k, v, m).backward(grad)             # attention, rope, residual_norm have gradients
 """
 import ctypes
 import os
@@ -32,7 +35,9 @@ __all__ = [
     "attention_exact",
     "dense_attention", "WINDOW_BASIC", "WINDOW_ADAPTIVE", "WINDOW_EXPANDED",
     "MAX_FRAMES", "Rope", "rope", "rope_backward", "KvCache", "kv_write", "kv_read",
-    "attention_cache", "ROPE_PAIRS", "ROPE_HALVES",
+    "attention_cache", "ROPE_PAIRS", "ROPE_HALVES", "attention_lse", "attention_backward",
+    "ResidualNorm", "residual_norm", "residual_norm_backward", "NORM_NONE", "NORM_LAYER",
+    "NORM_RMS",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -41,6 +46,7 @@ LIB_PATH = os.path.join(_HERE, "liblvsa.so")
 WINDOW_BASIC, WINDOW_ADAPTIVE, WINDOW_EXPANDED = 0, 1, 2
 MAX_FRAMES = 4096
 ROPE_PAIRS, ROPE_HALVES = 0, 1
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
 OK, EINVAL, ENOMEM, EDEVICE, EUNSUPPORTED = 0, -1, -2, -3, -4
 
 _i32 = ctypes.c_int32
@@ -99,6 +105,23 @@ class _Rope(ctypes.Structure):
 class _KvCache(ctypes.Structure):
     _fields_ = [("heads", _i32), ("capacity", _i32), ("block", _i32), ("n_tokens", _i32),
                 ("k", _p), ("v", _p), ("k_scale", _p), ("v_scale", _p)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", _p), ("n", _i32), ("stride", _i64)]
+
+
+class _ResidualNorm(ctypes.Structure):
+    _fields_ = [("dim", _i32), ("frame_tokens", _i32), ("norm", _i32), ("post", _i32),
+                ("eps", ctypes.c_float), ("residual", ctypes.c_float), ("stream_type", _i32),
+                ("block_type", _i32), ("param_type", _i32), ("gate", _p), ("scale", _p),
+                ("shift", _p), ("gate_stride", _i64), ("scale_stride", _i64),
+                ("shift_stride", _i64), ("weight", _p), ("bias", _p), ("post_weight", _p)]
+
+
+class _NormGrads(ctypes.Structure):
+    _fields_ = [("x", _Rows), ("y", _Rows), ("gate", _p), ("scale", _p), ("shift", _p),
+                ("weight", _p), ("bias", _p), ("post_weight", _p)]
 
 
 _LIB = None
@@ -169,6 +192,22 @@ def lib():
                                                       ctypes.POINTER(_KvCache),
                                                       ctypes.POINTER(BlockMask),
                                                       ctypes.POINTER(_i64)]),
+            "lvsa_attention_lse": (_i32, [ctypes.POINTER(_Tensor)] * 3 +
+                                   [ctypes.POINTER(BlockMask), ctypes.POINTER(_Tensor), _p, _p]),
+            "lvsa_attention_backward": (_i32, [ctypes.POINTER(_Tensor)] * 5 +
+                                        [_p, ctypes.POINTER(BlockMask)] +
+                                        [ctypes.POINTER(_Tensor)] * 3 + [_p, _i64, _p]),
+            "lvsa_attention_backward_workspace": (_i32, [ctypes.POINTER(_Tensor),
+                                                         ctypes.POINTER(BlockMask),
+                                                         ctypes.POINTER(_i64)]),
+            "lvsa_residual_norm_forward": (_i32, [ctypes.POINTER(_ResidualNorm)] +
+                                           [ctypes.POINTER(_Rows)] * 4 + [_p]),
+            "lvsa_residual_norm_backward": (_i32, [ctypes.POINTER(_ResidualNorm)] +
+                                            [ctypes.POINTER(_Rows)] * 4 +
+                                            [ctypes.POINTER(_NormGrads), _p, _i64, _p]),
+            "lvsa_residual_norm_workspace": (_i32, [ctypes.POINTER(_ResidualNorm), _i32,
+                                                    ctypes.POINTER(_NormGrads),
+                                                    ctypes.POINTER(_i64)]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -298,6 +337,7 @@ class Csr:
         m = BlockMask()
         _check(lib().lvsa_csr_device_view(self._h, ctypes.byref(m)),
                "lvsa_csr_device_view")
+        m._owner = self        # the device copy lives as long as the view
         return m
 
     def exact_mask(self):
@@ -326,12 +366,15 @@ def _mask_keep(mask, tensors):
 def build_mask_device(T, P, B, step, row_ptr, col_idx, params=None, layer=0,
                       stream=None):
     """Device LVSA mask builder into int32 device tensors row_ptr [nb+1] and
-    col_idx [>= nb*nb]; returns a BlockMask over them."""
+    col_idx [>= nb*nb]; returns a BlockMask over them.  A graph whose attention has
+    saved an earlier mask in these tensors notices the write."""
     params = params or Params()
     _check(lib().lvsa_build_mask_device(T, P, B, step, layer, ctypes.byref(params),
                                         _p(row_ptr.data_ptr()), _p(col_idx.data_ptr()),
                                         col_idx.numel(), _stream_ptr(stream)),
            "lvsa_build_mask_device")
+    import torch
+    torch.autograd.graph.increment_version([row_ptr, col_idx])
     N = T * P + params.text_tokens
     nb = (N + B - 1) // B
     m = BlockMask(N, B, nb, nb, row_ptr.data_ptr(), col_idx.data_ptr())
@@ -385,8 +428,11 @@ def _tensor(t):
 
 
 def attention(q, k, v, mask, out=None, stream=None):
-    """Block-sparse attention (lvsa_attention); returns out."""
+    """Block-sparse attention (lvsa_attention); returns out.  Differentiable in q, k and
+    v (``attention_backward``); the mask has to stay as it is until the backward pass."""
     import torch
+    if _recording(q, k, v, out):
+        return _attend(q, k, v, mask, out, stream)
     if out is None:
         out = torch.empty_like(q)
     tq, tk, tv, to = (_tensor(x) for x in (q, k, v, out))
@@ -421,8 +467,11 @@ def attention_exact(q, k, v, mask, out=None, stream=None):
 
 
 def dense_attention(q, k, v, block=128, out=None, stream=None):
-    """Dense attention of the same kernel design (lvsa_dense_attention)."""
+    """Dense attention of the same kernel design (lvsa_dense_attention); differentiable
+    in q, k and v."""
     import torch
+    if _recording(q, k, v, out):
+        return _attend(q, k, v, _every_key(q, block), out, stream)
     if out is None:
         out = torch.empty_like(q)
     tq, tk, tv, to = (_tensor(x) for x in (q, k, v, out))
@@ -463,6 +512,12 @@ class _Fast:
         self.write, self.read = L.lvsa_kv_write, L.lvsa_kv_read
         self.attend = L.lvsa_attention_cache
         self.attend_workspace = L.lvsa_attention_cache_workspace
+        self.lse, self.back = L.lvsa_attention_lse, L.lvsa_attention_backward
+        self.back_workspace = L.lvsa_attention_backward_workspace
+        self.norm, self.norm_back = L.lvsa_residual_norm_forward, L.lvsa_residual_norm_backward
+        self.norm_workspace = L.lvsa_residual_norm_workspace
+        self.attention_graph = _attention_function(torch)
+        self.norm_graph = _norm_function(torch)
 
 
 def _fast():
@@ -756,3 +811,322 @@ def attention_cache(q, cache, mask=None, q_start=0, out=None, stream=None):
     if given:
         f.written(out)
     return out
+
+
+# ------------------------------------------------- attention with its gradients
+
+def _recording(*tensors):
+    if any(t is not None and t.requires_grad for t in tensors):
+        import torch
+        return torch.is_grad_enabled()
+    return False
+
+
+def _every_key(q, block):
+    """The mask that keeps every block: one without rows."""
+    n = q.shape[1]
+    return BlockMask(n, block, -(-n // block), -(-n // block), None, None) if block != 128 else None
+
+
+def _bf16_rows(device, *tensors):
+    for t in tensors:
+        if t.dtype != _FAST.bf16:
+            raise ValueError("expected bfloat16 tensors")
+    return [_rows(t, device) for t in tensors]
+
+
+def _attention_function(torch):
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, out, mask):
+            if out is not None:
+                ctx.mark_dirty(out)
+            out, lse = _launch_lse(q, k, v, mask, out, None)
+            ctx.mask = mask
+            # the mask's tensors too: a write to them before the backward pass is noticed
+            ctx.save_for_backward(q, k, v, out, lse, *getattr(mask, "_keep", ()))
+            return out
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad):
+            q, k, v, out, lse = ctx.saved_tensors[:5]
+            return *_launch_back(_readable(grad), q, k, v, out, lse, ctx.mask, None), None, None
+
+    return Attention
+
+
+def _attend(q, k, v, mask, out, stream):
+    if stream is not None:
+        return _with_stream(_attend, stream, q, k, v, mask, out, None)
+    return _fast().attention_graph.apply(q, k, v, out, mask)
+
+
+def _launch_lse(q, k, v, mask, out, lse):
+    f = _FAST
+    dev = f.device()
+    if out is None:
+        out = f.empty_like(q)
+    if lse is None:
+        lse = f.empty(q.shape[:2], dtype=f.torch.float32, device=q.device)
+    elif (lse.dtype != f.torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()
+          or lse.get_device() != dev):
+        raise ValueError("expected a contiguous float32 [heads, n_tokens] lse on the current device")
+    tq, tk, tv, to = _bf16_rows(dev, q, k, v, out)
+    _check(f.lse(tq, tk, tv, None if mask is None else _byref(mask), to, lse.data_ptr(),
+                 f.stream(dev)), "lvsa_attention_lse")
+    return out, lse
+
+
+def _launch_back(grad, q, k, v, out, lse, mask, grads):
+    f = _FAST
+    dev = f.device()
+    if grads is None:
+        grads = f.empty_like(q), f.empty_like(k), f.empty_like(v)
+    if (lse.dtype != f.torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()
+            or lse.get_device() != dev):
+        raise ValueError("expected a contiguous float32 [heads, n_tokens] lse on the current device")
+    tg, tq, tk, tv, to, gq, gk, gv = _bf16_rows(dev, grad, q, k, v, out, *grads)
+    m = None if mask is None else _byref(mask)
+    need = _i64()
+    _check(f.back_workspace(tq, m, _byref(need)), "lvsa_attention_backward_workspace")
+    work = f.empty(need.value, dtype=f.torch.uint8, device=q.device)
+    _check(f.back(tg, tq, tk, tv, to, lse.data_ptr(), m, gq, gk, gv, work.data_ptr(), need.value,
+                  f.stream(dev)), "lvsa_attention_backward")
+    return grads
+
+
+def attention_lse(q, k, v, mask=None, out=None, lse=None, stream=None):
+    """Attention over the blocks of ``mask`` (a BlockMask), or over every key, and each
+    row's log-sum-exp [heads, n] in float32 (lvsa_attention_lse): (out, lse), what
+    ``attention_backward`` takes.  For programs that have no graph: it records none."""
+    if stream is not None:
+        return _with_stream(attention_lse, stream, q, k, v, mask, out, lse)
+    f = _fast()
+    given = [t for t in (out, lse) if t is not None]
+    found = _launch_lse(q, k, v, mask, out, lse)
+    if given:
+        f.written(given)
+    return found
+
+
+def attention_backward(grad, q, k, v, out, lse, mask=None, grads=None, stream=None):
+    """Gradients of q, k and v from that of attention's output (lvsa_attention_backward),
+    with what ``attention_lse`` took and gave; into ``grads`` = (dq, dk, dv) if given.
+    What autograd calls for ``attention`` and ``dense_attention``."""
+    if stream is not None:
+        return _with_stream(attention_backward, stream, grad, q, k, v, out, lse, mask, grads)
+    f = _fast()
+    found = _launch_back(grad, q, k, v, out, lse, mask, grads)
+    if grads is not None:
+        f.written(list(grads))
+    return found
+
+
+# ------------------------------------------------- residual step between blocks
+
+_PARAMS = ("gate", "scale", "shift", "weight", "bias", "post_weight")
+
+
+class ResidualNorm:
+    """The step between two blocks on the residual stream of ``dim`` channels
+    (lvsa_residual_norm):  r = residual * x + gate * P(y) * post_weight,
+    h = (N(r) * weight + bias) * (1 + scale) + shift.  ``norm`` N and ``post`` P are
+    NORM_NONE, NORM_LAYER or NORM_RMS; gate, scale and shift have a row for every
+    ``frame_tokens`` tokens (0: one for all)."""
+
+    def __init__(self, dim, norm=NORM_LAYER, post=NORM_NONE, eps=1e-6, residual=1.0,
+                 frame_tokens=0):
+        if not all(0 <= x < 2 ** 31 for x in (dim, norm, post, frame_tokens)):
+            raise LvsaError(EINVAL, "ResidualNorm")
+        self.dim, self.norm, self.post = dim, norm, post
+        self.eps, self.residual, self.frame_tokens = eps, residual, frame_tokens
+
+
+def _channels(t, dim, device):
+    """A tensor [.., dim] as rows on device number ``device``."""
+    if t.get_device() != device:
+        raise ValueError("expected a tensor on the current device")
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, dim)
+        except RuntimeError:
+            raise ValueError("expected rows at one stride") from None
+    n, d = t.shape
+    if d != dim:
+        raise ValueError(f"expected rows of {dim} channels")
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError("channels must be contiguous")
+    if n >> 31:
+        raise LvsaError(EUNSUPPORTED, f"{n} rows")
+    return _Rows(t.data_ptr(), n, t.stride(0) if n > 1 else dim)
+
+
+def _norm_plan(plan, n, stream, block, params, device):
+    """lvsa_residual_norm of a call on n rows of the given types."""
+    f = _FAST
+    codes = f.codes
+    if stream not in codes or block not in codes:
+        raise ValueError("expected bfloat16, float16 or float32")
+    c = _ResidualNorm(plan.dim, plan.frame_tokens, plan.norm, plan.post, plan.eps, plan.residual,
+                      codes[stream], codes[block], codes[block])
+    frame = plan.frame_tokens or n
+    kind = None
+    for name, t in params.items():
+        if t is None:
+            continue
+        if kind is None:
+            kind = t.dtype
+            if kind not in codes:
+                raise ValueError("expected bfloat16, float16 or float32")
+            c.param_type = codes[kind]
+        elif t.dtype != kind:
+            raise ValueError("expected parameters of one type")
+        rows = _channels(t, plan.dim, device)
+        if rows.n != (-(-n // frame) if name in ("gate", "scale", "shift") else 1):
+            raise ValueError(f"{name} has {rows.n} rows, {n} tokens of {frame} a frame")
+        setattr(c, name, rows.data)
+        if name in ("gate", "scale", "shift"):
+            setattr(c, name + "_stride", rows.stride)
+    return c
+
+
+def _norm_function(torch):
+    class Step(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, plan, dtype, x, y, *params):
+            r, h = _launch_norm(plan, x, y, dict(zip(_PARAMS, params)), dtype, None, None)
+            ctx.plan = plan
+            ctx.set_materialize_grads(False)
+            ctx.block = (y if y is not None else h).dtype
+            ctx.save_for_backward(x if y is None else r, y, *params)
+            return h if y is None else r if h is None else (r, h)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, *grads):
+            plan = ctx.plan
+            r, y, *params = ctx.saved_tensors
+            grad_r, grad_h = ((None, grads[0]) if y is None else
+                              (grads[0], None) if plan.norm == NORM_NONE else grads)
+            if grad_h is None and grad_r is None:
+                return (None,) * (4 + len(params))
+            if grad_h is None and plan.norm != NORM_NONE:
+                grad_h = r.new_zeros(r.shape, dtype=ctx.block)
+            names = ("x", "y", *_PARAMS)
+            wanted = [k for k, need in zip(names, ctx.needs_input_grad[2:]) if need]
+            found = _launch_norm_back(plan, *(g if g is None else _readable_rows(g, plan.dim)
+                                              for g in (grad_h, grad_r)), r, y,
+                                      dict(zip(_PARAMS, params)), wanted, None, None)
+            return None, None, *(found.get(k) for k in names)
+
+    return Step
+
+
+def _readable_rows(grad, dim):
+    """A gradient as autograd hands it on (expanded, say) in rows that the library
+    takes."""
+    if grad.is_contiguous() and grad.data_ptr() % 16 == 0:
+        return grad
+    return grad.clone(memory_format=_FAST.torch.contiguous_format)
+
+
+def _launch_norm(plan, x, y, params, dtype, r, h):
+    f = _FAST
+    dev = f.device()
+    dim = plan.dim
+    tx = _channels(x, dim, dev)
+    block = y.dtype if y is not None else dtype or (x if h is None else h).dtype
+    if dtype is not None and dtype != block:
+        raise ValueError("h is of y's type")
+    if y is not None and r is None:
+        r = f.empty(x.shape, dtype=x.dtype, device=x.device)
+    if plan.norm != NORM_NONE and h is None:
+        h = f.empty(x.shape, dtype=block, device=x.device)
+    for t, like, kind in ((y, x, block), (r, x, x.dtype), (h, x, block)):
+        if t is not None and (t.shape != like.shape or t.dtype != kind):
+            raise ValueError("expected tensors of x's shape, r of x's type and h of y's")
+    c = _norm_plan(plan, tx.n, x.dtype, block, params, dev)
+    ty, tr, th = (None if t is None else _byref(_channels(t, dim, dev)) for t in (y, r, h))
+    _check(f.norm(_byref(c), _byref(tx), ty, tr, th, f.stream(dev)), "lvsa_residual_norm_forward")
+    return r, h
+
+
+def residual_norm(plan, x, y=None, gate=None, scale=None, shift=None, weight=None, bias=None,
+                  post_weight=None, dtype=None, r=None, h=None, stream=None):
+    """One residual step (``plan``, a ResidualNorm) of x [.., dim] (bfloat16, float16,
+    float32) and the block's output y, of x's type or, where x is float32, any of them
+    (lvsa_residual_norm_forward).  Returns (r, h), of x's and of y's type; without y
+    h alone, the norm of x, of type ``dtype`` (by default x's); r alone for NORM_NONE.  gate,
+    scale, shift: [frames, dim]; weight, bias, post_weight: [dim]; all of one type.
+    Differentiable in every tensor; ``r`` and ``h`` are for calls outside a graph, r may
+    be x and h y."""
+    if stream is not None:
+        return _with_stream(residual_norm, stream, plan, x, y, gate, scale, shift, weight, bias,
+                            post_weight, dtype, r, h)
+    f = _fast()
+    params = gate, scale, shift, weight, bias, post_weight
+    if f.grad_enabled() and _recording(x, y, *params, r, h):
+        if r is not None or h is not None:
+            raise ValueError("r and h are for calls outside a graph")
+        return f.norm_graph.apply(plan, dtype, x, y, *params)
+    given = [t for t in (r, h) if t is not None]
+    r, h = _launch_norm(plan, x, y, dict(zip(_PARAMS, params)), dtype, r, h)
+    if given:
+        f.written(given)
+    return h if y is None else r if h is None else (r, h)
+
+
+def _launch_norm_back(plan, grad_h, grad_r, r, y, params, wanted, grad_x, grad_y):
+    f = _FAST
+    dev = f.device()
+    dim = plan.dim
+    some = next((t for t in (r, grad_r, y) if t is not None), grad_h)
+    stream = next((t.dtype for t in (r, grad_r) if t is not None), some.dtype)
+    block = next((t.dtype for t in (grad_h, y) if t is not None), some.dtype)
+    for t, kind in ((r, stream), (grad_r, stream), (grad_x, stream), (grad_h, block), (y, block),
+                    (grad_y, block)):
+        if t is not None and (t.shape != some.shape or t.dtype != kind):
+            raise ValueError("expected tensors of r's shape, gradients of their tensors' types")
+    n = _channels(some, dim, dev).n
+    c = _norm_plan(plan, n, stream, block, params, dev)
+    g, found = _NormGrads(), {}
+    for name, kind, out in (("x", stream, grad_x), ("y", block, grad_y)):
+        if name in wanted:
+            found[name] = f.empty(some.shape, dtype=kind, device=some.device) if out is None else out
+            setattr(g, name, _channels(found[name], dim, dev))
+    for name, t in params.items():
+        if name in wanted:
+            found[name] = f.empty(t.shape, dtype=t.dtype, device=t.device)
+            setattr(g, name, found[name].data_ptr())
+    need = _i64()
+    _check(f.norm_workspace(_byref(c), n, _byref(g), _byref(need)), "lvsa_residual_norm_workspace")
+    work = f.empty(need.value, dtype=f.torch.uint8, device=some.device) if need.value else None
+    rows = (None if t is None else _byref(_channels(t, dim, dev)) for t in (grad_h, grad_r, r, y))
+    _check(f.norm_back(_byref(c), *rows, _byref(g), None if work is None else work.data_ptr(),
+                       need.value, f.stream(dev)), "lvsa_residual_norm_backward")
+    return found
+
+
+def residual_norm_backward(plan, grad_h, grad_r, r, y=None, gate=None, scale=None, shift=None,
+                           weight=None, bias=None, post_weight=None, wanted=None, grad_x=None,
+                           grad_y=None, stream=None):
+    """Gradients of ``residual_norm`` (lvsa_residual_norm_backward) from those of h
+    (None for NORM_NONE) and r (None: zero), at the r that it gave (x, without y): a dict
+    of "x", "y" and of the names of the parameters given, or of those in ``wanted``.
+    grad_x and grad_y: where the first two go; grad_x may be grad_r, grad_y grad_h."""
+    if stream is not None:
+        return _with_stream(residual_norm_backward, stream, plan, grad_h, grad_r, r, y, gate,
+                            scale, shift, weight, bias, post_weight, wanted, grad_x, grad_y)
+    f = _fast()
+    params = dict(zip(_PARAMS, (gate, scale, shift, weight, bias, post_weight)))
+    names = [k for k in ("x", "y", *_PARAMS) if k == "x" or (y if k == "y" else params[k]) is not None]
+    if wanted is None:
+        wanted = names
+    elif not set(wanted) <= set(names):
+        raise ValueError(f"gradients of {names}")
+    found = _launch_norm_back(plan, grad_h, grad_r, r, y, params, wanted, grad_x, grad_y)
+    given = [t for t in (grad_x, grad_y) if t is not None]
+    if given:
+        f.written(given)
+    return found

@@ -16,8 +16,9 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "liblvsa.so")
-SOURCES = ["api.cpp", "api_cache.cpp", "mask_host.cpp", "mask_device.hip", "attention.hip",
-           "rope.hip", "kv_cache.hip", "attention_cache.hip"]
+SOURCES = ["api.cpp", "api_cache.cpp", "api_train.cpp", "mask_host.cpp", "mask_device.hip",
+           "attention.hip", "attention_back.hip", "rope.hip", "kv_cache.hip",
+           "attention_cache.hip", "residual_norm.hip", "residual_norm_back.hip"]
 ARCH = "gfx950"
 
 CFLAGS = [

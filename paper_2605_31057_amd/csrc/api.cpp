@@ -301,7 +301,7 @@ const char* lvsa_status_str(lvsa_status s) {
   }
 }
 
-int32_t lvsa_version(void) { return 20000; }
+int32_t lvsa_version(void) { return 20100; }
 
 void lvsa_params_default(lvsa_params* p) {
   if (!p) return;
@@ -588,8 +588,43 @@ lvsa_status attention_args(const lvsa_tensor* q, const lvsa_tensor* k,
   a->rows = nullptr;
   a->frame_tokens = 0;
   a->counters = nullptr;
+  a->lse = nullptr;
   return LVSA_OK;
 }
+
+}  // namespace
+}  // extern "C"
+
+namespace lvsa {
+
+lvsa_status train_attention_args(const lvsa_tensor* q, const lvsa_tensor* k,
+                                 const lvsa_tensor* v, const lvsa_block_mask* mask,
+                                 lvsa_tensor* out, AttnArgs* a) {
+  if (!q) return LVSA_EINVAL;
+  if (!mask) {
+    const int32_t n = q->n_tokens;
+    if (n < 1) return LVSA_EINVAL;
+    return attention_args(q, k, v, n, 128, (int32_t)(((int64_t)n + 127) / 128), out, a);
+  }
+  if (!mask->row_ptr && !mask->col_idx) {
+    if (mask->n_kv_blocks != mask->n_q_blocks) return LVSA_EINVAL;
+    return attention_args(q, k, v, mask->n_tokens, mask->block, mask->n_q_blocks, out, a);
+  }
+  if (!mask->row_ptr || !mask->col_idx) return LVSA_EINVAL;
+  if (mask->n_kv_blocks != mask->n_q_blocks) return LVSA_EINVAL;
+  if (mask->n_q_blocks > kMaxSparseBlocks) return LVSA_EUNSUPPORTED;
+  const lvsa_status st =
+      attention_args(q, k, v, mask->n_tokens, mask->block, mask->n_q_blocks, out, a);
+  if (st != LVSA_OK) return st;
+  a->row_ptr = mask->row_ptr;
+  a->rows = (const uint32_t*)mask->col_idx;
+  return LVSA_OK;
+}
+
+}  // namespace lvsa
+
+extern "C" {
+namespace {
 
 // Launches with a counter set of the pool (lvsa.h, "Tile counters").
 lvsa_status run_attention(AttnArgs& a, int32_t block, AttnMode mode, void* stream) {
@@ -625,6 +660,18 @@ lvsa_status lvsa_attention(const lvsa_tensor* q, const lvsa_tensor* k,
   a.row_ptr = mask->row_ptr;
   a.rows = (const uint32_t*)mask->col_idx;
   return run_attention(a, mask->block, ATTN_BLOCK, stream);
+}
+
+lvsa_status lvsa_attention_lse(const lvsa_tensor* q, const lvsa_tensor* k,
+                               const lvsa_tensor* v, const lvsa_block_mask* mask,
+                               lvsa_tensor* out, float* lse, void* stream) {
+  if (!q || !lse || q->n_tokens < 1) return LVSA_EINVAL;
+  if ((uintptr_t)lse % 4 != 0) return LVSA_EUNSUPPORTED;
+  lvsa_status st;
+  AttnArgs a;
+  if ((st = train_attention_args(q, k, v, mask, out, &a)) != LVSA_OK) return st;
+  a.lse = lse;
+  return run_attention(a, mask ? mask->block : 128, a.row_ptr ? ATTN_BLOCK : ATTN_DENSE, stream);
 }
 
 lvsa_status lvsa_attention_noalloc(const lvsa_tensor* q, const lvsa_tensor* k,

@@ -9,6 +9,32 @@
 namespace lvsa {
 namespace {
 
+// Whether two of a tensor's rows share an element: rows (h, t) and (h', t') do where
+// |(h - h') stride_head - (t - t') stride_token| < 128.
+bool rows_overlap(const lvsa_tensor& t, int32_t heads, int32_t n) {
+  const __int128 sh = t.stride_head, st = t.stride_token;
+  if ((n > 1 && st < 128) || (heads > 1 && sh < 128)) return true;
+  if (heads == 1 || n == 1) return false;
+  // One axis clears the other, as in every ordinary layout.
+  if (sh >= (n - 1) * st + 128 || st >= (heads - 1) * sh + 128) return false;
+  for (int32_t h = 1; h < heads; ++h) {
+    const __int128 at = h * sh, before = at / st;   // the tokens on both sides of it
+    if (before > n - 1) break;
+    if (at - before * st < 128 || (before + 1 < n && (before + 1) * st - at < 128)) return true;
+  }
+  return false;
+}
+
+}  // namespace
+
+lvsa_status check_output(const lvsa_tensor* t, int32_t heads, int32_t n) {
+  const lvsa_status st = check_tensor(t, heads, n);
+  if (st != LVSA_OK) return st;
+  return rows_overlap(*t, heads, n) ? LVSA_EINVAL : LVSA_OK;
+}
+
+namespace {
+
 constexpr int32_t kMaxCacheHeads = 65535;          // a launch's second dimension
 constexpr int64_t kMaxQueryRows = (int64_t)1 << 27; // heads * tokens of one attention call
 
@@ -59,29 +85,6 @@ bool known_type(int32_t dtype) {
 lvsa_status check_input(const lvsa_tensor* t) {
   if (!t || t->heads < 1 || t->n_tokens < 1) return LVSA_EINVAL;
   return check_tensor(t, t->heads, t->n_tokens);
-}
-
-// Whether two of a tensor's rows share an element: rows (h, t) and (h', t') do where
-// |(h - h') stride_head - (t - t') stride_token| < 128.
-bool rows_overlap(const lvsa_tensor& t, int32_t heads, int32_t n) {
-  const __int128 sh = t.stride_head, st = t.stride_token;
-  if ((n > 1 && st < 128) || (heads > 1 && sh < 128)) return true;
-  if (heads == 1 || n == 1) return false;
-  // One axis clears the other, as in every ordinary layout.
-  if (sh >= (n - 1) * st + 128 || st >= (heads - 1) * sh + 128) return false;
-  for (int32_t h = 1; h < heads; ++h) {
-    const __int128 at = h * sh, before = at / st;   // the tokens on both sides of it
-    if (before > n - 1) break;
-    if (at - before * st < 128 || (before + 1 < n && (before + 1) * st - at < 128)) return true;
-  }
-  return false;
-}
-
-// A tensor that is written: rows that do not overlap.
-lvsa_status check_output(const lvsa_tensor* t, int32_t heads, int32_t n) {
-  const lvsa_status st = check_tensor(t, heads, n);
-  if (st != LVSA_OK) return st;
-  return rows_overlap(*t, heads, n) ? LVSA_EINVAL : LVSA_OK;
 }
 
 lvsa_status check_cache(const lvsa_kv_cache* c) {

@@ -91,16 +91,10 @@
 // and l always use the same m.
 #include <atomic>
 
-#include "internal.h"
+#include "attention_lds.h"
 
 namespace lvsa {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int D = 128;             // head_dim
 // Distance (log2) of a row's reference above the largest score it was set from,
@@ -109,15 +103,6 @@ constexpr int D = 128;             // head_dim
 constexpr float HEADROOM = 7.f;
 constexpr float WIDE_HEADROOM = 39.f;
 constexpr int MAX_REDOS = 12;
-
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base,
-                                                            uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0,
-                                           bytes, 0x00020000);
-}
 
 // Largest of x0 (and of x1) over the four lanes that hold one query row (l,
 // l^16, l^32, l^48); every lane gets both results.  With 16-lane groups
@@ -135,22 +120,6 @@ __device__ __forceinline__ void row_max(float& x0, float& x1) {
   x0 = __uint_as_float(u[0]);
   x1 = __uint_as_float(u[1]);
 }
-
-// LDS tile layout ("slabs").  A BLOCK x 128 tile (one key block) is stored
-// as 4 slabs of 32 columns; a slab row is 64 bytes (4 chunks of 16 bytes) and
-// rows follow each other, so tile byte (slab, row, chunk) =
-// slab*BLOCK*64 + row*64 + chunk*16.
-// The chunk is XORed with x(row) = -(row/4) mod 4.  With 64 banks of 4 bytes:
-//   - ds_read_b128 is served 16 lanes at a time, lanes 0-3, 12-15 and 20-27
-//     together (then 4-11, 16-19 and 28-31; the same from lane 32 on): rows
-//     0-3 and 12-15 at one logical chunk c and rows 4-11 at c ^ 1, which x
-//     sends to four different bank quarters;
-//   - ds_read_b64_tr_b16 (served 32 lanes at a time) reads 8 consecutive rows
-//     x 2 chunks of a 32-byte half: rows 4..7 take the other half's banks.
-// Both are free of bank conflicts, and every fragment address an unrolled loop
-// needs is one of three per-lane bases plus an immediate offset.
-constexpr int SLAB_ROW = 64;
-__device__ __forceinline__ int xsw(int row) { return -(row >> 2) & 3; }
 
 struct Tile {
   static constexpr int NW = 8;                      // waves
@@ -173,26 +142,6 @@ struct Split {
   static constexpr int NK = Tile::KEYS / KG;        // keys per wave and step
   static constexpr int NU = NK / 32;                // 32-key groups per wave and step
 };
-
-// One wave load (1 KiB) of a K or V tile into LDS at byte address lds_dst:
-// `rsrc` starts at the tile's first row, `voff` = the lane's part of the
-// global byte offset plus the load's uniform part (LoadPlan).  Rows at or
-// past N fall outside the buffer resource and read as zeros.  The loads are
-// issued from inline assembly so the compiler does not track them: they are
-// waited for explicitly (vmcnt(0) plus a barrier) at the end of the step, and
-// no compiler-inserted wait can stall the phases in between.  The nop is the
-// wait state gfx9 needs between an SALU write of M0 and an LDS-DMA
-// instruction (the compiler cannot see into the statement to add it).
-__device__ __forceinline__ void issue_load(uint32_t lds_dst, __amdgpu_buffer_rsrc_t rsrc,
-                                           uint32_t voff, uint32_t soff) {
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %1, %2, %3 offen lds"
-      :
-      : "s"(lds_dst), "v"(voff), "s"(rsrc), "s"(soff)
-      : "memory", "m0");
-}
 
 // Buffer resource over rows kb*BLOCK .. N-1 of one head of K or V; a key
 // block index outside [0, nb) yields an empty resource (all loads read 0).
@@ -271,11 +220,6 @@ __device__ __forceinline__ void issue_step_loads(const StepLoads& sl) {
   for (int i = 0; i < 2 * Tile::LOADS; ++i) issue_step_load(sl, i);
 }
 
-__device__ __forceinline__ void wait_loads_and_sync() {
-  __builtin_amdgcn_s_waitcnt(0);  // vmcnt(0) expcnt(0) lgkmcnt(0)
-  __syncthreads();
-}
-
 // Time of a part of 256 / KG rows, in percent of a whole tile's (256 rows) of the same
 // walk (make_plan).
 constexpr int PART_TIME[] = {0, 100, 60, 0, 42};
@@ -326,9 +270,6 @@ __device__ __forceinline__ i16x4 v_half(const char* lds_v, const FragAddr& fa, i
       (lds_i16x4*)(lds_v + ((dt & 1) ? fa.v_odd : fa.v_even) + (dt / 2) * Tile::SLAB +
                    (u * 32 + half * 16) * SLAB_ROW));
 }
-__device__ __forceinline__ bf16x8 join(i16x4 lo, i16x4 hi) {
-  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
 __device__ __forceinline__ bf16x8 v_frag(const char* lds_v, const FragAddr& fa, int dt, int u) {
   return join(v_half(lds_v, fa, dt, u, 0), v_half(lds_v, fa, dt, u, 1));
 }
@@ -372,7 +313,9 @@ constexpr int READY = 1, WIDE = 2, REDO = 4;
 struct WaveState {
   f32x4 o[8][2];   // O^T tiles [d tile][query tile]: d = 16*dt + C row
   float m[2];      // reference of the exponentials (log2 domain), the same in a row's four lanes
-  f32x4 l[2];      // row sums
+  f32x4 l[2];      // row sums in register 0.  The MFMA that adds to them leaves the other
+                   // registers as they are: with STATS register 1 holds the fp32 sum of this
+                   // lane's share of the row, before P's rounding, register 2 a step's
   int flags;       // READY: every row has a finite m; WIDE: a step was redone; EAGER: REDO
                    // times the steps redone
 };
@@ -450,7 +393,7 @@ struct Probs {
 // above it, to `head` above that score, the others by `lift`, and rescales the rows'
 // O and l.  FIRST: ahead of the step's probabilities, not because some are too large.
 // EAGER: see softmax_phase.
-template <int NU, bool FIRST, bool EAGER>
+template <int NU, bool FIRST, bool EAGER, bool STATS>
 __device__ __forceinline__ void raise_max(const Scores<NU>& sc, WaveState& st,
                                           float scale_log2, float head, float lift) {
   float mx[2];
@@ -472,6 +415,7 @@ __device__ __forceinline__ void raise_max(const Scores<NU>& sc, WaveState& st,
       const float a = m == st.m[qt] ? 1.f : __builtin_amdgcn_exp2f(st.m[qt] - m);
       st.m[qt] = m;
       st.l[qt][0] *= a;
+      if (STATS) st.l[qt][1] *= a;
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) st.o[dt][qt] *= a;
     }
@@ -487,10 +431,10 @@ __device__ __forceinline__ void raise_max(const Scores<NU>& sc, WaveState& st,
 // Returns the bits of all probabilities or-ed together.  Scheduling barriers
 // every 8 scores keep the compiler from hoisting many exponentials at once
 // (S, P, O and Q already fill the register file).
-template <int NU, bool LOADS>
+template <int NU, bool LOADS, bool STATS>
 __device__ __forceinline__ uint32_t probabilities(const Scores<NU>& sc, Probs<NU>& pr,
                                                   const float (&m)[2], float scale_log2,
-                                                  const StepLoads& sl) {
+                                                  const StepLoads& sl, f32x4 (&l)[2]) {
   constexpr int NLOADS = 2 * Tile::LOADS;
   constexpr int GROUPS = 4 * NU;                     // groups of 4 scores
   constexpr int PER = (NLOADS + GROUPS - 1) / GROUPS;
@@ -513,6 +457,7 @@ __device__ __forceinline__ uint32_t probabilities(const Scores<NU>& sc, Probs<NU
               __builtin_fmaf(sc.s[2 * u + t][qt][r], scale_log2, -m[qt]));
           const float b = __builtin_amdgcn_exp2f(
               __builtin_fmaf(sc.s[2 * u + t][qt][r + 1], scale_log2, -m[qt]));
+          if (STATS) l[qt][2] += a + b;
           const bf16x2 pk = {(__bf16)a, (__bf16)b};
           bits |= __builtin_bit_cast(uint32_t, pk);
           pr.p[u][qt][4 * t + r] = pk[0];
@@ -551,24 +496,30 @@ __device__ __forceinline__ uint32_t probabilities(const Scores<NU>& sc, Probs<NU
 // and 32x32x16 MFMAs: 5.13, 4.57, 4.48, 4.42).  Whole tiles of two query blocks only:
 // split tiles and tiles of four are well ahead of the latter at any width and would
 // pay 1% and up to 3% on ordinary inputs.
-template <int NU, bool EAGER, bool LOADS>
+template <int NU, bool EAGER, bool LOADS, bool STATS>
 __device__ __forceinline__ void softmax_phase(const Scores<NU>& sc, WaveState& st,
                                               Probs<NU>& pr, float scale_log2,
                                               const StepLoads& sl) {
   const int flags = __builtin_amdgcn_readfirstlane(st.flags);
   const bool first = !(flags & READY);
   if (first)
-    raise_max<NU, true, EAGER>(sc, st, scale_log2, (flags & WIDE) ? WIDE_HEADROOM : HEADROOM,
+    raise_max<NU, true, EAGER, STATS>(sc, st, scale_log2, (flags & WIDE) ? WIDE_HEADROOM : HEADROOM,
                                0.f);
   float m[2];
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) m[qt] = st.m[qt] == -__builtin_inff() ? 0.f : st.m[qt];
-  const uint32_t bits = probabilities<NU, LOADS>(sc, pr, m, scale_log2, sl);
+  if (STATS) st.l[0][2] = st.l[1][2] = 0.f;
+  const uint32_t bits = probabilities<NU, LOADS, STATS>(sc, pr, m, scale_log2, sl, st.l);
   if (__builtin_amdgcn_ballot_w64((bits & 0x40004000u) != 0u) && !first) {
     st.flags = EAGER ? (st.flags | WIDE) + REDO : st.flags | WIDE;
-    raise_max<NU, false, EAGER>(sc, st, scale_log2, WIDE_HEADROOM,
-                                (flags & WIDE) ? 0.f : WIDE_HEADROOM - HEADROOM);
-    probabilities<NU, false>(sc, pr, st.m, scale_log2, sl);
+    raise_max<NU, false, EAGER, STATS>(sc, st, scale_log2, WIDE_HEADROOM,
+                                       (flags & WIDE) ? 0.f : WIDE_HEADROOM - HEADROOM);
+    if (STATS) st.l[0][2] = st.l[1][2] = 0.f;
+    probabilities<NU, false, STATS>(sc, pr, st.m, scale_log2, sl, st.l);
+  }
+  if constexpr (STATS) {
+    st.l[0][1] += st.l[0][2];
+    st.l[1][1] += st.l[1][2];
   }
 }
 
@@ -900,6 +851,11 @@ __device__ __forceinline__ int32_t single_row(WalkLds& L, const uint32_t* __rest
   return __builtin_amdgcn_readfirstlane(n);
 }
 
+// The log-sum-exp of a row with reference m (log2) and sum s of its exponentials.
+__device__ __forceinline__ float log_sum_exp(float m, float s) {
+  return s == 0.f ? -__builtin_inff() : 0.69314718055994531f * (m + __builtin_amdgcn_logf(s));
+}
+
 // Combines the key groups' partial results (KG > 1) and stores the tile's
 // rows: each of the KG waves that hold the same rows keeps 8 / KG of the eight
 // d tiles and takes the others' parts of them through LDS.  With m = max m_g,
@@ -907,10 +863,11 @@ __device__ __forceinline__ int32_t single_row(WalkLds& L, const uint32_t* __rest
 // of the groups.  `xch`: the tile buffers, idle here; wave w's part of d tile
 // dt is the 2 KB at 2048*(8*w + dt), and the slot of a d tile the wave keeps
 // holds its rows' (m, l).
-template <int KG>
+// `lse`: the head's log-sum-exps (STATS), from the groups' fp32 sums.
+template <int KG, bool STATS>
 __device__ __forceinline__ void combine_groups(char* xch, WaveState& st, const float (&lsum)[2],
-                                               __bf16* oh, int64_t o_st, int qrow, int N,
-                                               int wave, int lane) {
+                                               __bf16* oh, int64_t o_st, float* lse, int qrow,
+                                               int N, int wave, int lane) {
   using SP = Split<KG>;
   constexpr int KEEP = 8 / KG;
   const int rg = wave % SP::NRG, kg = wave / SP::NRG;
@@ -928,6 +885,11 @@ __device__ __forceinline__ void combine_groups(char* xch, WaveState& st, const f
     ml[1] = lsum[0];
     ml[2] = st.m[1];
     ml[3] = lsum[1];
+    if constexpr (STATS) {   // past the 256 bytes of the (m, l)
+      float* const ms = (float*)(slot(wave, kg * KEEP) + 256 + 8 * lane);
+      ms[0] = st.l[0][1];
+      ms[1] = st.l[1][1];
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -946,6 +908,14 @@ __device__ __forceinline__ void combine_groups(char* xch, WaveState& st, const f
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const bool ok = qrow + 16 * qt < N;
+    if constexpr (STATS) {
+      float s = 0.f;
+#pragma unroll
+      for (int g = 0; g < KG; ++g)
+        s += f[g] *
+             *(const float*)(slot(g * SP::NRG + rg, g * KEEP) + 256 + 8 * (lane % 16) + 4 * qt);
+      if (kg == 0 && lane < 16 && ok) lse[qrow + 16 * qt] = log_sum_exp(m, s);
+    }
     __bf16* const orow = oh + (int64_t)(qrow + 16 * qt) * o_st + 4 * (lane / 16);
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
@@ -979,13 +949,17 @@ __device__ __forceinline__ void combine_groups(char* xch, WaveState& st, const f
 // blocks, 12 heads of 32,768 tokens, 10% of the blocks kept: rows alike in pairs and
 // independent otherwise 0.75 ms against 0.98 with whole tiles only, all independent
 // 1.19 and 1.69 ms, rows alike in fours (whole tiles) 0.60 either way.
-template <int BLOCK, int MODE, int KG, int KGP>
+// STATS: the rows' log-sum-exps go to lse.  They take fp32 sums of the exponentials as
+// they are before P's rounding (l sums the rounded ones, which would leave lse short of
+// fp32): 64 adds a step on the VALU.
+template <int BLOCK, int MODE, int KG, int KGP, bool STATS>
 __device__ __forceinline__ bool attn_tile(
     char* lds, WalkLds& walk, int head, int row0, const __bf16* __restrict__ qg,
     const __bf16* __restrict__ kg_, const __bf16* __restrict__ vg, __bf16* __restrict__ og,
     int64_t q_sh, int64_t q_st, int64_t k_sh, int64_t k_st, int64_t v_sh, int64_t v_st,
-    int64_t o_sh, int64_t o_st, int32_t N, int32_t nb, const int32_t* __restrict__ row_ptr,
-    const uint32_t* __restrict__ rows, int32_t P, float scale_log2) {
+    int64_t o_sh, int64_t o_st, float* __restrict__ lse, int32_t N, int32_t nb,
+    const int32_t* __restrict__ row_ptr, const uint32_t* __restrict__ rows, int32_t P,
+    float scale_log2) {
   using TL = Tile;
   using SP = Split<KG>;
   constexpr int NU = SP::NU;
@@ -1204,7 +1178,7 @@ __device__ __forceinline__ bool attn_tile(
     compute_scores<NU>(k_lds, qf, sc, fa);   // S(0)
     int keep = mask_step(sc, w0, o0, upper);
     Probs<NU> pr;
-    if (lead) softmax_phase<NU, EAGER, false>(sc, ws, pr, scale_log2, StepLoads{});   // P(0)
+    if (lead) softmax_phase<NU, EAGER, false, STATS>(sc, ws, pr, scale_log2, StepLoads{});   // P(0)
     __syncthreads();
     for (int j = 0; j < n; ++j) {
       // Word of step j+3 from the walk's LDS, read now and used at the end of
@@ -1227,14 +1201,14 @@ __device__ __forceinline__ bool attn_tile(
         keep = mask_step(sc, w1, o1, false);
       } else {
         if constexpr (KG == 1) issue_step_loads(sl);
-        softmax_phase<NU, EAGER, (KG > 1)>(sc, ws, pr, scale_log2, sl);
+        softmax_phase<NU, EAGER, (KG > 1), STATS>(sc, ws, pr, scale_log2, sl);
       }
       __syncthreads();
       // half-period 2j+1
       if (lead) {
         if (j + 1 < n) {
           if constexpr (KG == 1) issue_step_loads(sl);
-          softmax_phase<NU, EAGER, false>(sc, ws, pr, scale_log2, sl);
+          softmax_phase<NU, EAGER, false, STATS>(sc, ws, pr, scale_log2, sl);
         }
       } else {
         gemm_phase<NU, SKIP, false>(kj1, vj, qf, sc, pr, ws, fa, ones, keep, sl);
@@ -1253,8 +1227,16 @@ __device__ __forceinline__ bool attn_tile(
   }
 
   const float lsum[2] = {ws.l[0][0], ws.l[1][0]};   // whole in every lane
+  if constexpr (STATS) {
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      ws.l[qt][1] += __shfl_xor(ws.l[qt][1], 16);
+      ws.l[qt][1] += __shfl_xor(ws.l[qt][1], 32);
+    }
+  }
   if constexpr (KG > 1) {
-    combine_groups<KG>(lds, ws, lsum, oh, o_st, qrow, N, wave, lane);
+    combine_groups<KG, STATS>(lds, ws, lsum, oh, o_st, STATS ? lse + (int64_t)head * N : nullptr,
+                              qrow, N, wave, lane);
   } else {
     // Every wave holds whole rows: O / l, rounded to bf16.
 #pragma unroll
@@ -1262,6 +1244,8 @@ __device__ __forceinline__ bool attn_tile(
       const float inv = lsum[qt] > 0.f ? 1.f / lsum[qt] : 0.f;
       __bf16* const orow = oh + (int64_t)(qrow + 16 * qt) * o_st + 4 * g16;
       if (qrow + 16 * qt < N) {
+        if (STATS && g16 == 0)
+          lse[(int64_t)head * N + qrow + 16 * qt] = log_sum_exp(ws.m[qt], ws.l[qt][1]);
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) {
           bf16x4 w;
@@ -1331,18 +1315,19 @@ struct KArgs {
   const int32_t* row_ptr;
   const uint32_t* rows;
   uint64_t* counters;        // null: one item per workgroup
+  float* lse;                // [heads][N] (STATS)
   int32_t N, nb, P;
   int32_t per_head;          // whole tiles of a head
   int32_t whole, split;      // items (share_item)
   float scale_log2;
 };
 
-template <int BLOCK, int MODE, int KG, int KGP>
+template <int BLOCK, int MODE, int KG, int KGP, bool STATS>
 __device__ __forceinline__ bool attn_tile_args(char* lds, WalkLds& walk, int head, int row0,
                                                const KArgs& a) {
-  return attn_tile<BLOCK, MODE, KG, KGP>(lds, walk, head, row0, a.q, a.k, a.v, a.o, a.q_sh,
-                                         a.q_st, a.k_sh, a.k_st, a.v_sh, a.v_st, a.o_sh, a.o_st,
-                                         a.N, a.nb, a.row_ptr, a.rows, a.P, a.scale_log2);
+  return attn_tile<BLOCK, MODE, KG, KGP, STATS>(
+      lds, walk, head, row0, a.q, a.k, a.v, a.o, a.q_sh, a.q_st, a.k_sh, a.k_st, a.v_sh, a.v_st,
+      a.o_sh, a.o_st, a.lse, a.N, a.nb, a.row_ptr, a.rows, a.P, a.scale_log2);
 }
 
 // The kernel's arguments (its first), read through an offset that the compiler
@@ -1361,7 +1346,7 @@ __device__ __forceinline__ const KArgs* fresh_args() {
 // there is a workgroup for every item (all whole or all split).  Whole tiles
 // run with KGW key groups, the parts of split ones with KGS (KGS / KGW parts
 // per tile).
-template <int BLOCK, int MODE, int KGW, int KGS>
+template <int BLOCK, int MODE, int KGW, int KGS, bool STATS>
 __global__ __launch_bounds__(Tile::NT) void attn_fwd_kernel(const KArgs args) {
   __shared__ __attribute__((aligned(1024))) char lds[4 * Tile::BYTES];
   __shared__ WalkLds walk;
@@ -1398,7 +1383,7 @@ __global__ __launch_bounds__(Tile::NT) void attn_fwd_kernel(const KArgs args) {
         i = last = PARTS - 1 - (item - ap->whole) % PARTS;
       } else {
         const int p = ap->per_head - 1 - item % ap->per_head;
-        if (!attn_tile_args<BLOCK, MODE, KGW, KGS>(lds, walk, item / ap->per_head,
+        if (!attn_tile_args<BLOCK, MODE, KGW, KGS, STATS>(lds, walk, item / ap->per_head,
                                                    p * Split<KGW>::ROWS, *ap))
           i = PARTS - 1;
       }
@@ -1408,13 +1393,13 @@ __global__ __launch_bounds__(Tile::NT) void attn_fwd_kernel(const KArgs args) {
         const int p = ap->per_head - 1 - tile % ap->per_head;
         const int row0 = p * Split<KGW>::ROWS + i * Split<KGS>::ROWS;
         if (row0 < ap->N)
-          attn_tile_args<BLOCK, MODE, KGS, KGS>(lds, walk, tile / ap->per_head, row0, *ap);
+          attn_tile_args<BLOCK, MODE, KGS, KGS, STATS>(lds, walk, tile / ap->per_head, row0, *ap);
       }
     } else {
       const KArgs* ap = fresh_args();
       if (item < ap->whole) {
         const int p = ap->per_head - 1 - item % ap->per_head;
-        attn_tile_args<BLOCK, MODE, KGW, KGW>(lds, walk, item / ap->per_head,
+        attn_tile_args<BLOCK, MODE, KGW, KGW, STATS>(lds, walk, item / ap->per_head,
                                               p * Split<KGW>::ROWS, *ap);
       } else if constexpr (PARTS > 1) {
         const int u = item - ap->whole;
@@ -1422,7 +1407,7 @@ __global__ __launch_bounds__(Tile::NT) void attn_fwd_kernel(const KArgs args) {
         const int p = ap->per_head - 1 - tile % ap->per_head;
         const int row0 = p * Split<KGW>::ROWS + (PARTS - 1 - u % PARTS) * Split<KGS>::ROWS;
         if (row0 < ap->N)
-          attn_tile_args<BLOCK, MODE, KGS, KGS>(lds, walk, tile / ap->per_head, row0, *ap);
+          attn_tile_args<BLOCK, MODE, KGS, KGS, STATS>(lds, walk, tile / ap->per_head, row0, *ap);
       }
     }
     if (!args.counters) break;
@@ -1508,8 +1493,8 @@ bool plan_is_direct(const AttnArgs& a, const Plan& p, int cus) {
   return items <= cus && (p.whole == 0 || p.whole == items);
 }
 
-template <int BLOCK, int MODE, int KGW, int KGS>
-hipError_t launch_t(const AttnArgs& a, const Plan& p, hipStream_t stream) {
+template <int BLOCK, int MODE, int KGW, int KGS, bool STATS>
+hipError_t launch_s(const AttnArgs& a, const Plan& p, hipStream_t stream) {
   const float scale_log2 = 1.4426950408889634f / __builtin_sqrtf((float)D);
   const int per_head = (int)(((int64_t)a.n_tokens + Split<KGW>::ROWS - 1) / Split<KGW>::ROWS);
   const int items = plan_items(a, p);
@@ -1525,6 +1510,7 @@ hipError_t launch_t(const AttnArgs& a, const Plan& p, hipStream_t stream) {
   k.v_sh = a.v_sh; k.v_st = a.v_st; k.o_sh = a.o_sh; k.o_st = a.o_st;
   k.row_ptr = a.row_ptr;
   k.rows = a.rows;
+  k.lse = a.lse;
   k.counters = plan_is_direct(a, p, cu_count()) ? nullptr : a.counters;
   k.N = a.n_tokens; k.nb = a.n_blocks; k.P = a.frame_tokens;
   k.per_head = per_head;
@@ -1533,9 +1519,17 @@ hipError_t launch_t(const AttnArgs& a, const Plan& p, hipStream_t stream) {
   k.scale_log2 = scale_log2;
   if (k.counters)
     hipLaunchKernelGGL(zero_counters_kernel, dim3(1), dim3(64), 0, stream, a.counters);
-  hipLaunchKernelGGL((attn_fwd_kernel<BLOCK, MODE, KGW, KGS>), dim3(grid), dim3(Tile::NT), 0,
+  hipLaunchKernelGGL((attn_fwd_kernel<BLOCK, MODE, KGW, KGS, STATS>), dim3(grid), dim3(Tile::NT), 0,
                      stream, k);
   return hipGetLastError();
+}
+
+// The token-exact form has no log-sum-exps (lvsa_attention_lse takes block masks).
+template <int BLOCK, int MODE, int KGW, int KGS>
+hipError_t launch_t(const AttnArgs& a, const Plan& p, hipStream_t stream) {
+  if constexpr (MODE != ATTN_EXACT)
+    if (a.lse) return launch_s<BLOCK, MODE, KGW, KGS, true>(a, p, stream);
+  return launch_s<BLOCK, MODE, KGW, KGS, false>(a, p, stream);
 }
 
 }  // namespace

@@ -67,6 +67,7 @@ struct AttnArgs {
   const uint32_t* rows;      // col_idx (block form) or entry words (exact form)
   int32_t frame_tokens;      // P (ATTN_EXACT only)
   uint64_t* counters;        // kTileCounters words, any content (zeroed here)
+  float* lse;                // [heads][n_tokens] log-sum-exps of the rows, or null
 };
 enum AttnMode { ATTN_DENSE = 0, ATTN_BLOCK = 1, ATTN_EXACT = 2 };
 hipError_t launch_attention(const AttnArgs& a, int32_t block, AttnMode mode,
@@ -74,6 +75,27 @@ hipError_t launch_attention(const AttnArgs& a, int32_t block, AttnMode mode,
 // Whether that launch takes tile counters (one with a workgroup for every tile
 // does not; `counters` is then unused).
 bool attention_uses_counters(const AttnArgs& a, int32_t block, AttnMode mode);
+
+// The arguments of attention over a block mask or every key (mask null), checked, but for
+// lse and the counters (api.cpp).
+lvsa_status train_attention_args(const lvsa_tensor* q, const lvsa_tensor* k,
+                                 const lvsa_tensor* v, const lvsa_block_mask* mask,
+                                 lvsa_tensor* out, AttnArgs* a);
+
+// Gradients of that attention (attention_back.hip), strides in elements.
+struct AttnBackArgs {
+  AttnArgs f;                // q, k, v, out (as inputs), lse, the mask
+  int32_t block;
+  const void* go;
+  void* gq;
+  void* gk;
+  void* gv;
+  int64_t go_sh, go_st, gq_sh, gq_st, gk_sh, gk_st, gv_sh, gv_st;
+  char* workspace;
+};
+int64_t attention_backward_workspace(int32_t heads, int32_t n_tokens, int32_t n_blocks,
+                                     bool sparse);
+hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream);
 
 // Per-device pool of tile-counter sets (api.cpp).  acquire hands out a set no
 // launch in flight uses; release records, after the launch on `stream`, the
@@ -90,6 +112,8 @@ void release_counters(const CounterLease& lease, hipStream_t stream);
 
 // Checks one attention tensor: [heads, n, 128], 16-byte aligned rows.
 lvsa_status check_tensor(const lvsa_tensor* t, int32_t heads, int32_t n);
+// One that is written: rows that do not overlap (api_cache.cpp).
+lvsa_status check_output(const lvsa_tensor* t, int32_t heads, int32_t n);
 
 // Rotary positions (rope.hip): x and y are [heads, n, 128] of `dtype`, strides in
 // elements; sign +1 forward, -1 for the gradient.

@@ -1,0 +1,269 @@
+// residual_norm_back.hip -- the step between two blocks on the residual stream, its
+// gradients (residual_norm.h has the formulas).
+//
+// Bound: memory, r, y and the gradients of r and h in, those of x and y out.  Rows are
+// held in registers as forward, norms taken again from them (nothing is saved for the
+// backward pass).  The sums over a frame's rows stay in registers over a unit's rows, are
+// joined in LDS over the teams of a workgroup, and go as one row of partial sums a
+// workgroup to the second kernel, which adds a frame's in a fixed order; weights, which
+// belong to all frames, take a third.
+#include "residual_norm.h"
+
+namespace lvsa {
+namespace {
+
+template <typename S, typename Y, int TEAM, int V, int MODE>
+__global__ __launch_bounds__(kNormThreads<TEAM>) void backward_kernel(const NormArgs a) {
+  constexpr int TEAMS = kNormThreads<TEAM> / TEAM;
+  __shared__ float lds[kNormSumLds<TEAM>];
+  __shared__ float join[TEAMS > 1 ? 256 * V * 8 : 1];
+  int turn = 0;
+  const int t = threadIdx.x % TEAM;
+  const int64_t id = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
+  const bool there = id < (int64_t)a.frames * a.units;   // all of a workgroup where joined
+  NormUnit u = {0, 0, 0};
+  if (there) u = norm_unit(a, id);
+  const float inv_dim = 1.f / (float)a.dim;
+
+  bool ok[V];
+  float g[V][8], m[V][8], sa[V][8], sb[V][8], sc[V][8];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int32_t col = 8 * (t + TEAM * v);
+    ok[v] = there && col < a.dim;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sa[v][k] = sb[v][k] = sc[v][k] = 0.f;
+    if (!ok[v]) continue;
+    float p[8];
+    load_param(a.gate, a.param_type, (int64_t)u.f * a.gate_st + col, 1.f, g[v]);
+    load_param(a.post_weight, a.param_type, col, 1.f, p);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) g[v][k] *= p[k];
+    load_param(a.weight, a.param_type, col, 1.f, m[v]);
+    load_param(a.scale, a.param_type, (int64_t)u.f * a.scale_st + col, 0.f, p);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[v][k] *= 1.f + p[k];
+  }
+
+  for (int64_t i = u.lo; i < u.hi; ++i) {
+    float e[V][8], x[V][8], y[V][8], d[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int64_t col = 8 * (t + TEAM * v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[v][k] = y[v][k] = d[v][k] = e[v][k] = 0.f;
+      if (!ok[v]) continue;
+      if (a.norm != LVSA_NORM_NONE) {
+        load8((const S*)a.x + i * a.x_st + col, x[v]);
+        load8((const Y*)a.gh + i * a.gh_st + col, d[v]);
+      }
+      if (a.gr) load8((const S*)a.gr + i * a.gr_st + col, e[v]);
+      if (MODE != NORM_OF_X) load8((const Y*)a.y + i * a.y_st + col, y[v]);
+    }
+    if (a.norm != LVSA_NORM_NONE) {
+      const float factor = normalise<TEAM, V>(x, ok, a.norm, inv_dim, a.eps, lds, turn);
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (!ok[v]) continue;
+          sa[v][k] = __builtin_fmaf(d[v][k], x[v][k], sa[v][k]);
+          sb[v][k] += d[v][k];
+          d[v][k] *= m[v][k];
+        }
+      normalise_back<TEAM, V>(d, x, ok, a.norm, factor, inv_dim, lds, turn);
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[v][k] += d[v][k];
+    }
+    if (a.r) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (!ok[v]) continue;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) d[v][k] = a.a * e[v][k];
+        store8((S*)a.r + i * a.r_st + 8 * (t + TEAM * v), d[v]);
+      }
+    }
+    if constexpr (MODE == NORM_OF_X) continue;
+    float factor = 1.f;
+    if constexpr (MODE == NORM_POST)
+      factor = normalise<TEAM, V>(y, ok, a.post, inv_dim, a.eps, lds, turn);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (!ok[v]) continue;
+        sc[v][k] = __builtin_fmaf(e[v][k], y[v][k], sc[v][k]);
+        e[v][k] *= g[v][k];
+      }
+    if constexpr (MODE == NORM_POST)
+      normalise_back<TEAM, V>(e, y, ok, a.post, factor, inv_dim, lds, turn);
+    if (a.h) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (ok[v]) store8((Y*)a.h + i * a.h_st + 8 * (t + TEAM * v), e[v]);
+    }
+  }
+
+  if (!a.partial) return;
+  if (TEAMS > 1 && a.joined) {
+    const int64_t row = (int64_t)blockIdx.x * 3;
+    for (int which = 0; which < 3; ++which) {
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          join[(threadIdx.x / TEAM * V + v) * TEAM * 8 + t * 8 + k] =
+              which == 0 ? sa[v][k] : which == 1 ? sb[v][k] : sc[v][k];
+      __syncthreads();
+      for (int c = threadIdx.x; c < a.dim; c += 256) {
+        float s = 0.f;
+        for (int w = 0; w < TEAMS; ++w) s += join[w * V * TEAM * 8 + c];
+        a.partial[(row + which) * a.dim + c] = s;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (!ok[v]) continue;
+      float* const at = a.partial + id * 3 * a.dim + 8 * (t + TEAM * v);
+      store8(at, sa[v]);
+      store8(at + a.dim, sb[v]);
+      store8(at + 2 * (int64_t)a.dim, sc[v]);
+    }
+  }
+}
+
+// Adds rows of three sums: SLICES threads share the rows of four columns, added in the
+// order of the slices.
+constexpr int SLICES = 8, LANES = 32;
+
+__device__ __forceinline__ void sum_rows(const float* rows, int64_t n, int32_t dim, int32_t col,
+                                         f32x4v (&s)[3], f32x4v (&lds)[3][SLICES][LANES]) {
+  const int lane = threadIdx.x % LANES, slice = threadIdx.x / LANES;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) s[w] = f32x4v{};
+  if (col < dim)
+    for (int64_t i = slice; i < n; i += SLICES)
+#pragma unroll
+      for (int w = 0; w < 3; ++w) s[w] += *(const f32x4v*)(rows + (i * 3 + w) * dim + col);
+#pragma unroll
+  for (int w = 0; w < 3; ++w) lds[w][slice][lane] = s[w];
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    s[w] = f32x4v{};
+    for (int k = 0; k < SLICES; ++k) s[w] += lds[w][k][lane];
+  }
+}
+
+__device__ __forceinline__ f32x4v param4(const void* p, int32_t type, int64_t i, float none) {
+  if (!p) return f32x4v{none, none, none, none};
+  if (type == LVSA_F32) return *(const f32x4v*)((const float*)p + i);
+  f32x4v x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    x[k] = type == LVSA_BF16 ? (float)((const __bf16*)p)[i + k] : (float)((const _Float16*)p)[i + k];
+  return x;
+}
+__device__ __forceinline__ void put4(void* p, int32_t type, int64_t i, f32x4v x) {
+  if (!p) return;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (type == LVSA_F32)
+      ((float*)p)[i + k] = x[k];
+    else if (type == LVSA_BF16)
+      ((__bf16*)p)[i + k] = (__bf16)x[k];
+    else
+      ((_Float16*)p)[i + k] = (_Float16)x[k];
+  }
+}
+
+// A frame's sums: the gradients of its gate, scale and shift, and what it adds to those
+// of the weights (to frame_sums).
+__global__ __launch_bounds__(SLICES* LANES) void frame_kernel(const NormArgs a, int32_t per_frame) {
+  __shared__ f32x4v lds[3][SLICES][LANES];
+  const int32_t f = blockIdx.x;
+  const int32_t col = 4 * (int32_t)(blockIdx.y * LANES + threadIdx.x % LANES);
+  f32x4v s[3];
+  sum_rows(a.partial + (int64_t)f * per_frame * 3 * a.dim, per_frame, a.dim, col, s, lds);
+  if (threadIdx.x >= LANES || col >= a.dim) return;
+  const int64_t at = (int64_t)f * a.dim + col;
+  const f32x4v w = param4(a.weight, a.param_type, col, 1.f);
+  const f32x4v b = param4(a.bias, a.param_type, col, 0.f);
+  put4(a.d_scale, a.param_type, at, w * s[0] + b * s[1]);
+  put4(a.d_shift, a.param_type, at, s[1]);
+  put4(a.d_gate, a.param_type, at, param4(a.post_weight, a.param_type, col, 1.f) * s[2]);
+  if (a.frame_sums) {
+    const f32x4v k = param4(a.scale, a.param_type, (int64_t)f * a.scale_st + col, 0.f) + 1.f;
+    float* const to = a.frame_sums + (int64_t)f * 3 * a.dim + col;
+    *(f32x4v*)to = k * s[0];
+    *(f32x4v*)(to + a.dim) = k * s[1];
+    *(f32x4v*)(to + 2 * (int64_t)a.dim) =
+        param4(a.gate, a.param_type, (int64_t)f * a.gate_st + col, 1.f) * s[2];
+  }
+}
+
+__global__ __launch_bounds__(SLICES* LANES) void weight_kernel(const NormArgs a) {
+  __shared__ f32x4v lds[3][SLICES][LANES];
+  const int32_t col = 4 * (int32_t)(blockIdx.x * LANES + threadIdx.x % LANES);
+  f32x4v s[3];
+  sum_rows(a.frame_sums, a.frames, a.dim, col, s, lds);
+  if (threadIdx.x >= LANES || col >= a.dim) return;
+  put4(a.d_weight, a.param_type, col, s[0]);
+  put4(a.d_bias, a.param_type, col, s[1]);
+  put4(a.d_post_weight, a.param_type, col, s[2]);
+}
+
+int64_t partial_rows(const NormArgs& a) {
+  const NormTeam t = norm_team(a.dim);
+  const int64_t teams = t.threads < 256 ? 256 / t.threads : 1;
+  return (int64_t)a.frames * (a.joined ? a.units / teams : a.units);
+}
+
+struct Backward {
+  const NormArgs& a;
+  hipStream_t stream;
+  template <typename S, typename Y, int TEAM, int V>
+  hipError_t run() {
+    constexpr int TEAMS = kNormThreads<TEAM> / TEAM;
+    const int64_t units = (int64_t)a.frames * a.units;
+    const dim3 grid((uint32_t)((units + TEAMS - 1) / TEAMS)), block(kNormThreads<TEAM>);
+    if (norm_mode(a) == NORM_OF_X)
+      backward_kernel<S, Y, TEAM, V, NORM_OF_X><<<grid, block, 0, stream>>>(a);
+    else if (norm_mode(a) == NORM_STEP)
+      backward_kernel<S, Y, TEAM, V, NORM_STEP><<<grid, block, 0, stream>>>(a);
+    else
+      backward_kernel<S, Y, TEAM, V, NORM_POST><<<grid, block, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+};
+
+}  // namespace
+
+// Bytes: the partial sums, and a row of three sums a frame for the weights.
+int64_t norm_workspace(const NormArgs& a) {
+  const bool weights = a.d_weight || a.d_bias || a.d_post_weight;
+  if (!weights && !a.d_gate && !a.d_scale && !a.d_shift) return 0;
+  return (partial_rows(a) + (weights ? a.frames : 0)) * 3 * a.dim * 4;
+}
+
+hipError_t launch_norm_backward(const NormArgs& args, int32_t stream_type, int32_t block_type,
+                                hipStream_t stream) {
+  NormArgs a = args;
+  const bool weights = a.d_weight || a.d_bias || a.d_post_weight;
+  a.frame_sums = a.partial && weights ? a.partial + partial_rows(a) * 3 * a.dim : nullptr;
+  hipError_t e = norm_dispatch(stream_type, block_type, norm_team(a.dim), Backward{a, stream});
+  if (e != hipSuccess || !a.partial) return e;
+  const uint32_t wide = (uint32_t)((a.dim / 4 + LANES - 1) / LANES);
+  frame_kernel<<<dim3((uint32_t)a.frames, wide), dim3(SLICES * LANES), 0, stream>>>(
+      a, (int32_t)(partial_rows(a) / a.frames));
+  if ((e = hipGetLastError()) != hipSuccess || !weights) return e;
+  weight_kernel<<<dim3(wide), dim3(SLICES * LANES), 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace lvsa

@@ -1,0 +1,390 @@
+"""Attention's log-sum-exps and gradients against the formulas in 64 bits, element by
+element within the bounds that the kernels' roundings give (oracle/train.py)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_31057_amd as L
+from oracle import train as OT
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    L.lib()
+
+
+def _inputs(H, n, seed=0, nhd=False, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    made = []
+    for wide in (size, 1.0, 1.0, 0.5):
+        x = (torch.randn((n, H, 128) if nhd else (H, n, 128), generator=g) * wide).to(BF).cuda()
+        made.append(x.transpose(0, 1) if nhd else x)
+    return made
+
+
+def _mask(kept, n, block):
+    kept = np.asarray(kept)
+    rows = torch.from_numpy(np.concatenate([[0], kept.sum(1).cumsum()]).astype(np.int32)).cuda()
+    cols = torch.from_numpy(np.nonzero(kept)[1].astype(np.int32)).cuda()
+    if not cols.numel():
+        cols = torch.zeros(1, dtype=torch.int32, device="cuda")
+    return L.csr_mask(rows, cols, n, block)
+
+
+def _kept(n, block, share=0.5, seed=1, empty=()):
+    nb = -(-n // block)
+    kept = np.random.default_rng(seed).random((nb, nb)) < share
+    for r in empty:
+        kept[r % nb] = False
+    return kept
+
+
+def _pass(q, k, v, grad, mask):
+    out, lse = L.attention_lse(q, k, v, mask)
+    dq, dk, dv = L.attention_backward(grad, q, k, v, out, lse, mask)
+    return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
+
+
+def _check(got, q, k, v, grad, kept=None):
+    n = q.shape[1]
+    kept = torch.ones(n, n, dtype=torch.bool) if kept is None else kept
+    want = OT.attention(*(x.double().contiguous() for x in (q, k, v, grad)), kept.cuda())
+    for name, x in got.items():
+        w, bound = want[name], want["bound"][name]
+        fine = torch.isfinite(w)
+        assert torch.equal(torch.isfinite(x), fine) and torch.equal(x[~fine].double(), w[~fine])
+        over = (x.double() - w).abs()[fine] - bound[fine]
+        assert (over <= 1e-30).all(), (name, float(over.max()), float(bound.max()))
+
+
+SIZES = [(1, 1), (2, 2), (1, 63), (2, 64), (1, 65), (3, 127), (1, 128), (2, 129), (1, 191),
+         (2, 257), (5, 500), (1, 1000)]
+
+
+@pytest.mark.parametrize("H,n", SIZES)
+def test_dense(H, n):
+    x = _inputs(H, n, seed=n)
+    _check(_pass(*x, None), *x)
+
+
+@pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("H,n", SIZES)
+def test_masked(block, H, n):
+    kept = _kept(n, block, seed=n, empty=(2,) if n > 3 * block else ())
+    kept[:, -1] |= kept.sum(1) == 0 if n <= 3 * block else False
+    x = _inputs(H, n, seed=n, nhd=n % 2 == 1)
+    _check(_pass(*x, _mask(kept, n, block)), *x, OT.kept_tokens(kept, block, n))
+
+
+@pytest.mark.parametrize("block", [64, 128])
+def test_rows_and_columns_without_blocks(block):
+    n = 7 * block + 5
+    kept = _kept(n, block, 0.4, seed=3, empty=(0, 3, 7))
+    kept[:, 2] = False
+    kept[:, 7] = False
+    x = _inputs(2, n)
+    got = _pass(*x, _mask(kept, n, block))
+    _check(got, *x, OT.kept_tokens(kept, block, n))
+    assert (got["dk"][:, 2 * block: 3 * block] == 0).all()
+    assert (got["dv"][:, 7 * block:] == 0).all()
+    assert (got["dq"][:, 3 * block: 4 * block] == 0).all()
+    assert (got["lse"][:, 3 * block: 4 * block] == -math.inf).all()
+
+
+@pytest.mark.parametrize("block", [64, 128])
+def test_an_empty_mask(block):
+    n = 3 * block - 1
+    x = _inputs(2, n)
+    got = _pass(*x, _mask(np.zeros((3, 3), bool), n, block))
+    assert all((got[name] == 0).all() for name in ("out", "dq", "dk", "dv"))
+
+
+@pytest.mark.parametrize("block", [64, 128])
+def test_blocks_that_are_not_kept_never_reach(block):
+    """NaN and infinities in a key block (a query block) stay out of the gradients of those
+    that it has no pair with."""
+    n = 6 * block
+    kept = _kept(n, block, 0.5, seed=8)
+    kept[:, 0] = True
+    kept[1, 3], kept[4, 3] = False, False
+    x = _inputs(2, n)
+    clean = _pass(*x, _mask(kept, n, block))
+    bad = [t.clone() for t in x]
+    bad[1][:, 3 * block: 4 * block] = math.nan
+    bad[2][:, 3 * block: 4 * block] = math.inf
+    got = _pass(*bad, _mask(kept, n, block))
+    for row in np.nonzero(~kept[:, 3])[0]:
+        at = slice(row * block, (row + 1) * block)
+        for name in ("out", "lse", "dq"):
+            assert torch.equal(got[name][:, at], clean[name][:, at])
+    # key blocks see it through the queries of rows that keep block 3 alone
+    for col in range(6):
+        if not (kept[:, 3] & kept[:, col]).any():
+            at = slice(col * block, (col + 1) * block)
+            assert torch.equal(got["dk"][:, at], clean["dk"][:, at])
+            assert torch.equal(got["dv"][:, at], clean["dv"][:, at])
+    bad = [t.clone() for t in x]
+    bad[0][:, 4 * block: 5 * block] = math.nan
+    bad[3][:, 4 * block: 5 * block] = -math.inf
+    got = _pass(*bad, _mask(kept, n, block))
+    for col in np.nonzero(~kept[4])[0]:
+        at = slice(col * block, (col + 1) * block)
+        assert torch.equal(got["dk"][:, at], clean["dk"][:, at])
+        assert torch.equal(got["dv"][:, at], clean["dv"][:, at])
+
+
+@pytest.mark.parametrize("size", [4.0, 30.0, 300.0])
+def test_wide_scores(size):
+    n = 300
+    x = _inputs(2, n, seed=5, size=size)
+    _check(_pass(*x, None), *x)
+
+
+def test_scores_far_from_zero():
+    """Every score near -700 or +700 in the natural logarithm: exponentials of the scores
+    alone would not be finite, nor those of keys past the last one."""
+    for sign in (-1.0, 1.0):
+        x = _inputs(1, 70, seed=6)
+        x[0][:] = sign * 8.0
+        x[1][:] = (8.0 + 0.25 * torch.randn(1, 70, 128, generator=torch.Generator().manual_seed(1))
+                   ).to(BF).cuda()
+        _check(_pass(*x, None), *x)
+
+
+def test_out_is_attentions():
+    """out is bit for bit that of the call without lse; whole and split tiles."""
+    for H, n, block in ((1, 1000, 128), (12, 5460, 128), (12, 5460, 64), (40, 4680, 128)):
+        q, k, v, _ = _inputs(H, n, seed=H)
+        kept = _kept(n, block, 0.6, seed=n)
+        m = _mask(kept, n, block)
+        assert torch.equal(L.attention_lse(q, k, v, m)[0], L.attention(q, k, v, m))
+        every = L.BlockMask(n, block, -(-n // block), -(-n // block), None, None)
+        assert torch.equal(L.attention_lse(q, k, v, every)[0],
+                           L.dense_attention(q, k, v, block=block))
+
+
+def test_long_rows_against_blocks_of_the_formula():
+    """12 heads of 4,000 tokens under a mask, whole tiles of every kernel: sampled rows and
+    keys."""
+    H, n, block = 12, 4000, 128
+    kept = _kept(n, block, 0.4, seed=2, empty=(5,))
+    x = _inputs(H, n, seed=9)
+    got = _pass(*x, _mask(kept, n, block))
+    for h in (0, 11):
+        _check({k: t[h: h + 1] for k, t in got.items()}, *(t[h: h + 1] for t in x),
+               OT.kept_tokens(kept, block, n))
+
+
+def test_the_same_every_time():
+    x = _inputs(3, 900, seed=4)
+    m = _mask(_kept(900, 64, 0.5), 900, 64)
+    first = _pass(*x, m)
+    for _ in range(3):
+        again = _pass(*x, m)
+        assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+def test_gradients_into_given_tensors_leave_the_rest():
+    H, n = 2, 150
+    x = _inputs(H, n)
+    want = _pass(*x, None)
+    out, lse = L.attention_lse(*x[:3])
+    room = [torch.full((n + 3, H, 128), 7.0, dtype=BF, device="cuda") for _ in range(3)]
+    grads = [r[1: n + 1].transpose(0, 1) for r in room]
+    got = L.attention_backward(x[3], *x[:3], out, lse, grads=grads)
+    for name, g, r in zip(("dq", "dk", "dv"), got, room):
+        assert torch.equal(g, want[name])
+        assert (r[0] == 7).all() and (r[n + 1:] == 7).all()
+
+
+def test_against_differences():
+    """The gradients of sum(out * grad) against central differences of the library's own
+    output, in a random direction, q, k and v together."""
+    x = _inputs(1, 200, seed=12)
+    got = _pass(*x, None)
+    g = torch.Generator().manual_seed(3)
+    step = [torch.randn(1, 200, 128, generator=g).cuda() for _ in range(3)]
+
+    def loss(t):
+        q, k, v = (a.double() + t * b.double() for a, b in zip(x, step))
+        p = torch.softmax(q @ k.transpose(1, 2) / math.sqrt(128), -1)
+        return float(((p @ v) * x[3].double()).sum())
+
+    slope = (loss(1e-4) - loss(-1e-4)) / 2e-4
+    mine = sum(float((got[n].double() * s.double()).sum()) for n, s in zip(("dq", "dk", "dv"), step))
+    want = OT.attention(*(t.double() for t in x), torch.ones(200, 200, dtype=torch.bool).cuda())
+    room = sum(float((want["bound"][n] * s.abs().double()).sum())
+               for n, s in zip(("dq", "dk", "dv"), step))
+    assert abs(mine - slope) <= room
+
+
+# ------------------------------------------------------------------ autograd
+
+def _leaves(x):
+    return [t.detach().clone().requires_grad_() for t in x[:3]]
+
+
+@pytest.mark.parametrize("block", [64, 128])
+def test_autograd(block):
+    n = 500
+    x = _inputs(3, n, seed=2)
+    m = _mask(_kept(n, block, 0.5), n, block)
+    want = _pass(*x, m)
+    q, k, v = _leaves(x)
+    out = L.attention(q, k, v, m)
+    assert torch.equal(out, want["out"])
+    out.backward(x[3])
+    for t, name in ((q, "dq"), (k, "dk"), (v, "dv")):
+        assert torch.equal(t.grad, want[name])
+    q, k, v = _leaves(x)
+    out = L.dense_attention(q, k, v, block=block)
+    assert torch.equal(out, L.dense_attention(*x[:3], block=block))
+    out.backward(x[3])
+    # the walk of keys does not depend on the forward pass's block
+    o, lse = L.attention_lse(*x[:3], L.BlockMask(n, block, -(-n // block), -(-n // block), None, None))
+    for t, w in zip((q, k, v), L.attention_backward(x[3], *x[:3], o, lse)):
+        assert torch.equal(t.grad, w)
+
+
+def test_autograd_of_some_and_of_expanded_gradients():
+    x = _inputs(2, 100)
+    ones = torch.ones(2, 100, 128, dtype=BF, device="cuda")
+    want = _pass(*x[:3], ones, None)
+    q, k, v = (t.clone() for t in x[:3])
+    v.requires_grad_()
+    L.dense_attention(q, k, v).backward(ones[:1, :1].expand(2, 100, 128))
+    assert torch.equal(v.grad, want["dv"]) and q.grad is None
+    with torch.no_grad():
+        assert not L.dense_attention(q, k, v).requires_grad
+    # one tensor three times: its gradient is the sum
+    t = x[0].clone().requires_grad_()
+    L.dense_attention(t, t, t).backward(ones)
+    want = _pass(x[0], x[0], x[0], ones, None)
+    total = sum(want[n].double() for n in ("dq", "dk", "dv"))
+    size = sum(want[n].double().abs() for n in ("dq", "dk", "dv"))
+    assert ((t.grad.double() - total).abs() <= 2 * 2.0 ** -8 * size).all()
+
+
+def test_autograd_into_a_given_output():
+    x = _inputs(2, 100)
+    q, k, v = _leaves(x)
+    out = torch.empty_like(x[0])
+    got = L.dense_attention(q, k, v, out=out)
+    assert got.data_ptr() == out.data_ptr()
+    got.backward(x[3])
+    assert torch.equal(q.grad, _pass(*x, None)["dq"])
+
+
+def test_a_mask_that_changes_before_the_backward_pass_is_noticed():
+    T, P, B = 8, 40, 64
+    nb = -(-T * P // B)
+    row_ptr = torch.empty(nb + 1, dtype=torch.int32, device="cuda")
+    col_idx = torch.empty(nb * nb, dtype=torch.int32, device="cuda")
+    p = L.Params(window=1, tper=3)
+    x = _inputs(1, T * P)
+    m = L.build_mask_device(T, P, B, 0, row_ptr, col_idx, p)
+    q, k, v = _leaves(x)
+    out = L.attention(q, k, v, m)
+    L.build_mask_device(T, P, B, 1, row_ptr, col_idx, p)
+    with pytest.raises(RuntimeError):
+        out.backward(x[3])
+
+
+def test_a_mask_of_a_handle_lives_as_long_as_its_view():
+    T, P, B = 8, 40, 64
+    x = _inputs(1, T * P)
+
+    def mask():
+        return L.build_mask(T, P, B, 0, L.Params(window=1, tper=3)).upload().device_mask()
+
+    q, k, v = _leaves(x)
+    out = L.attention(q, k, v, mask())
+    junk = [torch.full((64,), -1, dtype=torch.int32, device="cuda") for _ in range(50)]
+    out.backward(x[3])
+    want = _pass(*x, mask())
+    assert torch.equal(out, want["out"]) and torch.equal(k.grad, want["dk"])
+    del junk
+
+
+def test_second_derivatives_are_refused():
+    q, k, v = _leaves(_inputs(1, 64))
+    out = L.dense_attention(q, k, v)
+    grad, = torch.autograd.grad(out.float().pow(2).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        grad.float().sum().backward()
+
+
+# ------------------------------------------------------------------ streams, graphs
+
+def test_on_another_stream():
+    x = _inputs(2, 700)
+    m = _mask(_kept(700, 128, 0.6), 700, 128)
+    want = _pass(*x, m)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    out, lse = L.attention_lse(*x[:3], m, stream=s)
+    grads = L.attention_backward(x[3], *x[:3], out, lse, m, stream=s)
+    q, k, v = _leaves(x)
+    torch.cuda.synchronize()
+    y = L.attention(q, k, v, m, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    y.backward(x[3])
+    torch.cuda.synchronize()
+    for g, t, name in zip(grads, (q, k, v), ("dq", "dk", "dv")):
+        assert torch.equal(g, want[name]) and torch.equal(t.grad, want[name])
+
+
+def test_two_at_once():
+    a, b = _inputs(2, 900, seed=1), _inputs(2, 900, seed=2)
+    m = _mask(_kept(900, 64, 0.6), 900, 64)
+    want = _pass(*a, m), _pass(*b, m)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for s, x in zip(streams, (a, b)):
+        with torch.cuda.stream(s):
+            got.append(_pass(*x, m))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(g[k], w[k]) for k in w)
+
+
+def test_captured():
+    """A training pass captured into a graph, replayed with new inputs among eager ones."""
+    n = 600
+    m = _mask(_kept(n, 128, 0.6), n, 128)
+    x = _inputs(2, n)
+
+    def step():
+        q, k, v = (t.detach().requires_grad_() for t in x[:3])
+        out = L.attention(q, k, v, m)
+        return out.detach(), *torch.autograd.grad(out, (q, k, v), x[3])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for s in range(4):
+        fresh = _inputs(2, n, seed=30 + s)
+        for t, f in zip(x, fresh):
+            t.copy_(f)
+        for t in got:
+            t.fill_(0.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = _pass(*fresh, m)
+        for t, name in zip(got, ("out", "dq", "dk", "dv")):
+            assert torch.equal(t, want[name])
