@@ -433,7 +433,7 @@ typedef struct lvsa_rows {
 #define LVSA_NORM_NONE 0
 #define LVSA_NORM_LAYER 1
 #define LVSA_NORM_RMS 2
-#define LVSA_MAX_NORM_DIM 32768
+#define LVSA_MAX_NORM_DIM 16384
 typedef struct lvsa_residual_norm {
   int32_t dim;
   int32_t frame_tokens;

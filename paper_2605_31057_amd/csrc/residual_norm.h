@@ -64,18 +64,19 @@ hipError_t launch_norm_backward(const NormArgs& a, int32_t stream_type, int32_t 
 void norm_units(NormArgs& a, bool backward);
 int64_t norm_workspace(const NormArgs& a);
 
-// Threads that work a row, and eights of columns of each.
+// Threads that work a row: 16 or 64 of a workgroup of 256, or the whole workgroup
+// (`team` 0), eight columns each, past 8192 columns sixteen.
 struct NormTeam {
-  int32_t threads, eights;
+  int32_t team, threads, eights;
 };
 inline NormTeam norm_team(int32_t dim) {
   const int32_t c8 = dim / 8;
-  if (c8 <= 16) return {16, 1};
-  if (c8 <= 256) return {64, (c8 + 63) / 64};
-  if (c8 <= 1024) return {256, c8 <= 512 ? 2 : (c8 + 255) / 256};
-  return {1024, 4};
+  if (c8 <= 16) return {16, 16, 1};
+  if (c8 <= 64) return {64, 64, 1};
+  if (c8 <= 1024) return {0, (c8 + 63) / 64 * 64, 1};
+  return {0, 1024, 2};
 }
-constexpr int32_t kMaxNormDim = 1024 * 4 * 8;
+constexpr int kNormGroup = 256;   // threads of a workgroup of several teams
 
 // Eight parameters from element i on, as floats (`none` without them).
 __device__ __forceinline__ void load_param(const void* p, int32_t type, int64_t i, float none,
@@ -101,37 +102,140 @@ __device__ __forceinline__ void store_param(void* p, int32_t type, int64_t i,
     store8((_Float16*)p + i, x);
 }
 
-// Sums of K values over a team of TEAM threads (consecutive ones of the workgroup),
-// the same in each of them; teams of more than a wave are the whole workgroup.
-// `turn` alternates from call to call, so one barrier a call is enough: a wave writes
-// a buffer again only past the barrier of the call between.
-template <int TEAM, int K>
-__device__ __forceinline__ void team_sum(float (&v)[K], float* lds, int& turn) {
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int d = (TEAM < 64 ? TEAM : 64) / 2; d; d /= 2) v[k] += __shfl_xor(v[k], d);
-  if constexpr (TEAM > 64) {
-    constexpr int WAVES = TEAM / 64;
-    float* const at = lds + turn * (WAVES * 4);
-    turn ^= 1;
-    if (threadIdx.x % 64 == 0) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) at[threadIdx.x / 64 * 4 + k] = v[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      v[k] = 0.f;
-      for (int w = 0; w < WAVES; ++w) v[k] += at[w * 4 + k];
+// Eight elements as they are in memory: a row's are loaded while the row before is worked.
+template <typename T>
+struct Raw8 {
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  t8 v;
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (sizeof(T) == 4) {
+      const f32x4v a = *(const f32x4v*)p, b = *(const f32x4v*)(p + 4);
+      v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      v = *(const t8*)p;
     }
   }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = (float)v[k];
+  }
+};
+
+// x plus its value in another lane of the same 16: CTRL a DPP control.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float x) {
+  return x + __uint_as_float(
+                 __builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, true));
+}
+// Sum over 16 consecutive lanes, the same in each: pairs and quads by quad_perm, then
+// mirrored halves and rows.
+__device__ __forceinline__ float sum16(float x) {
+  x = add_dpp<0xB1>(x);    // quad_perm [1 0 3 2]
+  x = add_dpp<0x4E>(x);    // quad_perm [2 3 0 1]
+  x = add_dpp<0x141>(x);   // row_half_mirror
+  return add_dpp<0x140>(x);   // row_mirror
+}
+// Over the wave: the four rows by swaps, [x0 x0 x2 x2] + [x1 x1 x3 x3], then halves.
+__device__ __forceinline__ float sum64(float x) {
+  x = sum16(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+template <int TEAM>
+__device__ __forceinline__ float sum_team_wave(float x) {
+  return TEAM == 16 ? sum16(x) : sum64(x);
 }
 
-template <int TEAM>
-constexpr int kNormThreads = TEAM > 256 ? TEAM : 256;
-template <int TEAM>
-constexpr int kNormSumLds = TEAM > 64 ? 2 * 4 * TEAM / 64 : 1;
+// What a row's norm and its gradient need of the whole row: mean (0 for the RMS norm),
+// factor = 1 / sqrt(mean square of the deviations + eps), and of a gradient g of the
+// normalised row u its mean and the mean of g u.
+struct RowStats {
+  float mean, factor, g_mean, gu_mean;
+};
+// LDS of a workgroup that is one team: five sums a wave, in two buffers that alternate, so
+// one barrier a call is enough (a wave writes a buffer again only past the barrier of the
+// call between).
+struct StatsLds {
+  float v[2][16][8];
+};
+
+// RowStats of x (and g, BACK).  Columns a thread does not have hold 0 in both; `count`:
+// columns it has.  Deviations are taken from the wave's own mean before they are squared or
+// multiplied, and the waves' results put together about the row's mean,
+//   sum (x - m)^2 = sum_w [sum (x - m_w)^2 + n_w (m_w - m)^2],
+//   sum g (x - m) = sum_w [sum g (x - m_w) + (m_w - m) sum g],
+// so a mean far larger than the deviations costs nothing, and waves meet once.
+template <int TEAM, int V, bool BACK>
+__device__ __forceinline__ RowStats row_stats(const float (&x)[V][8], const float (&g)[V][8],
+                                              const bool (&ok)[V], int32_t kind, float inv_dim,
+                                              int32_t dim, float eps, StatsLds* lds, int& turn) {
+  constexpr int WAVE = TEAM == 0 ? 64 : TEAM;
+  const bool layer = kind == LVSA_NORM_LAYER;
+  float n = (float)dim;
+  if constexpr (TEAM == 0) {
+    // Columns of this wave: eights 64 w .. 64 w + 63 of each of the V stretches.
+    n = 0.f;
+    for (int v = 0; v < V; ++v) {
+      const int at = 8 * ((int)(threadIdx.x & ~63u) + (int)blockDim.x * v);
+      n += (float)max(0, min(512, dim - at));
+    }
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += x[v][k];
+  s = sum_team_wave<WAVE>(s);
+  const float mean = layer ? s / fmaxf(n, 1.f) : 0.f;
+  float m2 = 0.f, gs = 0.f, gx = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float d = ok[v] ? x[v][k] - mean : 0.f;
+      m2 = __builtin_fmaf(d, d, m2);
+      if (BACK) {
+        gx = __builtin_fmaf(g[v][k], d, gx);
+        gs += g[v][k];
+      }
+    }
+  m2 = sum_team_wave<WAVE>(m2);
+  if (BACK) {
+    gx = sum_team_wave<WAVE>(gx);
+    gs = sum_team_wave<WAVE>(gs);
+  }
+  RowStats r = {mean, 0.f, 0.f, 0.f};
+  if constexpr (TEAM == 0) {
+    const int wave = threadIdx.x / 64, waves = blockDim.x / 64, lane = threadIdx.x % 16;
+    float(*const at)[8] = lds->v[turn];
+    turn ^= 1;
+    if (threadIdx.x % 64 == 0) {
+      *(f32x4v*)at[wave] = f32x4v{n, mean, m2, gx};
+      at[wave][4] = gs;
+    }
+    __syncthreads();
+    // Lane w of every 16 takes wave w's.
+    const f32x4v o = lane < waves ? *(const f32x4v*)at[lane] : f32x4v{};
+    r.mean = sum16(o[0] * o[1]) * inv_dim;
+    const float off = o[1] - r.mean;
+    m2 = sum16(__builtin_fmaf(o[0] * off, off, o[2]));
+    if (BACK) {
+      const float og = lane < waves ? at[lane][4] : 0.f;
+      gx = sum16(__builtin_fmaf(off, og, o[3]));
+      gs = sum16(og);
+    }
+  }
+  r.factor = 1.f / __builtin_sqrtf(__builtin_fmaf(m2, inv_dim, eps));
+  if (BACK) {
+    r.g_mean = layer ? gs * inv_dim : 0.f;
+    r.gu_mean = gx * r.factor * inv_dim;
+  }
+  return r;
+}
 
 // The rows of unit `id`: frame f, rows lo .. hi - 1 (none where the frame has fewer).
 struct NormUnit {
@@ -148,62 +252,6 @@ __device__ __forceinline__ NormUnit norm_unit(const NormArgs& a, int64_t id) {
   return u;
 }
 
-// x becomes normalised over the row's `dim` columns, of which this thread has those
-// of `ok`; returns the factor 1 / sqrt(var + eps).  The RMS norm takes the mean too and
-// multiplies it by 0: with a branch around it the compiler (clang 20, ROCm 7.2) lost the
-// columns of the thread's second eight on one side of it, and a sum over a team costs little
-// beside the row's way from memory.
-template <int TEAM, int V>
-__device__ __forceinline__ float normalise(float (&x)[V][8], const bool (&ok)[V], int32_t kind,
-                                           float inv_dim, float eps, float* lds, int& turn) {
-  float s[1] = {0.f};
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s[0] += x[v][k];   // columns it does not have hold 0
-  team_sum<TEAM>(s, lds, turn);
-  const float mean = kind == LVSA_NORM_LAYER ? s[0] * inv_dim : 0.f;
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[v][k] = ok[v] ? x[v][k] - mean : 0.f;
-  s[0] = 0.f;
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s[0] = __builtin_fmaf(x[v][k], x[v][k], s[0]);
-  team_sum<TEAM>(s, lds, turn);
-  const float factor = 1.f / __builtin_sqrtf(__builtin_fmaf(s[0], inv_dim, eps));
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[v][k] *= factor;
-  return factor;
-}
-
-// Gradient of what normalise() took, in place of that of what it gave: `unit` is that,
-// `factor` what it returned.
-template <int TEAM, int V>
-__device__ __forceinline__ void normalise_back(float (&g)[V][8], const float (&unit)[V][8],
-                                               const bool (&ok)[V], int32_t kind, float factor,
-                                               float inv_dim, float* lds, int& turn) {
-  float s[2] = {0.f, 0.f};
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      s[0] = __builtin_fmaf(g[v][k], unit[v][k], s[0]);
-      s[1] += g[v][k];
-    }
-  team_sum<TEAM>(s, lds, turn);
-  const float along = s[0] * inv_dim, mean = kind == LVSA_NORM_LAYER ? s[1] * inv_dim : 0.f;
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      g[v][k] = ok[v] ? factor * (g[v][k] - mean - unit[v][k] * along) : 0.f;
-}
-
 // What a launch has of a block's output: nothing, y, or y and a norm of it.
 enum NormMode { NORM_OF_X = 0, NORM_STEP = 1, NORM_POST = 2 };
 inline NormMode norm_mode(const NormArgs& a) {
@@ -213,19 +261,10 @@ inline NormMode norm_mode(const NormArgs& a) {
 // Calls fn.run<S, Y, TEAM, V>() for a launch's types and team.
 template <typename S, typename Y, typename F>
 hipError_t norm_dispatch_team(const NormTeam& t, F&& fn) {
-  if (t.threads == 16) return fn.template run<S, Y, 16, 1>();
-  if (t.threads == 64) {
-    if (t.eights == 1) return fn.template run<S, Y, 64, 1>();
-    if (t.eights == 2) return fn.template run<S, Y, 64, 2>();
-    if (t.eights == 3) return fn.template run<S, Y, 64, 3>();
-    return fn.template run<S, Y, 64, 4>();
-  }
-  if (t.threads == 256) {
-    if (t.eights == 2) return fn.template run<S, Y, 256, 2>();
-    if (t.eights == 3) return fn.template run<S, Y, 256, 3>();
-    return fn.template run<S, Y, 256, 4>();
-  }
-  return fn.template run<S, Y, 1024, 4>();
+  if (t.team == 16) return fn.template run<S, Y, 16, 1>();
+  if (t.team == 64) return fn.template run<S, Y, 64, 1>();
+  if (t.eights == 1) return fn.template run<S, Y, 0, 1>();
+  return fn.template run<S, Y, 0, 2>();
 }
 template <typename F>
 hipError_t norm_dispatch(int32_t stream_type, int32_t block_type, const NormTeam& t, F&& fn) {

@@ -1,23 +1,21 @@
 // residual_norm.hip -- the step between two blocks on the residual stream, forward
 // (residual_norm.h has the formulas).
 //
-// Bound: memory, x and y in, r and h out.  A team of 16, 64, 256 or 1024 threads holds a
-// row in registers (at most 32 columns a thread), so every element is read once and
-// written once whatever norms are taken; mean and variance are two passes over the
-// registers, in fp32.  Parameters stay in registers over a unit's rows, which are of one
-// frame.
+// Bound: memory, x and y in, r and h out.  A team of threads holds a row in registers,
+// eight columns a thread, so every element is read once and written once whatever norms are
+// taken.  Parameters stay in registers over a unit's rows, which are of one frame.
 #include "residual_norm.h"
 
 namespace lvsa {
 namespace {
 
 template <typename S, typename Y, int TEAM, int V, int MODE>
-__global__ __launch_bounds__(kNormThreads<TEAM>) void forward_kernel(const NormArgs a) {
-  constexpr int TEAMS = kNormThreads<TEAM> / TEAM;
-  __shared__ float lds[kNormSumLds<TEAM>];
+__global__ __launch_bounds__(TEAM ? kNormGroup : 1024) void forward_kernel(const NormArgs a) {
+  __shared__ StatsLds lds;
   int turn = 0;
-  const int t = threadIdx.x % TEAM;
-  const int64_t id = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
+  const int team = TEAM ? TEAM : (int)blockDim.x, teams = TEAM ? kNormGroup / TEAM : 1;
+  const int t = TEAM ? threadIdx.x % TEAM : threadIdx.x;
+  const int64_t id = (int64_t)blockIdx.x * teams + (TEAM ? threadIdx.x / TEAM : 0);
   if (id >= (int64_t)a.frames * a.units) return;
   const NormUnit u = norm_unit(a, id);
   if (u.lo >= u.hi) return;
@@ -27,7 +25,7 @@ __global__ __launch_bounds__(kNormThreads<TEAM>) void forward_kernel(const NormA
   float g[V][8], m[V][8], c[V][8];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int32_t col = 8 * (t + TEAM * v);
+    const int32_t col = 8 * (t + team * v);
     ok[v] = col < a.dim;
     if (!ok[v]) continue;
     float p[8], s[8];
@@ -46,36 +44,55 @@ __global__ __launch_bounds__(kNormThreads<TEAM>) void forward_kernel(const NormA
     }
   }
 
+  Raw8<S> rx[V];
+  Raw8<Y> ry[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) rx[v].v = 0, ry[v].v = 0;
+  auto load_row = [&](int64_t i) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int64_t col = 8 * (t + team * v);
+      if (!ok[v]) continue;
+      rx[v].load((const S*)a.x + i * a.x_st + col);
+      if (MODE != NORM_OF_X) ry[v].load((const Y*)a.y + i * a.y_st + col);
+    }
+  };
+  load_row(u.lo);
   for (int64_t i = u.lo; i < u.hi; ++i) {
     float x[V][8], y[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int64_t col = 8 * (t + TEAM * v);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[v][k] = y[v][k] = 0.f;
-      if (!ok[v]) continue;
-      load8((const S*)a.x + i * a.x_st + col, x[v]);
-      if (MODE != NORM_OF_X) load8((const Y*)a.y + i * a.y_st + col, y[v]);
+      rx[v].get(x[v]);
+      ry[v].get(y[v]);
     }
+    if (i + 1 < u.hi) load_row(i + 1);
     if constexpr (MODE != NORM_OF_X) {
-      if constexpr (MODE == NORM_POST)
-        normalise<TEAM, V>(y, ok, a.post, inv_dim, a.eps, lds, turn);
+      if constexpr (MODE == NORM_POST) {
+        const RowStats r =
+            row_stats<TEAM, V, false>(y, y, ok, a.post, inv_dim, a.dim, a.eps, &lds, turn);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[v][k] = (y[v][k] - r.mean) * r.factor;
+      }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if (!ok[v]) continue;
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[v][k] = __builtin_fmaf(g[v][k], y[v][k], a.a * x[v][k]);
-        store8((S*)a.r + i * a.r_st + 8 * (t + TEAM * v), x[v]);
+        store8((S*)a.r + i * a.r_st + 8 * (t + team * v), x[v]);
       }
     }
     if (a.norm == LVSA_NORM_NONE) continue;
-    normalise<TEAM, V>(x, ok, a.norm, inv_dim, a.eps, lds, turn);
+    const RowStats r =
+        row_stats<TEAM, V, false>(x, x, ok, a.norm, inv_dim, a.dim, a.eps, &lds, turn);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (!ok[v]) continue;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[v][k] = __builtin_fmaf(x[v][k], m[v][k], c[v][k]);
-      store8((Y*)a.h + i * a.h_st + 8 * (t + TEAM * v), x[v]);
+      for (int k = 0; k < 8; ++k)
+        x[v][k] = __builtin_fmaf((x[v][k] - r.mean) * r.factor, m[v][k], c[v][k]);
+      store8((Y*)a.h + i * a.h_st + 8 * (t + team * v), x[v]);
     }
   }
 }
@@ -85,9 +102,10 @@ struct Forward {
   hipStream_t stream;
   template <typename S, typename Y, int TEAM, int V>
   hipError_t run() {
-    constexpr int TEAMS = kNormThreads<TEAM> / TEAM;
+    constexpr int TEAMS = TEAM ? kNormGroup / TEAM : 1;
     const int64_t units = (int64_t)a.frames * a.units;
-    const dim3 grid((uint32_t)((units + TEAMS - 1) / TEAMS)), block(kNormThreads<TEAM>);
+    const dim3 grid((uint32_t)((units + TEAMS - 1) / TEAMS));
+    const dim3 block(TEAM ? kNormGroup : norm_team(a.dim).threads);
     if (norm_mode(a) == NORM_OF_X)
       forward_kernel<S, Y, TEAM, V, NORM_OF_X><<<grid, block, 0, stream>>>(a);
     else if (norm_mode(a) == NORM_STEP)
@@ -105,12 +123,18 @@ hipError_t launch_norm_forward(const NormArgs& a, int32_t stream_type, int32_t b
   return norm_dispatch(stream_type, block_type, norm_team(a.dim), Forward{a, stream});
 }
 
-// Forward: workgroups for every compute unit several times over.  Backward: fewer, as
-// each leaves partial sums.
+// Rows are shared out to about twice as many teams as the chip's 256 compute units hold at
+// once (16 waves each).  Backward, where a team leaves a row of three sums (12 bytes a column,
+// written and read again, beside 12 to 18 a column and row), to as many as they hold or, with
+// fewer than 16 rows each, to half of that.
 void norm_units(NormArgs& a, bool backward) {
   const NormTeam t = norm_team(a.dim);
-  const int64_t teams = t.threads < 256 ? 256 / t.threads : 1;
-  const int64_t target = (backward ? 1024 : 2048) * teams;
+  const int64_t teams = t.team ? kNormGroup / t.team : 1;
+  int64_t target = (int64_t)256 * 2048 / t.threads;
+  if (backward) {
+    const int64_t full = target / 2, half = target / 4, sixteens = (a.n + 15) / 16;
+    target = sixteens < half ? half : sixteens < full ? sixteens : full;
+  }
   int64_t units = target * a.frame / a.n;
   units = units < 1 ? 1 : units > a.frame ? a.frame : units;
   a.joined = backward && teams > 1 && a.frame >= 4 * teams;

@@ -13,13 +13,13 @@ namespace lvsa {
 namespace {
 
 template <typename S, typename Y, int TEAM, int V, int MODE>
-__global__ __launch_bounds__(kNormThreads<TEAM>) void backward_kernel(const NormArgs a) {
-  constexpr int TEAMS = kNormThreads<TEAM> / TEAM;
-  __shared__ float lds[kNormSumLds<TEAM>];
-  __shared__ float join[TEAMS > 1 ? 256 * V * 8 : 1];
+__global__ __launch_bounds__(TEAM ? kNormGroup : 1024) void backward_kernel(const NormArgs a) {
+  __shared__ StatsLds lds;
+  __shared__ float join[TEAM ? kNormGroup * 8 : 1];
   int turn = 0;
-  const int t = threadIdx.x % TEAM;
-  const int64_t id = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
+  const int team = TEAM ? TEAM : (int)blockDim.x, teams = TEAM ? kNormGroup / TEAM : 1;
+  const int t = TEAM ? threadIdx.x % TEAM : threadIdx.x;
+  const int64_t id = (int64_t)blockIdx.x * teams + (TEAM ? threadIdx.x / TEAM : 0);
   const bool there = id < (int64_t)a.frames * a.units;   // all of a workgroup where joined
   NormUnit u = {0, 0, 0};
   if (there) u = norm_unit(a, id);
@@ -29,10 +29,10 @@ __global__ __launch_bounds__(kNormThreads<TEAM>) void backward_kernel(const Norm
   float g[V][8], m[V][8], sa[V][8], sb[V][8], sc[V][8];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int32_t col = 8 * (t + TEAM * v);
+    const int32_t col = 8 * (t + team * v);
     ok[v] = there && col < a.dim;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sa[v][k] = sb[v][k] = sc[v][k] = 0.f;
+    for (int k = 0; k < 8; ++k) sa[v][k] = sb[v][k] = sc[v][k] = g[v][k] = m[v][k] = 0.f;
     if (!ok[v]) continue;
     float p[8];
     load_param(a.gate, a.param_type, (int64_t)u.f * a.gate_st + col, 1.f, g[v]);
@@ -45,83 +45,109 @@ __global__ __launch_bounds__(kNormThreads<TEAM>) void backward_kernel(const Norm
     for (int k = 0; k < 8; ++k) m[v][k] *= 1.f + p[k];
   }
 
+  Raw8<S> rx[V], re[V];
+  Raw8<Y> rd[V], ry[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) rx[v].v = 0, re[v].v = 0, rd[v].v = 0, ry[v].v = 0;
+  auto load_row = [&](int64_t i) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int64_t col = 8 * (t + team * v);
+      if (!ok[v]) continue;
+      if (a.norm != LVSA_NORM_NONE) {
+        rx[v].load((const S*)a.x + i * a.x_st + col);
+        rd[v].load((const Y*)a.gh + i * a.gh_st + col);
+      }
+      if (a.gr) re[v].load((const S*)a.gr + i * a.gr_st + col);
+      if (MODE != NORM_OF_X) ry[v].load((const Y*)a.y + i * a.y_st + col);
+    }
+  };
+  if (u.lo < u.hi) load_row(u.lo);
   for (int64_t i = u.lo; i < u.hi; ++i) {
     float e[V][8], x[V][8], y[V][8], d[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int64_t col = 8 * (t + TEAM * v);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[v][k] = y[v][k] = d[v][k] = e[v][k] = 0.f;
-      if (!ok[v]) continue;
-      if (a.norm != LVSA_NORM_NONE) {
-        load8((const S*)a.x + i * a.x_st + col, x[v]);
-        load8((const Y*)a.gh + i * a.gh_st + col, d[v]);
-      }
-      if (a.gr) load8((const S*)a.gr + i * a.gr_st + col, e[v]);
-      if (MODE != NORM_OF_X) load8((const Y*)a.y + i * a.y_st + col, y[v]);
+      re[v].get(e[v]);
+      rx[v].get(x[v]);
+      ry[v].get(y[v]);
+      rd[v].get(d[v]);
     }
+    if (i + 1 < u.hi) load_row(i + 1);
     if (a.norm != LVSA_NORM_NONE) {
-      const float factor = normalise<TEAM, V>(x, ok, a.norm, inv_dim, a.eps, lds, turn);
+      float dm[V][8];
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dm[v][k] = d[v][k] * m[v][k];
+      const RowStats r =
+          row_stats<TEAM, V, true>(x, dm, ok, a.norm, inv_dim, a.dim, a.eps, &lds, turn);
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          if (!ok[v]) continue;
-          sa[v][k] = __builtin_fmaf(d[v][k], x[v][k], sa[v][k]);
+          const float unit = (x[v][k] - r.mean) * r.factor;
+          sa[v][k] = __builtin_fmaf(d[v][k], unit, sa[v][k]);
           sb[v][k] += d[v][k];
-          d[v][k] *= m[v][k];
+          const float back =
+              r.factor * (d[v][k] * m[v][k] - r.g_mean - unit * r.gu_mean);
+          e[v][k] = ok[v] ? e[v][k] + back : 0.f;
         }
-      normalise_back<TEAM, V>(d, x, ok, a.norm, factor, inv_dim, lds, turn);
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) e[v][k] += d[v][k];
     }
     if (a.r) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if (!ok[v]) continue;
+        float w[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) d[v][k] = a.a * e[v][k];
-        store8((S*)a.r + i * a.r_st + 8 * (t + TEAM * v), d[v]);
+        for (int k = 0; k < 8; ++k) w[k] = a.a * e[v][k];
+        store8((S*)a.r + i * a.r_st + 8 * (t + team * v), w);
       }
     }
     if constexpr (MODE == NORM_OF_X) continue;
-    float factor = 1.f;
-    if constexpr (MODE == NORM_POST)
-      factor = normalise<TEAM, V>(y, ok, a.post, inv_dim, a.eps, lds, turn);
+    if constexpr (MODE == NORM_POST) {
+      float eg[V][8];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+      for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (!ok[v]) continue;
-        sc[v][k] = __builtin_fmaf(e[v][k], y[v][k], sc[v][k]);
-        e[v][k] *= g[v][k];
-      }
-    if constexpr (MODE == NORM_POST)
-      normalise_back<TEAM, V>(e, y, ok, a.post, factor, inv_dim, lds, turn);
+        for (int k = 0; k < 8; ++k) eg[v][k] = e[v][k] * g[v][k];
+      const RowStats r =
+          row_stats<TEAM, V, true>(y, eg, ok, a.post, inv_dim, a.dim, a.eps, &lds, turn);
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float unit = (y[v][k] - r.mean) * r.factor;
+          sc[v][k] = __builtin_fmaf(e[v][k], unit, sc[v][k]);
+          y[v][k] = r.factor * (e[v][k] * g[v][k] - r.g_mean - unit * r.gu_mean);
+        }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          sc[v][k] = __builtin_fmaf(e[v][k], y[v][k], sc[v][k]);
+          y[v][k] = e[v][k] * g[v][k];
+        }
+    }
     if (a.h) {
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (ok[v]) store8((Y*)a.h + i * a.h_st + 8 * (t + TEAM * v), e[v]);
+        if (ok[v]) store8((Y*)a.h + i * a.h_st + 8 * (t + team * v), y[v]);
     }
   }
 
   if (!a.partial) return;
-  if (TEAMS > 1 && a.joined) {
+  if (TEAM && a.joined) {
+    // V is 1: a team's columns are 8 t .. 8 t + 7.
     const int64_t row = (int64_t)blockIdx.x * 3;
+#pragma unroll
     for (int which = 0; which < 3; ++which) {
       __syncthreads();
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          join[(threadIdx.x / TEAM * V + v) * TEAM * 8 + t * 8 + k] =
-              which == 0 ? sa[v][k] : which == 1 ? sb[v][k] : sc[v][k];
+      store8(join + threadIdx.x * 8, which == 0 ? sa[0] : which == 1 ? sb[0] : sc[0]);
       __syncthreads();
-      for (int c = threadIdx.x; c < a.dim; c += 256) {
+      for (int c = threadIdx.x; c < a.dim; c += kNormGroup) {
         float s = 0.f;
-        for (int w = 0; w < TEAMS; ++w) s += join[w * V * TEAM * 8 + c];
+        for (int w = 0; w < teams; ++w) s += join[w * team * 8 + c];
         a.partial[(row + which) * a.dim + c] = s;
       }
     }
@@ -129,7 +155,7 @@ __global__ __launch_bounds__(kNormThreads<TEAM>) void backward_kernel(const Norm
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (!ok[v]) continue;
-      float* const at = a.partial + id * 3 * a.dim + 8 * (t + TEAM * v);
+      float* const at = a.partial + id * 3 * a.dim + 8 * (t + team * v);
       store8(at, sa[v]);
       store8(at + a.dim, sb[v]);
       store8(at + 2 * (int64_t)a.dim, sc[v]);
@@ -138,26 +164,31 @@ __global__ __launch_bounds__(kNormThreads<TEAM>) void backward_kernel(const Norm
 }
 
 // Adds rows of three sums: SLICES threads share the rows of four columns, added in the
-// order of the slices.
-constexpr int SLICES = 8, LANES = 32;
+// order of the slices.  The results are in the first LANES threads.
+constexpr int SLICES = 16, LANES = 32;
 
 __device__ __forceinline__ void sum_rows(const float* rows, int64_t n, int32_t dim, int32_t col,
                                          f32x4v (&s)[3], f32x4v (&lds)[3][SLICES][LANES]) {
   const int lane = threadIdx.x % LANES, slice = threadIdx.x / LANES;
 #pragma unroll
   for (int w = 0; w < 3; ++w) s[w] = f32x4v{};
-  if (col < dim)
+  if (col < dim) {
+#pragma unroll 4
     for (int64_t i = slice; i < n; i += SLICES)
 #pragma unroll
       for (int w = 0; w < 3; ++w) s[w] += *(const f32x4v*)(rows + (i * 3 + w) * dim + col);
+  }
 #pragma unroll
   for (int w = 0; w < 3; ++w) lds[w][slice][lane] = s[w];
   __syncthreads();
+  f32x4v sum = f32x4v{};
+  if (slice < 3)
+    for (int k = 0; k < SLICES; ++k) sum += lds[slice][k][lane];
+  __syncthreads();
+  if (slice < 3) lds[slice][0][lane] = sum;
+  __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 3; ++w) {
-    s[w] = f32x4v{};
-    for (int k = 0; k < SLICES; ++k) s[w] += lds[w][k][lane];
-  }
+  for (int w = 0; w < 3; ++w) s[w] = lds[w][0][lane];
 }
 
 __device__ __forceinline__ f32x4v param4(const void* p, int32_t type, int64_t i, float none) {
@@ -220,7 +251,7 @@ __global__ __launch_bounds__(SLICES* LANES) void weight_kernel(const NormArgs a)
 
 int64_t partial_rows(const NormArgs& a) {
   const NormTeam t = norm_team(a.dim);
-  const int64_t teams = t.threads < 256 ? 256 / t.threads : 1;
+  const int64_t teams = t.team ? kNormGroup / t.team : 1;
   return (int64_t)a.frames * (a.joined ? a.units / teams : a.units);
 }
 
@@ -229,9 +260,10 @@ struct Backward {
   hipStream_t stream;
   template <typename S, typename Y, int TEAM, int V>
   hipError_t run() {
-    constexpr int TEAMS = kNormThreads<TEAM> / TEAM;
+    constexpr int TEAMS = TEAM ? kNormGroup / TEAM : 1;
     const int64_t units = (int64_t)a.frames * a.units;
-    const dim3 grid((uint32_t)((units + TEAMS - 1) / TEAMS)), block(kNormThreads<TEAM>);
+    const dim3 grid((uint32_t)((units + TEAMS - 1) / TEAMS));
+    const dim3 block(TEAM ? kNormGroup : norm_team(a.dim).threads);
     if (norm_mode(a) == NORM_OF_X)
       backward_kernel<S, Y, TEAM, V, NORM_OF_X><<<grid, block, 0, stream>>>(a);
     else if (norm_mode(a) == NORM_STEP)

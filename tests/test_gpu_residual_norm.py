@@ -121,7 +121,7 @@ def _backward(plan, t, gr, gh, kind, post, a, frame):
 
 SHAPES = [(1, 8, 1), (1, 1536, 1), (3, 128, 2), (17, 136, 4), (50, 512, 7), (33, 520, 0), (9, 1024, 3),
           (70, 1536, 32), (5, 2048, 5), (6, 2056, 4), (7, 5120, 3), (4, 8192, 2), (3, 8200, 2),
-          (2, 32768, 1), (300, 64, 100), (1000, 256, 130)]
+          (2, 16384, 1), (40, 16000, 15), (11, 72, 3), (300, 64, 100), (1000, 256, 130)]
 
 
 @pytest.mark.parametrize("n,dim,frame", SHAPES)
