@@ -17,8 +17,9 @@
 //   kernel then  dv' += X1' P  and both  (dq or dk)' += X0' E.  Scores are computed in
 //   both, 7 products in all for the 5 that the gradients need; one kernel would have to add
 //   up dq over workgroups, by atomics (an order that changes) or through memory.
-//   The queries kernel runs first and leaves (lse in base 2, delta) of its rows for the
-//   keys kernel.
+//   The queries kernel runs first and leaves (lse, delta) of its rows for the keys
+//   kernel; S and T begin with them (negated, lse times sqrt(d)) instead of zeros, so an
+//   element takes a product, an exponential and a product.
 //
 // The mask is taken as bitmaps (mask_bits_kernel): of every query block's key blocks and,
 // transposed, of every key block's query blocks; a workgroup walks the set bits of its
@@ -38,15 +39,18 @@ constexpr int D = 128;
 constexpr int ROWS = 128;             // resident rows of a workgroup
 constexpr int STEP = 64;              // streamed rows of a step
 constexpr int WAVES = 4;
+// Fragments read ahead of their products: as many as registers allow.
+template <bool KEYS>
+constexpr int AHEAD_OF = KEYS ? 3 : 4;
 constexpr int SLAB = STEP * SLAB_ROW; // bytes of a slab
 constexpr int TILE = 4 * SLAB;        // bytes of a streamed tile
 constexpr int MAX_WORDS = (kMaxSparseBlocks + 31) / 32;   // of a bitmap
 
-// What a streamed row brings beside its elements to the keys kernel, and a resident one
-// to the queries kernel.
+// Of every query, from the queries kernel to the keys kernel: what S and T begin with, so
+// that they end as (s - lse) sqrt(d) and do v' - delta.
 struct Stats {
-  float* lse2;      // [heads][N] log-sum-exp in base 2, +inf for rows without keys
-  float* delta;     // [heads][N]
+  float* lse;       // [heads][N] -lse sqrt(d), -inf for rows without keys (p = 0 then)
+  float* delta;     // [heads][N] -delta
 };
 
 struct BArgs {
@@ -66,22 +70,11 @@ struct BArgs {
   int32_t N, nb, heads, tiles;
 };
 
-// S and T of 32 streamed and 32 resident rows.
-struct Tile32 {
-  f32x4 v[2][2];   // [streamed 16][resident 16]
-};
-
 __device__ __forceinline__ bf16x8 row_frag(const char* tile, uint32_t at, int row0, int stp) {
   return *(const bf16x8*)(tile + at + stp * SLAB + row0 * SLAB_ROW);
 }
-// Fragment of the transposed tile: columns 16*dt .. +15, rows row0 .. row0 + 31; k-slot
-// e < 4 of lane group g is row 4g + e, e >= 4 row 16 + 4g + e - 4.
-__device__ __forceinline__ bf16x8 col_frag(const char* tile, uint32_t even, uint32_t odd, int row0,
-                                           int dt) {
-  const char* const p = tile + ((dt & 1) ? odd : even) + (dt / 2) * SLAB + row0 * SLAB_ROW;
-  return join(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p),
-              __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * SLAB_ROW)));
-}
+// (A fragment of the transposed tile, columns 16*dt .. +15 of 32 rows, is two transposing
+// reads of 16 rows: k-slot e < 4 of lane group g is row 4g + e, e >= 4 row 16 + 4g + e - 4.)
 
 // Walks the set bits of a bitmap (or all blocks), ascending.
 template <bool SPARSE>
@@ -140,12 +133,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
       r1[stp][t] = row < N ? *(const bf16x8*)(a.r1 + head * a.r1_sh + row * a.r1_st + c) : bf16x8{};
     }
   }
-  float lse2[2], delta[2];
+  float lse[2], delta[2];   // -lse / scale and -delta
   if constexpr (!KEYS) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int row = wrow + 16 * t + li;
-      lse2[t] = __builtin_inff();
+      lse[t] = -__builtin_inff();
       delta[t] = 0.f;
       if (row < N) {
 #pragma unroll
@@ -154,15 +147,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
               *(const bf16x8*)(a.o + head * a.o_sh + row * a.o_st + 32 * stp + 8 * g);
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            delta[t] = __builtin_fmaf((float)o[k], (float)r1[stp][t][k], delta[t]);
+            delta[t] = __builtin_fmaf(-(float)o[k], (float)r1[stp][t][k], delta[t]);
         }
         const float l = a.lse[(int64_t)head * N + row];
-        lse2[t] = l == -__builtin_inff() ? __builtin_inff() : l * 1.4426950408889634f;
+        lse[t] = l == -__builtin_inff() ? -__builtin_inff() : l * (-1.f / SCALE);
       }
       delta[t] += __shfl_xor(delta[t], 16);
       delta[t] += __shfl_xor(delta[t], 32);
       if (row < N && g == 0) {
-        a.stats.lse2[(int64_t)head * N + row] = lse2[t];
+        a.stats.lse[(int64_t)head * N + row] = lse[t];
         a.stats.delta[(int64_t)head * N + row] = delta[t];
       }
     }
@@ -189,7 +182,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
 
   const __bf16* const x0 = a.x0 + head * a.x0_sh;
   const __bf16* const x1 = a.x1 + head * a.x1_sh;
-  const float* const sl = a.stats.lse2 + (int64_t)head * N;
+  const float* const sl = a.stats.lse + (int64_t)head * N;
   const float* const sd = a.stats.delta + (int64_t)head * N;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_void*)&lds[0][0][0];
   const uint32_t stat_base = (uint32_t)(uintptr_t)(lds_void*)&stat[0][0][0];
@@ -257,59 +250,100 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
     }
     const char* const t0 = lds[s][0];
     const char* const t1 = lds[s][1];
+    // Fragments of the step, in the order of their use: for each 32 rows u the row fragments
+    // of S and T (16 rows x, 32 columns stp, both tensors), then the column fragments of the
+    // gradients (16 columns dt; both tensors in the keys kernel).  Each is read AHEAD of its
+    // two products.
+    constexpr int NA = 16, NB = KEYS ? 16 : 8, NF = NA + NB, AHEAD = AHEAD_OF<KEYS>;
+    bf16x8 fr[2 * NF];
+    i16x4 lo = i16x4{};
+    auto row_of = [&](int i) {
+      const int u = i / NF, f = i % NF;
+      return row_frag(f % 2 ? t1 : t0, at_row, 32 * u + 16 * (f / 8), f / 2 % 4);
+    };
+    auto col_half = [&](int i, int half) {
+      const int u = i / NF, f = i % NF - NA, dt = KEYS ? f / 2 : f;
+      const char* const tile = KEYS && f % 2 ? t1 : t0;
+      return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_i16x4*)(tile + ((dt & 1) ? at_odd : at_even) + (dt / 2) * SLAB +
+                       (32 * u + 16 * half) * SLAB_ROW));
+    };
+    // What goes along with product `m` of fragment i: the read of fragment i + AHEAD.
+    auto carry = [&](int i, int m) {
+      const int n = i + AHEAD;
+      if (n >= 2 * NF) return;
+      if (n % NF < NA) {
+        if (m == 0) fr[n] = row_of(n);
+      } else if (m == 0) {
+        lo = col_half(n, 0);
+      } else {
+        fr[n] = join(lo, col_half(n, 1));
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fr[i] = row_of(i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      if (row + 32 * u >= N) break;
-      Tile32 sc, tp;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) sc.v[x][t] = tp.v[x][t] = f32x4{};
-#pragma unroll
-        for (int stp = 0; stp < 4; ++stp) {
-          const bf16x8 f0 = row_frag(t0, at_row, 32 * u + 16 * x, stp);
-          const bf16x8 f1 = row_frag(t1, at_row, 32 * u + 16 * x, stp);
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            sc.v[x][t] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0, r0[stp][t], sc.v[x][t], 0, 0, 0);
-            tp.v[x][t] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1, r1[stp][t], tp.v[x][t], 0, 0, 0);
-          }
-        }
-      }
       bf16x8 pb[2], eb[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        f32x4 ls, ds;
+        // S and T begin with -lse / scale and -delta of their queries.
+        f32x4 sc[2], tp[2];
         if constexpr (KEYS) {
-          ls = *(const f32x4*)&stat[s][0][32 * u + 16 * x + 4 * g];
-          ds = *(const f32x4*)&stat[s][1][32 * u + 16 * x + 4 * g];
+          sc[0] = sc[1] = *(const f32x4*)&stat[s][0][32 * u + 16 * x + 4 * g];
+          tp[0] = tp[1] = *(const f32x4*)&stat[s][1][32 * u + 16 * x + 4 * g];
+        } else {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            sc[t] = f32x4{lse[t], lse[t], lse[t], lse[t]};
+            tp[t] = f32x4{delta[t], delta[t], delta[t], delta[t]};
+          }
+        }
+#pragma unroll
+        for (int stp = 0; stp < 4; ++stp)
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const int i = u * NF + 8 * x + 2 * stp + w;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              carry(i, t);
+              if (w == 0)
+                sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i], r0[stp][t], sc[t], 0, 0, 0);
+              else
+                tp[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i], r1[stp][t], tp[t], 0, 0, 0);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+        // Keys past the last: their elements are zeros, their scores would be 0.
+        if (!KEYS && row + STEP > N) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (row + 32 * u + 16 * x + 4 * g + r >= N) sc[t][r] = -__builtin_inff();
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float l = KEYS ? ls[r] : lse2[t], d = KEYS ? ds[r] : delta[t];
-            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc.v[x][t][r], SCALE_LOG2, -l));
-            // Keys past the last (their elements are zeros, their scores 0).
-            if (!KEYS && row + 32 * u + 16 * x + 4 * g + r >= N) p = 0.f;
-            const float e = p * (tp.v[x][t][r] - d);
-            pb[t][4 * x + r] = (__bf16)p;
+            const float p = __builtin_amdgcn_exp2f(sc[t][r] * SCALE_LOG2);
+            const float e = p * tp[t][r];
+            if (KEYS) pb[t][4 * x + r] = (__bf16)p;
             eb[t][4 * x + r] = (__bf16)e;
           }
       }
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) {
-        const bf16x8 f0 = col_frag(t0, at_even, at_odd, 32 * u, dt);
+      for (int f = 0; f < NB; ++f) {
+        const int i = u * NF + NA + f, dt = KEYS ? f / 2 : f;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          acc0[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0, eb[t], acc0[dt][t], 0, 0, 0);
-        if constexpr (KEYS) {
-          const bf16x8 f1 = col_frag(t1, at_even, at_odd, 32 * u, dt);
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            acc1[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1, pb[t], acc1[dt][t], 0, 0, 0);
+        for (int t = 0; t < 2; ++t) {
+          carry(i, t);
+          if (KEYS && f % 2)
+            acc1[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i], pb[t], acc1[dt][t], 0, 0, 0);
+          else
+            acc0[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i], eb[t], acc0[dt][t], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
