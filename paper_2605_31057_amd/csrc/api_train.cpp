@@ -27,6 +27,9 @@ lvsa_status check_read(const lvsa_tensor* t, int32_t heads, int32_t n) {
              : LVSA_OK;
 }
 
+// Rows past which a launch of the gradients could pass 2^32 work-items.
+bool too_long(int32_t heads, int32_t n) { return (int64_t)heads * n >= (int64_t)1 << 29; }
+
 // The step's parameters and the rows of each frame; n rows.
 lvsa_status norm_args(const lvsa_residual_norm* p, int32_t n, bool backward, NormArgs* a) {
   if (!p || n < 1) return LVSA_EINVAL;
@@ -93,7 +96,8 @@ extern "C" {
 lvsa_status lvsa_attention_backward_workspace(const lvsa_tensor* q, const lvsa_block_mask* mask,
                                               int64_t* bytes) {
   if (!q || !bytes || q->heads < 1 || q->n_tokens < 1) return LVSA_EINVAL;
-  int32_t nb = 0;
+  if (too_long(q->heads, q->n_tokens)) return LVSA_EUNSUPPORTED;
+  int32_t nb = (int32_t)(((int64_t)q->n_tokens + 127) / 128);
   bool sparse = false;
   if (mask) {
     if (mask->block != 64 && mask->block != 128) return LVSA_EUNSUPPORTED;
@@ -102,6 +106,7 @@ lvsa_status lvsa_attention_backward_workspace(const lvsa_tensor* q, const lvsa_b
     if (mask->n_q_blocks != nb || mask->n_kv_blocks != nb) return LVSA_EINVAL;
     sparse = mask->row_ptr != nullptr;
     if (sparse && nb > kMaxSparseBlocks) return LVSA_EUNSUPPORTED;
+    if (!sparse) nb = (int32_t)(((int64_t)q->n_tokens + 127) / 128);
   }
   *bytes = attention_backward_workspace(q->heads, q->n_tokens, nb, sparse);
   return LVSA_OK;
@@ -119,6 +124,7 @@ lvsa_status lvsa_attention_backward(const lvsa_tensor* grad_out, const lvsa_tens
   lvsa_status st;
   if ((st = train_attention_args(q, k, v, mask, &o, &a.f)) != LVSA_OK) return st;
   const int32_t H = q->heads, n = q->n_tokens;
+  if (too_long(H, n)) return LVSA_EUNSUPPORTED;
   if ((st = check_read(q, H, n)) != LVSA_OK) return st;
   if ((st = check_read(grad_out, H, n)) != LVSA_OK) return st;
   if (!aligned(lse, 4)) return LVSA_EUNSUPPORTED;
@@ -132,15 +138,15 @@ lvsa_status lvsa_attention_backward(const lvsa_tensor* grad_out, const lvsa_tens
   if (grad_q->data == grad_k->data || grad_q->data == grad_v->data ||
       grad_k->data == grad_v->data)
     return LVSA_EINVAL;
-  const int64_t need = attention_backward_workspace(H, n, a.f.n_blocks, a.f.row_ptr != nullptr);
-  if (!workspace || workspace_bytes < need) return LVSA_EINVAL;
-  if (!aligned(workspace, 16)) return LVSA_EUNSUPPORTED;
-  a.f.lse = const_cast<float*>(lse);
   a.block = mask ? mask->block : 128;
   if (!a.f.row_ptr) {   // every block: the walk is of 128-token ones
     a.block = 128;
     a.f.n_blocks = (int32_t)(((int64_t)n + 127) / 128);
   }
+  const int64_t need = attention_backward_workspace(H, n, a.f.n_blocks, a.f.row_ptr != nullptr);
+  if (!workspace || workspace_bytes < need) return LVSA_EINVAL;
+  if (!aligned(workspace, 16)) return LVSA_EUNSUPPORTED;
+  a.f.lse = const_cast<float*>(lse);
   a.go = grad_out->data, a.go_sh = grad_out->stride_head, a.go_st = grad_out->stride_token;
   a.gq = grad_q->data, a.gq_sh = grad_q->stride_head, a.gq_st = grad_q->stride_token;
   a.gk = grad_k->data, a.gk_sh = grad_k->stride_head, a.gk_st = grad_k->stride_token;

@@ -7,29 +7,34 @@
 // them would move 2 bytes a pair, 150 GB for the Wan-1.3B layer at 6x.
 //
 // Work decomposition
-//   Two kernels of one design.  A workgroup of four waves keeps 128 rows of two tensors
-//   ("resident": R0, R1) in registers, 32 a wave, and streams 64-row tiles of two others
-//   (X0, X1) through LDS:
+//   An item is 128 rows of two tensors ("resident": R0, R1), kept in the registers of four
+//   waves, 32 rows each, and a stretch of the rows they meet, streamed in tiles of 64 rows
+//   of two other tensors (X0, X1) through LDS:
 //     queries  R0 = q, R1 = do, X0 = k, X1 = v: dq of 128 queries over their kept keys
 //     keys     R0 = k, R1 = v,  X0 = q, X1 = do: dk and dv of 128 keys over the queries
 //              that keep them
-//   Both take  S = X0 R0',  T = X1 R1'  (scores and do v', [streamed][resident]), the keys
-//   kernel then  dv' += X1' P  and both  (dq or dk)' += X0' E.  Scores are computed in
-//   both, 7 products in all for the 5 that the gradients need; one kernel would have to add
-//   up dq over workgroups, by atomics (an order that changes) or through memory.
-//   The queries kernel runs first and leaves (lse, delta) of its rows for the keys
-//   kernel; S and T begin with them (negated, lse times sqrt(d)) instead of zeros, so an
-//   element takes a product, an exponential and a product.
+//   Both take  S = X0 R0',  T = X1 R1'  (scores and do v', [streamed][resident]), keys
+//   then  dv' += X1' P  and both  (dq or dk)' += X0' E.  Scores are computed in both, 7
+//   products in all for the 5 that the gradients need; adding up dq over workgroups instead
+//   would take atomics (an order that changes) or all of dq's parts in memory.
+//   One launch works both, the longest items first, two workgroups a compute unit.  Items
+//   longer than their share of the launch are split along the streamed rows, their parts
+//   left in memory in fp32 and added by combine_kernel in their order: where a few key
+//   blocks are kept by every query and the others by few, and where there are few rows.
 //
-// The mask is taken as bitmaps (mask_bits_kernel): of every query block's key blocks and,
-// transposed, of every key block's query blocks; a workgroup walks the set bits of its
-// rows' bitmaps.
+// Before it, prep_kernel takes what S and T begin with, -lse sqrt(d) and -delta of every
+// query (so that an element takes a product, an exponential and a product), and the mask
+// as bitmaps, of every query block's key blocks and, transposed, of every key block's
+// query blocks; plan_kernel makes the items from them.
 //
 // Contractions (bf16 MFMA 16x16x32, fp32 accumulate), as in attention.hip: a lane (group
 // g = lane/16, i = lane%16) holds resident row i of a 16-row tile in its columns, so P and
 // E go from the accumulators of S and T to the B operand of the next products without
 // leaving registers, and X0 and X1 are read from LDS twice, by rows (ds_read_b128) and
 // transposed (ds_read_b64_tr_b16).
+#include <algorithm>
+#include <atomic>
+
 #include "attention_lds.h"
 
 namespace lvsa {
@@ -45,29 +50,56 @@ constexpr int AHEAD_OF = KEYS ? 3 : 4;
 constexpr int SLAB = STEP * SLAB_ROW; // bytes of a slab
 constexpr int TILE = 4 * SLAB;        // bytes of a streamed tile
 constexpr int MAX_WORDS = (kMaxSparseBlocks + 31) / 32;   // of a bitmap
+constexpr int UNIT = ROWS * D;        // floats of a part's sums: one for dq, two for dk and dv
 
-// Of every query, from the queries kernel to the keys kernel: what S and T begin with, so
-// that they end as (s - lse) sqrt(d) and do v' - delta.
-struct Stats {
-  float* lse;       // [heads][N] -lse sqrt(d), -inf for rows without keys (p = 0 then)
-  float* delta;     // [heads][N] -delta
+// Costs of a step of 64 streamed rows, in products; an item longer than MIN_COST and than
+// SHARE of a workgroup slot's part of the whole launch is split.
+constexpr int COST[2] = {3, 4};       // queries, keys
+constexpr int MIN_COST = 12;
+constexpr double SHARE = 0.8;
+constexpr int SLOTS = 2;              // workgroups a compute unit
+
+enum { Q = 0, GO = 1, K = 2, V = 3, O = 4 };   // tensors read
+
+struct Item {
+  int32_t tile;      // bit 31: keys
+  int32_t first;     // its stretch: blocks of its walk, from the first'th on
+  int32_t count;
+  int32_t unit;      // where its part goes, -1: it is the whole walk
+};
+struct Split {       // an item in parts
+  int32_t tile, unit, parts, pad;
+};
+struct Plan {        // of one head, the same for all
+  int32_t items, splits;
+  int32_t done;      // workgroups of plan_kernel that are through
 };
 
 struct BArgs {
-  const __bf16* r0;
-  const __bf16* r1;
-  const __bf16* x0;
-  const __bf16* x1;
-  const __bf16* o;           // queries kernel: the forward output
-  const float* lse;          // queries kernel: natural log
-  __bf16* g0;                // dq or dk
-  __bf16* g1;                // dv
-  int64_t r0_sh, r0_st, r1_sh, r1_st, x0_sh, x0_st, x1_sh, x1_st, o_sh, o_st;
-  int64_t g0_sh, g0_st, g1_sh, g1_st;
-  Stats stats;
-  const uint32_t* bits;      // bitmaps of the resident blocks, null: every block
-  int64_t bits_word, bits_block;   // strides of a word and of a block's bitmap
-  int32_t N, nb, heads, tiles;
+  const __bf16* t[5];
+  int64_t sh[5], st[5];
+  __bf16* g[3];              // dq, dk, dv
+  int64_t g_sh[3], g_st[3];
+  const float* lse;          // natural log
+  // Of every query, what S and T begin with: -lse sqrt(d) (-inf for rows without keys: p
+  // is 0 then) and -delta.
+  float* row_lse;
+  float* row_delta;
+  const int32_t* row_ptr;
+  const int32_t* col_idx;
+  uint32_t* by_row;          // [nb][words], null without a mask
+  uint32_t* by_col;          // [words][nb]
+  Plan* plan;
+  int32_t* counts;           // blocks of the walks, queries' tiles and then keys'
+  Item* list;
+  Split* splits;
+  float* units;
+  int32_t N, nb, heads, tiles, words;
+  int32_t stat_groups;       // prep: workgroups of 64 rows
+  int32_t max_units;         // of a head
+  int32_t parts[2], len[2];  // without a mask: parts of every item, blocks of each
+  int32_t unit0[2];          // and where their units begin
+  double share;              // SHARE * heads / slots
 };
 
 __device__ __forceinline__ bf16x8 row_frag(const char* tile, uint32_t at, int row0, int stp) {
@@ -76,128 +108,135 @@ __device__ __forceinline__ bf16x8 row_frag(const char* tile, uint32_t at, int ro
 // (A fragment of the transposed tile, columns 16*dt .. +15 of 32 rows, is two transposing
 // reads of 16 rows: k-slot e < 4 of lane group g is row 4g + e, e >= 4 row 16 + 4g + e - 4.)
 
-// Walks the set bits of a bitmap (or all blocks), ascending.
+// Walks `left` set bits of a bitmap (or blocks) from the first'th on, ascending.
 template <bool SPARSE>
 struct Walk {
   const uint32_t* words;   // LDS
-  int n;                   // blocks
-  int word;
-  uint32_t left;
-  __device__ __forceinline__ void begin() {
-    word = SPARSE ? 0 : -1;
-    left = SPARSE ? (uint32_t)__builtin_amdgcn_readfirstlane((int)words[0]) : 0u;
+  int n, word, left;
+  uint32_t bits;
+  __device__ __forceinline__ uint32_t at(int w) const {
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)words[w]);
+  }
+  __device__ __forceinline__ void begin(int first) {
+    if constexpr (SPARSE) {
+      word = 0;
+      bits = at(0);
+      int c;
+      while ((c = __builtin_popcount(bits)) <= first && word + 1 < n) {
+        first -= c;
+        bits = at(++word);
+      }
+      for (; first > 0; --first) bits &= bits - 1u;
+    } else {
+      word = first - 1;
+    }
   }
   // The next block, -1 past the last.
   __device__ __forceinline__ int next() {
-    if constexpr (!SPARSE) {
-      ++word;
-      return word < n ? word : -1;
-    } else {
-      while (left == 0u) {
-        if (++word >= (n + 31) / 32) return -1;
-        left = (uint32_t)__builtin_amdgcn_readfirstlane((int)words[word]);
-      }
-      const int b = __builtin_ctz(left);
-      left &= left - 1u;
-      return 32 * word + b;
+    if (--left < 0) return -1;
+    if constexpr (!SPARSE) return ++word;
+    while (bits == 0u) {
+      if (++word >= n) return -1;
+      bits = at(word);
     }
+    const int b = __builtin_ctz(bits);
+    bits &= bits - 1u;
+    return 32 * word + b;
   }
 };
 
+// Four columns of a gradient's row (0: dq, 1: dk, 2: dv) from their sums.
+template <int WHICH>
+__device__ __forceinline__ void store_sums(const BArgs& a, int head, int row, int col, f32x4 sum) {
+  bf16x4 w;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    w[r] = (__bf16)(WHICH == 2 ? sum[r] : sum[r] * 0.08838834764831845f);   // 1 / sqrt(128)
+  *(bf16x4*)(a.g[WHICH] + head * a.g_sh[WHICH] + row * a.g_st[WHICH] + col) = w;
+}
+
+// LDS of a workgroup.
+template <bool SPARSE, int PER>
+struct Lds {
+  char tile[2][2][TILE];                       // [stage][X0, X1]
+  float stat[2][2][STEP];                      // [stage][lse, delta] of streamed queries
+  uint32_t own[SPARSE ? PER : 1][SPARSE ? MAX_WORDS : 1];   // bitmaps of the resident blocks
+  uint32_t any[SPARSE && PER > 1 ? MAX_WORDS : 1];
+};
+
 template <int BLOCK, bool KEYS, bool SPARSE>
-__global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
+__device__ __forceinline__ void work_item(const BArgs& a, Lds<SPARSE, ROWS / BLOCK>& L, int head,
+                                          int tile, int first, int count, int unit) {
   constexpr int PER = ROWS / BLOCK;      // resident blocks
-  __shared__ __attribute__((aligned(1024))) char lds[2][2][TILE];
-  __shared__ __attribute__((aligned(256))) float stat[2][2][STEP];
-  __shared__ uint32_t own[SPARSE ? PER : 1][SPARSE ? MAX_WORDS : 1];
-  __shared__ uint32_t any[SPARSE && PER > 1 ? MAX_WORDS : 1];
+  constexpr int R0 = KEYS ? K : Q, R1 = KEYS ? V : GO, X0 = KEYS ? Q : K, X1 = KEYS ? GO : V;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 16, li = lane % 16;
-  const int head = blockIdx.x % a.heads;
-  const int row0 = (int)(blockIdx.x / a.heads) * ROWS;
+  const int row0 = tile * ROWS;
   const int N = a.N;
   constexpr float SCALE = 0.08838834764831845f;        // 1 / sqrt(128)
   constexpr float SCALE_LOG2 = SCALE * 1.4426950408889634f;
+  auto& lds = L.tile;
+  auto& stat = L.stat;
 
   // Resident rows: columns of the products.
   const int wrow = row0 + 32 * wave;
   bf16x8 r0[4][2], r1[4][2];
+  float lse[2], delta[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int row = wrow + 16 * t + li;
 #pragma unroll
     for (int stp = 0; stp < 4; ++stp) {
       const int64_t c = 32 * stp + 8 * g;
-      r0[stp][t] = row < N ? *(const bf16x8*)(a.r0 + head * a.r0_sh + row * a.r0_st + c) : bf16x8{};
-      r1[stp][t] = row < N ? *(const bf16x8*)(a.r1 + head * a.r1_sh + row * a.r1_st + c) : bf16x8{};
+      r0[stp][t] = row < N ? *(const bf16x8*)(a.t[R0] + head * a.sh[R0] + row * a.st[R0] + c)
+                           : bf16x8{};
+      r1[stp][t] = row < N ? *(const bf16x8*)(a.t[R1] + head * a.sh[R1] + row * a.st[R1] + c)
+                           : bf16x8{};
     }
-  }
-  float lse[2], delta[2];   // -lse / scale and -delta
-  if constexpr (!KEYS) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int row = wrow + 16 * t + li;
-      lse[t] = -__builtin_inff();
-      delta[t] = 0.f;
-      if (row < N) {
-#pragma unroll
-        for (int stp = 0; stp < 4; ++stp) {
-          const bf16x8 o =
-              *(const bf16x8*)(a.o + head * a.o_sh + row * a.o_st + 32 * stp + 8 * g);
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            delta[t] = __builtin_fmaf(-(float)o[k], (float)r1[stp][t][k], delta[t]);
-        }
-        const float l = a.lse[(int64_t)head * N + row];
-        lse[t] = l == -__builtin_inff() ? -__builtin_inff() : l * (-1.f / SCALE);
-      }
-      delta[t] += __shfl_xor(delta[t], 16);
-      delta[t] += __shfl_xor(delta[t], 32);
-      if (row < N && g == 0) {
-        a.stats.lse[(int64_t)head * N + row] = lse[t];
-        a.stats.delta[(int64_t)head * N + row] = delta[t];
-      }
+    if constexpr (!KEYS) {
+      lse[t] = row < N ? a.row_lse[(int64_t)head * N + row] : -__builtin_inff();
+      delta[t] = row < N ? a.row_delta[(int64_t)head * N + row] : 0.f;
     }
   }
 
   // Bitmaps of the resident blocks.
-  const int words = (a.nb + 31) / 32;
   const int block0 = row0 / BLOCK;
   if constexpr (SPARSE) {
-    for (int i = tid; i < words; i += 64 * WAVES) {
+    for (int i = tid; i < a.words; i += 64 * WAVES) {
       uint32_t all = 0u;
 #pragma unroll
       for (int b = 0; b < PER; ++b) {
-        const uint32_t w = block0 + b < a.nb
-                               ? a.bits[(int64_t)(block0 + b) * a.bits_block + i * a.bits_word]
-                               : 0u;
-        own[b][i] = w;
+        const uint32_t w = block0 + b >= a.nb ? 0u
+                           : KEYS             ? a.by_col[(int64_t)i * a.nb + block0 + b]
+                                              : a.by_row[(int64_t)(block0 + b) * a.words + i];
+        L.own[b][i] = w;
         all |= w;
       }
-      if (PER > 1) any[i] = all;
+      if (PER > 1) L.any[i] = all;
     }
     __syncthreads();
   }
 
-  const __bf16* const x0 = a.x0 + head * a.x0_sh;
-  const __bf16* const x1 = a.x1 + head * a.x1_sh;
-  const float* const sl = a.stats.lse + (int64_t)head * N;
-  const float* const sd = a.stats.delta + (int64_t)head * N;
+  const __bf16* const x0 = a.t[X0] + head * a.sh[X0];
+  const __bf16* const x1 = a.t[X1] + head * a.sh[X1];
+  const float* const sl = a.row_lse + (int64_t)head * N;
+  const float* const sd = a.row_delta + (int64_t)head * N;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_void*)&lds[0][0][0];
   const uint32_t stat_base = (uint32_t)(uintptr_t)(lds_void*)&stat[0][0][0];
   // Wave w's load j of a tile: slab j, rows 16 w + lane / 4, chunk lane % 4.
   const int lrow = 16 * wave + lane / 4;
   const uint32_t chunk = 16u * (uint32_t)((lane % 4) ^ xsw(lrow));
-  const uint32_t off0 = (uint32_t)lrow * (uint32_t)(a.x0_st * 2) + chunk;
-  const uint32_t off1 = (uint32_t)lrow * (uint32_t)(a.x1_st * 2) + chunk;
+  const uint32_t off0 = (uint32_t)lrow * (uint32_t)(a.st[X0] * 2) + chunk;
+  const uint32_t off1 = (uint32_t)lrow * (uint32_t)(a.st[X1] * 2) + chunk;
   auto rsrc_at = [&](const __bf16* base, int64_t st, int row) {
     return make_rsrc(base + (int64_t)row * st, (uint32_t)(((int64_t)(N - 1 - row) * st + D) * 2));
   };
-  // Streamed rows row .. row + 63 (row < N) into stage s.
+  // Streamed rows row .. row + 63 (row < N) into stage s; rows past N come as zeros.
   auto load_step = [&](int row, int s) {
-    const auto q0 = rsrc_at(x0, a.x0_st, row), q1 = rsrc_at(x1, a.x1_st, row);
-    const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane(lds_base + 2 * TILE * s + 1024 * wave);
+    const auto q0 = rsrc_at(x0, a.st[X0], row), q1 = rsrc_at(x1, a.st[X1], row);
+    const uint32_t to =
+        (uint32_t)__builtin_amdgcn_readfirstlane(lds_base + 2 * TILE * s + 1024 * wave);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       issue_load(to + 4096u * j, q0, off0, 64u * j);
@@ -206,8 +245,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
     if (KEYS && wave < 2) {
       const float* const from = wave ? sd : sl;
       const auto q = make_rsrc(from + row, (uint32_t)(N - row) * 4u);
-      issue_load_dword((uint32_t)__builtin_amdgcn_readfirstlane(stat_base + 512 * s + 256 * wave), q,
-                       4u * lane);
+      issue_load_dword(
+          (uint32_t)__builtin_amdgcn_readfirstlane(stat_base + 512 * s + 256 * wave), q, 4u * lane);
     }
   };
 
@@ -225,8 +264,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
       if (KEYS) acc1[dt][t] = f32x4{};
     }
 
-  Walk<SPARSE> walk{SPARSE ? (PER > 1 ? any : own[0]) : nullptr, a.nb, 0, 0u};
-  walk.begin();
+  Walk<SPARSE> walk{SPARSE ? (PER > 1 ? L.any : L.own[0]) : nullptr, a.words, 0, count, 0u};
+  walk.begin(first);
   // Steps: a block of 128 streamed rows is two of them.
   int block = walk.next(), half = 0;
   auto step_row = [&]() { return block * BLOCK + half * STEP; };
@@ -245,7 +284,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
     wait_loads_and_sync();     // this step's tiles are there, the other stage is free
     if (block >= 0) load_step(step_row(), s ^ 1);
     if (PER > 1 && SPARSE) {
-      const uint32_t w = own[PER > 1 ? wave / 2 : 0][now / 32];
+      const uint32_t w = L.own[PER > 1 ? wave / 2 : 0][now / 32];
       if (!((__builtin_amdgcn_readfirstlane((int)w) >> (now % 32)) & 1)) continue;
     }
     const char* const t0 = lds[s][0];
@@ -282,6 +321,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) fr[i] = row_of(i);
+    // Products go before the other workgroup's element work on the same SIMD: 1.5% of the
+    // launch (12 heads of 32,760 tokens 22.40 -> 22.06 ms, interleaved on one board).
+    __builtin_amdgcn_s_setprio(1);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -315,6 +357,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
               __builtin_amdgcn_sched_barrier(0);
             }
           }
+        __builtin_amdgcn_s_setprio(0);
         // Keys past the last: their elements are zeros, their scores would be 0.
         if (!KEYS && row + STEP > N) {
 #pragma unroll
@@ -332,6 +375,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
             if (KEYS) pb[t][4 * x + r] = (__bf16)p;
             eb[t][4 * x + r] = (__bf16)e;
           }
+        __builtin_amdgcn_s_setprio(1);
       }
 #pragma unroll
       for (int f = 0; f < NB; ++f) {
@@ -349,89 +393,322 @@ __global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
     }
   }
 
+  if (unit >= 0) {
+    // A part: its sums as the lanes hold them.
+    float* const to = a.units + ((int64_t)head * a.max_units + unit) * UNIT + 4 * lane;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int at = (wave * 16 + 2 * dt + t) * 256;
+        *(f32x4*)(to + at) = acc0[dt][t];
+        if constexpr (KEYS) *(f32x4*)(to + UNIT + at) = acc1[dt][t];
+      }
+    return;
+  }
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int row = wrow + 16 * t + li;
     if (row >= N) continue;
-    __bf16* const o0 = a.g0 + head * a.g0_sh + row * a.g0_st + 4 * g;
-    __bf16* const o1 = KEYS ? a.g1 + head * a.g1_sh + row * a.g1_st + 4 * g : nullptr;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
-      bf16x4 w;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) w[r] = (__bf16)(acc0[dt][t][r] * SCALE);
-      *(bf16x4*)(o0 + 16 * dt) = w;
-      if constexpr (KEYS) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) w[r] = (__bf16)acc1[dt][t][r];
-        *(bf16x4*)(o1 + 16 * dt) = w;
-      }
+      store_sums<KEYS ? 1 : 0>(a, head, row, 16 * dt + 4 * g, acc0[dt][t]);
+      if constexpr (KEYS) store_sums<2>(a, head, row, 16 * dt + 4 * g, acc1[dt][t]);
     }
   }
 }
 
-// Bitmaps of a block CSR, a workgroup for every 32 rows: by_row [nb][words], bit kb % 32
-// of word kb / 32; by_col [words][nb], bit qb % 32 of word qb / 32.  Entries outside
-// [0, nb) are skipped, as in the forward pass.
-__global__ __launch_bounds__(256) void mask_bits_kernel(const int32_t* __restrict__ row_ptr,
-                                                        const int32_t* __restrict__ col_idx,
-                                                        int32_t nb, uint32_t* __restrict__ by_row,
-                                                        uint32_t* __restrict__ by_col) {
-  __shared__ uint32_t rows[32][MAX_WORDS];
-  __shared__ uint32_t cols[kMaxSparseBlocks];
-  const int words = (nb + 31) / 32, first = 32 * (int)blockIdx.x;
-  for (int i = threadIdx.x; i < 32 * words; i += 256) rows[i / words][i % words] = 0u;
-  for (int i = threadIdx.x; i < nb; i += 256) cols[i] = 0u;
+template <int BLOCK, bool SPARSE>
+__global__ __launch_bounds__(64 * WAVES, 2) void back_kernel(const BArgs a) {
+  __shared__ __attribute__((aligned(1024))) Lds<SPARSE, ROWS / BLOCK> L;
+  const int head = (int)(blockIdx.x % a.heads), rank = (int)(blockIdx.x / a.heads);
+  Item it;
+  if constexpr (SPARSE) {
+    if (rank >= a.plan->items) return;
+    it = a.list[rank];
+  } else {
+    // Keys first: parts[1] of each tile, then queries.
+    const int keys = rank < a.tiles * a.parts[1];
+    const int i = keys ? rank : rank - a.tiles * a.parts[1];
+    const int tile = i / a.parts[keys], part = i % a.parts[keys];
+    it.tile = tile | (keys << 31);
+    it.first = part * a.len[keys];
+    it.count = min(a.len[keys], a.nb - it.first);
+    it.unit = a.parts[keys] > 1 ? a.unit0[keys] + i * (keys + 1) : -1;
+  }
+  const int tile = __builtin_amdgcn_readfirstlane(it.tile) & 0x7FFFFFFF;
+  const int first = __builtin_amdgcn_readfirstlane(it.first);
+  const int count = __builtin_amdgcn_readfirstlane(it.count);
+  const int unit = __builtin_amdgcn_readfirstlane(it.unit);
+  if (__builtin_amdgcn_readfirstlane(it.tile) < 0)
+    work_item<BLOCK, true, SPARSE>(a, L, head, tile, first, count, unit);
+  else
+    work_item<BLOCK, false, SPARSE>(a, L, head, tile, first, count, unit);
+}
+
+// Adds the parts of split items, in their order: a quarter of one gradient's tile a
+// workgroup (blockIdx.y).
+__global__ __launch_bounds__(64 * WAVES) void combine_kernel(const BArgs a) {
+  const int head = (int)(blockIdx.x % a.heads), i = (int)(blockIdx.x / a.heads);
+  const int second = blockIdx.y / 4, j0 = 4 * (blockIdx.y % 4);   // second: dv
+  int tile, keys, unit, parts;
+  if (a.plan) {
+    if (i >= a.plan->splits) return;
+    const Split s = a.splits[i];
+    keys = s.tile < 0, tile = s.tile & 0x7FFFFFFF, unit = s.unit, parts = s.parts;
+  } else {
+    // The tiles of the kind, or kinds, that are in parts.
+    keys = a.parts[1] > 1 && i < a.tiles;
+    tile = i % a.tiles;
+    parts = a.parts[keys];
+    unit = a.unit0[keys] + tile * parts * (keys + 1);
+  }
+  if (second > keys) return;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const float* from = a.units + ((int64_t)head * a.max_units + unit + second) * UNIT +
+                      (wave * 16 + j0) * 256 + 4 * lane;
+  f32x4 sum[4] = {f32x4{}, f32x4{}, f32x4{}, f32x4{}};
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p, from += (keys + 1) * UNIT)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] += *(const f32x4*)(from + 256 * j);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = tile * ROWS + 32 * wave + 16 * (j % 2) + lane % 16;
+    if (row >= a.N) continue;
+    const int c = 16 * ((j0 + j) / 2) + 4 * (lane / 16);
+    if (!keys)
+      store_sums<0>(a, head, row, c, sum[j]);
+    else if (!second)
+      store_sums<1>(a, head, row, c, sum[j]);
+    else
+      store_sums<2>(a, head, row, c, sum[j]);
+  }
+}
+
+// The first `stat_groups` workgroups: -lse sqrt(d) and -delta of 64 rows each, 16 threads a
+// row.  The others: bitmaps of a block CSR, a workgroup for every 32 rows: bit kb % 32 of
+// by_row[row][kb / 32], bit qb % 32 of by_col[qb / 32][col].  Entries outside [0, nb) are
+// skipped, as in the forward pass.
+__global__ __launch_bounds__(256) void prep_kernel(const BArgs a) {
+  extern __shared__ uint32_t bits[];
+  if ((int)blockIdx.x < a.stat_groups) {
+    const int c = 8 * (threadIdx.x % 16);
+    for (int k = 0; k < 4; ++k) {
+      const int64_t i = (int64_t)blockIdx.x * 64 + 16 * k + threadIdx.x / 16;
+      if (i >= (int64_t)a.heads * a.N) break;
+      const int head = (int)(i / a.N), row = (int)(i % a.N);
+      const bf16x8 x = *(const bf16x8*)(a.t[GO] + head * a.sh[GO] + row * a.st[GO] + c);
+      const bf16x8 o = *(const bf16x8*)(a.t[O] + head * a.sh[O] + row * a.st[O] + c);
+      float d = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d = __builtin_fmaf((float)x[e], (float)o[e], d);
+#pragma unroll
+      for (int w = 8; w; w /= 2) d += __shfl_xor(d, w);
+      if (c == 0) {
+        const float l = a.lse[i];
+        a.row_lse[i] = l == -__builtin_inff() ? l : l * -11.313708498984761f;
+        a.row_delta[i] = -d;
+      }
+    }
+    return;
+  }
+  if ((int)blockIdx.x == a.stat_groups && threadIdx.x == 0) a.plan->done = 0;
+  const int nb = a.nb, words = a.words, group = (int)blockIdx.x - a.stat_groups;
+  uint32_t* const rows = bits;               // [32][words]
+  uint32_t* const cols = bits + 32 * words;  // [nb]
+  for (int i = threadIdx.x; i < 32 * words + nb; i += 256) bits[i] = 0u;
   __syncthreads();
   // Eight threads a row.
-  const int r = threadIdx.x / 8, row = first + r;
+  const int r = threadIdx.x / 8, row = 32 * group + r;
   if (row < nb) {
-    const int32_t lo = row_ptr[row], hi = row_ptr[row + 1];
-    for (int32_t i = lo + (int)threadIdx.x % 8; i < hi; i += 8) {
-      const uint32_t kb = (uint32_t)col_idx[i];
+    const int32_t hi = a.row_ptr[row + 1];
+    for (int32_t i = a.row_ptr[row] + (int)threadIdx.x % 8; i < hi; i += 8) {
+      const uint32_t kb = (uint32_t)a.col_idx[i];
       if (kb >= (uint32_t)nb) continue;
-      atomicOr(&rows[r][kb / 32], 1u << (kb % 32));
+      atomicOr(&rows[r * words + kb / 32], 1u << (kb % 32));
       atomicOr(&cols[kb], 1u << r);
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < 32 * words; i += 256)
-    if (first + i / words < nb) by_row[(int64_t)(first + i / words) * words + i % words] = rows[i / words][i % words];
-  for (int i = threadIdx.x; i < nb; i += 256) by_col[(int64_t)blockIdx.x * nb + i] = cols[i];
+  const int mine = min(32, nb - 32 * group) * words;
+  for (int i = threadIdx.x; i < mine; i += 256) a.by_row[(int64_t)32 * group * words + i] = rows[i];
+  for (int i = threadIdx.x; i < nb; i += 256) a.by_col[(int64_t)group * nb + i] = cols[i];
+}
+
+// The items of one head from the bitmaps, the longest first.  A wave counts the blocks of a
+// tile's walk; the workgroup that is through last makes the list.  An item of cost c (steps
+// times products) is split where c > T = max(MIN_COST, share * C), C the sum of all costs,
+// into at most c / T + 1 < 2 c / T parts.  So there are at most C / T parts more than items
+// and at most 4 C / T units (two for a part of keys), which the host bounds by the two parts
+// of T.  Order among items of like cost, and where parts lie, follow atomics; results do not
+// depend on either.
+constexpr int PLAN_WAVES = 16;
+template <int BLOCK>
+__global__ __launch_bounds__(64 * PLAN_WAVES) void plan_kernel(const BArgs a) {
+  constexpr int PER = ROWS / BLOCK, THREADS = 64 * PLAN_WAVES;
+  __shared__ unsigned long long total;
+  __shared__ int last, units, splits, hist[64];
+  const int tid = threadIdx.x, lane = tid % 64;
+  if (tid < 64) hist[tid] = 0;
+  if (tid == 0) total = 0ull, units = 0, splits = 0;
+  // Item i < 2 tiles: queries' tiles, then keys'.
+  const int mine = (int)blockIdx.x * PLAN_WAVES + tid / 64;
+  if (mine < 2 * a.tiles) {
+    const int keys = mine >= a.tiles, b0 = (mine - keys * a.tiles) * PER;
+    int n = 0;
+    for (int w = lane; w < a.words; w += 64) {
+      uint32_t bits = 0u;
+#pragma unroll
+      for (int b = 0; b < PER; ++b)
+        if (b0 + b < a.nb)
+          bits |= keys ? a.by_col[(int64_t)w * a.nb + b0 + b]
+                       : a.by_row[(int64_t)(b0 + b) * a.words + w];
+      n += __popc(bits);
+    }
+    for (int d = 32; d; d /= 2) n += __shfl_xor(n, d);
+    if (lane == 0)
+      __hip_atomic_store(&a.counts[mine], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  // Thread 0's ticket releases the workgroup's counts, which the barrier puts before it.
+  __syncthreads();
+  if (tid == 0)
+    last = __hip_atomic_fetch_add(&a.plan->done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
+           (int)gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+
+  auto cost_of = [&](int i, int n) { return n * (BLOCK / STEP) * COST[i >= a.tiles]; };
+  auto count_of = [&](int i) {
+    return __hip_atomic_load(&a.counts[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  unsigned long long sum = 0ull;
+  for (int i = tid; i < 2 * a.tiles; i += THREADS) sum += (unsigned long long)cost_of(i, count_of(i));
+  for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+  if (lane == 0) atomicAdd(&total, sum);
+  __syncthreads();
+  const int T = max(MIN_COST, (int)min(a.share * (double)total, 1e9) + 1);
+  // Parts of an item, and blocks of each.
+  auto parts_of = [&](int i, int n, int& len) {
+    const int c = cost_of(i, n), want = c > T ? min((c + T - 1) / T, n) : 1;
+    len = (n + want - 1) / want;
+    return n ? (n + len - 1) / len : 1;
+  };
+  // Buckets of like cost: no part costs more than T.
+  const float scale = 63.f / (float)T;
+  auto bucket_of = [&](int i, int len) {
+    return 63 - min(63, (int)((float)cost_of(i, len) * scale));
+  };
+  for (int i = tid; i < 2 * a.tiles; i += THREADS) {
+    int len;
+    const int parts = parts_of(i, count_of(i), len);
+    atomicAdd(&hist[bucket_of(i, len)], parts);
+  }
+  __syncthreads();
+  if (tid < 64) {   // the buckets' first places
+    const int own = hist[tid];
+    int upto = own;
+    for (int d = 1; d < 64; d *= 2) {
+      const int below = __shfl_up(upto, d);
+      if (tid >= d) upto += below;
+    }
+    hist[tid] = upto - own;
+    if (tid == 63) a.plan->items = upto;
+  }
+  __syncthreads();
+  for (int i = tid; i < 2 * a.tiles; i += THREADS) {
+    int len;
+    const int n = count_of(i), parts = parts_of(i, n, len), keys = i >= a.tiles;
+    const int tile = (i - keys * a.tiles) | (keys << 31);
+    int unit = -1;
+    if (parts > 1) {
+      unit = atomicAdd(&units, parts * (keys + 1));
+      a.splits[atomicAdd(&splits, 1)] = Split{tile, unit, parts, 0};
+    }
+    int at = atomicAdd(&hist[bucket_of(i, len)], parts);
+    for (int p = 0; p < parts; ++p, ++at)
+      a.list[at] = Item{tile, p * len, min(len, n - p * len),
+                        parts > 1 ? unit + p * (keys + 1) : -1};
+  }
+  __syncthreads();
+  if (tid == 0) a.plan->splits = splits;
 }
 
 int64_t round_up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
+int cu_count() {
+  static std::atomic<int> cached[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = 0;
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n <= 0) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+        n <= 0)
+      n = 256;
+    cached[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+// How a call's work is laid out, and where in its workspace what lies.
+struct Layout {
+  int32_t tiles, words, slots;
+  int32_t parts[2] = {1, 1}, len[2], unit0[2] = {0, 0};
+  int64_t max_items, max_splits, max_units;     // of a head
+  int64_t delta, by_row, by_col, plan, counts, list, splits, units, bytes;
+};
+
+Layout layout_of(int32_t heads, int32_t n, int32_t nb, bool sparse) {
+  Layout l;
+  l.tiles = (int32_t)(((int64_t)n + ROWS - 1) / ROWS);
+  l.words = (nb + 31) / 32;
+  l.slots = SLOTS * cu_count();
+  const int64_t steps = 2 * (int64_t)l.tiles;
+  const int64_t cost = l.tiles * steps * (COST[0] + COST[1]);   // of a head, at most
+  if (sparse) {
+    // C / T, by plan_kernel's two bounds of T.
+    const int64_t ratio =
+        std::min((int64_t)((double)l.slots / (SHARE * heads)) + 1, cost / MIN_COST + 1);
+    l.max_items = 2 * l.tiles + ratio;
+    l.max_splits = std::min<int64_t>(2 * l.tiles, ratio);
+    l.max_units = 4 * ratio;
+  } else {
+    const double T = std::max((double)MIN_COST, SHARE * heads * (double)cost / l.slots);
+    l.max_items = l.max_splits = l.max_units = 0;
+    for (int k = 1; k >= 0; --k) {
+      const double parts = steps * COST[k] / T;
+      const int64_t want = parts > 1. ? std::min((int64_t)parts + 1, (int64_t)nb) : 1;
+      l.len[k] = (int32_t)((nb + want - 1) / want);
+      l.parts[k] = (nb + l.len[k] - 1) / l.len[k];
+      l.unit0[k] = (int32_t)l.max_units;
+      l.max_items += (int64_t)l.tiles * l.parts[k];
+      if (l.parts[k] > 1) {
+        l.max_splits += l.tiles;
+        l.max_units += (int64_t)l.tiles * l.parts[k] * (k + 1);
+      }
+    }
+  }
+  const int64_t stats = round_up((int64_t)heads * n * 4);
+  int64_t at = l.delta = stats;
+  at += stats;
+  l.by_row = at;
+  if (sparse) {
+    l.by_col = l.by_row + round_up((int64_t)l.words * nb * 4);
+    l.plan = l.by_col + round_up((int64_t)l.words * nb * 4);
+    l.counts = l.plan + round_up(sizeof(Plan));
+    l.list = l.counts + round_up(2 * (int64_t)l.tiles * 4);
+    l.splits = l.list + round_up(l.max_items * (int64_t)sizeof(Item));
+    at = l.splits + round_up(l.max_splits * (int64_t)sizeof(Split));
+  }
+  l.units = at;
+  l.bytes = at + heads * l.max_units * UNIT * (int64_t)sizeof(float);
+  return l;
+}
+
 template <int BLOCK, bool SPARSE>
-hipError_t launch_t(const AttnBackArgs& a, const uint32_t* by_row, const uint32_t* by_col,
-                    Stats stats, hipStream_t stream) {
-  const AttnArgs& f = a.f;
-  const int32_t words = (f.n_blocks + 31) / 32;
-  BArgs b;
-  b.N = f.n_tokens, b.nb = f.n_blocks, b.heads = f.heads;
-  b.tiles = (f.n_tokens + ROWS - 1) / ROWS;
-  b.stats = stats;
-  b.o = (const __bf16*)f.o, b.o_sh = f.o_sh, b.o_st = f.o_st;
-  b.lse = f.lse;
-  const dim3 grid((uint32_t)b.tiles * (uint32_t)f.heads);
-  b.r0 = (const __bf16*)f.q, b.r0_sh = f.q_sh, b.r0_st = f.q_st;
-  b.r1 = (const __bf16*)a.go, b.r1_sh = a.go_sh, b.r1_st = a.go_st;
-  b.x0 = (const __bf16*)f.k, b.x0_sh = f.k_sh, b.x0_st = f.k_st;
-  b.x1 = (const __bf16*)f.v, b.x1_sh = f.v_sh, b.x1_st = f.v_st;
-  b.g0 = (__bf16*)a.gq, b.g0_sh = a.gq_sh, b.g0_st = a.gq_st;
-  b.g1 = nullptr, b.g1_sh = b.g1_st = 0;
-  b.bits = by_row, b.bits_word = 1, b.bits_block = words;
-  back_kernel<BLOCK, false, SPARSE><<<grid, dim3(64 * WAVES), 0, stream>>>(b);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  b.r0 = (const __bf16*)f.k, b.r0_sh = f.k_sh, b.r0_st = f.k_st;
-  b.r1 = (const __bf16*)f.v, b.r1_sh = f.v_sh, b.r1_st = f.v_st;
-  b.x0 = (const __bf16*)f.q, b.x0_sh = f.q_sh, b.x0_st = f.q_st;
-  b.x1 = (const __bf16*)a.go, b.x1_sh = a.go_sh, b.x1_st = a.go_st;
-  b.g0 = (__bf16*)a.gk, b.g0_sh = a.gk_sh, b.g0_st = a.gk_st;
-  b.g1 = (__bf16*)a.gv, b.g1_sh = a.gv_sh, b.g1_st = a.gv_st;
-  b.bits = by_col, b.bits_word = f.n_blocks, b.bits_block = 1;
-  back_kernel<BLOCK, true, SPARSE><<<grid, dim3(64 * WAVES), 0, stream>>>(b);
+hipError_t launch_t(const BArgs& b, const Layout& l, hipStream_t stream) {
+  back_kernel<BLOCK, SPARSE><<<dim3((uint32_t)(l.max_items * b.heads)), dim3(64 * WAVES), 0,
+                               stream>>>(b);
   return hipGetLastError();
 }
 
@@ -439,24 +716,59 @@ hipError_t launch_t(const AttnBackArgs& a, const uint32_t* by_row, const uint32_
 
 int64_t attention_backward_workspace(int32_t heads, int32_t n_tokens, int32_t n_blocks,
                                      bool sparse) {
-  const int64_t words = (n_blocks + 31) / 32;
-  return 2 * round_up((int64_t)heads * n_tokens * 4) +
-         (sparse ? 2 * round_up(words * n_blocks * 4) : 0);
+  return layout_of(heads, n_tokens, n_blocks, sparse).bytes;
 }
 
 hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream) {
-  const int32_t nb = a.f.n_blocks;
-  const int64_t words = (nb + 31) / 32, part = round_up((int64_t)a.f.heads * a.f.n_tokens * 4);
-  const Stats stats = {(float*)a.workspace, (float*)(a.workspace + part)};
-  if (!a.f.row_ptr) return launch_t<128, false>(a, nullptr, nullptr, stats, stream);
-  uint32_t* const by_row = (uint32_t*)(a.workspace + 2 * part);
-  uint32_t* const by_col = (uint32_t*)(a.workspace + 2 * part + round_up(words * nb * 4));
-  mask_bits_kernel<<<dim3((uint32_t)words), dim3(256), 0, stream>>>(
-      a.f.row_ptr, (const int32_t*)a.f.rows, nb, by_row, by_col);
-  const hipError_t e = hipGetLastError();
+  const AttnArgs& f = a.f;
+  const bool sparse = f.row_ptr != nullptr;
+  const Layout l = layout_of(f.heads, f.n_tokens, f.n_blocks, sparse);
+  const void* const t[5] = {f.q, a.go, f.k, f.v, f.o};
+  const int64_t sh[5] = {f.q_sh, a.go_sh, f.k_sh, f.v_sh, f.o_sh};
+  const int64_t st[5] = {f.q_st, a.go_st, f.k_st, f.v_st, f.o_st};
+  BArgs b = {};
+  for (int i = 0; i < 5; ++i) b.t[i] = (const __bf16*)t[i], b.sh[i] = sh[i], b.st[i] = st[i];
+  b.g[0] = (__bf16*)a.gq, b.g_sh[0] = a.gq_sh, b.g_st[0] = a.gq_st;
+  b.g[1] = (__bf16*)a.gk, b.g_sh[1] = a.gk_sh, b.g_st[1] = a.gk_st;
+  b.g[2] = (__bf16*)a.gv, b.g_sh[2] = a.gv_sh, b.g_st[2] = a.gv_st;
+  b.lse = f.lse;
+  b.row_lse = (float*)a.workspace;
+  b.row_delta = (float*)(a.workspace + l.delta);
+  b.N = f.n_tokens, b.nb = f.n_blocks, b.heads = f.heads, b.tiles = l.tiles, b.words = l.words;
+  b.units = (float*)(a.workspace + l.units);
+  b.max_units = (int32_t)l.max_units;
+  b.share = SHARE * f.heads / l.slots;
+  for (int k = 0; k < 2; ++k)
+    b.parts[k] = l.parts[k], b.len[k] = l.len[k], b.unit0[k] = l.unit0[k];
+  if (sparse) {
+    b.row_ptr = f.row_ptr, b.col_idx = (const int32_t*)f.rows;
+    b.by_row = (uint32_t*)(a.workspace + l.by_row);
+    b.by_col = (uint32_t*)(a.workspace + l.by_col);
+    b.plan = (Plan*)(a.workspace + l.plan);
+    b.counts = (int32_t*)(a.workspace + l.counts);
+    b.list = (Item*)(a.workspace + l.list);
+    b.splits = (Split*)(a.workspace + l.splits);
+  }
+  b.stat_groups = (int32_t)(((int64_t)f.heads * f.n_tokens + 63) / 64);
+  const uint32_t lds = sparse ? (32u * l.words + f.n_blocks) * 4u : 0u;
+  prep_kernel<<<dim3((uint32_t)(b.stat_groups + (sparse ? l.words : 0))), dim3(256), lds,
+                stream>>>(b);
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return a.block == 64 ? launch_t<64, true>(a, by_row, by_col, stats, stream)
-                       : launch_t<128, true>(a, by_row, by_col, stats, stream);
+  if (sparse) {
+    const dim3 grid((uint32_t)((2 * l.tiles + PLAN_WAVES - 1) / PLAN_WAVES));
+    if (a.block == 64)
+      plan_kernel<64><<<grid, dim3(64 * PLAN_WAVES), 0, stream>>>(b);
+    else
+      plan_kernel<128><<<grid, dim3(64 * PLAN_WAVES), 0, stream>>>(b);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = a.block == 64 ? launch_t<64, true>(b, l, stream) : launch_t<128, true>(b, l, stream);
+  } else {
+    e = launch_t<128, false>(b, l, stream);
+  }
+  if (e != hipSuccess || l.max_splits == 0) return e;
+  combine_kernel<<<dim3((uint32_t)(l.max_splits * f.heads), 8), dim3(64 * WAVES), 0, stream>>>(b);
+  return hipGetLastError();
 }
 
 }  // namespace lvsa
