@@ -7,6 +7,12 @@ import torch
 # half a step of each type, relative to the value
 HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
 
+# The 2-norm of what attention's results are off by, relative to them, for scores of a few
+# units: up to three roundings to bf16 that do not know of each other (of p or e, of the
+# output in delta, of the result), each uniform within 2^-8 of the value and so 2^-8 / sqrt(3)
+# in the mean, 2^-8 together; twice that.
+NORM = 2.0 ** -7
+
 
 def attention(q, k, v, grad, kept):
     """q, k, v, grad [H, N, d] in float64, kept [N, N] boolean.  A dict of out, lse, dq, dk,

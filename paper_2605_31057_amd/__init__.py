@@ -926,6 +926,7 @@ def attention_backward(grad, q, k, v, out, lse, mask=None, grads=None, stream=No
 # ------------------------------------------------- residual step between blocks
 
 _PARAMS = ("gate", "scale", "shift", "weight", "bias", "post_weight")
+_FRAMED = {"gate": "gate_stride", "scale": "scale_stride", "shift": "shift_stride"}
 
 
 class ResidualNorm:
@@ -939,55 +940,59 @@ class ResidualNorm:
                  frame_tokens=0):
         if not all(0 <= x < 2 ** 31 for x in (dim, norm, post, frame_tokens)):
             raise LvsaError(EINVAL, "ResidualNorm")
-        self.dim, self.norm, self.post = dim, norm, post
-        self.eps, self.residual, self.frame_tokens = eps, residual, frame_tokens
+        self.dim, self.norm, self.frame_tokens = dim, norm, frame_tokens
+        self._c = _ResidualNorm(dim, frame_tokens, norm, post, eps, residual)
 
 
 def _channels(t, dim, device):
-    """A tensor [.., dim] as rows on device number ``device``."""
+    """A tensor [.., dim] as rows on device number ``device``: address, rows, stride."""
     if t.get_device() != device:
         raise ValueError("expected a tensor on the current device")
-    if t.dim() != 2:
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2:
         try:
             t = t.view(-1, dim)
         except RuntimeError:
             raise ValueError("expected rows at one stride") from None
-    n, d = t.shape
+        shape, strides = t.shape, t.stride()
+    n, d = shape
     if d != dim:
         raise ValueError(f"expected rows of {dim} channels")
-    if d > 1 and t.stride(1) != 1:
+    if strides[1] != 1 and d > 1:
         raise ValueError("channels must be contiguous")
     if n >> 31:
         raise LvsaError(EUNSUPPORTED, f"{n} rows")
-    return _Rows(t.data_ptr(), n, t.stride(0) if n > 1 else dim)
+    return t.data_ptr(), n, strides[0] if n > 1 else dim
 
 
 def _norm_plan(plan, n, stream, block, params, device):
     """lvsa_residual_norm of a call on n rows of the given types."""
-    f = _FAST
-    codes = f.codes
-    if stream not in codes or block not in codes:
+    codes = _FAST.codes
+    first, second = codes.get(stream), codes.get(block)
+    if first is None or second is None:
         raise ValueError("expected bfloat16, float16 or float32")
-    c = _ResidualNorm(plan.dim, plan.frame_tokens, plan.norm, plan.post, plan.eps, plan.residual,
-                      codes[stream], codes[block], codes[block])
+    c = _ResidualNorm.from_buffer_copy(plan._c)
+    c.stream_type, c.block_type = first, second
     frame = plan.frame_tokens or n
-    kind = None
-    for name, t in params.items():
+    kind, dim = None, plan.dim
+    for name, t in zip(_PARAMS, params):
         if t is None:
             continue
-        if kind is None:
+        if t.dtype is not kind:
+            if kind is not None:
+                raise ValueError("expected parameters of one type")
             kind = t.dtype
-            if kind not in codes:
+            code = codes.get(kind)
+            if code is None:
                 raise ValueError("expected bfloat16, float16 or float32")
-            c.param_type = codes[kind]
-        elif t.dtype != kind:
-            raise ValueError("expected parameters of one type")
-        rows = _channels(t, plan.dim, device)
-        if rows.n != (-(-n // frame) if name in ("gate", "scale", "shift") else 1):
-            raise ValueError(f"{name} has {rows.n} rows, {n} tokens of {frame} a frame")
-        setattr(c, name, rows.data)
-        if name in ("gate", "scale", "shift"):
-            setattr(c, name + "_stride", rows.stride)
+            c.param_type = code
+        at, rows, stride = _channels(t, dim, device)
+        framed = name in _FRAMED
+        if rows != (-(-n // frame) if framed else 1):
+            raise ValueError(f"{name} has {rows} rows, {n} tokens of {frame} a frame")
+        setattr(c, name, at)
+        if framed:
+            setattr(c, _FRAMED[name], stride)
     return c
 
 
@@ -995,7 +1000,7 @@ def _norm_function(torch):
     class Step(torch.autograd.Function):
         @staticmethod
         def forward(ctx, plan, dtype, x, y, *params):
-            r, h = _launch_norm(plan, x, y, dict(zip(_PARAMS, params)), dtype, None, None)
+            r, h = _launch_norm(plan, x, y, params, dtype, None, None)
             ctx.plan = plan
             ctx.set_materialize_grads(False)
             ctx.block = (y if y is not None else h).dtype
@@ -1016,8 +1021,8 @@ def _norm_function(torch):
             names = ("x", "y", *_PARAMS)
             wanted = [k for k, need in zip(names, ctx.needs_input_grad[2:]) if need]
             found = _launch_norm_back(plan, *(g if g is None else _readable_rows(g, plan.dim)
-                                              for g in (grad_h, grad_r)), r, y,
-                                      dict(zip(_PARAMS, params)), wanted, None, None)
+                                              for g in (grad_h, grad_r)), r, y, params, wanted,
+                                      None, None)
             return None, None, *(found.get(k) for k in names)
 
     return Step
@@ -1035,20 +1040,34 @@ def _launch_norm(plan, x, y, params, dtype, r, h):
     f = _FAST
     dev = f.device()
     dim = plan.dim
-    tx = _channels(x, dim, dev)
-    block = y.dtype if y is not None else dtype or (x if h is None else h).dtype
+    at, n, stride = _channels(x, dim, dev)
+    kind = x.dtype
+    block = y.dtype if y is not None else dtype or (kind if h is None else h.dtype)
     if dtype is not None and dtype != block:
         raise ValueError("h is of y's type")
-    if y is not None and r is None:
-        r = f.empty(x.shape, dtype=x.dtype, device=x.device)
-    if plan.norm != NORM_NONE and h is None:
-        h = f.empty(x.shape, dtype=block, device=x.device)
-    for t, like, kind in ((y, x, block), (r, x, x.dtype), (h, x, block)):
-        if t is not None and (t.shape != like.shape or t.dtype != kind):
+    shape = x.shape
+    for t, of in ((y, block), (r, kind), (h, block)):
+        if t is not None and (t.shape != shape or t.dtype != of):
             raise ValueError("expected tensors of x's shape, r of x's type and h of y's")
-    c = _norm_plan(plan, tx.n, x.dtype, block, params, dev)
-    ty, tr, th = (None if t is None else _byref(_channels(t, dim, dev)) for t in (y, r, h))
-    _check(f.norm(_byref(c), _byref(tx), ty, tr, th, f.stream(dev)), "lvsa_residual_norm_forward")
+    c = _norm_plan(plan, n, kind, block, params, dev)
+    ty = tr = th = None
+    if y is not None:
+        ty = _byref(_Rows(*_channels(y, dim, dev)))
+        if r is None:
+            r = f.empty(shape, dtype=kind, device=x.device)
+            tr = _byref(_Rows(r.data_ptr(), n, dim))
+        else:
+            tr = _byref(_Rows(*_channels(r, dim, dev)))
+    elif r is not None:
+        raise ValueError("r is for calls with y")
+    if h is not None:
+        th = _byref(_Rows(*_channels(h, dim, dev)))
+    elif c.norm:
+        h = f.empty(shape, dtype=block, device=x.device)
+        th = _byref(_Rows(h.data_ptr(), n, dim))
+    status = f.norm(_byref(c), _byref(_Rows(at, n, stride)), ty, tr, th, f.stream(dev))
+    if status:
+        raise LvsaError(status, "lvsa_residual_norm_forward")
     return r, h
 
 
@@ -1066,12 +1085,14 @@ def residual_norm(plan, x, y=None, gate=None, scale=None, shift=None, weight=Non
                             post_weight, dtype, r, h)
     f = _fast()
     params = gate, scale, shift, weight, bias, post_weight
-    if f.grad_enabled() and _recording(x, y, *params, r, h):
-        if r is not None or h is not None:
-            raise ValueError("r and h are for calls outside a graph")
-        return f.norm_graph.apply(plan, dtype, x, y, *params)
-    given = [t for t in (r, h) if t is not None]
-    r, h = _launch_norm(plan, x, y, dict(zip(_PARAMS, params)), dtype, r, h)
+    given = [] if r is None and h is None else [t for t in (r, h) if t is not None]
+    if f.grad_enabled():
+        for t in (x, y, *params, *given):
+            if t is not None and t.requires_grad:
+                if given:
+                    raise ValueError("r and h are for calls outside a graph")
+                return f.norm_graph.apply(plan, dtype, x, y, *params)
+    r, h = _launch_norm(plan, x, y, params, dtype, r, h)
     if given:
         f.written(given)
     return h if y is None else r if h is None else (r, h)
@@ -1088,23 +1109,26 @@ def _launch_norm_back(plan, grad_h, grad_r, r, y, params, wanted, grad_x, grad_y
                     (grad_y, block)):
         if t is not None and (t.shape != some.shape or t.dtype != kind):
             raise ValueError("expected tensors of r's shape, gradients of their tensors' types")
-    n = _channels(some, dim, dev).n
+    rows = [None if t is None else _Rows(*_channels(t, dim, dev)) for t in (grad_h, grad_r, r, y)]
+    n = next(t.n for t in rows if t is not None)
     c = _norm_plan(plan, n, stream, block, params, dev)
     g, found = _NormGrads(), {}
     for name, kind, out in (("x", stream, grad_x), ("y", block, grad_y)):
         if name in wanted:
-            found[name] = f.empty(some.shape, dtype=kind, device=some.device) if out is None else out
-            setattr(g, name, _channels(found[name], dim, dev))
-    for name, t in params.items():
+            if out is None:
+                out = f.empty(some.shape, dtype=kind, device=some.device)
+            setattr(g, name, _Rows(*_channels(out, dim, dev)))
+            found[name] = out
+    for name, t in zip(_PARAMS, params):
         if name in wanted:
-            found[name] = f.empty(t.shape, dtype=t.dtype, device=t.device)
-            setattr(g, name, found[name].data_ptr())
+            found[name] = out = f.empty(t.shape, dtype=t.dtype, device=t.device)
+            setattr(g, name, out.data_ptr())
     need = _i64()
     _check(f.norm_workspace(_byref(c), n, _byref(g), _byref(need)), "lvsa_residual_norm_workspace")
     work = f.empty(need.value, dtype=f.torch.uint8, device=some.device) if need.value else None
-    rows = (None if t is None else _byref(_channels(t, dim, dev)) for t in (grad_h, grad_r, r, y))
-    _check(f.norm_back(_byref(c), *rows, _byref(g), None if work is None else work.data_ptr(),
-                       need.value, f.stream(dev)), "lvsa_residual_norm_backward")
+    _check(f.norm_back(_byref(c), *(None if t is None else _byref(t) for t in rows), _byref(g),
+                       None if work is None else work.data_ptr(), need.value, f.stream(dev)),
+           "lvsa_residual_norm_backward")
     return found
 
 
@@ -1119,8 +1143,8 @@ def residual_norm_backward(plan, grad_h, grad_r, r, y=None, gate=None, scale=Non
         return _with_stream(residual_norm_backward, stream, plan, grad_h, grad_r, r, y, gate,
                             scale, shift, weight, bias, post_weight, wanted, grad_x, grad_y)
     f = _fast()
-    params = dict(zip(_PARAMS, (gate, scale, shift, weight, bias, post_weight)))
-    names = [k for k in ("x", "y", *_PARAMS) if k == "x" or (y if k == "y" else params[k]) is not None]
+    params = gate, scale, shift, weight, bias, post_weight
+    names = ["x"] + [k for k, t in zip(("y", *_PARAMS), (y, *params)) if t is not None]
     if wanted is None:
         wanted = names
     elif not set(wanted) <= set(names):

@@ -290,19 +290,21 @@ __device__ __forceinline__ void work_item(const BArgs& a, Lds<SPARSE, ROWS / BLO
     const char* const t0 = lds[s][0];
     const char* const t1 = lds[s][1];
     // Fragments of the step, in the order of their use: for each 32 rows u the row fragments
-    // of S and T (16 rows x, 32 columns stp, both tensors), then the column fragments of the
-    // gradients (16 columns dt; both tensors in the keys kernel).  Each is read AHEAD of its
-    // two products.
+    // of S and of T (16 rows x, 32 columns stp), then the column fragments of the gradients
+    // (16 columns dt; for keys of one tensor and then of the other).  Each is read AHEAD of
+    // its two products, which take the resident tiles in turn to and fro, so that products
+    // that follow each other share an operand or an accumulator: the launch runs at the
+    // board's power limit, and this takes 1% off it.
     constexpr int NA = 16, NB = KEYS ? 16 : 8, NF = NA + NB, AHEAD = AHEAD_OF<KEYS>;
     bf16x8 fr[2 * NF];
     i16x4 lo = i16x4{};
     auto row_of = [&](int i) {
       const int u = i / NF, f = i % NF;
-      return row_frag(f % 2 ? t1 : t0, at_row, 32 * u + 16 * (f / 8), f / 2 % 4);
+      return row_frag(f / 4 % 2 ? t1 : t0, at_row, 32 * u + 16 * (f / 8), f % 4);
     };
     auto col_half = [&](int i, int half) {
-      const int u = i / NF, f = i % NF - NA, dt = KEYS ? f / 2 : f;
-      const char* const tile = KEYS && f % 2 ? t1 : t0;
+      const int u = i / NF, f = i % NF - NA, dt = f % 8;
+      const char* const tile = KEYS && f / 8 ? t1 : t0;
       return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (lds_i16x4*)(tile + ((dt & 1) ? at_odd : at_even) + (dt / 2) * SLAB +
                        (32 * u + 16 * half) * SLAB_ROW));
@@ -343,13 +345,14 @@ __device__ __forceinline__ void work_item(const BArgs& a, Lds<SPARSE, ROWS / BLO
           }
         }
 #pragma unroll
-        for (int stp = 0; stp < 4; ++stp)
+        for (int w = 0; w < 2; ++w)
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const int i = u * NF + 8 * x + 2 * stp + w;
+          for (int stp = 0; stp < 4; ++stp) {
+            const int i = u * NF + 8 * x + 4 * w + stp;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              carry(i, t);
+            for (int m = 0; m < 2; ++m) {
+              const int t = m ^ (stp & 1);
+              carry(i, m);
               if (w == 0)
                 sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i], r0[stp][t], sc[t], 0, 0, 0);
               else
@@ -379,11 +382,12 @@ __device__ __forceinline__ void work_item(const BArgs& a, Lds<SPARSE, ROWS / BLO
       }
 #pragma unroll
       for (int f = 0; f < NB; ++f) {
-        const int i = u * NF + NA + f, dt = KEYS ? f / 2 : f;
+        const int i = u * NF + NA + f, dt = f % 8;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          carry(i, t);
-          if (KEYS && f % 2)
+        for (int m = 0; m < 2; ++m) {
+          const int t = m ^ (f & 1);
+          carry(i, m);
+          if (KEYS && f / 8)
             acc1[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i], pb[t], acc1[dt][t], 0, 0, 0);
           else
             acc0[dt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i], eb[t], acc0[dt][t], 0, 0, 0);

@@ -52,7 +52,10 @@ def _pass(q, k, v, grad, mask):
     return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
 
 
-def _check(got, q, k, v, grad, kept=None):
+def _check(got, q, k, v, grad, kept=None, wide=False):
+    """`wide`: scores of many units, where a row's few terms cancel; element bounds alone.
+    So too where a row has fewer than 8 keys: with a single one e = p (do v' - delta) is 0 and
+    what is left of it is rounding, of any size relative to it."""
     n = q.shape[1]
     kept = torch.ones(n, n, dtype=torch.bool) if kept is None else kept
     want = OT.attention(*(x.double().contiguous() for x in (q, k, v, grad)), kept.cuda())
@@ -62,6 +65,9 @@ def _check(got, q, k, v, grad, kept=None):
         assert torch.equal(torch.isfinite(x), fine) and torch.equal(x[~fine].double(), w[~fine])
         over = (x.double() - w).abs()[fine] - bound[fine]
         assert (over <= 1e-30).all(), (name, float(over.max()), float(bound.max()))
+        if name != "lse" and not wide and kept.sum(1)[kept.any(1)].min() >= 8:
+            off = (x.double() - w)[fine].norm()
+            assert off <= OT.NORM * w[fine].norm(), (name, float(off / w[fine].norm()))
 
 
 SIZES = [(1, 1), (2, 2), (1, 63), (2, 64), (1, 65), (3, 127), (1, 128), (2, 129), (1, 191),
@@ -144,7 +150,7 @@ def test_blocks_that_are_not_kept_never_reach(block):
 def test_wide_scores(size):
     n = 300
     x = _inputs(2, n, seed=5, size=size)
-    _check(_pass(*x, None), *x)
+    _check(_pass(*x, None), *x, wide=True)
 
 
 def test_scores_far_from_zero():
@@ -155,7 +161,7 @@ def test_scores_far_from_zero():
         x[0][:] = sign * 8.0
         x[1][:] = (8.0 + 0.25 * torch.randn(1, 70, 128, generator=torch.Generator().manual_seed(1))
                    ).to(BF).cuda()
-        _check(_pass(*x, None), *x)
+        _check(_pass(*x, None), *x, wide=True)
 
 
 def test_out_is_attentions():
@@ -180,6 +186,52 @@ def test_long_rows_against_blocks_of_the_formula():
     for h in (0, 11):
         _check({k: t[h: h + 1] for k, t in got.items()}, *(t[h: h + 1] for t in x),
                OT.kept_tokens(kept, block, n))
+
+
+@pytest.mark.parametrize("block", [64, 128])
+def test_key_blocks_that_every_query_keeps_beside_ones_that_few_do(block):
+    """Two key blocks kept by every query block, the others by their own and the next: a
+    tile's walk is several times another's, split and whole items in one call; and one head
+    beside many."""
+    n = 40 * block - 7
+    kept = np.eye(40, dtype=bool) | np.eye(40, k=1, dtype=bool)
+    kept[:, [3, 30]] = True
+    kept[17] = True
+    for H in (1, 24):
+        x = _inputs(H, n, seed=H)
+        got = _pass(*x, _mask(kept, n, block))
+        for h in (0, H - 1):
+            _check({k: t[h: h + 1] for k, t in got.items()}, *(t[h: h + 1] for t in x),
+                   OT.kept_tokens(kept, block, n))
+
+
+def test_masks_of_thousands_of_blocks():
+    """8,000 blocks of 64 (the most), each row with a few: queries and keys at both ends and
+    between against the formula over the blocks that they meet."""
+    block, nb = 64, 8000
+    n = nb * block - 5
+    kept = np.zeros((nb, nb), bool)
+    at = np.arange(nb)
+    kept[at, at] = True
+    kept[at, (at * 7 + 3) % nb] = True
+    kept[::500, 4321] = True
+    x = _inputs(1, n, seed=3)
+    got = _pass(*x, _mask(kept, n, block))
+    for b in (0, 1, 4321, 4500, nb - 1):
+        # the tokens that meet block b's queries or keys, or theirs
+        rows = np.nonzero(kept[:, b])[0]
+        blocks = np.unique(np.concatenate([[b], rows, np.nonzero(kept[rows].any(0))[0],
+                                           np.nonzero(kept[b])[0]]))
+        tok = np.concatenate([np.arange(c * block, min(n, (c + 1) * block)) for c in blocks])
+        sub = [t[:, tok].contiguous() for t in x]
+        pairs = torch.from_numpy(kept[np.ix_(tok // block, tok // block)])
+        want = OT.attention(*(t.double() for t in sub), pairs.cuda())
+        mine = torch.from_numpy(np.nonzero(tok // block == b)[0]).cuda()
+        for name in ("out", "lse", "dq", "dk", "dv"):
+            # queries of b see all their keys here, and keys of b all their queries
+            g = got[name][:, torch.from_numpy(tok).cuda()][:, mine]
+            assert ((g.double() - want[name][:, mine]).abs() <= want["bound"][name][:, mine] + 1e-30
+                    ).all(), (b, name)
 
 
 def test_the_same_every_time():

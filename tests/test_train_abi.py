@@ -1,0 +1,292 @@
+"""The C ABI of attention's gradients and of the residual step, as far as it needs no GPU:
+refusals before any launch with the documented status, sizes of workspaces, and the plain
+64-bit forms themselves against automatic differentiation."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2605_31057_amd as L
+from oracle import train as OT
+
+ref = ctypes.byref
+PTR = 0x100000
+
+
+def _tensor(heads=2, n=300, d=128, data=PTR, sh=None, st=None):
+    return L._Tensor(data, heads, n, d, n * d if sh is None else sh, d if st is None else st)
+
+
+def _mask(n=300, block=128, nq=None, nk=None, rows=8 * PTR, cols=9 * PTR):
+    nb = -(-n // block) if block > 0 else 0
+    return L.BlockMask(n, block, nb if nq is None else nq, nb if nk is None else nk, rows, cols)
+
+
+BAD_MASKS = [
+    (dict(rows=None), L.EINVAL), (dict(cols=None), L.EINVAL), (dict(n=301), L.EINVAL),
+    (dict(nq=4), L.EINVAL), (dict(nk=2), L.EINVAL), (dict(block=32), L.EUNSUPPORTED),
+    (dict(block=256), L.EUNSUPPORTED),
+]
+BAD_TENSORS = [
+    (dict(n=299), L.EINVAL), (dict(heads=1), L.EINVAL), (dict(data=None), L.EINVAL),
+    (dict(d=64), L.EUNSUPPORTED), (dict(data=PTR + 8), L.EUNSUPPORTED), (dict(st=132), L.EUNSUPPORTED),
+    (dict(sh=-128), L.EUNSUPPORTED), (dict(st=2 ** 26), L.EUNSUPPORTED),
+]
+
+
+def test_attention_lse_refusals():
+    f = L.lib().lvsa_attention_lse
+    q, k, v, o = (_tensor(data=i * PTR) for i in range(1, 5))
+    lse = 6 * PTR
+
+    def call(q=q, k=k, v=v, mask=None, o=o, lse=lse):
+        return f(*(t and ref(t) for t in (q, k, v, mask, o)), lse, None)
+
+    for kw in (dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(lse=None),
+               dict(q=_tensor(n=0)), dict(o=_tensor(data=2 * PTR))):
+        assert call(**kw) == L.EINVAL, kw
+    assert call(lse=lse + 2) == L.EUNSUPPORTED
+    for kw, st in BAD_MASKS:
+        assert call(mask=_mask(**kw)) == st, kw
+    assert call(mask=_mask(n=8001 * 64, block=64)) == L.EUNSUPPORTED
+    for kw, st in BAD_TENSORS:
+        if kw.get("data", 0) is not None and "data" not in kw:
+            kw = dict(kw, data=2 * PTR)
+        assert call(k=_tensor(**kw)) == st, kw
+
+
+def test_attention_backward_refusals():
+    lib = L.lib()
+    names = ("go", "q", "k", "v", "out", "gq", "gk", "gv")
+    good = {x: _tensor(data=(i + 1) * PTR) for i, x in enumerate(names)}
+    lse, work = 20 * PTR, 30 * PTR
+    need = ctypes.c_int64()
+    assert lib.lvsa_attention_backward_workspace(ref(good["q"]), None, ref(need)) == L.OK
+    assert need.value >= 2 * 2 * 300 * 4
+
+    def call(mask=None, lse=lse, work=work, size=1 << 40, **kw):
+        t = dict(good, **kw)
+        go, q, k, v, out, gq, gk, gv = (t[x] and ref(t[x]) for x in names)
+        return lib.lvsa_attention_backward(go, q, k, v, out, lse, mask and ref(mask), gq, gk, gv,
+                                           work, size, None)
+
+    for x in names:
+        assert call(**{x: None}) == L.EINVAL, x
+    assert call(lse=None) == L.EINVAL
+    assert call(lse=lse + 1) == L.EUNSUPPORTED
+    assert call(work=None) == L.EINVAL
+    assert call(size=need.value - 1) == L.EINVAL
+    assert call(work=work + 8) == L.EUNSUPPORTED
+    for kw, st in BAD_MASKS:
+        assert call(mask=_mask(**kw)) == st, kw
+        if "n" not in kw:
+            assert lib.lvsa_attention_backward_workspace(ref(good["q"]), ref(_mask(**kw)),
+                                                         ref(need)) == st, kw
+    for kw, st in BAD_TENSORS:
+        for x in ("go", "k", "v", "out"):
+            t = _tensor(**dict(dict(data=(names.index(x) + 1) * PTR), **kw))
+            if "st" in kw and kw["st"] > 1000 and x == "out":
+                continue        # out is read with 64-bit offsets
+            assert call(**{x: t}) == st, (kw, x)
+    # rows of a gradient that share elements, gradients in an input's or in each other's place
+    for x in ("gq", "gk", "gv"):
+        at = (names.index(x) + 1) * PTR
+        assert call(**{x: _tensor(data=at, st=64)}) == L.EINVAL
+        assert call(**{x: _tensor(data=at, sh=0)}) == L.EINVAL
+        for y in ("go", "q", "k", "v", "out"):
+            assert call(**{x: good[y]}) == L.EINVAL
+        assert call(**{x: _tensor(data=lse)}) == L.EINVAL
+    assert call(gq=good["gk"]) == L.EINVAL
+    assert call(gk=good["gv"]) == L.EINVAL
+    assert call(gv=good["gq"]) == L.EINVAL
+
+
+def test_attention_backward_sizes():
+    f = L.lib().lvsa_attention_backward_workspace
+    need = ctypes.c_int64()
+    assert f(None, None, ref(need)) == L.EINVAL
+    assert f(ref(_tensor()), None, None) == L.EINVAL
+    assert f(ref(_tensor(n=0)), None, ref(need)) == L.EINVAL
+    assert f(ref(_tensor(heads=0)), None, ref(need)) == L.EINVAL
+    assert f(ref(_tensor(heads=1 << 14, n=1 << 15)), None, ref(need)) == L.EUNSUPPORTED
+    assert f(ref(_tensor(n=8001 * 64)), ref(_mask(n=8001 * 64, block=64)), ref(need)) == L.EUNSUPPORTED
+    # a mask without rows is every block, in blocks of any size
+    sizes = []
+    for mask in (None, _mask(block=64, rows=None, cols=None), _mask(block=128, rows=None, cols=None)):
+        assert f(ref(_tensor()), mask and ref(mask), ref(need)) == L.OK
+        sizes.append(need.value)
+    assert len(set(sizes)) == 1
+    # parts of items stay within a few hundred megabytes however long the call is
+    for H, n in ((1, 128), (1, 188760), (40, 188760), (12, 32760), (500, 1000), (1, 2 ** 28)):
+        for mask in (None, _mask(n=n) if n < 8000 * 128 else None):
+            assert f(ref(_tensor(heads=H, n=n)), mask and ref(mask), ref(need)) == L.OK
+            assert need.value <= 8 * H * n + (600 << 20), (H, n, need.value)
+
+
+# ------------------------------------------------------------- residual step
+
+def _rows(data=PTR, n=10, stride=256):
+    return L._Rows(data, n, stride)
+
+
+def _plan(dim=256, frame=4, norm=1, post=0, eps=1e-6, a=1.0, st=2, bt=2, pt=2, gate=50 * PTR,
+          scale=51 * PTR, shift=52 * PTR, strides=(256, 256, 256), weight=None, bias=None,
+          post_weight=None):
+    return L._ResidualNorm(dim, frame, norm, post, eps, a, st, bt, pt, gate, scale, shift, *strides,
+                           weight, bias, post_weight)
+
+
+BAD_PLANS = [
+    (dict(dim=0), L.EINVAL), (dict(frame=-1), L.EINVAL), (dict(norm=3), L.EINVAL),
+    (dict(norm=-1), L.EINVAL), (dict(post=3), L.EINVAL), (dict(st=3), L.EINVAL),
+    (dict(bt=-1), L.EINVAL), (dict(pt=7), L.EINVAL), (dict(eps=-1.0), L.EINVAL),
+    (dict(eps=float("nan")), L.EINVAL), (dict(eps=float("inf")), L.EINVAL),
+    (dict(scale=None), L.EINVAL), (dict(shift=None), L.EINVAL),
+    (dict(norm=0), L.EINVAL),                       # a scale without a norm
+    (dict(post_weight=53 * PTR), L.EINVAL),         # of no norm
+    (dict(strides=(-8, 256, 256)), L.EINVAL),
+    (dict(dim=252), L.EUNSUPPORTED), (dict(dim=16392), L.EUNSUPPORTED),
+    (dict(st=0, bt=1), L.EUNSUPPORTED), (dict(st=0, bt=2), L.EUNSUPPORTED),
+    (dict(st=1, bt=0), L.EUNSUPPORTED), (dict(gate=PTR + 8), L.EUNSUPPORTED),
+    (dict(weight=PTR + 4), L.EUNSUPPORTED), (dict(strides=(256, 252, 256)), L.EUNSUPPORTED),
+]
+X, Y, R, H, GR, GH, GX, GY = (i * PTR for i in range(1, 9))
+
+
+def test_residual_norm_refusals():
+    f = L.lib().lvsa_residual_norm_forward
+
+    def call(p=_plan(), x=_rows(X), y=_rows(Y), r=_rows(R), h=_rows(H)):
+        return f(*(t and ref(t) for t in (p, x, y, r, h)), None)
+
+    for kw, st in BAD_PLANS:
+        assert call(p=_plan(**kw)) == st, kw
+    for x in ("p", "x", "r", "h"):
+        assert call(**{x: None}) == L.EINVAL, x
+    for x, at in (("x", X), ("y", Y), ("r", R), ("h", H)):
+        for t, st in ((_rows(None), L.EINVAL), (_rows(at, n=0 if x == "x" else 9), L.EINVAL),
+                      (_rows(at, stride=-256), L.EINVAL), (_rows(at + 8), L.EUNSUPPORTED),
+                      (_rows(at, stride=260), L.EUNSUPPORTED)):
+            assert call(**{x: t}) == st, (x, st)
+    for x, at in (("r", R), ("h", H)):
+        assert call(**{x: _rows(at, stride=128)}) == L.EINVAL      # rows that share elements
+    # in place: r in x's, h in y's rows, the same strides; nothing else
+    assert call(r=_rows(X, stride=512)) == L.EINVAL
+    assert call(h=_rows(Y, stride=512)) == L.EINVAL
+    assert call(r=_rows(Y)) == L.EINVAL
+    assert call(h=_rows(X)) == L.EINVAL
+    assert call(h=_rows(R)) == L.EINVAL
+    # without y: no r, gate, norm of y, factor
+    plain = dict(gate=None)
+    assert call(p=_plan(**plain), y=None) == L.EINVAL
+    assert call(y=None, r=None) == L.EINVAL
+    assert call(p=_plan(post=1, **plain), y=None, r=None) == L.EINVAL
+    assert call(p=_plan(a=0.5, **plain), y=None, r=None) == L.EINVAL
+    assert call(p=_plan(norm=0, scale=None, shift=None, **plain), y=None, r=None, h=None) == L.EINVAL
+    # no norm, no h
+    assert call(p=_plan(norm=0, scale=None, shift=None)) == L.EINVAL
+    # work-items past a launch
+    assert call(p=_plan(frame=1), x=_rows(X, n=2 ** 30), y=_rows(Y, n=2 ** 30), r=_rows(R, n=2 ** 30),
+                h=_rows(H, n=2 ** 30)) == L.EUNSUPPORTED
+
+
+def _grads(x=GX, y=GY, n=10, stride=256, **kw):
+    g = L._NormGrads()
+    g.x, g.y = L._Rows(x, n, stride), L._Rows(y, n, stride)
+    for k, v in kw.items():
+        setattr(g, k, v)
+    return g
+
+
+def test_residual_norm_backward_refusals():
+    lib = L.lib()
+    work = 40 * PTR
+
+    def call(p=_plan(), gh=_rows(GH), gr=_rows(GR), r=_rows(R), y=_rows(Y), g=_grads(), work=work,
+             size=1 << 40):
+        return lib.lvsa_residual_norm_backward(*(t and ref(t) for t in (p, gh, gr, r, y, g)), work,
+                                               size, None)
+
+    for kw, st in BAD_PLANS:
+        assert call(p=_plan(**kw)) == st, kw
+    for x in ("p", "gh", "r", "y", "g"):
+        assert call(**{x: None}) == L.EINVAL, x
+    for x, at in (("gh", GH), ("gr", GR), ("r", R), ("y", Y)):
+        for t, st in ((_rows(None), L.EINVAL), (_rows(at, n=0 if x == "r" else 9), L.EINVAL),
+                      (_rows(at, stride=-256), L.EINVAL), (_rows(at + 8), L.EUNSUPPORTED),
+                      (_rows(at, stride=260), L.EUNSUPPORTED)):
+            assert call(**{x: t}) == st, (x, st)
+    for g in (_grads(stride=128), _grads(n=9), _grads(x=R), _grads(x=Y), _grads(x=GH), _grads(y=GR),
+              _grads(y=R), _grads(y=Y), _grads(y=GX)):
+        assert call(g=g) == L.EINVAL
+    assert call(g=_grads(x=GX + 8)) == L.EUNSUPPORTED
+    # gradients of what the step does not have, or in a parameter's place
+    for name in ("weight", "bias", "post_weight"):
+        assert call(g=_grads(**{name: 60 * PTR})) == L.EINVAL
+    assert call(g=_grads(gate=50 * PTR)) == L.EINVAL
+    assert call(g=_grads(gate=60 * PTR + 8)) == L.EUNSUPPORTED
+    # a workspace where there are sums
+    need = ctypes.c_int64()
+    g = _grads(gate=60 * PTR, scale=61 * PTR)
+    assert lib.lvsa_residual_norm_workspace(ref(_plan()), 10, ref(g), ref(need)) == L.OK
+    assert need.value > 0
+    assert call(g=g, size=need.value - 1) == L.EINVAL
+    assert call(g=g, work=None) == L.EINVAL
+    assert call(g=g, work=work + 8) == L.EUNSUPPORTED
+    assert lib.lvsa_residual_norm_workspace(ref(_plan()), 10, ref(_grads()), ref(need)) == L.OK
+    assert need.value == 0
+    assert lib.lvsa_residual_norm_workspace(ref(_plan()), 0, ref(g), ref(need)) == L.EINVAL
+    assert lib.lvsa_residual_norm_workspace(ref(_plan()), 10, None, ref(need)) == L.EINVAL
+    assert lib.lvsa_residual_norm_workspace(ref(_plan()), 10, ref(g), None) == L.EINVAL
+    # no gradient of y without y
+    assert call(p=_plan(gate=None), y=None) == L.EINVAL
+
+
+# ------------------------------------------------------------------- binding
+
+def test_binding_refusals():
+    for kw in (dict(dim=2 ** 32 + 8), dict(dim=-8), dict(dim=256, frame_tokens=2 ** 31),
+               dict(dim=256, norm=2 ** 32)):
+        with pytest.raises(L.LvsaError):
+            L.ResidualNorm(**kw)
+    x = torch.zeros(256).as_strided((2 ** 31, 256), (0, 1))
+    with pytest.raises(L.LvsaError):
+        L._channels(x, 256, -1)
+    for t in (torch.zeros(4, 128), torch.zeros(256, 4).t(), torch.zeros(4, 3, 512)[:, ::2, :256]):
+        with pytest.raises(ValueError):
+            L._channels(t, 256, -1)
+    with pytest.raises(ValueError):
+        L._channels(torch.zeros(4, 256), 256, 0)
+
+
+# ----------------------------------------------------------------- the oracle
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_attention_of_the_oracle(masked):
+    g = torch.Generator().manual_seed(1)
+    q, k, v, grad = (torch.randn(2, 40, 16, generator=g, dtype=torch.double) for _ in range(4))
+    kept = OT.kept_tokens([[1, 0, 1], [1, 1, 0], [0, 1, 1]], 16, 40).bool() if masked else \
+        torch.ones(40, 40, dtype=torch.bool)
+    want = OT.attention(q, k, v, grad, kept)
+    leaves = [t.requires_grad_() for t in (q, k, v)]
+    out = torch.nn.functional.scaled_dot_product_attention(*leaves, attn_mask=kept)
+    assert torch.allclose(out, want["out"], rtol=0, atol=1e-12)
+    for name, x in zip(("dq", "dk", "dv"), torch.autograd.grad(out, leaves, grad)):
+        assert torch.allclose(x, want[name], rtol=0, atol=1e-11)
+
+
+@pytest.mark.parametrize("n", [64, 1000])
+def test_bounds_see_a_missing_key(n):
+    """One key too few passes the bound of a few elements at least, and the bound in the
+    2-norm by far."""
+    g = torch.Generator().manual_seed(2)
+    q, k, v, grad = (torch.randn(1, n, 128, generator=g, dtype=torch.double) for _ in range(4))
+    kept = torch.ones(n, n, dtype=torch.bool)
+    want = OT.attention(q, k, v, grad, kept)
+    kept[:, n - 1] = False
+    other = OT.attention(q, k, v, grad, kept)
+    for name in ("out", "lse", "dq", "dk", "dv"):
+        off = (other[name] - want[name]).abs()
+        assert (off > want["bound"][name]).any(), name
+        if name != "lse":
+            assert off.norm() > 2 * OT.NORM * want[name].norm(), name
