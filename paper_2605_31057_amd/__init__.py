@@ -1054,7 +1054,7 @@ def _launch_norm(plan, x, y, params, dtype, r, h):
     if y is not None:
         ty = _byref(_Rows(*_channels(y, dim, dev)))
         if r is None:
-            r = f.empty(shape, dtype=kind, device=x.device)
+            r = f.empty_like(x) if x.is_contiguous() else f.empty(shape, dtype=kind, device=x.device)
             tr = _byref(_Rows(r.data_ptr(), n, dim))
         else:
             tr = _byref(_Rows(*_channels(r, dim, dev)))
@@ -1063,7 +1063,9 @@ def _launch_norm(plan, x, y, params, dtype, r, h):
     if h is not None:
         th = _byref(_Rows(*_channels(h, dim, dev)))
     elif c.norm:
-        h = f.empty(shape, dtype=block, device=x.device)
+        like = x if y is None else y
+        h = (f.empty_like(like) if like.dtype is block and like.is_contiguous()
+             else f.empty(shape, dtype=block, device=x.device))
         th = _byref(_Rows(h.data_ptr(), n, dim))
     status = f.norm(_byref(c), _byref(_Rows(at, n, stride)), ty, tr, th, f.stream(dev))
     if status:

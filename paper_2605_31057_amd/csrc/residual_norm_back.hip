@@ -12,6 +12,10 @@
 namespace lvsa {
 namespace {
 
+// Sums over rows (sum_rows): SLICES threads share the rows of four columns, a workgroup works
+// LANES fours of columns.
+constexpr int SLICES = 32, LANES = 16;
+
 template <typename S, typename Y, int TEAM, int V, int MODE>
 __global__ __launch_bounds__(TEAM ? kNormGroup : 1024) void backward_kernel(const NormArgs a) {
   __shared__ StatsLds lds;
@@ -163,10 +167,7 @@ __global__ __launch_bounds__(TEAM ? kNormGroup : 1024) void backward_kernel(cons
   }
 }
 
-// Adds rows of three sums: SLICES threads share the rows of four columns, added in the
-// order of the slices.  The results are in the first LANES threads.
-constexpr int SLICES = 16, LANES = 32;
-
+// Adds rows of three sums, in the order of the slices; the results are in every thread.
 __device__ __forceinline__ void sum_rows(const float* rows, int64_t n, int32_t dim, int32_t col,
                                          f32x4v (&s)[3], f32x4v (&lds)[3][SLICES][LANES]) {
   const int lane = threadIdx.x % LANES, slice = threadIdx.x / LANES;
@@ -221,23 +222,27 @@ __global__ __launch_bounds__(SLICES* LANES) void frame_kernel(const NormArgs a, 
   const int32_t col = 4 * (int32_t)(blockIdx.y * LANES + threadIdx.x % LANES);
   f32x4v s[3];
   sum_rows(a.partial + (int64_t)f * per_frame * 3 * a.dim, per_frame, a.dim, col, s, lds);
-  if (threadIdx.x >= LANES || col >= a.dim) return;
-  const int64_t at = (int64_t)f * a.dim + col;
-  const f32x4v w = param4(a.weight, a.param_type, col, 1.f);
-  const f32x4v b = param4(a.bias, a.param_type, col, 0.f);
-  put4(a.d_scale, a.param_type, at, w * s[0] + b * s[1]);
-  put4(a.d_shift, a.param_type, at, s[1]);
-  put4(a.d_gate, a.param_type, at, param4(a.post_weight, a.param_type, col, 1.f) * s[2]);
-  if (a.frame_sums) {
-    const f32x4v k = param4(a.scale, a.param_type, (int64_t)f * a.scale_st + col, 0.f) + 1.f;
-    float* const to = a.frame_sums + (int64_t)f * 3 * a.dim + col;
-    *(f32x4v*)to = k * s[0];
-    *(f32x4v*)(to + a.dim) = k * s[1];
-    *(f32x4v*)(to + 2 * (int64_t)a.dim) =
-        param4(a.gate, a.param_type, (int64_t)f * a.gate_st + col, 1.f) * s[2];
+  if (threadIdx.x < LANES && col < a.dim) {
+    const int64_t at = (int64_t)f * a.dim + col;
+    const f32x4v w = param4(a.weight, a.param_type, col, 1.f);
+    const f32x4v b = param4(a.bias, a.param_type, col, 0.f);
+    put4(a.d_scale, a.param_type, at, w * s[0] + b * s[1]);
+    put4(a.d_shift, a.param_type, at, s[1]);
+    put4(a.d_gate, a.param_type, at, param4(a.post_weight, a.param_type, col, 1.f) * s[2]);
+    if (a.frame_sums) {
+      const f32x4v k = param4(a.scale, a.param_type, (int64_t)f * a.scale_st + col, 0.f) + 1.f;
+      float* const to = a.frame_sums + (int64_t)f * 3 * a.dim + col;
+      *(f32x4v*)to = k * s[0];
+      *(f32x4v*)(to + a.dim) = k * s[1];
+      *(f32x4v*)(to + 2 * (int64_t)a.dim) =
+          param4(a.gate, a.param_type, (int64_t)f * a.gate_st + col, 1.f) * s[2];
+    }
   }
 }
 
+// Those of the weights, over the frames.  (The frame kernel's last workgroup of each group of
+// columns doing it instead takes a release of every workgroup's sums: 68 us against 16 for
+// both kernels at 21 frames of 5,120 columns.)
 __global__ __launch_bounds__(SLICES* LANES) void weight_kernel(const NormArgs a) {
   __shared__ f32x4v lds[3][SLICES][LANES];
   const int32_t col = 4 * (int32_t)(blockIdx.x * LANES + threadIdx.x % LANES);
@@ -276,7 +281,7 @@ struct Backward {
 
 }  // namespace
 
-// Bytes: the partial sums, and a row of three sums a frame for the weights.
+// Bytes: the partial sums and, for the weights, a row of three sums a frame.
 int64_t norm_workspace(const NormArgs& a) {
   const bool weights = a.d_weight || a.d_bias || a.d_post_weight;
   if (!weights && !a.d_gate && !a.d_scale && !a.d_shift) return 0;
