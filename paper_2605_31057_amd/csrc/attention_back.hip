@@ -25,7 +25,7 @@
 // Before it, prep_kernel takes what S and T begin with, -lse sqrt(d) and -delta of every
 // query (so that an element takes a product, an exponential and a product), and the mask
 // as bitmaps, of every query block's key blocks and, transposed, of every key block's
-// query blocks; plan_kernel makes the items from them.
+// query blocks; plan_kernel (for few blocks prep_kernel itself) makes the items from them.
 //
 // Contractions (bf16 MFMA 16x16x32, fp32 accumulate), as in attention.hip: a lane (group
 // g = lane/16, i = lane%16) holds resident row i of a 16-row tile in its columns, so P and
@@ -94,7 +94,8 @@ struct BArgs {
   Item* list;
   Split* splits;
   float* units;
-  int32_t N, nb, heads, tiles, words;
+  int32_t N, nb, block, heads, tiles, words;
+  int32_t list_here;         // prep_kernel makes the list (one word: up to 32 blocks)
   int32_t stat_groups;       // prep: workgroups of 64 rows
   int32_t max_units;         // of a head
   int32_t parts[2], len[2];  // without a mask: parts of every item, blocks of each
@@ -490,26 +491,125 @@ __global__ __launch_bounds__(64 * WAVES) void combine_kernel(const BArgs a) {
   }
 }
 
+// The items of one head from the blocks of its walks, count_of(i) for item i < 2 tiles
+// (queries' tiles, then keys'), the longest first, by one workgroup.  An item of cost c
+// (steps times products) is split where c > T = max(MIN_COST, share * C), C the sum of all
+// costs, into at most c / T + 1 < 2 c / T parts.  So there are at most C / T parts more than
+// items and at most 4 C / T units (two for a part of keys), which the host bounds by the two
+// parts of T.  Order among items of like cost, and where parts lie, follow atomics; results
+// do not depend on either.
+struct PlanLds {
+  unsigned long long total;
+  int last, units, splits, hist[64];
+};
+template <int THREADS, typename F>
+__device__ __forceinline__ void make_list(const BArgs& a, PlanLds& L, F&& count_of) {
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int steps = a.block / STEP;
+  if (tid < 64) L.hist[tid] = 0;
+  if (tid == 0) L.total = 0ull, L.units = 0, L.splits = 0;
+  __syncthreads();
+  auto cost_of = [&](int i, int n) { return n * steps * COST[i >= a.tiles]; };
+  unsigned long long sum = 0ull;
+  for (int i = tid; i < 2 * a.tiles; i += THREADS) sum += (unsigned long long)cost_of(i, count_of(i));
+  for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+  if (lane == 0) atomicAdd(&L.total, sum);
+  __syncthreads();
+  const int T = max(MIN_COST, (int)min(a.share * (double)L.total, 1e9) + 1);
+  // Parts of an item, and blocks of each.
+  auto parts_of = [&](int i, int n, int& len) {
+    const int c = cost_of(i, n), want = c > T ? min((c + T - 1) / T, n) : 1;
+    len = (n + want - 1) / want;
+    return n ? (n + len - 1) / len : 1;
+  };
+  // Buckets of like cost: no part costs more than T.
+  const float scale = 63.f / (float)T;
+  auto bucket_of = [&](int i, int len) {
+    return 63 - min(63, (int)((float)cost_of(i, len) * scale));
+  };
+  for (int i = tid; i < 2 * a.tiles; i += THREADS) {
+    int len;
+    const int parts = parts_of(i, count_of(i), len);
+    atomicAdd(&L.hist[bucket_of(i, len)], parts);
+  }
+  __syncthreads();
+  if (tid < 64) {   // the buckets' first places
+    const int own = L.hist[tid];
+    int upto = own;
+    for (int d = 1; d < 64; d *= 2) {
+      const int below = __shfl_up(upto, d);
+      if (tid >= d) upto += below;
+    }
+    L.hist[tid] = upto - own;
+    if (tid == 63) a.plan->items = upto;
+  }
+  __syncthreads();
+  for (int i = tid; i < 2 * a.tiles; i += THREADS) {
+    int len;
+    const int n = count_of(i), parts = parts_of(i, n, len), keys = i >= a.tiles;
+    const int tile = (i - keys * a.tiles) | (keys << 31);
+    int unit = -1;
+    if (parts > 1) {
+      unit = atomicAdd(&L.units, parts * (keys + 1));
+      a.splits[atomicAdd(&L.splits, 1)] = Split{tile, unit, parts, 0};
+    }
+    int at = atomicAdd(&L.hist[bucket_of(i, len)], parts);
+    for (int p = 0; p < parts; ++p, ++at)
+      a.list[at] = Item{tile, p * len, min(len, n - p * len),
+                        parts > 1 ? unit + p * (keys + 1) : -1};
+  }
+  __syncthreads();
+  if (tid == 0) a.plan->splits = L.splits;
+}
+
+// Blocks in word w of the walk of item i.
+__device__ __forceinline__ int walk_word(const BArgs& a, int i, int w) {
+  const int per = ROWS / a.block, keys = i >= a.tiles, b0 = (i - keys * a.tiles) * per;
+  uint32_t bits = 0u;
+  for (int b = b0; b < min(b0 + per, a.nb); ++b)
+    bits |= keys ? a.by_col[(int64_t)w * a.nb + b] : a.by_row[(int64_t)b * a.words + w];
+  return __popc(bits);
+}
+
+// Whether this workgroup is the last of `groups` to come here.  Its thread 0's ticket
+// releases what the workgroup has written, which the barrier puts before it, and acquires
+// what the others have.
+__device__ __forceinline__ bool last_group(const BArgs& a, PlanLds& L, int groups) {
+  __syncthreads();
+  if (threadIdx.x == 0)
+    L.last = __hip_atomic_fetch_add(&a.plan->done, 1, __ATOMIC_ACQ_REL,
+                                    __HIP_MEMORY_SCOPE_AGENT) == groups - 1;
+  __syncthreads();
+  return L.last;
+}
+
 // The first `stat_groups` workgroups: -lse sqrt(d) and -delta of 64 rows each, 16 threads a
 // row.  The others: bitmaps of a block CSR, a workgroup for every 32 rows: bit kb % 32 of
 // by_row[row][kb / 32], bit qb % 32 of by_col[qb / 32][col].  Entries outside [0, nb) are
 // skipped, as in the forward pass.
 __global__ __launch_bounds__(256) void prep_kernel(const BArgs a) {
   extern __shared__ uint32_t bits[];
+  __shared__ PlanLds plan;
   if ((int)blockIdx.x < a.stat_groups) {
     const int c = 8 * (threadIdx.x % 16);
+    bf16x8 x[4], o[4];
+#pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int64_t i = (int64_t)blockIdx.x * 64 + 16 * k + threadIdx.x / 16;
-      if (i >= (int64_t)a.heads * a.N) break;
-      const int head = (int)(i / a.N), row = (int)(i % a.N);
-      const bf16x8 x = *(const bf16x8*)(a.t[GO] + head * a.sh[GO] + row * a.st[GO] + c);
-      const bf16x8 o = *(const bf16x8*)(a.t[O] + head * a.sh[O] + row * a.st[O] + c);
+      const bool there = i < (int64_t)a.heads * a.N;
+      const int head = there ? (int)(i / a.N) : 0, row = there ? (int)(i % a.N) : 0;
+      x[k] = *(const bf16x8*)(a.t[GO] + head * a.sh[GO] + row * a.st[GO] + c);
+      o[k] = *(const bf16x8*)(a.t[O] + head * a.sh[O] + row * a.st[O] + c);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t i = (int64_t)blockIdx.x * 64 + 16 * k + threadIdx.x / 16;
       float d = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d = __builtin_fmaf((float)x[e], (float)o[e], d);
+      for (int e = 0; e < 8; ++e) d = __builtin_fmaf((float)x[k][e], (float)o[k][e], d);
 #pragma unroll
       for (int w = 8; w; w /= 2) d += __shfl_xor(d, w);
-      if (c == 0) {
+      if (c == 0 && i < (int64_t)a.heads * a.N) {
         const float l = a.lse[i];
         a.row_lse[i] = l == -__builtin_inff() ? l : l * -11.313708498984761f;
         a.row_delta[i] = -d;
@@ -517,7 +617,7 @@ __global__ __launch_bounds__(256) void prep_kernel(const BArgs a) {
     }
     return;
   }
-  if ((int)blockIdx.x == a.stat_groups && threadIdx.x == 0) a.plan->done = 0;
+  if (!a.list_here && (int)blockIdx.x == a.stat_groups && threadIdx.x == 0) a.plan->done = 0;
   const int nb = a.nb, words = a.words, group = (int)blockIdx.x - a.stat_groups;
   uint32_t* const rows = bits;               // [32][words]
   uint32_t* const cols = bits + 32 * words;  // [nb]
@@ -538,104 +638,30 @@ __global__ __launch_bounds__(256) void prep_kernel(const BArgs a) {
   const int mine = min(32, nb - 32 * group) * words;
   for (int i = threadIdx.x; i < mine; i += 256) a.by_row[(int64_t)32 * group * words + i] = rows[i];
   for (int i = threadIdx.x; i < nb; i += 256) a.by_col[(int64_t)group * nb + i] = cols[i];
+  // One workgroup has all bitmaps: it makes the list too, which saves a launch (5 us of the
+  // 42 of one head of 1,024 tokens).
+  if (!a.list_here) return;
+  __syncthreads();
+  make_list<256>(a, plan, [&](int i) { return walk_word(a, i, 0); });
 }
 
-// The items of one head from the bitmaps, the longest first.  A wave counts the blocks of a
-// tile's walk; the workgroup that is through last makes the list.  An item of cost c (steps
-// times products) is split where c > T = max(MIN_COST, share * C), C the sum of all costs,
-// into at most c / T + 1 < 2 c / T parts.  So there are at most C / T parts more than items
-// and at most 4 C / T units (two for a part of keys), which the host bounds by the two parts
-// of T.  Order among items of like cost, and where parts lie, follow atomics; results do not
-// depend on either.
+// The list where there are many blocks: a wave counts each walk's, the workgroup that is
+// through last makes the list.
 constexpr int PLAN_WAVES = 16;
-template <int BLOCK>
 __global__ __launch_bounds__(64 * PLAN_WAVES) void plan_kernel(const BArgs a) {
-  constexpr int PER = ROWS / BLOCK, THREADS = 64 * PLAN_WAVES;
-  __shared__ unsigned long long total;
-  __shared__ int last, units, splits, hist[64];
-  const int tid = threadIdx.x, lane = tid % 64;
-  if (tid < 64) hist[tid] = 0;
-  if (tid == 0) total = 0ull, units = 0, splits = 0;
-  // Item i < 2 tiles: queries' tiles, then keys'.
-  const int mine = (int)blockIdx.x * PLAN_WAVES + tid / 64;
+  __shared__ PlanLds L;
+  const int mine = (int)blockIdx.x * PLAN_WAVES + (int)threadIdx.x / 64, lane = threadIdx.x % 64;
   if (mine < 2 * a.tiles) {
-    const int keys = mine >= a.tiles, b0 = (mine - keys * a.tiles) * PER;
     int n = 0;
-    for (int w = lane; w < a.words; w += 64) {
-      uint32_t bits = 0u;
-#pragma unroll
-      for (int b = 0; b < PER; ++b)
-        if (b0 + b < a.nb)
-          bits |= keys ? a.by_col[(int64_t)w * a.nb + b0 + b]
-                       : a.by_row[(int64_t)(b0 + b) * a.words + w];
-      n += __popc(bits);
-    }
+    for (int w = lane; w < a.words; w += 64) n += walk_word(a, mine, w);
     for (int d = 32; d; d /= 2) n += __shfl_xor(n, d);
     if (lane == 0)
       __hip_atomic_store(&a.counts[mine], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  // Thread 0's ticket releases the workgroup's counts, which the barrier puts before it.
-  __syncthreads();
-  if (tid == 0)
-    last = __hip_atomic_fetch_add(&a.plan->done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
-           (int)gridDim.x - 1;
-  __syncthreads();
-  if (!last) return;
-
-  auto cost_of = [&](int i, int n) { return n * (BLOCK / STEP) * COST[i >= a.tiles]; };
-  auto count_of = [&](int i) {
+  if (!last_group(a, L, (int)gridDim.x)) return;
+  make_list<64 * PLAN_WAVES>(a, L, [&](int i) {
     return __hip_atomic_load(&a.counts[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  };
-  unsigned long long sum = 0ull;
-  for (int i = tid; i < 2 * a.tiles; i += THREADS) sum += (unsigned long long)cost_of(i, count_of(i));
-  for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
-  if (lane == 0) atomicAdd(&total, sum);
-  __syncthreads();
-  const int T = max(MIN_COST, (int)min(a.share * (double)total, 1e9) + 1);
-  // Parts of an item, and blocks of each.
-  auto parts_of = [&](int i, int n, int& len) {
-    const int c = cost_of(i, n), want = c > T ? min((c + T - 1) / T, n) : 1;
-    len = (n + want - 1) / want;
-    return n ? (n + len - 1) / len : 1;
-  };
-  // Buckets of like cost: no part costs more than T.
-  const float scale = 63.f / (float)T;
-  auto bucket_of = [&](int i, int len) {
-    return 63 - min(63, (int)((float)cost_of(i, len) * scale));
-  };
-  for (int i = tid; i < 2 * a.tiles; i += THREADS) {
-    int len;
-    const int parts = parts_of(i, count_of(i), len);
-    atomicAdd(&hist[bucket_of(i, len)], parts);
-  }
-  __syncthreads();
-  if (tid < 64) {   // the buckets' first places
-    const int own = hist[tid];
-    int upto = own;
-    for (int d = 1; d < 64; d *= 2) {
-      const int below = __shfl_up(upto, d);
-      if (tid >= d) upto += below;
-    }
-    hist[tid] = upto - own;
-    if (tid == 63) a.plan->items = upto;
-  }
-  __syncthreads();
-  for (int i = tid; i < 2 * a.tiles; i += THREADS) {
-    int len;
-    const int n = count_of(i), parts = parts_of(i, n, len), keys = i >= a.tiles;
-    const int tile = (i - keys * a.tiles) | (keys << 31);
-    int unit = -1;
-    if (parts > 1) {
-      unit = atomicAdd(&units, parts * (keys + 1));
-      a.splits[atomicAdd(&splits, 1)] = Split{tile, unit, parts, 0};
-    }
-    int at = atomicAdd(&hist[bucket_of(i, len)], parts);
-    for (int p = 0; p < parts; ++p, ++at)
-      a.list[at] = Item{tile, p * len, min(len, n - p * len),
-                        parts > 1 ? unit + p * (keys + 1) : -1};
-  }
-  __syncthreads();
-  if (tid == 0) a.plan->splits = splits;
+  });
 }
 
 int64_t round_up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -739,6 +765,8 @@ hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream) 
   b.row_lse = (float*)a.workspace;
   b.row_delta = (float*)(a.workspace + l.delta);
   b.N = f.n_tokens, b.nb = f.n_blocks, b.heads = f.heads, b.tiles = l.tiles, b.words = l.words;
+  b.block = a.block;
+  b.list_here = l.words == 1;
   b.units = (float*)(a.workspace + l.units);
   b.max_units = (int32_t)l.max_units;
   b.share = SHARE * f.heads / l.slots;
@@ -760,12 +788,11 @@ hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream) 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (sparse) {
-    const dim3 grid((uint32_t)((2 * l.tiles + PLAN_WAVES - 1) / PLAN_WAVES));
-    if (a.block == 64)
-      plan_kernel<64><<<grid, dim3(64 * PLAN_WAVES), 0, stream>>>(b);
-    else
-      plan_kernel<128><<<grid, dim3(64 * PLAN_WAVES), 0, stream>>>(b);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (!b.list_here) {
+      plan_kernel<<<dim3((uint32_t)((2 * l.tiles + PLAN_WAVES - 1) / PLAN_WAVES)),
+                    dim3(64 * PLAN_WAVES), 0, stream>>>(b);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     e = a.block == 64 ? launch_t<64, true>(b, l, stream) : launch_t<128, true>(b, l, stream);
   } else {
     e = launch_t<128, false>(b, l, stream);
