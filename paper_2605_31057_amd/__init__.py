@@ -949,16 +949,16 @@ def _channels(t, dim, device):
     if t.get_device() != device:
         raise ValueError("expected a tensor on the current device")
     shape, strides = t.shape, t.stride()
+    if not shape or shape[-1] != dim:
+        raise ValueError(f"expected rows of {dim} channels")
     if len(shape) != 2:
         try:
             t = t.view(-1, dim)
         except RuntimeError:
             raise ValueError("expected rows at one stride") from None
         shape, strides = t.shape, t.stride()
-    n, d = shape
-    if d != dim:
-        raise ValueError(f"expected rows of {dim} channels")
-    if strides[1] != 1 and d > 1:
+    n = shape[0]
+    if strides[1] != 1:
         raise ValueError("channels must be contiguous")
     if n >> 31:
         raise LvsaError(EUNSUPPORTED, f"{n} rows")

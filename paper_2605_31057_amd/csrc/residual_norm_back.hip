@@ -4,7 +4,8 @@
 // Bound: memory, r, y and the gradients of r and h in, those of x and y out.  Rows are
 // held in registers as forward, norms taken again from them (nothing is saved for the
 // backward pass).  The sums over a frame's rows stay in registers over a unit's rows, are
-// joined in LDS over the teams of a workgroup, and go as one row of partial sums a
+// joined in LDS over the teams of a workgroup, and (unless they are the whole frame's) go as
+// one row of partial sums a
 // workgroup to the second kernel, which adds a frame's in a fixed order; weights, which
 // belong to all frames, take a third.
 #include "residual_norm.h"
@@ -140,6 +141,26 @@ __global__ __launch_bounds__(TEAM ? kNormGroup : 1024) void backward_kernel(cons
     }
   }
 
+  if (a.direct) {   // the team has had all of the frame's rows
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (!ok[v]) continue;
+      const int32_t col = 8 * (t + team * v);
+      const int64_t at = (int64_t)u.f * a.dim + col;
+      float w[8], b[8];
+      load_param(a.weight, a.param_type, col, 1.f, w);
+      load_param(a.bias, a.param_type, col, 0.f, b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = w[k] * sa[v][k] + b[k] * sb[v][k];
+      if (a.d_scale) store_param(a.d_scale, a.param_type, at, w);
+      if (a.d_shift) store_param(a.d_shift, a.param_type, at, sb[v]);
+      load_param(a.post_weight, a.param_type, col, 1.f, w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] *= sc[v][k];
+      if (a.d_gate) store_param(a.d_gate, a.param_type, at, w);
+    }
+    return;
+  }
   if (!a.partial) return;
   if (TEAM && a.joined) {
     // V is 1: a team's columns are 8 t .. 8 t + 7.
@@ -281,10 +302,16 @@ struct Backward {
 
 }  // namespace
 
+// Frames of few rows, one team each: their sums are whole in its registers.  (With sums for
+// the weights too they go the other way.)
+bool norm_direct(const NormArgs& a) {
+  return a.units == 1 && !a.d_weight && !a.d_bias && !a.d_post_weight;
+}
+
 // Bytes: the partial sums and, for the weights, a row of three sums a frame.
 int64_t norm_workspace(const NormArgs& a) {
   const bool weights = a.d_weight || a.d_bias || a.d_post_weight;
-  if (!weights && !a.d_gate && !a.d_scale && !a.d_shift) return 0;
+  if (norm_direct(a) || (!weights && !a.d_gate && !a.d_scale && !a.d_shift)) return 0;
   return (partial_rows(a) + (weights ? a.frames : 0)) * 3 * a.dim * 4;
 }
 
@@ -292,6 +319,7 @@ hipError_t launch_norm_backward(const NormArgs& args, int32_t stream_type, int32
                                 hipStream_t stream) {
   NormArgs a = args;
   const bool weights = a.d_weight || a.d_bias || a.d_post_weight;
+  a.direct = norm_direct(a);
   a.frame_sums = a.partial && weights ? a.partial + partial_rows(a) * 3 * a.dim : nullptr;
   hipError_t e = norm_dispatch(stream_type, block_type, norm_team(a.dim), Backward{a, stream});
   if (e != hipSuccess || !a.partial) return e;

@@ -440,3 +440,111 @@ def test_captured():
         want = _pass(*fresh, m)
         for t, name in zip(got, ("out", "dq", "dk", "dv")):
             assert torch.equal(t, want[name])
+
+
+def test_shared_heads_and_slices_of_a_projection():
+    """Keys and values that all heads share (expanded), queries as a slice of a fused
+    projection: the shared tensors' gradients are the sums over the heads."""
+    H, n = 4, 300
+    g = torch.Generator().manual_seed(5)
+    qkv = torch.randn(n, H + 2, 128, generator=g).to(BF).cuda()
+    grad = torch.randn(H, n, 128, generator=g).to(BF).cuda()
+    leaf = qkv.clone().requires_grad_()
+    q = leaf[:, :H].transpose(0, 1)
+    k, v = (leaf[:, H + i: H + i + 1].transpose(0, 1).expand(H, n, 128) for i in range(2))
+    L.dense_attention(q, k, v).backward(grad)
+    full = [qkv[:, :H].transpose(0, 1).contiguous(),
+            *(qkv[:, H + i].expand(H, n, 128).contiguous() for i in range(2))]
+    want = _pass(*full, grad, None)
+    assert torch.equal(leaf.grad[:, :H].transpose(0, 1), want["dq"])
+    for i, name in ((0, "dk"), (1, "dv")):
+        total = want[name].double().sum(0)
+        # autograd adds four bf16 gradients, a rounding each time
+        room = 4 * 2.0 ** -8 * want[name].double().abs().sum(0)
+        assert ((leaf.grad[:, H + i].double() - total).abs() <= room).all()
+
+
+def test_from_two_threads():
+    import threading
+    m = _mask(_kept(700, 64, 0.6), 700, 64)
+    x = [_inputs(2, 700, seed=s) for s in range(2)]
+    want = [_pass(*t, m) for t in x]
+    torch.cuda.synchronize()
+    got = [None, None]
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(5):
+                got[i] = _pass(*x[i], m)
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for g, w in zip(got, want):
+        assert all(torch.equal(g[k], w[k]) for k in w)
+
+
+def test_a_training_step_of_a_block():
+    """Norm and modulation, rotary positions, attention under an LVSA mask, gate and
+    residual, the next norm, as a block of a video transformer has them: gradients of the
+    input and of every parameter against the same step in 64 bits."""
+    T, h, w, H = 6, 8, 10, 3
+    P, n, dim = h * w, T * h * w, H * 128
+    g = torch.Generator().manual_seed(11)
+
+    def normal(*shape, size=1.0):
+        return torch.randn(*shape, generator=g) * size
+
+    params = {"x": normal(n, dim), "mod": normal(T, 5, dim, size=0.3),
+              "wqkv": normal(dim, 3 * dim, size=dim ** -0.5), "wo": normal(dim, dim, size=dim ** -0.5),
+              "qk": 1 + normal(2, 128, size=0.1)}
+    grad = normal(n, dim), normal(n, dim)
+    csr = L.build_mask(T, P, 64, 3, L.Params(window=1, tper=3))
+    row_ptr, col_idx = csr.arrays()
+    nb = len(row_ptr) - 1
+    kept = np.zeros((nb, nb), bool)
+    for r in range(nb):
+        kept[r, col_idx[row_ptr[r]: row_ptr[r + 1]]] = True
+    csr.upload()
+
+    # the library's step: products in bf16, the stream in 32 bits
+    leaf = {k: v.cuda().requires_grad_() for k, v in params.items()}
+    shift, scale, gate, scale2, shift2 = leaf["mod"].unbind(1)
+    first = L.ResidualNorm(dim, frame_tokens=P)
+    heads = L.ResidualNorm(128, norm=L.NORM_RMS)
+    rope = L.Rope(T, h, w)
+    a = L.residual_norm(first, leaf["x"], scale=scale, shift=shift, dtype=BF)
+    q, k, v = (a @ leaf["wqkv"].to(BF)).view(n, 3, H, 128).unbind(1)
+    q, k = (L.residual_norm(heads, t.contiguous(), weight=leaf["qk"][i]) for i, t in ((0, q), (1, k)))
+    q, k = (L.rope(t.transpose(0, 1), rope) for t in (q, k))
+    o = L.attention(q, k, v.transpose(0, 1), csr.device_mask())
+    y = o.transpose(0, 1).reshape(n, dim) @ leaf["wo"].to(BF)
+    r, out = L.residual_norm(first, leaf["x"], y.float(), gate=gate, scale=scale2, shift=shift2)
+    torch.autograd.backward((r, out), [t.cuda() for t in grad])
+
+    # in 64 bits
+    wide = {k: v.double().cuda().requires_grad_() for k, v in params.items()}
+    wide["wqkv"].data.copy_(params["wqkv"].to(BF).double())
+    wide["wo"].data.copy_(params["wo"].to(BF).double())
+    shift, scale, gate, scale2, shift2 = wide["mod"].unbind(1)
+    of = torch.arange(n, device="cuda") // P
+    a = OT.after(wide["x"], "layer", 1e-6, of, scale=scale, shift=shift)
+    q, k, v = (a @ wide["wqkv"]).view(n, 3, H, 128).unbind(1)
+    eye = torch.eye(128, device="cuda")[:, None].expand(128, n, 128).contiguous()
+    turn = L.rope(eye, rope).double().permute(1, 0, 2)          # [token, element, rotated]
+    q, k = (OT.unit(t, "rms", 1e-6) * wide["qk"][i] for i, t in ((0, q), (1, k)))
+    q, k = (torch.bmm(t, turn).transpose(0, 1) for t in (q, k))
+    s = q @ k.transpose(1, 2) / math.sqrt(128)
+    s = s.masked_fill(~OT.kept_tokens(kept, 64, n).cuda(), -math.inf)
+    y = (torch.softmax(s, -1) @ v.transpose(0, 1)).transpose(0, 1).reshape(n, dim) @ wide["wo"]
+    r2, out2 = OT.residual_norm(wide["x"], y, "layer", "none", 1e-6, 1.0, P, gate=gate, scale=scale2,
+                                shift=shift2)
+    torch.autograd.backward((r2, out2), [t.double().cuda() for t in grad])
+    # a dozen tensors on the way are rounded to bf16, 2^-8 / sqrt(3) of their values in the
+    # mean each, independently: below 12 ** 0.5 * 2^-8 / 3 ** 0.5 = 2^-7 together; twice that
+    for got, want in ((r, r2), (out, out2), *((leaf[k].grad, wide[k].grad) for k in leaf)):
+        off = (got.detach().double() - want.detach()).norm() / want.detach().norm()
+        assert off <= 2.0 ** -6, float(off)

@@ -134,6 +134,25 @@ def test_shapes(n, dim, frame, kind):
     _backward(plan, t, gr, gh, kind, "none", 1.0, frame)
 
 
+@pytest.mark.parametrize("n,dim,frame", [(200, 128, 1), (90, 512, 3), (77, 1536, 1), (2100, 640, 2),
+                                         (33, 16000, 1)])
+@pytest.mark.parametrize("names", [("gate", "scale", "shift"), ("gate",),
+                                   ("gate", "scale", "shift", "weight", "bias", "post_weight")])
+def test_frames_of_few_tokens(n, dim, frame, names):
+    """A row of gate, scale and shift for each token or two: a frame is one team's, its
+    gradients written without partial sums (with the weights' too, without)."""
+    plan, t, gr, gh = _case(n, dim, frame, params=BF, post="rms", names=names)
+    _forward(plan, t, "layer", "rms", 1.0, frame)
+    _backward(plan, t, gr, gh, "layer", "rms", 1.0, frame)
+    params = {k: v for k, v in t.items() if k not in ("x", "y")}
+    every = L.residual_norm_backward(plan, gh, gr, t["x"], t["y"], **params)
+    few = [k for k in ("x", "y", "gate", "scale", "shift") if k in t]
+    got = L.residual_norm_backward(plan, gh, gr, t["x"], t["y"], wanted=few, **params)
+    for k in few:      # the same sums either way, but for fused roundings
+        a, b = got[k].double(), every[k].double()
+        assert ((a - b).abs() <= 2.0 ** -7 * b.abs() + 2.0 ** -20).all(), k
+
+
 TYPES = [(BF, BF), (HF, HF), (SF, SF), (SF, BF), (SF, HF)]
 
 

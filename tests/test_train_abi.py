@@ -252,7 +252,8 @@ def test_binding_refusals():
     x = torch.zeros(256).as_strided((2 ** 31, 256), (0, 1))
     with pytest.raises(L.LvsaError):
         L._channels(x, 256, -1)
-    for t in (torch.zeros(4, 128), torch.zeros(256, 4).t(), torch.zeros(4, 3, 512)[:, ::2, :256]):
+    for t in (torch.zeros(4, 128), torch.zeros(256, 4).t(), torch.zeros(4, 3, 512)[:, ::2, :256],
+              torch.zeros(4, 3, 512), torch.zeros(512), torch.zeros(())):
         with pytest.raises(ValueError):
             L._channels(t, 256, -1)
     with pytest.raises(ValueError):
