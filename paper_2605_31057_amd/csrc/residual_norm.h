@@ -66,18 +66,23 @@ void norm_units(NormArgs& a, bool backward);
 int64_t norm_workspace(const NormArgs& a);
 bool norm_direct(const NormArgs& a);
 
-// Threads that work a row: 16 or 64 of a workgroup of 256, or the whole workgroup
-// (`team` 0), eight columns each, past 8192 columns sixteen.
+// Threads that work a row: 16 or 64 of a workgroup of 256, or the whole workgroup of at most
+// 768 or 1024 (`team`), eight columns each, past 8192 columns sixteen.  The bound is also one
+// on registers, 168 or 128 a thread; the gradients of a stream in 32 bits take 148 (with 128
+// they spill: 32,760 rows of 5,120 columns 692 us against 654).
 struct NormTeam {
   int32_t team, threads, eights;
 };
 inline NormTeam norm_team(int32_t dim) {
-  const int32_t c8 = dim / 8;
+  const int32_t c8 = dim / 8, threads = (c8 + 63) / 64 * 64;
   if (c8 <= 16) return {16, 16, 1};
   if (c8 <= 64) return {64, 64, 1};
-  if (c8 <= 1024) return {0, (c8 + 63) / 64 * 64, 1};
-  return {0, 1024, 2};
+  if (threads <= 768) return {768, threads, 1};
+  if (c8 <= 1024) return {1024, threads, 1};
+  return {1024, 1024, 2};
 }
+inline __host__ __device__ constexpr bool whole_group(int team) { return team > 64; }
+inline __host__ __device__ constexpr int norm_bound(int team) { return team > 64 ? team : 256; }
 constexpr int kNormGroup = 256;   // threads of a workgroup of several teams
 
 // Eight parameters from element i on, as floats (`none` without them).
@@ -175,10 +180,10 @@ template <int TEAM, int V, bool BACK>
 __device__ __forceinline__ RowStats row_stats(const float (&x)[V][8], const float (&g)[V][8],
                                               const bool (&ok)[V], int32_t kind, float inv_dim,
                                               int32_t dim, float eps, StatsLds* lds, int& turn) {
-  constexpr int WAVE = TEAM == 0 ? 64 : TEAM;
+  constexpr int WAVE = whole_group(TEAM) ? 64 : TEAM;
   const bool layer = kind == LVSA_NORM_LAYER;
   float n = (float)dim;
-  if constexpr (TEAM == 0) {
+  if constexpr (whole_group(TEAM)) {
     // Columns of this wave: eights 64 w .. 64 w + 63 of each of the V stretches.
     n = 0.f;
     for (int v = 0; v < V; ++v) {
@@ -211,7 +216,7 @@ __device__ __forceinline__ RowStats row_stats(const float (&x)[V][8], const floa
     gs = sum_team_wave<WAVE>(gs);
   }
   RowStats r = {mean, 0.f, 0.f, 0.f};
-  if constexpr (TEAM == 0) {
+  if constexpr (whole_group(TEAM)) {
     const int wave = threadIdx.x / 64, waves = blockDim.x / 64, lane = threadIdx.x % 16;
     float(*const at)[8] = lds->v[turn];
     turn ^= 1;
@@ -265,8 +270,9 @@ template <typename S, typename Y, typename F>
 hipError_t norm_dispatch_team(const NormTeam& t, F&& fn) {
   if (t.team == 16) return fn.template run<S, Y, 16, 1>();
   if (t.team == 64) return fn.template run<S, Y, 64, 1>();
-  if (t.eights == 1) return fn.template run<S, Y, 0, 1>();
-  return fn.template run<S, Y, 0, 2>();
+  if (t.team == 768) return fn.template run<S, Y, 768, 1>();
+  if (t.eights == 1) return fn.template run<S, Y, 1024, 1>();
+  return fn.template run<S, Y, 1024, 2>();
 }
 template <typename F>
 hipError_t norm_dispatch(int32_t stream_type, int32_t block_type, const NormTeam& t, F&& fn) {
