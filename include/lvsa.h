@@ -622,7 +622,9 @@ lvsa_status lvsa_attention_lse(const lvsa_tensor* q, const lvsa_tensor* k,
  * lvsa_attention_backward_workspace gives for the same q and mask; any content; written
  * by the call, so calls that may overlap in time need one each.
  * No atomics on floats: the result is the same every time for given shapes, mask and
- * device.  Shape limits are lvsa_attention's.
+ * device.  Shape limits are lvsa_attention's, and heads * n_tokens < 2^29.  delta, the row
+ * sums of grad_out out, takes out as it was rounded: a query whose weight lies on a few
+ * keys, where e is what is left of a difference, has up to 2^-8 of that difference in e.
  * Errors: EINVAL (nulls, shape mismatch, overlapping, workspace too small), EUNSUPPORTED
  * (head_dim, block, alignment, strides, sizes), EDEVICE (launch). */
 lvsa_status lvsa_attention_backward(const lvsa_tensor* grad_out, const lvsa_tensor* q,
@@ -639,7 +641,8 @@ lvsa_status lvsa_attention_backward_workspace(const lvsa_tensor* q,
  * NULL; h is NULL for norm NONE.  r may be x itself and h y itself (same type and
  * strides), else they overlap neither each other nor an input.
  * Errors: EINVAL (nulls, ranges, shapes, rows of r or h that share elements),
- * EUNSUPPORTED (dim, types, alignment, strides), EDEVICE (launch). */
+ * EUNSUPPORTED (dim, types, alignment, strides, work-items of a launch: rows times dim / 8
+ * past 2^31 or so, back 2^22 frames), EDEVICE (launch). */
 lvsa_status lvsa_residual_norm_forward(const lvsa_residual_norm* p, const lvsa_rows* x,
                                        const lvsa_rows* y, lvsa_rows* r, lvsa_rows* h,
                                        void* stream);

@@ -64,7 +64,8 @@ lvsa_status norm_args(const lvsa_residual_norm* p, int32_t n, bool backward, Nor
   a->gate_st = p->gate_stride, a->scale_st = p->scale_stride, a->shift_st = p->shift_stride;
   a->weight = p->weight, a->bias = p->bias, a->post_weight = p->post_weight;
   norm_units(*a, backward);
-  // Work-items of a launch.
+  // Work-items of a launch; back, of that which adds up frames too.
+  if (backward && a->frames > 1 << 22) return LVSA_EUNSUPPORTED;
   if ((int64_t)a->frames * a->units * norm_team(a->dim).threads + 1024 > INT32_MAX)
     return LVSA_EUNSUPPORTED;
   return LVSA_OK;

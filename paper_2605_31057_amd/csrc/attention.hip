@@ -1418,7 +1418,8 @@ __global__ __launch_bounds__(64) void zero_counters_kernel(uint64_t* __restrict_
   if (threadIdx.x < kTileCounters) ctr[threadIdx.x] = 0;
 }
 
-// Compute units of the current device (cached per device).
+}  // namespace
+
 int cu_count() {
   static std::atomic<int> cached[64];
   int dev = 0;
@@ -1432,6 +1433,8 @@ int cu_count() {
   }
   return n;
 }
+
+namespace {
 
 // How a launch's tiles are split (see Split): `whole` tiles of 256 / kgw rows,
 // the rest in parts of 256 / kgs rows.

@@ -33,7 +33,6 @@
 // leaving registers, and X0 and X1 are read from LDS twice, by rows (ds_read_b128) and
 // transposed (ds_read_b64_tr_b16).
 #include <algorithm>
-#include <atomic>
 
 #include "attention_lds.h"
 
@@ -55,7 +54,7 @@ constexpr int UNIT = ROWS * D;        // floats of a part's sums: one for dq, tw
 // Costs of a step of 64 streamed rows, in products; an item longer than MIN_COST and than
 // SHARE of a workgroup slot's part of the whole launch is split.
 constexpr int COST[2] = {3, 4};       // queries, keys
-constexpr int MIN_COST = 12;
+constexpr int MIN_COST = 8;
 constexpr double SHARE = 0.8;
 constexpr int SLOTS = 2;              // workgroups a compute unit
 
@@ -665,20 +664,6 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void plan_kernel(const BArgs a) {
 }
 
 int64_t round_up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-
-int cu_count() {
-  static std::atomic<int> cached[64];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = 0;
-  int n = cached[dev].load(std::memory_order_relaxed);
-  if (n <= 0) {
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
-        n <= 0)
-      n = 256;
-    cached[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
 
 // How a call's work is laid out, and where in its workspace what lies.
 struct Layout {

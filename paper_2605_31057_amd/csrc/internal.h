@@ -97,6 +97,9 @@ int64_t attention_backward_workspace(int32_t heads, int32_t n_tokens, int32_t n_
                                      bool sparse);
 hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream);
 
+// Compute units of the current device, cached per device (attention.hip).
+int cu_count();
+
 // Per-device pool of tile-counter sets (api.cpp).  acquire hands out a set no
 // launch in flight uses; release records, after the launch on `stream`, the
 // event that frees it again (or keeps the set for good when the stream is

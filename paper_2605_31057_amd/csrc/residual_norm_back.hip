@@ -6,11 +6,11 @@
 // in 32 bits 612 and 15 (4.8 TB/s in all).  Rows are held in registers as forward, norms taken
 // again from them (nothing is saved for the backward pass); eight columns a thread, as the
 // sums of three more rows stay there too (32 columns a thread took 300 registers, one wave a
-// SIMD: 315 us), the next row's loads going out before a row is worked (170 us without).  The sums over a frame's rows stay in registers over a unit's rows, are
-// joined in LDS over the teams of a workgroup, and (unless they are the whole frame's) go as
-// one row of partial sums a
-// workgroup to the second kernel, which adds a frame's in a fixed order; weights, which
-// belong to all frames, take a third.
+// SIMD: 315 us), the next row's loads going out before a row is worked (170 us without).
+// The sums over a frame's rows stay in registers over a unit's rows, are joined in LDS over
+// the teams of a workgroup, and (unless they are the whole frame's) go as one row of partial
+// sums a workgroup to the second kernel, which adds a frame's in a fixed order; weights,
+// which belong to all frames, take a third.
 #include "residual_norm.h"
 
 namespace lvsa {

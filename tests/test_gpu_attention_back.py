@@ -234,6 +234,33 @@ def test_masks_of_thousands_of_blocks():
                     ).all(), (b, name)
 
 
+def test_every_key_past_8000_blocks():
+    """One head of 8,001 blocks of 64 and some, every key: log-sum-exps and dq of sampled
+    queries, dk and dv of sampled keys (with the call's own log-sum-exps and output, which the
+    first part checks)."""
+    n = 8001 * 64 + 21
+    q, k, v, grad = _inputs(1, n, seed=4)
+    every = L.BlockMask(n, 64, -(-n // 64), -(-n // 64), None, None)
+    out, lse = L.attention_lse(q, k, v, every)
+    dq, dk, dv = L.attention_backward(grad, q, k, v, out, lse, every)
+    at = torch.tensor([0, 1, 63, 64, 300000, n - 22, n - 21, n - 1], device="cuda")
+    wide = [t[0].double() for t in (q, k, v, grad)]
+    s = wide[0][at] @ wide[1].T / math.sqrt(128)
+    want = torch.logsumexp(s, -1)
+    assert ((lse[0, at].double() - want).abs() <= 1e-5 * (1 + want.abs())).all()
+    p = torch.exp(s - want[:, None])
+    o = p @ wide[2]
+    # out and gradients: roundings that do not know of each other, in the 2-norm
+    assert (out[0, at].double() - o).norm() <= OT.NORM * o.norm()
+    e = p * (wide[3][at] @ wide[2].T - (wide[3][at] * o).sum(-1, keepdim=True))
+    w = e @ wide[1] / math.sqrt(128)
+    assert (dq[0, at].double() - w).norm() <= OT.NORM * w.norm()
+    p = torch.exp(wide[0] @ wide[1][at].T / math.sqrt(128) - lse[0].double()[:, None])
+    e = p * (wide[3] @ wide[2][at].T - (wide[3] * out[0].double()).sum(-1, keepdim=True))
+    for got, w in ((dv, p.T @ wide[3]), (dk, e.T @ wide[0] / math.sqrt(128))):
+        assert (got[0, at].double() - w).norm() <= OT.NORM * w.norm()
+
+
 def test_the_same_every_time():
     x = _inputs(3, 900, seed=4)
     m = _mask(_kept(900, 64, 0.5), 900, 64)

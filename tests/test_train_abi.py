@@ -238,6 +238,8 @@ def test_residual_norm_backward_refusals():
     assert lib.lvsa_residual_norm_workspace(ref(_plan()), 0, ref(g), ref(need)) == L.EINVAL
     assert lib.lvsa_residual_norm_workspace(ref(_plan()), 10, None, ref(need)) == L.EINVAL
     assert lib.lvsa_residual_norm_workspace(ref(_plan()), 10, ref(g), None) == L.EINVAL
+    assert call(p=_plan(frame=1, dim=64), gh=_rows(GH, n=2 ** 23), gr=_rows(GR, n=2 ** 23),
+                r=_rows(R, n=2 ** 23), y=_rows(Y, n=2 ** 23), g=_grads(n=2 ** 23)) == L.EUNSUPPORTED
     # no gradient of y without y
     assert call(p=_plan(gate=None), y=None) == L.EINVAL
 
