@@ -500,6 +500,7 @@ class _Fast:
         self.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         self.bf16 = torch.bfloat16
         self.empty, self.empty_like = torch.empty, torch.empty_like
+        self.contiguous = torch.contiguous_format
         self.device = torch.cuda.current_device
         # The current stream of a device, as an address.
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -1054,7 +1055,7 @@ def _launch_norm(plan, x, y, params, dtype, r, h):
     if y is not None:
         ty = _byref(_Rows(*_channels(y, dim, dev)))
         if r is None:
-            r = f.empty_like(x) if x.is_contiguous() else f.empty(shape, dtype=kind, device=x.device)
+            r = f.empty_like(x, memory_format=f.contiguous)
             tr = _byref(_Rows(r.data_ptr(), n, dim))
         else:
             tr = _byref(_Rows(*_channels(r, dim, dev)))
@@ -1063,9 +1064,7 @@ def _launch_norm(plan, x, y, params, dtype, r, h):
     if h is not None:
         th = _byref(_Rows(*_channels(h, dim, dev)))
     elif c.norm:
-        like = x if y is None else y
-        h = (f.empty_like(like) if like.dtype is block and like.is_contiguous()
-             else f.empty(shape, dtype=block, device=x.device))
+        h = f.empty_like(x, dtype=block, memory_format=f.contiguous)
         th = _byref(_Rows(h.data_ptr(), n, dim))
     status = f.norm(_byref(c), _byref(_Rows(at, n, stride)), ty, tr, th, f.stream(dev))
     if status:
@@ -1104,12 +1103,16 @@ def _launch_norm_back(plan, grad_h, grad_r, r, y, params, wanted, grad_x, grad_y
     f = _FAST
     dev = f.device()
     dim = plan.dim
-    some = next((t for t in (r, grad_r, y) if t is not None), grad_h)
-    stream = next((t.dtype for t in (r, grad_r) if t is not None), some.dtype)
-    block = next((t.dtype for t in (grad_h, y) if t is not None), some.dtype)
+    of_stream = r if r is not None else grad_r
+    of_block = grad_h if grad_h is not None else y
+    some = of_stream if of_stream is not None else of_block
+    if some is None:
+        raise ValueError("expected a gradient")
+    shape, stream = some.shape, some.dtype
+    block = stream if of_block is None else of_block.dtype
     for t, kind in ((r, stream), (grad_r, stream), (grad_x, stream), (grad_h, block), (y, block),
                     (grad_y, block)):
-        if t is not None and (t.shape != some.shape or t.dtype != kind):
+        if t is not None and (t.shape != shape or t.dtype != kind):
             raise ValueError("expected tensors of r's shape, gradients of their tensors' types")
     rows = [None if t is None else _Rows(*_channels(t, dim, dev)) for t in (grad_h, grad_r, r, y)]
     n = next(t.n for t in rows if t is not None)
@@ -1118,12 +1121,14 @@ def _launch_norm_back(plan, grad_h, grad_r, r, y, params, wanted, grad_x, grad_y
     for name, kind, out in (("x", stream, grad_x), ("y", block, grad_y)):
         if name in wanted:
             if out is None:
-                out = f.empty(some.shape, dtype=kind, device=some.device)
-            setattr(g, name, _Rows(*_channels(out, dim, dev)))
+                out = f.empty_like(some, dtype=kind, memory_format=f.contiguous)
+                setattr(g, name, _Rows(out.data_ptr(), n, dim))
+            else:
+                setattr(g, name, _Rows(*_channels(out, dim, dev)))
             found[name] = out
     for name, t in zip(_PARAMS, params):
         if name in wanted:
-            found[name] = out = f.empty(t.shape, dtype=t.dtype, device=t.device)
+            found[name] = out = f.empty_like(t, memory_format=f.contiguous)
             setattr(g, name, out.data_ptr())
     need = _i64()
     _check(f.norm_workspace(_byref(c), n, _byref(g), _byref(need)), "lvsa_residual_norm_workspace")
