@@ -571,8 +571,7 @@ __device__ __forceinline__ int walk_word(const BArgs& a, int i, int w) {
 }
 
 // Whether this workgroup is the last of `groups` to come here.  Its thread 0's ticket
-// releases what the workgroup has written, which the barrier puts before it, and acquires
-// what the others have.
+// releases what its wave has written, and acquires what the others' first waves have.
 __device__ __forceinline__ bool last_group(const BArgs& a, PlanLds& L, int groups) {
   __syncthreads();
   if (threadIdx.x == 0)
@@ -649,14 +648,19 @@ __global__ __launch_bounds__(256) void prep_kernel(const BArgs a) {
 constexpr int PLAN_WAVES = 16;
 __global__ __launch_bounds__(64 * PLAN_WAVES) void plan_kernel(const BArgs a) {
   __shared__ PlanLds L;
-  const int mine = (int)blockIdx.x * PLAN_WAVES + (int)threadIdx.x / 64, lane = threadIdx.x % 64;
-  if (mine < 2 * a.tiles) {
-    int n = 0;
-    for (int w = lane; w < a.words; w += 64) n += walk_word(a, mine, w);
-    for (int d = 32; d; d /= 2) n += __shfl_xor(n, d);
-    if (lane == 0)
-      __hip_atomic_store(&a.counts[mine], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
+  __shared__ int own[PLAN_WAVES];
+  const int first = (int)blockIdx.x * PLAN_WAVES;
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+  int n = 0;
+  if (first + wave < 2 * a.tiles)
+    for (int w = lane; w < a.words; w += 64) n += walk_word(a, first + wave, w);
+  for (int d = 32; d; d /= 2) n += __shfl_xor(n, d);
+  if (lane == 0) own[wave] = n;
+  __syncthreads();
+  // The first wave stores them all: the ticket's release waits for its wave's stores alone.
+  if (tid < PLAN_WAVES && first + tid < 2 * a.tiles)
+    __hip_atomic_store(&a.counts[first + tid], own[tid], __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
   if (!last_group(a, L, (int)gridDim.x)) return;
   make_list<64 * PLAN_WAVES>(a, L, [&](int i) {
     return __hip_atomic_load(&a.counts[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
