@@ -51,12 +51,20 @@ constexpr int TILE = 4 * SLAB;        // bytes of a streamed tile
 constexpr int MAX_WORDS = (kMaxSparseBlocks + 31) / 32;   // of a bitmap
 constexpr int UNIT = ROWS * D;        // floats of a part's sums: one for dq, two for dk and dv
 
-// Costs of a step of 64 streamed rows, in products; an item longer than MIN_COST and than
-// SHARE of a workgroup slot's part of the whole launch is split.
+// Costs of a step of 64 streamed rows, in products.  An item of cost c is split into c / T
+// parts.  Fewer items than workgroup slots: T is the least (of FITS, each 2% above the one
+// before, from a slot's share of the launch on) that leaves no more parts than slots.  A
+// compute unit with one workgroup runs it nearly twice as fast as one of two, so slots left
+// over cost little and a second round of few much: 8 heads of 4,096 tokens 191 us in 512
+// whole items, 214 in 1,024 parts; 1 of 16,384 380 in 512 parts, 398 in 768, 449 in 640.
+// More items than slots: T = (0.8 + 0.7 / rounds) shares, so that long ones end with the
+// rest.  Never below MIN_COST.
 constexpr int COST[2] = {3, 4};       // queries, keys
 constexpr int MIN_COST = 8;
-constexpr double SHARE = 0.8;
+constexpr double SHARE = 0.8, SHARE_ROUND = 0.7;
 constexpr int SLOTS = 2;              // workgroups a compute unit
+constexpr int FITS = 64, FIT_ITEMS = 512;   // items of a head for which T is sought
+__host__ __device__ inline int fit_at(int T, int j) { return (int)(T * exp2f(j * (1.f / 35.f))); }
 
 enum { Q = 0, GO = 1, K = 2, V = 3, O = 4 };   // tensors read
 
@@ -99,7 +107,8 @@ struct BArgs {
   int32_t max_units;         // of a head
   int32_t parts[2], len[2];  // without a mask: parts of every item, blocks of each
   int32_t unit0[2];          // and where their units begin
-  double share;              // SHARE * heads / slots
+  int32_t room;              // parts of a head that fit at once, 0: not sought
+  double share;              // T: parts of a head's costs
 };
 
 __device__ __forceinline__ bf16x8 row_frag(const char* tile, uint32_t at, int row0, int stp) {
@@ -492,29 +501,47 @@ __global__ __launch_bounds__(64 * WAVES) void combine_kernel(const BArgs a) {
 
 // The items of one head from the blocks of its walks, count_of(i) for item i < 2 tiles
 // (queries' tiles, then keys'), the longest first, by one workgroup.  An item of cost c
-// (steps times products) is split where c > T = max(MIN_COST, share * C), C the sum of all
+// (steps times products) is split where c > T >= max(MIN_COST, share * C), C the sum of all
 // costs, into at most c / T + 1 < 2 c / T parts.  So there are at most C / T parts more than
-// items and at most 4 C / T units (two for a part of keys), which the host bounds by the two
-// parts of T.  Order among items of like cost, and where parts lie, follow atomics; results
+// items and at most 4 C / T units (two for a part of keys), which the host bounds by T's two
+// bounds.  Order among items of like cost, and where parts lie, follow atomics; results
 // do not depend on either.
 struct PlanLds {
   unsigned long long total;
-  int last, units, splits, hist[64];
+  int last, units, splits, fit, hist[64];
+  int cost[FIT_ITEMS];
 };
 template <int THREADS, typename F>
 __device__ __forceinline__ void make_list(const BArgs& a, PlanLds& L, F&& count_of) {
   const int tid = threadIdx.x, lane = tid % 64;
   const int steps = a.block / STEP;
   if (tid < 64) L.hist[tid] = 0;
-  if (tid == 0) L.total = 0ull, L.units = 0, L.splits = 0;
+  if (tid == 0) L.total = 0ull, L.units = 0, L.splits = 0, L.fit = FITS;
   __syncthreads();
   auto cost_of = [&](int i, int n) { return n * steps * COST[i >= a.tiles]; };
   unsigned long long sum = 0ull;
-  for (int i = tid; i < 2 * a.tiles; i += THREADS) sum += (unsigned long long)cost_of(i, count_of(i));
+  for (int i = tid; i < 2 * a.tiles; i += THREADS) {
+    const int c = cost_of(i, count_of(i));
+    sum += (unsigned long long)c;
+    if (a.room) L.cost[i] = c;
+  }
   for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
   if (lane == 0) atomicAdd(&L.total, sum);
   __syncthreads();
-  const int T = max(MIN_COST, (int)min(a.share * (double)L.total, 1e9) + 1);
+  int T = max(MIN_COST, (int)min(a.share * (double)L.total, 1e9) + 1);
+  if (a.room) {   // each wave up to the least of its T
+    bool fits = false;
+    for (int j = tid / 64; j < FITS && !fits; j += THREADS / 64) {
+      const int t = fit_at(T, j);
+      int parts = 0;
+      for (int i = lane; i < 2 * a.tiles; i += 64) parts += max(1, (L.cost[i] + t - 1) / t);
+      for (int d = 32; d; d /= 2) parts += __shfl_xor(parts, d);
+      fits = parts <= a.room;
+      if (lane == 0 && fits) atomicMin(&L.fit, j);
+    }
+    __syncthreads();
+    if (L.fit < FITS) T = fit_at(T, L.fit);
+  }
   // Parts of an item, and blocks of each.
   auto parts_of = [&](int i, int n, int& len) {
     const int c = cost_of(i, n), want = c > T ? min((c + T - 1) / T, n) : 1;
@@ -672,6 +699,8 @@ int64_t round_up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // How a call's work is laid out, and where in its workspace what lies.
 struct Layout {
   int32_t tiles, words, slots;
+  int32_t room;
+  double share;
   int32_t parts[2] = {1, 1}, len[2], unit0[2] = {0, 0};
   int64_t max_items, max_splits, max_units;     // of a head
   int64_t delta, by_row, by_col, plan, counts, list, splits, units, bytes;
@@ -684,6 +713,9 @@ Layout layout_of(int32_t heads, int32_t n, int32_t nb, bool sparse) {
   l.slots = SLOTS * cu_count();
   const int64_t steps = 2 * (int64_t)l.tiles;
   const int64_t cost = l.tiles * steps * (COST[0] + COST[1]);   // of a head, at most
+  const double rounds = 2. * l.tiles * heads / l.slots;
+  l.room = rounds <= 1. && 2 * l.tiles <= FIT_ITEMS ? l.slots / heads : 0;
+  l.share = (l.room ? 1. : SHARE + SHARE_ROUND / rounds) * heads / l.slots;
   if (sparse) {
     // C / T, by plan_kernel's two bounds of T.
     const int64_t ratio =
@@ -692,11 +724,18 @@ Layout layout_of(int32_t heads, int32_t n, int32_t nb, bool sparse) {
     l.max_splits = std::min<int64_t>(2 * l.tiles, ratio);
     l.max_units = 4 * ratio;
   } else {
-    const double T = std::max((double)MIN_COST, SHARE * heads * (double)cost / l.slots);
+    int T = std::max(MIN_COST, (int)std::min(l.share * (double)cost, 1e9) + 1);
+    auto parts_of = [&](int k, int t) { return (steps * COST[k] + t - 1) / t; };
+    for (int j = 0; l.room && j < FITS; ++j) {
+      const int t = fit_at(T, j);
+      if (l.tiles * (parts_of(0, t) + parts_of(1, t)) <= l.room) {
+        T = t;
+        break;
+      }
+    }
     l.max_items = l.max_splits = l.max_units = 0;
     for (int k = 1; k >= 0; --k) {
-      const double parts = steps * COST[k] / T;
-      const int64_t want = parts > 1. ? std::min((int64_t)parts + 1, (int64_t)nb) : 1;
+      const int64_t want = std::min(parts_of(k, T), (int64_t)nb);
       l.len[k] = (int32_t)((nb + want - 1) / want);
       l.parts[k] = (nb + l.len[k] - 1) / l.len[k];
       l.unit0[k] = (int32_t)l.max_units;
@@ -758,7 +797,8 @@ hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream) 
   b.list_here = l.words == 1;
   b.units = (float*)(a.workspace + l.units);
   b.max_units = (int32_t)l.max_units;
-  b.share = SHARE * f.heads / l.slots;
+  b.room = l.room;
+  b.share = l.share;
   for (int k = 0; k < 2; ++k)
     b.parts[k] = l.parts[k], b.len[k] = l.len[k], b.unit0[k] = l.unit0[k];
   if (sparse) {

@@ -205,6 +205,23 @@ def test_key_blocks_that_every_query_keeps_beside_ones_that_few_do(block):
                    OT.kept_tokens(kept, block, n))
 
 
+@pytest.mark.parametrize("block", [0, 64, 128])
+@pytest.mark.parametrize("more", [0, 1])
+@pytest.mark.parametrize("tiles", [4, 16, 32])
+def test_as_many_items_as_fit_at_once(tiles, more, block):
+    """Tiles of queries and of keys as many as the device takes at once (two workgroups a
+    compute unit), whole or with room for parts, and of a token more."""
+    slots = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    for H in {max(1, slots // (2 * tiles)), max(1, slots // (5 * tiles))}:
+        n = 128 * tiles + more
+        kept = _kept(n, block, 0.3, seed=tiles) | np.eye(-(-n // block), dtype=bool) if block else None
+        x = _inputs(H, n, seed=tiles + more)
+        got = _pass(*x, _mask(kept, n, block) if block else None)
+        for h in {0, H - 1}:
+            _check({k: t[h: h + 1] for k, t in got.items()}, *(t[h: h + 1] for t in x),
+                   OT.kept_tokens(kept, block, n) if block else None)
+
+
 def test_masks_of_thousands_of_blocks():
     """8,000 blocks of 64 (the most), each row with a few: queries and keys at both ends and
     between against the formula over the blocks that they meet."""
