@@ -508,6 +508,27 @@ def test_shared_heads_and_slices_of_a_projection():
         assert ((leaf.grad[:, H + i].double() - total).abs() <= room).all()
 
 
+def test_heads_past_32_bits():
+    """90 heads of 190,000 tokens, 2.19e9 elements a tensor, each block of keys kept by its own
+    queries: heads at both ends and between as in calls of their own."""
+    H, n, block = 90, 190000, 128
+    m = _mask(np.eye(-(-n // block), dtype=bool), n, block)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = [torch.randn(H, n, 128, dtype=BF, device="cuda", generator=g) for _ in range(4)]
+    got = _pass(*x, m)
+    for h in (0, 45, H - 1):
+        q, k, v, grad = (t[h: h + 1] for t in x)
+        out, lse = L.attention_lse(q, k, v, m)
+        # rows' sums may be in other parts: a rounding of out, and fp32 ones
+        assert ((got["out"][h].double() - out[0].double()).abs()
+                <= 2.0 ** -8 * out[0].double().abs() + 1e-5).all()
+        assert ((got["lse"][h] - lse[0]).abs() <= 1e-5 * (1 + lse[0].abs())).all()
+        own = L.attention_backward(grad, q, k, v, got["out"][h: h + 1],
+                                   got["lse"][h: h + 1].contiguous(), m)
+        for name, t in zip(("dq", "dk", "dv"), own):
+            assert torch.equal(got[name][h], t[0]), (h, name)
+
+
 def test_from_two_threads():
     import threading
     m = _mask(_kept(700, 64, 0.6), 700, 64)

@@ -279,6 +279,28 @@ def test_the_same_every_time():
         assert all(torch.equal(first[k], again[k]) for k in first)
 
 
+def test_rows_past_32_bits():
+    """270,000 rows of 8,192 columns, 2.2e9 elements a tensor: rows at both ends and between as
+    in calls of their own, and the sums over all rows of whole numbers, which are exact."""
+    n, dim = 270000, 8192
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, y = (torch.randn(n, dim, dtype=BF, device="cuda", generator=g) for _ in range(2))
+    gh = torch.randint(-2, 3, (n, dim), dtype=torch.int8, device="cuda", generator=g).to(BF)
+    params = {k: torch.randn(1, dim, device="cuda", generator=g) for k in ("gate", "scale", "shift")}
+    plan = L.ResidualNorm(dim, eps=EPS)
+    r, h = L.residual_norm(plan, x, y, **params)
+    grads = L.residual_norm_backward(plan, gh, None, r, y, **params)
+    for at in (slice(0, 3), slice(134000, 134005), slice(n - 7, n)):
+        few = L.residual_norm(plan, x[at], y[at], **params)
+        assert torch.equal(r[at], few[0]) and torch.equal(h[at], few[1])
+        few = L.residual_norm_backward(plan, gh[at], None, r[at], y[at], **params)
+        assert torch.equal(grads["x"][at], few["x"]) and torch.equal(grads["y"][at], few["y"])
+    total = torch.zeros(dim, dtype=torch.float64, device="cuda")
+    for i in range(0, n, 10000):
+        total += gh[i: i + 10000].double().sum(0)
+    assert torch.equal(grads["shift"][0].double(), total)
+
+
 def test_wanted():
     plan, t, gr, gh = _case(60, 256, 16)
     params = {k: t[k] for k in ("gate", "scale", "shift")}
