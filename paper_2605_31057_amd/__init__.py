@@ -972,6 +972,8 @@ def _norm_plan(plan, n, stream, block, params, device):
     first, second = codes.get(stream), codes.get(block)
     if first is None or second is None:
         raise ValueError("expected bfloat16, float16 or float32")
+    if n < 1:
+        raise LvsaError(EINVAL, "no rows")
     c = _ResidualNorm.from_buffer_copy(plan._c)
     c.stream_type, c.block_type = first, second
     frame = plan.frame_tokens or n

@@ -262,6 +262,16 @@ def test_binding_refusals():
         L._channels(torch.zeros(4, 256), 256, 0)
 
 
+def test_no_rows_are_refused_as_by_the_library():
+    L._fast()
+    empty = torch.zeros(0, 256)
+    for frame in (0, 10):
+        plan = L.ResidualNorm(256, frame_tokens=frame)
+        with pytest.raises(L.LvsaError) as e:
+            L._norm_plan(plan, 0, torch.float32, torch.float32, (None, empty, empty) + (None,) * 3, -1)
+        assert e.value.status == L.EINVAL
+
+
 # ----------------------------------------------------------------- the oracle
 
 @pytest.mark.parametrize("masked", [False, True])
