@@ -55,8 +55,6 @@ lvsa_status norm_args(const lvsa_residual_norm* p, int32_t n, bool backward, Nor
       if (st < 0) return LVSA_EINVAL;
       if (st % 8 != 0) return LVSA_EUNSUPPORTED;
     }
-  // Backward, without frames of their own: rows in shares whose sums are added at the end.
-  if (!frames && backward) a->frame = (int32_t)(((int64_t)n + 31) / 32);
   a->frames = (int32_t)(((int64_t)n + a->frame - 1) / a->frame);
   a->norm = p->norm, a->post = p->post, a->param_type = p->param_type;
   a->eps = p->eps, a->a = p->residual;

@@ -9,8 +9,10 @@
 // SIMD: 315 us), the next row's loads going out before a row is worked (170 us without).
 // The sums over a frame's rows stay in registers over a unit's rows, are joined in LDS over
 // the teams of a workgroup, and (unless they are the whole frame's) go as one row of partial
-// sums a workgroup to the second kernel, which adds a frame's in a fixed order; weights,
-// which belong to all frames, take a third.
+// sums a workgroup to the second kernel, which adds a frame's in a fixed order (few frames of
+// many take it in two steps); weights, which belong to all frames, take another.
+#include <algorithm>
+
 #include "residual_norm.h"
 
 namespace lvsa {
@@ -19,6 +21,8 @@ namespace {
 // Sums over rows (sum_rows): SLICES threads share the rows of four columns, a workgroup works
 // LANES fours of columns.
 constexpr int SLICES = 32, LANES = 16;
+constexpr int MIN_SHARED = 192;   // partial sums of a frame from which on they are shared out
+                                  // (share_kernel; 191 of them 13.8 us, 256 shared out 14.0)
 
 template <typename S, typename Y, int TEAM, int V, int MODE>
 __global__ __launch_bounds__(norm_bound(TEAM)) void backward_kernel(const NormArgs a) {
@@ -240,13 +244,15 @@ __device__ __forceinline__ void put4(void* p, int32_t type, int64_t i, f32x4v x)
 }
 
 // A frame's sums: the gradients of its gate, scale and shift, and what it adds to those
-// of the weights (to frame_sums).
-__global__ __launch_bounds__(SLICES* LANES) void frame_kernel(const NormArgs a, int32_t per_frame) {
+// of the weights (to frame_sums; a single frame's are the gradients, which saves a launch:
+// 64 rows of 1,536 columns with five parameters 11.8 -> 9.4 us).
+__global__ __launch_bounds__(SLICES* LANES) void frame_kernel(const NormArgs a, const float* rows,
+                                                              int32_t per_frame) {
   __shared__ f32x4v lds[3][SLICES][LANES];
   const int32_t f = blockIdx.x;
   const int32_t col = 4 * (int32_t)(blockIdx.y * LANES + threadIdx.x % LANES);
   f32x4v s[3];
-  sum_rows(a.partial + (int64_t)f * per_frame * 3 * a.dim, per_frame, a.dim, col, s, lds);
+  sum_rows(rows + (int64_t)f * per_frame * 3 * a.dim, per_frame, a.dim, col, s, lds);
   if (threadIdx.x < LANES && col < a.dim) {
     const int64_t at = (int64_t)f * a.dim + col;
     const f32x4v w = param4(a.weight, a.param_type, col, 1.f);
@@ -254,15 +260,36 @@ __global__ __launch_bounds__(SLICES* LANES) void frame_kernel(const NormArgs a, 
     put4(a.d_scale, a.param_type, at, w * s[0] + b * s[1]);
     put4(a.d_shift, a.param_type, at, s[1]);
     put4(a.d_gate, a.param_type, at, param4(a.post_weight, a.param_type, col, 1.f) * s[2]);
+    const f32x4v k = param4(a.scale, a.param_type, (int64_t)f * a.scale_st + col, 0.f) + 1.f;
+    const f32x4v g = param4(a.gate, a.param_type, (int64_t)f * a.gate_st + col, 1.f);
     if (a.frame_sums) {
-      const f32x4v k = param4(a.scale, a.param_type, (int64_t)f * a.scale_st + col, 0.f) + 1.f;
       float* const to = a.frame_sums + (int64_t)f * 3 * a.dim + col;
       *(f32x4v*)to = k * s[0];
       *(f32x4v*)(to + a.dim) = k * s[1];
-      *(f32x4v*)(to + 2 * (int64_t)a.dim) =
-          param4(a.gate, a.param_type, (int64_t)f * a.gate_st + col, 1.f) * s[2];
+      *(f32x4v*)(to + 2 * (int64_t)a.dim) = g * s[2];
+    } else if (a.frames == 1) {
+      put4(a.d_weight, a.param_type, col, k * s[0]);
+      put4(a.d_bias, a.param_type, col, k * s[1]);
+      put4(a.d_post_weight, a.param_type, col, g * s[2]);
     }
   }
+}
+
+// Few frames of many partial sums: of each frame's `per_frame` rows `shares` equal stretches'
+// sums, [frame][share][3][dim], for the frame kernel.  (One frame of 1,000 rows of 1,536
+// columns 45 -> 24 us, of 32,760 rows 159 -> 140; of 256 rows 18.9 -> 14.0.)
+__global__ __launch_bounds__(SLICES* LANES) void share_kernel(const NormArgs a, float* to,
+                                                              int32_t per_frame, int32_t shares) {
+  __shared__ f32x4v lds[3][SLICES][LANES];
+  const int32_t f = blockIdx.x / shares, share = blockIdx.x % shares;
+  const int32_t col = 4 * (int32_t)(blockIdx.y * LANES + threadIdx.x % LANES);
+  const int32_t len = (per_frame + shares - 1) / shares, first = min(share * len, per_frame);
+  f32x4v s[3];
+  sum_rows(a.partial + ((int64_t)f * per_frame + first) * 3 * a.dim, min(len, per_frame - first),
+           a.dim, col, s, lds);
+  if (threadIdx.x >= LANES || col >= a.dim) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) *(f32x4v*)(to + ((int64_t)blockIdx.x * 3 + w) * a.dim + col) = s[w];
 }
 
 // Those of the weights, over the frames.  (The frame kernel's last workgroup of each group of
@@ -283,6 +310,15 @@ int64_t partial_rows(const NormArgs& a) {
   const NormTeam t = norm_team(a.dim);
   const int64_t teams = whole_group(t.team) ? 1 : kNormGroup / t.team;
   return (int64_t)a.frames * (a.joined ? a.units / teams : a.units);
+}
+
+// Workgroups that add up four columns each, and a frame's shares, 1: its sums in one go.
+uint32_t wide_of(const NormArgs& a) { return (uint32_t)((a.dim / 4 + LANES - 1) / LANES); }
+int32_t shares_of(const NormArgs& a) {
+  const int64_t per = partial_rows(a) / a.frames;
+  return per < MIN_SHARED || a.frames * (int64_t)wide_of(a) >= 512
+             ? 1
+             : (int32_t)std::min<int64_t>(SLICES, (per + SLICES - 1) / SLICES);
 }
 
 struct Backward {
@@ -316,20 +352,31 @@ bool norm_direct(const NormArgs& a) {
 int64_t norm_workspace(const NormArgs& a) {
   const bool weights = a.d_weight || a.d_bias || a.d_post_weight;
   if (norm_direct(a) || (!weights && !a.d_gate && !a.d_scale && !a.d_shift)) return 0;
-  return (partial_rows(a) + (weights ? a.frames : 0)) * 3 * a.dim * 4;
+  const int64_t shares = shares_of(a);
+  return (partial_rows(a) + (shares > 1 ? shares * a.frames : 0) +
+          (weights && a.frames > 1 ? a.frames : 0)) * 3 * a.dim * 4;
 }
 
 hipError_t launch_norm_backward(const NormArgs& args, int32_t stream_type, int32_t block_type,
                                 hipStream_t stream) {
   NormArgs a = args;
-  const bool weights = a.d_weight || a.d_bias || a.d_post_weight;
+  const bool weights = (a.d_weight || a.d_bias || a.d_post_weight) && a.frames > 1;
   a.direct = norm_direct(a);
-  a.frame_sums = a.partial && weights ? a.partial + partial_rows(a) * 3 * a.dim : nullptr;
+  const int32_t per_frame = (int32_t)(partial_rows(a) / a.frames), shares = shares_of(a);
+  float* const shared = a.partial ? a.partial + partial_rows(a) * 3 * a.dim : nullptr;
+  a.frame_sums = a.partial && weights
+                     ? shared + (shares > 1 ? (int64_t)shares * a.frames : 0) * 3 * a.dim
+                     : nullptr;
   hipError_t e = norm_dispatch(stream_type, block_type, norm_team(a.dim), Backward{a, stream});
   if (e != hipSuccess || !a.partial) return e;
-  const uint32_t wide = (uint32_t)((a.dim / 4 + LANES - 1) / LANES);
+  const uint32_t wide = wide_of(a);
+  if (shares > 1) {
+    share_kernel<<<dim3((uint32_t)(a.frames * shares), wide), dim3(SLICES * LANES), 0, stream>>>(
+        a, shared, per_frame, shares);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   frame_kernel<<<dim3((uint32_t)a.frames, wide), dim3(SLICES * LANES), 0, stream>>>(
-      a, (int32_t)(partial_rows(a) / a.frames));
+      a, shares > 1 ? shared : a.partial, shares > 1 ? shares : per_frame);
   if ((e = hipGetLastError()) != hipSuccess || !weights) return e;
   weight_kernel<<<dim3(wide), dim3(SLICES * LANES), 0, stream>>>(a);
   return hipGetLastError();

@@ -124,6 +124,20 @@ SHAPES = [(1, 8, 1), (1, 1536, 1), (3, 128, 2), (17, 136, 4), (50, 512, 7), (33,
           (2, 16384, 1), (40, 16000, 15), (11, 72, 3), (300, 64, 100), (1000, 256, 130)]
 
 
+FEW = [(1, 1536, 0), (191, 1536, 0), (192, 1536, 0), (400, 1536, 300), (1000, 520, 0), (900, 2056, 400),
+       (5000, 128, 0), (9000, 64, 4100), (300, 5120, 0), (420, 9000, 0), (2000, 520, 450)]
+
+
+@pytest.mark.parametrize("n,dim,frame", FEW)
+@pytest.mark.parametrize("names", [("gate", "scale", "shift", "weight", "bias", "post_weight"),
+                                   ("gate", "scale", "shift"), ("weight", "bias"), ("post_weight",)])
+def test_few_frames(n, dim, frame, names):
+    """One frame or a few of many rows, whose sums are added in two steps from some number on."""
+    post = "rms" if "post_weight" in names else "none"
+    plan, t, gr, gh = _case(n, dim, frame, BF, BF, post=post, names=names, seed=n)
+    _backward(plan, t, gr, gh, "layer", post, 1.0, frame)
+
+
 @pytest.mark.parametrize("n,dim,frame", SHAPES)
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 def test_shapes(n, dim, frame, kind):
