@@ -66,7 +66,7 @@ void norm_units(NormArgs& a, bool backward);
 int64_t norm_workspace(const NormArgs& a);
 bool norm_direct(const NormArgs& a);
 
-// Threads that work a row: 16 or 64 of a workgroup of 256, or the whole workgroup of at most
+// Threads that work a row: 16, 32 or 64 of a workgroup of 256, or the whole workgroup of at most
 // 768 or 1024 (`team`), eight columns each, past 8192 columns sixteen.  The bound is also one
 // on registers, 168 or 128 a thread; the gradients of a stream in 32 bits take 148 (with 128
 // they spill: 32,760 rows of 5,120 columns 692 us against 654).
@@ -76,6 +76,7 @@ struct NormTeam {
 inline NormTeam norm_team(int32_t dim) {
   const int32_t c8 = dim / 8, threads = (c8 + 63) / 64 * 64;
   if (c8 <= 16) return {16, 16, 1};
+  if (c8 <= 32) return {32, 32, 1};
   if (c8 <= 64) return {64, 64, 1};
   if (threads <= 768) return {768, threads, 1};
   if (c8 <= 1024) return {1024, threads, 1};
@@ -142,19 +143,22 @@ __device__ __forceinline__ float sum16(float x) {
   x = add_dpp<0x141>(x);   // row_half_mirror
   return add_dpp<0x140>(x);   // row_mirror
 }
-// Over the wave: the four rows by swaps, [x0 x0 x2 x2] + [x1 x1 x3 x3], then halves.
-__device__ __forceinline__ float sum64(float x) {
+// Over 32, and over the wave: rows of 16 by swaps, [x0 x0 x2 x2] + [x1 x1 x3 x3], then halves.
+__device__ __forceinline__ float sum32(float x) {
   x = sum16(x);
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
                                                   false);
-  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float sum64(float x) {
+  x = sum32(x);
   const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
                                                   false);
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 template <int TEAM>
 __device__ __forceinline__ float sum_team_wave(float x) {
-  return TEAM == 16 ? sum16(x) : sum64(x);
+  return TEAM == 16 ? sum16(x) : TEAM == 32 ? sum32(x) : sum64(x);
 }
 
 // What a row's norm and its gradient need of the whole row: mean (0 for the RMS norm),
@@ -269,6 +273,7 @@ inline NormMode norm_mode(const NormArgs& a) {
 template <typename S, typename Y, typename F>
 hipError_t norm_dispatch_team(const NormTeam& t, F&& fn) {
   if (t.team == 16) return fn.template run<S, Y, 16, 1>();
+  if (t.team == 32) return fn.template run<S, Y, 32, 1>();
   if (t.team == 64) return fn.template run<S, Y, 64, 1>();
   if (t.team == 768) return fn.template run<S, Y, 768, 1>();
   if (t.eights == 1) return fn.template run<S, Y, 1024, 1>();
