@@ -63,6 +63,7 @@ constexpr int COST[2] = {3, 4};       // queries, keys
 constexpr int MIN_COST = 8;
 constexpr double SHARE = 0.8, SHARE_ROUND = 0.7;
 constexpr int SLOTS = 2;              // workgroups a compute unit
+constexpr int HERE = 2;               // words of a bitmap that one workgroup of prep_kernel works
 constexpr int FITS = 64, FIT_ITEMS = 512;   // items of a head for which T is sought
 __host__ __device__ inline int fit_at(int T, int j) { return (int)(T * exp2f(j * (1.f / 35.f))); }
 
@@ -102,7 +103,7 @@ struct BArgs {
   Split* splits;
   float* units;
   int32_t N, nb, block, heads, tiles, words;
-  int32_t list_here;         // prep_kernel makes the list (one word: up to 32 blocks)
+  int32_t list_here;         // prep_kernel makes the list (up to 32 HERE blocks)
   int32_t stat_groups;       // prep: workgroups of 64 rows
   int32_t max_units;         // of a head
   int32_t parts[2], len[2];  // without a mask: parts of every item, blocks of each
@@ -615,6 +616,7 @@ __device__ __forceinline__ bool last_group(const BArgs& a, PlanLds& L, int group
 __global__ __launch_bounds__(256) void prep_kernel(const BArgs a) {
   extern __shared__ uint32_t bits[];
   __shared__ PlanLds plan;
+  __shared__ int counts[2 * 32 * HERE];
   if ((int)blockIdx.x < a.stat_groups) {
     const int c = 8 * (threadIdx.x % 16);
     bf16x8 x[4], o[4];
@@ -643,31 +645,43 @@ __global__ __launch_bounds__(256) void prep_kernel(const BArgs a) {
     return;
   }
   if (!a.list_here && (int)blockIdx.x == a.stat_groups && threadIdx.x == 0) a.plan->done = 0;
-  const int nb = a.nb, words = a.words, group = (int)blockIdx.x - a.stat_groups;
+  const int nb = a.nb, words = a.words;
   uint32_t* const rows = bits;               // [32][words]
   uint32_t* const cols = bits + 32 * words;  // [nb]
-  for (int i = threadIdx.x; i < 32 * words + nb; i += 256) bits[i] = 0u;
-  __syncthreads();
-  // Eight threads a row.
-  const int r = threadIdx.x / 8, row = 32 * group + r;
-  if (row < nb) {
-    const int32_t hi = a.row_ptr[row + 1];
-    for (int32_t i = a.row_ptr[row] + (int)threadIdx.x % 8; i < hi; i += 8) {
-      const uint32_t kb = (uint32_t)a.col_idx[i];
-      if (kb >= (uint32_t)nb) continue;
-      atomicOr(&rows[r * words + kb / 32], 1u << (kb % 32));
-      atomicOr(&cols[kb], 1u << r);
+  const int own = (int)blockIdx.x - a.stat_groups;
+  for (int group = own; group < (a.list_here ? words : own + 1); ++group) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * words + nb; i += 256) bits[i] = 0u;
+    __syncthreads();
+    // Eight threads a row.
+    const int r = threadIdx.x / 8, row = 32 * group + r;
+    if (row < nb) {
+      const int32_t hi = a.row_ptr[row + 1];
+      for (int32_t i = a.row_ptr[row] + (int)threadIdx.x % 8; i < hi; i += 8) {
+        const uint32_t kb = (uint32_t)a.col_idx[i];
+        if (kb >= (uint32_t)nb) continue;
+        atomicOr(&rows[r * words + kb / 32], 1u << (kb % 32));
+        atomicOr(&cols[kb], 1u << r);
+      }
     }
+    __syncthreads();
+    const int mine = min(32, nb - 32 * group) * words;
+    for (int i = threadIdx.x; i < mine; i += 256)
+      a.by_row[(int64_t)32 * group * words + i] = rows[i];
+    for (int i = threadIdx.x; i < nb; i += 256) a.by_col[(int64_t)group * nb + i] = cols[i];
   }
-  __syncthreads();
-  const int mine = min(32, nb - 32 * group) * words;
-  for (int i = threadIdx.x; i < mine; i += 256) a.by_row[(int64_t)32 * group * words + i] = rows[i];
-  for (int i = threadIdx.x; i < nb; i += 256) a.by_col[(int64_t)group * nb + i] = cols[i];
   // One workgroup has all bitmaps: it makes the list too, which saves a launch (5 us of the
-  // 42 of one head of 1,024 tokens).
+  // 42 of one head of 1,024 tokens; two of 4,200 in blocks of 128 47.3 -> 43.3 us; with 94
+  // blocks 63.5 -> 62.3 where they are few a row and 103 -> 105 where they are many).
   if (!a.list_here) return;
   __syncthreads();
-  make_list<256>(a, plan, [&](int i) { return walk_word(a, i, 0); });
+  for (int i = threadIdx.x; i < 2 * a.tiles; i += 256) {
+    int n = 0;
+    for (int w = 0; w < words; ++w) n += walk_word(a, i, w);
+    counts[i] = n;
+  }
+  __syncthreads();
+  make_list<256>(a, plan, [&](int i) { return counts[i]; });
 }
 
 // The list where there are many blocks: a wave counts each walk's, the workgroup that is
@@ -794,7 +808,7 @@ hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream) 
   b.row_delta = (float*)(a.workspace + l.delta);
   b.N = f.n_tokens, b.nb = f.n_blocks, b.heads = f.heads, b.tiles = l.tiles, b.words = l.words;
   b.block = a.block;
-  b.list_here = l.words == 1;
+  b.list_here = l.words <= HERE;
   b.units = (float*)(a.workspace + l.units);
   b.max_units = (int32_t)l.max_units;
   b.room = l.room;
@@ -812,7 +826,7 @@ hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream) 
   }
   b.stat_groups = (int32_t)(((int64_t)f.heads * f.n_tokens + 63) / 64);
   const uint32_t lds = sparse ? (32u * l.words + f.n_blocks) * 4u : 0u;
-  prep_kernel<<<dim3((uint32_t)(b.stat_groups + (sparse ? l.words : 0))), dim3(256), lds,
+  prep_kernel<<<dim3((uint32_t)(b.stat_groups + (!sparse ? 0 : b.list_here ? 1 : l.words))), dim3(256), lds,
                 stream>>>(b);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

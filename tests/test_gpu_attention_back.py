@@ -105,6 +105,16 @@ def test_rows_and_columns_without_blocks(block):
 
 
 @pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("blocks", [31, 32, 33, 63, 64, 65, 97])
+def test_bitmaps_of_whole_words_and_a_block_more(blocks, block):
+    n = blocks * block - 3
+    kept = _kept(n, block, 0.3, seed=blocks, empty=(4,)) & ~(np.arange(blocks) == 31)[None]
+    kept[:, -1] = True
+    x = _inputs(1, n, seed=blocks)
+    _check(_pass(*x, _mask(kept, n, block)), *x, OT.kept_tokens(kept, block, n))
+
+
+@pytest.mark.parametrize("block", [64, 128])
 def test_an_empty_mask(block):
     n = 3 * block - 1
     x = _inputs(2, n)
