@@ -49,6 +49,7 @@ struct NormArgs {
   float* frame_sums;               // [frames][3][dim], weighted for the weights' gradients
   int32_t joined;                  // the teams of a workgroup share a partial sum
   int32_t direct;                  // a frame is one unit, its gradients need no partial sums
+  int32_t weights;                 // gradients of weight, bias or post_weight are wanted
   void* d_gate;
   void* d_scale;
   void* d_shift;
@@ -64,7 +65,6 @@ hipError_t launch_norm_backward(const NormArgs& a, int32_t stream_type, int32_t 
 // Sets a's units for a pass over its rows (backward: with sums of columns).
 void norm_units(NormArgs& a, bool backward);
 int64_t norm_workspace(const NormArgs& a);
-bool norm_direct(const NormArgs& a);
 
 // Threads that work a row: 16, 32 or 64 of a workgroup of 256, or the whole workgroup of at most
 // 768 or 1024 (`team`), eight columns each, past 8192 columns sixteen.  The bound is also one

@@ -9,8 +9,8 @@
 // SIMD: 315 us), the next row's loads going out before a row is worked (170 us without).
 // The sums over a frame's rows stay in registers over a unit's rows, are joined in LDS over
 // the teams of a workgroup, and (unless they are the whole frame's) go as one row of partial
-// sums a workgroup to the second kernel, which adds a frame's in a fixed order (few frames of
-// many take it in two steps); weights, which belong to all frames, take another.
+// sums a workgroup to the second kernel, which adds a frame's in a fixed order; weights, which
+// belong to all frames, take another, and long sums a step between.
 #include <algorithm>
 
 #include "residual_norm.h"
@@ -23,6 +23,8 @@ namespace {
 constexpr int SLICES = 32, LANES = 16;
 constexpr int MIN_SHARED = 192;   // partial sums of a frame from which on they are shared out
                                   // (share_kernel; 191 of them 13.8 us, 256 shared out 14.0)
+constexpr int MAX_SHARES = 512;
+constexpr int ENOUGH = 512;       // workgroups that need no shares
 
 template <typename S, typename Y, int TEAM, int V, int MODE>
 __global__ __launch_bounds__(norm_bound(TEAM)) void backward_kernel(const NormArgs a) {
@@ -166,6 +168,25 @@ __global__ __launch_bounds__(norm_bound(TEAM)) void backward_kernel(const NormAr
 #pragma unroll
       for (int k = 0; k < 8; ++k) w[k] *= sc[v][k];
       if (a.d_gate) store_param(a.d_gate, a.param_type, at, w);
+      if (!a.weights) continue;
+      load_param(a.scale, a.param_type, (int64_t)u.f * a.scale_st + col, 0.f, w);
+      load_param(a.gate, a.param_type, (int64_t)u.f * a.gate_st + col, 1.f, b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        sa[v][k] *= 1.f + w[k];
+        sb[v][k] *= 1.f + w[k];
+        sc[v][k] *= b[k];
+      }
+      if (a.frame_sums) {
+        float* const to = a.frame_sums + 3 * (int64_t)u.f * a.dim + col;
+        store8(to, sa[v]);
+        store8(to + a.dim, sb[v]);
+        store8(to + 2 * (int64_t)a.dim, sc[v]);
+      } else {   // the only frame
+        if (a.d_weight) store_param(a.d_weight, a.param_type, col, sa[v]);
+        if (a.d_bias) store_param(a.d_bias, a.param_type, col, sb[v]);
+        if (a.d_post_weight) store_param(a.d_post_weight, a.param_type, col, sc[v]);
+      }
     }
     return;
   }
@@ -277,15 +298,18 @@ __global__ __launch_bounds__(SLICES* LANES) void frame_kernel(const NormArgs a, 
 
 // Few frames of many partial sums: of each frame's `per_frame` rows `shares` equal stretches'
 // sums, [frame][share][3][dim], for the frame kernel.  (One frame of 1,000 rows of 1,536
-// columns 45 -> 24 us, of 32,760 rows 159 -> 140; of 256 rows 18.9 -> 14.0.)
-__global__ __launch_bounds__(SLICES* LANES) void share_kernel(const NormArgs a, float* to,
-                                                              int32_t per_frame, int32_t shares) {
+// columns 45 -> 24 us, of 32,760 rows 159 -> 140; of 256 rows 18.9 -> 14.0.)  And of many
+// frames' sums for the weights (4,000 rows of 1,536 columns, each a frame, 422 -> 77 us, with
+// the frames' gradients from the first kernel).
+__global__ __launch_bounds__(SLICES* LANES) void share_kernel(const NormArgs a, const float* rows,
+                                                              float* to, int32_t per_frame,
+                                                              int32_t shares) {
   __shared__ f32x4v lds[3][SLICES][LANES];
   const int32_t f = blockIdx.x / shares, share = blockIdx.x % shares;
   const int32_t col = 4 * (int32_t)(blockIdx.y * LANES + threadIdx.x % LANES);
   const int32_t len = (per_frame + shares - 1) / shares, first = min(share * len, per_frame);
   f32x4v s[3];
-  sum_rows(a.partial + ((int64_t)f * per_frame + first) * 3 * a.dim, min(len, per_frame - first),
+  sum_rows(rows + ((int64_t)f * per_frame + first) * 3 * a.dim, min(len, per_frame - first),
            a.dim, col, s, lds);
   if (threadIdx.x >= LANES || col >= a.dim) return;
 #pragma unroll
@@ -295,11 +319,12 @@ __global__ __launch_bounds__(SLICES* LANES) void share_kernel(const NormArgs a, 
 // Those of the weights, over the frames.  (The frame kernel's last workgroup of each group of
 // columns doing it instead takes a release of every workgroup's sums: 68 us against 16 for
 // both kernels at 21 frames of 5,120 columns.)
-__global__ __launch_bounds__(SLICES* LANES) void weight_kernel(const NormArgs a) {
+__global__ __launch_bounds__(SLICES* LANES) void weight_kernel(const NormArgs a, const float* rows,
+                                                               int32_t n) {
   __shared__ f32x4v lds[3][SLICES][LANES];
   const int32_t col = 4 * (int32_t)(blockIdx.x * LANES + threadIdx.x % LANES);
   f32x4v s[3];
-  sum_rows(a.frame_sums, a.frames, a.dim, col, s, lds);
+  sum_rows(rows, n, a.dim, col, s, lds);
   if (threadIdx.x >= LANES || col >= a.dim) return;
   put4(a.d_weight, a.param_type, col, s[0]);
   put4(a.d_bias, a.param_type, col, s[1]);
@@ -312,13 +337,10 @@ int64_t partial_rows(const NormArgs& a) {
   return (int64_t)a.frames * (a.joined ? a.units / teams : a.units);
 }
 
-// Workgroups that add up four columns each, and a frame's shares, 1: its sums in one go.
+// Workgroups along the columns of a sum, and the shares of `n` rows, 1: added in one go.
 uint32_t wide_of(const NormArgs& a) { return (uint32_t)((a.dim / 4 + LANES - 1) / LANES); }
-int32_t shares_of(const NormArgs& a) {
-  const int64_t per = partial_rows(a) / a.frames;
-  return per < MIN_SHARED || a.frames * (int64_t)wide_of(a) >= 512
-             ? 1
-             : (int32_t)std::min<int64_t>(SLICES, (per + SLICES - 1) / SLICES);
+int32_t shares_of(int64_t n) {
+  return n < MIN_SHARED ? 1 : (int32_t)std::min<int64_t>(MAX_SHARES, (n + SLICES - 1) / SLICES);
 }
 
 struct Backward {
@@ -340,45 +362,65 @@ struct Backward {
   }
 };
 
+// Where the sums lie, in rows of three: a workgroup's or team's, the shares of each frame's,
+// the frames' weighted for the weights, and shares of those.
+struct Sums {
+  bool direct, any, weights;
+  int32_t per_frame, shares, weight_shares;
+  int64_t shared, frames, weight_shared, rows;
+};
+Sums sums_of(const NormArgs& a) {
+  Sums s = {};
+  s.weights = a.d_weight || a.d_bias || a.d_post_weight;
+  s.any = s.weights || a.d_gate || a.d_scale || a.d_shift;
+  s.direct = a.units == 1;
+  if (!s.any) return s;
+  s.per_frame = (int32_t)(partial_rows(a) / a.frames);
+  s.shares = s.direct || a.frames * (int64_t)wide_of(a) >= ENOUGH ? 1 : shares_of(s.per_frame);
+  s.weight_shares = wide_of(a) >= ENOUGH ? 1 : shares_of(a.frames);
+  s.shared = s.direct ? 0 : partial_rows(a);
+  s.frames = s.shared + (s.shares > 1 ? (int64_t)s.shares * a.frames : 0);
+  s.weight_shared = s.frames + (s.weights && a.frames > 1 ? a.frames : 0);
+  s.rows = s.weight_shared + (s.weights && s.weight_shares > 1 ? s.weight_shares : 0);
+  return s;
+}
+
 }  // namespace
 
-// Frames of few rows, one team each: their sums are whole in its registers.  (With sums for
-// the weights too they go the other way.)
-bool norm_direct(const NormArgs& a) {
-  return a.units == 1 && !a.d_weight && !a.d_bias && !a.d_post_weight;
-}
-
-// Bytes: the partial sums and, for the weights, a row of three sums a frame.
-int64_t norm_workspace(const NormArgs& a) {
-  const bool weights = a.d_weight || a.d_bias || a.d_post_weight;
-  if (norm_direct(a) || (!weights && !a.d_gate && !a.d_scale && !a.d_shift)) return 0;
-  const int64_t shares = shares_of(a);
-  return (partial_rows(a) + (shares > 1 ? shares * a.frames : 0) +
-          (weights && a.frames > 1 ? a.frames : 0)) * 3 * a.dim * 4;
-}
+int64_t norm_workspace(const NormArgs& a) { return sums_of(a).rows * 3 * a.dim * 4; }
 
 hipError_t launch_norm_backward(const NormArgs& args, int32_t stream_type, int32_t block_type,
                                 hipStream_t stream) {
   NormArgs a = args;
-  const bool weights = (a.d_weight || a.d_bias || a.d_post_weight) && a.frames > 1;
-  a.direct = norm_direct(a);
-  const int32_t per_frame = (int32_t)(partial_rows(a) / a.frames), shares = shares_of(a);
-  float* const shared = a.partial ? a.partial + partial_rows(a) * 3 * a.dim : nullptr;
-  a.frame_sums = a.partial && weights
-                     ? shared + (shares > 1 ? (int64_t)shares * a.frames : 0) * 3 * a.dim
-                     : nullptr;
+  const Sums s = sums_of(a);
+  auto at = [&](int64_t row) { return args.partial + row * 3 * a.dim; };
+  // Frames of few rows, one team each: their sums are whole in its registers.
+  a.direct = s.direct && s.any;
+  a.weights = s.weights;
+  a.frame_sums = s.weights && a.frames > 1 ? at(s.frames) : nullptr;
+  if (s.direct || !s.any) a.partial = nullptr;
   hipError_t e = norm_dispatch(stream_type, block_type, norm_team(a.dim), Backward{a, stream});
-  if (e != hipSuccess || !a.partial) return e;
   const uint32_t wide = wide_of(a);
-  if (shares > 1) {
-    share_kernel<<<dim3((uint32_t)(a.frames * shares), wide), dim3(SLICES * LANES), 0, stream>>>(
-        a, shared, per_frame, shares);
+  const dim3 block(SLICES * LANES);
+  if (e == hipSuccess && s.any && !s.direct) {
+    if (s.shares > 1) {
+      share_kernel<<<dim3((uint32_t)(a.frames * s.shares), wide), block, 0, stream>>>(
+          a, a.partial, at(s.shared), s.per_frame, s.shares);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    frame_kernel<<<dim3((uint32_t)a.frames, wide), block, 0, stream>>>(
+        a, s.shares > 1 ? at(s.shared) : a.partial, s.shares > 1 ? s.shares : s.per_frame);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || !a.frame_sums) return e;
+  if (s.weight_shares > 1) {
+    share_kernel<<<dim3((uint32_t)s.weight_shares, wide), block, 0, stream>>>(
+        a, a.frame_sums, at(s.weight_shared), a.frames, s.weight_shares);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  frame_kernel<<<dim3((uint32_t)a.frames, wide), dim3(SLICES * LANES), 0, stream>>>(
-      a, shares > 1 ? shared : a.partial, shares > 1 ? shares : per_frame);
-  if ((e = hipGetLastError()) != hipSuccess || !weights) return e;
-  weight_kernel<<<dim3(wide), dim3(SLICES * LANES), 0, stream>>>(a);
+  weight_kernel<<<dim3(wide), block, 0, stream>>>(
+      a, s.weight_shares > 1 ? at(s.weight_shared) : a.frame_sums,
+      s.weight_shares > 1 ? s.weight_shares : a.frames);
   return hipGetLastError();
 }
 

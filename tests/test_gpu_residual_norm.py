@@ -167,6 +167,18 @@ def test_frames_of_few_tokens(n, dim, frame, names):
         assert ((a - b).abs() <= 2.0 ** -7 * b.abs() + 2.0 ** -20).all(), k
 
 
+@pytest.mark.parametrize("n,dim,frame", [(3200, 128, 16), (4001, 136, 21), (800, 1536, 4), (191, 520, 1),
+                                         (192, 520, 1), (200, 9000, 1), (7000, 64, 7), (1, 1536, 0)])
+@pytest.mark.parametrize("names", [("gate", "scale", "shift", "weight", "bias", "post_weight"),
+                                   ("scale", "shift", "weight"), ("gate", "bias")])
+def test_weights_over_many_frames(n, dim, frame, names):
+    """Weights beside a row of gate, scale and shift for every few tokens: their sums over
+    the frames in one step and in two, of frames that are one team's and of longer ones."""
+    post = "rms" if "post_weight" in names else "none"
+    plan, t, gr, gh = _case(n, dim, frame, post=post, names=names, seed=n)
+    _backward(plan, t, gr, gh, "layer", post, 1.0, frame)
+
+
 TYPES = [(BF, BF), (HF, HF), (SF, SF), (SF, BF), (SF, HF)]
 
 
