@@ -58,10 +58,14 @@ constexpr int UNIT = ROWS * D;        // floats of a part's sums: one for dq, tw
 // over cost little and a second round of few much: 8 heads of 4,096 tokens 191 us in 512
 // whole items, 214 in 1,024 parts; 1 of 16,384 380 in 512 parts, 398 in 768, 449 in 640.
 // More items than slots: T = (0.8 + 0.7 / rounds) shares, so that long ones end with the
-// rest.  Never below MIN_COST.
+// rest, but 0.6 without a mask for up to a quarter more of LONG tiles, which whole would take a
+// round of their own (6 heads of 5,723 tokens, 1.05 rounds, 361 us whole, 328 so; 14 of 3,200,
+// 1.37 rounds, 223 and 244; 19 of 2,000, 16 tiles, 143 and 159; under masks, whose items end
+// at different times, 4 of 8,200 in 64-token blocks 199 and 211).  Never below MIN_COST.
 constexpr int COST[2] = {3, 4};       // queries, keys
 constexpr int MIN_COST = 8;
-constexpr double SHARE = 0.8, SHARE_ROUND = 0.7;
+constexpr double SHARE = 0.8, SHARE_ROUND = 0.7, SHARE_FEW_MORE = 0.6, FEW_MORE = 1.25;
+constexpr int LONG = 24;
 constexpr int SLOTS = 2;              // workgroups a compute unit
 constexpr int HERE = 2;               // words of a bitmap that one workgroup of prep_kernel works
 constexpr int FITS = 64, FIT_ITEMS = 512;   // items of a head for which T is sought
@@ -729,11 +733,13 @@ Layout layout_of(int32_t heads, int32_t n, int32_t nb, bool sparse) {
   const int64_t cost = l.tiles * steps * (COST[0] + COST[1]);   // of a head, at most
   const double rounds = 2. * l.tiles * heads / l.slots;
   l.room = rounds <= 1. && 2 * l.tiles <= FIT_ITEMS ? l.slots / heads : 0;
-  l.share = (l.room ? 1. : SHARE + SHARE_ROUND / rounds) * heads / l.slots;
+  const bool few_more = !sparse && rounds < FEW_MORE && l.tiles >= LONG;
+  l.share = (l.room     ? 1.
+             : few_more ? SHARE_FEW_MORE
+                        : SHARE + SHARE_ROUND / rounds) * heads / l.slots;
   if (sparse) {
-    // C / T, by plan_kernel's two bounds of T.
-    const int64_t ratio =
-        std::min((int64_t)((double)l.slots / (SHARE * heads)) + 1, cost / MIN_COST + 1);
+    // C / T, by make_list's two bounds of T.
+    const int64_t ratio = std::min((int64_t)(1. / l.share) + 1, cost / MIN_COST + 1);
     l.max_items = 2 * l.tiles + ratio;
     l.max_splits = std::min<int64_t>(2 * l.tiles, ratio);
     l.max_units = 4 * ratio;

@@ -232,6 +232,17 @@ def test_as_many_items_as_fit_at_once(tiles, more, block):
                    OT.kept_tokens(kept, block, n) if block else None)
 
 
+@pytest.mark.parametrize("tiles", [23, 24, 25])
+def test_a_few_items_more_than_fit_at_once(tiles):
+    """Every key, as many heads as make a few tiles more than the device takes at once."""
+    H = torch.cuda.get_device_properties(0).multi_processor_count // tiles + 1
+    n = 128 * tiles - 5
+    x = _inputs(H, n, seed=tiles)
+    got = _pass(*x, None)
+    for h in (0, H - 1):
+        _check({k: t[h: h + 1] for k, t in got.items()}, *(t[h: h + 1] for t in x))
+
+
 def test_masks_of_thousands_of_blocks():
     """8,000 blocks of 64 (the most), each row with a few: queries and keys at both ends and
     between against the formula over the blocks that they meet."""
