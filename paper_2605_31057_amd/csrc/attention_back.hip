@@ -61,9 +61,10 @@ constexpr int UNIT = ROWS * D;        // floats of a part's sums: one for dq, tw
 // rest, but 0.6 without a mask for up to a quarter more of LONG tiles, which whole would take a
 // round of their own (6 heads of 5,723 tokens, 1.05 rounds, 361 us whole, 328 so; 14 of 3,200,
 // 1.37 rounds, 223 and 244; 19 of 2,000, 16 tiles, 143 and 159; under masks, whose items end
-// at different times, 4 of 8,200 in 64-token blocks 199 and 211).  Never below MIN_COST.
+// at different times, 4 of 8,200 in 64-token blocks 199 and 211).  Never below MIN_COST (4 heads of 1,024 tokens 27.6 us,
+// with 8 33, with 16 28.8).
 constexpr int COST[2] = {3, 4};       // queries, keys
-constexpr int MIN_COST = 8;
+constexpr int MIN_COST = 12;
 constexpr double SHARE = 0.8, SHARE_ROUND = 0.7, SHARE_FEW_MORE = 0.6, FEW_MORE = 1.25;
 constexpr int LONG = 24;
 constexpr int SLOTS = 2;              // workgroups a compute unit
