@@ -61,8 +61,8 @@ constexpr int UNIT = ROWS * D;        // floats of a part's sums: one for dq, tw
 // rest, but 0.6 without a mask for up to a quarter more of LONG tiles, which whole would take a
 // round of their own (6 heads of 5,723 tokens, 1.05 rounds, 361 us whole, 328 so; 14 of 3,200,
 // 1.37 rounds, 223 and 244; 19 of 2,000, 16 tiles, 143 and 159; under masks, whose items end
-// at different times, 4 of 8,200 in 64-token blocks 199 and 211).  Never below MIN_COST (4 heads of 1,024 tokens 27.6 us,
-// with 8 33, with 16 28.8).
+// at different times, 4 of 8,200 in 64-token blocks 199 and 211).  Never below MIN_COST
+// (4 heads of 1,024 tokens 27.6 us, with 8 33, with 16 28.8).
 constexpr int COST[2] = {3, 4};       // queries, keys
 constexpr int MIN_COST = 12;
 constexpr double SHARE = 0.8, SHARE_ROUND = 0.7, SHARE_FEW_MORE = 0.6, FEW_MORE = 1.25;
@@ -833,8 +833,8 @@ hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream) 
   }
   b.stat_groups = (int32_t)(((int64_t)f.heads * f.n_tokens + 63) / 64);
   const uint32_t lds = sparse ? (32u * l.words + f.n_blocks) * 4u : 0u;
-  prep_kernel<<<dim3((uint32_t)(b.stat_groups + (!sparse ? 0 : b.list_here ? 1 : l.words))), dim3(256), lds,
-                stream>>>(b);
+  const int32_t mask_groups = !sparse ? 0 : b.list_here ? 1 : l.words;
+  prep_kernel<<<dim3((uint32_t)(b.stat_groups + mask_groups)), dim3(256), lds, stream>>>(b);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (sparse) {
