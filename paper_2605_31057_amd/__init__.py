@@ -363,6 +363,13 @@ def _mask_keep(mask, tensors):
     return mask
 
 
+def _written(*tensors):
+    """Raises the versions of tensors that the library has written: a graph that has saved
+    one notices."""
+    import torch
+    torch.autograd.graph.increment_version(tensors)
+
+
 def build_mask_device(T, P, B, step, row_ptr, col_idx, params=None, layer=0,
                       stream=None):
     """Device LVSA mask builder into int32 device tensors row_ptr [nb+1] and
@@ -373,8 +380,7 @@ def build_mask_device(T, P, B, step, row_ptr, col_idx, params=None, layer=0,
                                         _p(row_ptr.data_ptr()), _p(col_idx.data_ptr()),
                                         col_idx.numel(), _stream_ptr(stream)),
            "lvsa_build_mask_device")
-    import torch
-    torch.autograd.graph.increment_version([row_ptr, col_idx])
+    _written(row_ptr, col_idx)
     N = T * P + params.text_tokens
     nb = (N + B - 1) // B
     m = BlockMask(N, B, nb, nb, row_ptr.data_ptr(), col_idx.data_ptr())
@@ -384,12 +390,14 @@ def build_mask_device(T, P, B, step, row_ptr, col_idx, params=None, layer=0,
 def build_exact_mask_device(T, P, B, step, row_ptr, entry, params=None, layer=0,
                             stream=None):
     """Device builder of the token-exact form into device tensors (row_ptr
-    int32 [nb+1], entry int32/uint32 [>= nb*nb]); returns an ExactMask."""
+    int32 [nb+1], entry int32/uint32 [>= nb*nb]); returns an ExactMask.  A graph that has
+    saved either notices the write."""
     params = params or Params()
     _check(lib().lvsa_build_exact_mask_device(
         T, P, B, step, layer, ctypes.byref(params), _p(row_ptr.data_ptr()),
         _p(entry.data_ptr()), entry.numel(), _stream_ptr(stream)),
         "lvsa_build_exact_mask_device")
+    _written(row_ptr, entry)
     N = T * P + params.text_tokens
     nb = (N + B - 1) // B
     m = ExactMask(N, B, nb, P, row_ptr.data_ptr(), entry.data_ptr())
@@ -433,12 +441,15 @@ def attention(q, k, v, mask, out=None, stream=None):
     import torch
     if _recording(q, k, v, out):
         return _attend(q, k, v, mask, out, stream)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty_like(q)
     tq, tk, tv, to = (_tensor(x) for x in (q, k, v, out))
     _check(lib().lvsa_attention(ctypes.byref(tq), ctypes.byref(tk), ctypes.byref(tv),
                                 ctypes.byref(mask), ctypes.byref(to),
                                 _stream_ptr(stream)), "lvsa_attention")
+    if given:
+        _written(out)
     return out
 
 
@@ -450,19 +461,23 @@ def attention_noalloc(q, k, v, mask, out, stream=None):
                                         ctypes.byref(tv), ctypes.byref(mask),
                                         ctypes.byref(to), _stream_ptr(stream)),
            "lvsa_attention_noalloc")
+    _written(out)
     return out
 
 
 def attention_exact(q, k, v, mask, out=None, stream=None):
     """Token-exact attention (lvsa_attention_exact): Eq. 2 token for token."""
     import torch
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty_like(q)
     tq, tk, tv, to = (_tensor(x) for x in (q, k, v, out))
     _check(lib().lvsa_attention_exact(ctypes.byref(tq), ctypes.byref(tk),
                                       ctypes.byref(tv), ctypes.byref(mask),
                                       ctypes.byref(to), _stream_ptr(stream)),
            "lvsa_attention_exact")
+    if given:
+        _written(out)
     return out
 
 
@@ -472,12 +487,15 @@ def dense_attention(q, k, v, block=128, out=None, stream=None):
     import torch
     if _recording(q, k, v, out):
         return _attend(q, k, v, _every_key(q, block), out, stream)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty_like(q)
     tq, tk, tv, to = (_tensor(x) for x in (q, k, v, out))
     _check(lib().lvsa_dense_attention(ctypes.byref(tq), ctypes.byref(tk),
                                       ctypes.byref(tv), block, ctypes.byref(to),
                                       _stream_ptr(stream)), "lvsa_dense_attention")
+    if given:
+        _written(out)
     return out
 
 
