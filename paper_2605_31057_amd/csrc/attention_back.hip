@@ -244,18 +244,24 @@ __device__ __forceinline__ void work_item(const BArgs& a, Lds<SPARSE, ROWS / BLO
   const uint32_t chunk = 16u * (uint32_t)((lane % 4) ^ xsw(lrow));
   const uint32_t off0 = (uint32_t)lrow * (uint32_t)(a.st[X0] * 2) + chunk;
   const uint32_t off1 = (uint32_t)lrow * (uint32_t)(a.st[X1] * 2) + chunk;
-  auto rsrc_at = [&](const __bf16* base, int64_t st, int row) {
-    return make_rsrc(base + (int64_t)row * st, (uint32_t)(((int64_t)(N - 1 - row) * st + D) * 2));
+  auto bytes_at = [&](int64_t st, int row) {
+    return (uint32_t)(((int64_t)(N - 1 - row) * st + D) * 2);
   };
-  // Streamed rows row .. row + 63 (row < N) into stage s; rows past N come as zeros.
+  // Streamed rows row .. row + 63 (row < N) into stage s; rows past N come as zeros: their
+  // offsets lie past the buffer's end, also where rows are less than D apart and the next
+  // ones would begin before it.
   auto load_step = [&](int row, int s) {
-    const auto q0 = rsrc_at(x0, a.st[X0], row), q1 = rsrc_at(x1, a.st[X1], row);
+    const uint32_t n0 = bytes_at(a.st[X0], row), n1 = bytes_at(a.st[X1], row);
+    const auto q0 = make_rsrc(x0 + (int64_t)row * a.st[X0], n0);
+    const auto q1 = make_rsrc(x1 + (int64_t)row * a.st[X1], n1);
+    const bool there = row + lrow < N;
+    const uint32_t v0 = there ? off0 : n0, v1 = there ? off1 : n1;
     const uint32_t to =
         (uint32_t)__builtin_amdgcn_readfirstlane(lds_base + 2 * TILE * s + 1024 * wave);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      issue_load(to + 4096u * j, q0, off0, 64u * j);
-      issue_load(to + TILE + 4096u * j, q1, off1, 64u * j);
+      issue_load(to + 4096u * j, q0, v0, 64u * j);
+      issue_load(to + TILE + 4096u * j, q1, v1, 64u * j);
     }
     if (KEYS && wave < 2) {
       const float* const from = wave ? sd : sl;

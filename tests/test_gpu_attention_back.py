@@ -1,5 +1,6 @@
 """Attention's log-sum-exps and gradients against the formulas in 64 bits, element by
 element within the bounds that the kernels' roundings give (oracle/train.py)."""
+import ctypes
 import math
 
 import numpy as np
@@ -634,3 +635,59 @@ def test_a_training_step_of_a_block():
     for got, want in ((r, r2), (out, out2), *((leaf[k].grad, wide[k].grad) for k in leaf)):
         off = (got.detach().double() - want.detach()).norm() / want.detach().norm()
         assert off <= 2.0 ** -6, float(off)
+
+
+@pytest.mark.parametrize("block", [0, 64, 128])
+@pytest.mark.parametrize("H,n", [(1, 1), (2, 5), (2, 70), (1, 127), (3, 150), (1, 321)])
+@pytest.mark.parametrize("stride", [8, 64, 120])
+def test_inputs_whose_rows_share_elements(stride, H, n, block):
+    """Rows a stride of less than 128 apart, each input in turn and all together: the same
+    as their contiguous copies, where rows past the last are not a tail of the last."""
+    kept = _kept(n, block, 0.6, seed=n) | np.eye(-(-n // block), dtype=bool) if block else None
+    m = _mask(kept, n, block) if block else None
+    g = torch.Generator().manual_seed(n)
+
+    def shared(size=1.0):
+        flat = (torch.randn(H, (n - 1) * stride + 128, generator=g) * size).to(BF).cuda()
+        return flat.as_strided((H, n, 128), (flat.stride(0), stride, 1))
+
+    apart = _inputs(H, n, seed=n)
+    # queries whose scores, without a log-sum-exp, would have no finite exponential
+    whole = [shared(30.0), *(shared() for _ in range(3))]
+    out, lse = L.attention_lse(*apart[:3], m)
+    for which in ((0,), (1,), (2,), (3,), (0, 1, 2, 3)):
+        x = [whole[i] if i in which else apart[i] for i in range(4)]
+        alone = [t.contiguous() for t in x]
+        want = _pass(*alone, m)
+        got = {k: torch.empty_like(alone[0]) for k in ("out", "dq", "dk", "dv")}
+        _, got["lse"] = L.attention_lse(*x[:3], m, out=got["out"])
+        L.attention_backward(x[3], *x[:3], got["out"], got["lse"], m,
+                             grads=[got[k] for k in ("dq", "dk", "dv")])
+        assert all(torch.equal(got[k], want[k]) for k in want), which
+    # an output read back through such rows, and gradients as autograd hands them on
+    want = L.attention_backward(apart[3], *apart[:3], whole[0].contiguous(), lse, m)
+    got = L.attention_backward(apart[3], *apart[:3], whole[0], lse, m)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    q, k, v = _leaves(apart)
+    y = L.attention(q, k, v, m) if block else L.dense_attention(q, k, v)
+    y.backward(whole[3])
+    want = L.attention_backward(whole[3].contiguous(), *apart[:3], out, lse, m)
+    assert all(torch.equal(t.grad, w) for t, w in zip((q, k, v), want))
+
+
+def test_a_single_token_of_any_stride():
+    """Through the library itself, as the binding gives a single token the stride of a
+    contiguous one."""
+    ref, f = ctypes.byref, L._fast()
+    x = _inputs(1, 1, seed=3)
+    want = _pass(*x, None)
+    grads = [torch.empty_like(x[0]) for _ in range(3)]
+    need = ctypes.c_int64()
+    for st in (8, 64, 128, 4096):
+        t = [L._Tensor(i.data_ptr(), 1, 1, 128, 128, st) for i in (x[3], *x[:3], want["out"], *grads)]
+        assert f.back_workspace(ref(t[1]), None, ref(need)) == L.OK
+        work = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+        assert f.back(*(ref(i) for i in t[:5]), want["lse"].data_ptr(), None, *(ref(i) for i in t[5:]),
+                      work.data_ptr(), need.value, f.stream(f.device())) == L.OK
+        for g, name in zip(grads, ("dq", "dk", "dv")):
+            assert torch.equal(g, want[name]), (st, name)
