@@ -514,9 +514,9 @@ __global__ __launch_bounds__(64 * WAVES) void combine_kernel(const BArgs a) {
 // The items of one head from the blocks of its walks, count_of(i) for item i < 2 tiles
 // (queries' tiles, then keys'), the longest first, by one workgroup.  An item of cost c
 // (steps times products) is split where c > T >= max(MIN_COST, share * C), C the sum of all
-// costs, into at most c / T + 1 < 2 c / T parts.  So there are at most C / T parts more than
-// items and at most 4 C / T units (two for a part of keys), which the host bounds by T's two
-// bounds.  Order among items of like cost, and where parts lie, follow atomics; results
+// costs, into at most ceil(c / T) <= 2 floor(c / T) parts.  So there are at most C / T parts more
+// than items, no more split ones and at most 4 C / T units (two for a part of keys), which the
+// host bounds by T's two bounds.  Order among items of like cost, and where parts lie, follow atomics; results
 // do not depend on either.
 struct PlanLds {
   unsigned long long total;
@@ -745,11 +745,14 @@ Layout layout_of(int32_t heads, int32_t n, int32_t nb, bool sparse) {
              : few_more ? SHARE_FEW_MORE
                         : SHARE + SHARE_ROUND / rounds) * heads / l.slots;
   if (sparse) {
-    // C / T, by make_list's two bounds of T.
-    const int64_t ratio = std::min((int64_t)(1. / l.share) + 1, cost / MIN_COST + 1);
-    l.max_items = 2 * l.tiles + ratio;
-    l.max_splits = std::min<int64_t>(2 * l.tiles, ratio);
-    l.max_units = 4 * ratio;
+    // C / T by make_list's two bounds of T (the first against the rounding of the division),
+    // and none where no item can cost more than either: a head of 64 tokens would else take
+    // 256 KB, 17 GB for 65,536 of them.
+    int64_t more = std::min((int64_t)(1. / l.share * (1. + 1e-9)), cost / MIN_COST);
+    if (l.share >= 1. || steps * COST[1] <= MIN_COST) more = 0;
+    l.max_items = 2 * l.tiles + more;
+    l.max_splits = std::min<int64_t>(2 * l.tiles, more);
+    l.max_units = 4 * more;
   } else {
     int T = std::max(MIN_COST, (int)std::min(l.share * (double)cost, 1e9) + 1);
     auto parts_of = [&](int k, int t) { return (steps * COST[k] + t - 1) / t; };

@@ -691,3 +691,18 @@ def test_a_single_token_of_any_stride():
                       work.data_ptr(), need.value, f.stream(f.device())) == L.OK
         for g, name in zip(grads, ("dq", "dk", "dv")):
             assert torch.equal(g, want[name]), (st, name)
+
+
+@pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("H,n", [(640, 64), (1, 100), (500, 128), (4096, 17), (256, 256), (512, 250),
+                                 (520, 256), (530, 256), (120, 385), (700, 640)])
+def test_heads_of_few_tokens_under_a_mask(H, n, block):
+    """Calls of so many heads or so few tokens that no item is in parts, and ones on both
+    sides of that; every head kept blocks of all sorts, a column that all rows keep."""
+    kept = _kept(n, block, 0.4, seed=n + H)
+    kept[:, -1] = True
+    x = _inputs(H, n, seed=H)
+    got = _pass(*x, _mask(kept, n, block))
+    for h in {0, H // 2, H - 1}:
+        _check({k: t[h: h + 1] for k, t in got.items()}, *(t[h: h + 1] for t in x),
+               OT.kept_tokens(kept, block, n))

@@ -303,3 +303,22 @@ def test_bounds_see_a_missing_key(n):
         assert (off > want["bound"][name]).any(), name
         if name != "lse":
             assert off.norm() > 2 * OT.NORM * want[name].norm(), name
+
+
+@pytest.mark.parametrize("n", [1, 64, 100, 128, 200, 256, 400, 1000])
+@pytest.mark.parametrize("block", [0, 64, 128])
+def test_workspaces_of_many_short_heads(block, n):
+    """Parts are reserved only where an item can be split, and then for as many as the launch's
+    workgroup slots call for: beyond the rows' statistics, bitmaps and lists a few hundred
+    megabytes at any number of heads, and next to nothing for heads of one tile."""
+    need = ctypes.c_int64()
+    for heads in (1, 64, 200, 256, 300, 512, 513, 640, 1000, 4096, 65536, 2 ** 20):
+        if heads * n >= 2 ** 29:
+            continue
+        mask = ref(_mask(n=n, block=block)) if block else None
+        assert L.lib().lvsa_attention_backward_workspace(ref(_tensor(heads=heads, n=n)), mask,
+                                                         ref(need)) == L.OK
+        parts = need.value - 8 * heads * n
+        assert parts <= (256 << 20), (heads, parts)
+        if n <= 128:
+            assert parts <= 64 * 1024, (heads, parts)
