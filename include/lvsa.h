@@ -622,8 +622,9 @@ lvsa_status lvsa_attention_lse(const lvsa_tensor* q, const lvsa_tensor* k,
  * lvsa_attention_backward_workspace gives for the same q and mask; any content; written
  * by the call, so calls that may overlap in time need one each.
  * No atomics on floats: the result is the same every time for given shapes, mask and
- * device.  Shape limits are lvsa_attention's, and heads * n_tokens < 2^29.  delta, the row
- * sums of grad_out out, takes out as it was rounded: a query whose weight lies on a few
+ * device.  Shape limits are lvsa_attention's, heads * n_tokens < 2^29, and fewer than 2^24
+ * items (128 queries or 128 keys of a head, and parts of such): 2^23 heads of up to 128
+ * tokens are refused.  delta, the row sums of grad_out out, takes out as it was rounded: a query whose weight lies on a few
  * keys, where e is what is left of a difference, has up to 2^-8 of that difference in e.
  * Errors: EINVAL (nulls, shape mismatch, overlapping, workspace too small), EUNSUPPORTED
  * (head_dim, block, alignment, strides, sizes), EDEVICE (launch). */

@@ -27,7 +27,8 @@ lvsa_status check_read(const lvsa_tensor* t, int32_t heads, int32_t n) {
              : LVSA_OK;
 }
 
-// Rows past which a launch of the gradients could pass 2^32 work-items.
+// The rows' statistics take four work-items a row: below 2^31 in a launch.  (The items' launch
+// has its own bound, attention_backward_workspace.)
 bool too_long(int32_t heads, int32_t n) { return (int64_t)heads * n >= (int64_t)1 << 29; }
 
 // The step's parameters and the rows of each frame; n rows.
@@ -107,7 +108,9 @@ lvsa_status lvsa_attention_backward_workspace(const lvsa_tensor* q, const lvsa_b
     if (sparse && nb > kMaxSparseBlocks) return LVSA_EUNSUPPORTED;
     if (!sparse) nb = (int32_t)(((int64_t)q->n_tokens + 127) / 128);
   }
-  *bytes = attention_backward_workspace(q->heads, q->n_tokens, nb, sparse);
+  const int64_t need = attention_backward_workspace(q->heads, q->n_tokens, nb, sparse);
+  if (need < 0) return LVSA_EUNSUPPORTED;
+  *bytes = need;
   return LVSA_OK;
 }
 
@@ -143,6 +146,7 @@ lvsa_status lvsa_attention_backward(const lvsa_tensor* grad_out, const lvsa_tens
     a.f.n_blocks = (int32_t)(((int64_t)n + 127) / 128);
   }
   const int64_t need = attention_backward_workspace(H, n, a.f.n_blocks, a.f.row_ptr != nullptr);
+  if (need < 0) return LVSA_EUNSUPPORTED;
   if (!workspace || workspace_bytes < need) return LVSA_EINVAL;
   if (!aligned(workspace, 16)) return LVSA_EUNSUPPORTED;
   a.f.lse = const_cast<float*>(lse);

@@ -804,7 +804,9 @@ hipError_t launch_t(const BArgs& b, const Layout& l, hipStream_t stream) {
 
 int64_t attention_backward_workspace(int32_t heads, int32_t n_tokens, int32_t n_blocks,
                                      bool sparse) {
-  return layout_of(heads, n_tokens, n_blocks, sparse).bytes;
+  const Layout l = layout_of(heads, n_tokens, n_blocks, sparse);
+  // A launch holds less than 2^32 work-items (and there are no more split items than items).
+  return l.max_items * heads >= ((int64_t)1 << 32) / (64 * WAVES) ? -1 : l.bytes;
 }
 
 hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream) {

@@ -93,6 +93,7 @@ struct AttnBackArgs {
   int64_t go_sh, go_st, gq_sh, gq_st, gk_sh, gk_st, gv_sh, gv_st;
   char* workspace;
 };
+// Bytes of its workspace; -1: more work-items than a launch holds.
 int64_t attention_backward_workspace(int32_t heads, int32_t n_tokens, int32_t n_blocks,
                                      bool sparse);
 hipError_t launch_attention_backward(const AttnBackArgs& a, hipStream_t stream);

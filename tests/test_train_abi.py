@@ -322,3 +322,19 @@ def test_workspaces_of_many_short_heads(block, n):
         assert parts <= (256 << 20), (heads, parts)
         if n <= 128:
             assert parts <= 64 * 1024, (heads, parts)
+
+
+@pytest.mark.parametrize("mask", [None, _mask(n=1, block=64), _mask(n=1, block=128),
+                                  _mask(n=1, block=64, rows=None, cols=None)])
+def test_more_heads_than_a_launch_holds(mask):
+    """Two items a head of few tokens, a workgroup of 256 each: 2^23 heads would pass 2^32
+    work-items, which both entry points refuse before any launch."""
+    lib, need = L.lib(), ctypes.c_int64()
+    m = mask and ref(mask)
+    size = lib.lvsa_attention_backward_workspace
+    assert size(ref(_tensor(heads=2 ** 23 - 1, n=1)), m, ref(need)) == L.OK
+    for heads in (2 ** 23, 2 ** 24 - 1, 2 ** 29 - 1):
+        assert size(ref(_tensor(heads=heads, n=1)), m, ref(need)) == L.EUNSUPPORTED, heads
+    t = [_tensor(heads=2 ** 23, n=1, data=(i + 1) * PTR) for i in range(8)]
+    assert lib.lvsa_attention_backward(*map(ref, t[:5]), 20 * PTR, m, *map(ref, t[5:]), 30 * PTR,
+                                       1 << 60, None) == L.EUNSUPPORTED
