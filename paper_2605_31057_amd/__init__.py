@@ -435,10 +435,21 @@ def _tensor(t):
                    t.stride(0), t.stride(1))
 
 
+def _no_tangents(*tensors):
+    """Refuses tensors that carry a tangent of forward-mode differentiation: what the
+    library gives would carry none, which reads as zero."""
+    from torch.autograd import forward_ad
+    if forward_ad._current_level >= 0:      # within dual_level
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise NotImplementedError("no forward-mode derivative")
+
+
 def attention(q, k, v, mask, out=None, stream=None):
     """Block-sparse attention (lvsa_attention); returns out.  Differentiable in q, k and
     v (``attention_backward``); the mask has to stay as it is until the backward pass."""
     import torch
+    _no_tangents(q, k, v, out)
     if _recording(q, k, v, out):
         return _attend(q, k, v, mask, out, stream)
     given = out is not None
@@ -485,6 +496,7 @@ def dense_attention(q, k, v, block=128, out=None, stream=None):
     """Dense attention of the same kernel design (lvsa_dense_attention); differentiable
     in q, k and v."""
     import torch
+    _no_tangents(q, k, v, out)
     if _recording(q, k, v, out):
         return _attend(q, k, v, _every_key(q, block), out, stream)
     given = out is not None
@@ -514,7 +526,7 @@ class _Fast:
     def __init__(self):
         import torch
         L = lib()
-        self.torch = torch
+        self.torch, self.forward_ad = torch, torch.autograd.forward_ad
         self.codes = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
         self.bf16 = torch.bfloat16
         self.empty, self.empty_like = torch.empty, torch.empty_like
@@ -674,6 +686,8 @@ def _launch_turn(x, r, start, out, back):
 
 def _rotate(x, r, start, out, back):
     f = _fast()
+    if f.forward_ad._current_level >= 0:
+        _no_tangents(x, out)
     if (x.requires_grad or (out is not None and out.requires_grad)) and f.grad_enabled():
         return f.turn.apply(x, out, r, start, back)
     if out is None:
@@ -1107,6 +1121,8 @@ def residual_norm(plan, x, y=None, gate=None, scale=None, shift=None, weight=Non
     f = _fast()
     params = gate, scale, shift, weight, bias, post_weight
     given = [] if r is None and h is None else [t for t in (r, h) if t is not None]
+    if f.forward_ad._current_level >= 0:
+        _no_tangents(x, y, *params, *given)
     if f.grad_enabled():
         for t in (x, y, *params, *given):
             if t is not None and t.requires_grad:

@@ -78,3 +78,51 @@ def test_outputs_made_without_versions(no_library, name):
         WRITERS[name](out)
     with torch.no_grad():
         WRITERS[name](out)
+
+
+def _differentiable():
+    """Each differentiable call with its tensors, by name."""
+    x, p = torch.zeros(4, 128), torch.zeros(1, 128)
+    plan = L.ResidualNorm(128)
+    (q, k, v), mask = _qkv(), _masks()[0]
+    return {
+        "attention": (lambda **t: L.attention(mask=mask, **t), dict(q=q, k=k, v=v, out=q.clone())),
+        "dense_attention": (L.dense_attention, dict(q=q, k=k, v=v, out=q.clone())),
+        "residual_norm": (lambda **t: L.residual_norm(plan, **t),
+                          dict(x=x, y=x.clone(), gate=p, scale=p.clone(), shift=p.clone(),
+                               weight=p[0].clone(), bias=p[0].clone())),
+        "rope": (lambda **t: L.rope(r=None, **t), dict(x=q)),
+        "rope_backward": (lambda **t: L.rope_backward(r=None, **t), dict(grad=q)),
+    }
+
+
+@pytest.mark.parametrize("call", _differentiable())
+@pytest.mark.parametrize("recorded", [False, True])
+def test_forward_mode_is_refused(call, recorded):
+    """A tangent would be dropped without a word: no call has a forward-mode derivative."""
+    fn, tensors = _differentiable()[call]
+    if recorded:
+        first = next(iter(tensors))
+        tensors[first] = tensors[first].clone().requires_grad_()
+    for name in tensors:
+        with torch.autograd.forward_ad.dual_level():
+            t = tensors[name]
+            dual = torch.autograd.forward_ad.make_dual(t, torch.ones_like(t))
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                fn(**dict(tensors, **{name: dual}))
+
+
+@pytest.mark.parametrize("call", ["attention", "dense_attention", "rope", "residual_norm"])
+def test_forward_mode_of_a_function_is_refused(call):
+    fn, tensors = _differentiable()[call]
+    first = next(iter(tensors))
+    rest = {k: t for k, t in tensors.items() if k != first}
+    x = tensors[first]
+    with pytest.raises(NotImplementedError, match="forward-mode"):
+        torch.func.jvp(lambda t: fn(**{first: t}, **rest), (x,), (torch.ones_like(x),))
+
+
+def test_tensors_without_tangents_are_taken_at_a_dual_level(no_library):
+    with torch.autograd.forward_ad.dual_level(), torch.no_grad():
+        L.attention(*_qkv(), _masks()[0])
+        L.dense_attention(*_qkv())
