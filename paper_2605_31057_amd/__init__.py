@@ -877,7 +877,9 @@ def _attention_function(torch):
             out, lse = _launch_lse(q, k, v, mask, out, None)
             ctx.mask = mask
             # the mask's tensors too: a write to them before the backward pass is noticed
-            ctx.save_for_backward(q, k, v, out, lse, *getattr(mask, "_keep", ()))
+            # (those of inference mode cannot be saved, nor their writes noticed)
+            ctx.save_for_backward(q, k, v, out, lse, *(t for t in getattr(mask, "_keep", ())
+                                                       if not t.is_inference()))
             return out
 
         @staticmethod

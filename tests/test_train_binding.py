@@ -126,3 +126,26 @@ def test_tensors_without_tangents_are_taken_at_a_dual_level(no_library):
     with torch.autograd.forward_ad.dual_level(), torch.no_grad():
         L.attention(*_qkv(), _masks()[0])
         L.dense_attention(*_qkv())
+
+
+@pytest.fixture
+def no_kernels(monkeypatch):
+    """Attention's graph without its kernels: an output of ones, gradients of ones."""
+    def forward(q, k, v, mask, out, lse):
+        out = torch.empty_like(q) if out is None else out
+        with torch.no_grad():
+            out.fill_(1.0)
+        return out, torch.zeros(q.shape[:2])
+
+    monkeypatch.setattr(L, "_launch_lse", forward)
+    monkeypatch.setattr(L, "_launch_back",
+                        lambda grad, q, k, v, *rest: tuple(torch.ones_like(t) for t in (q, k, v)))
+
+
+def test_masks_of_inference_mode(no_kernels):
+    """A mask's tensors that were made in inference mode, which a graph cannot save."""
+    with torch.inference_mode():
+        mask = _masks()[0]
+    q, k, v = (t.requires_grad_() for t in _qkv())
+    L.attention(q, k, v, mask).sum().backward()
+    assert q.grad is not None
