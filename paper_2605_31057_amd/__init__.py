@@ -894,6 +894,11 @@ def _attention_function(torch):
 def _attend(q, k, v, mask, out, stream):
     if stream is not None:
         return _with_stream(_attend, stream, q, k, v, mask, out, None)
+    # Everything in out is overwritten: without the graph that gave it, or a loop over one
+    # tensor would keep what every call has saved.  (Of a view autograd keeps it.)
+    if (out is not None and out.grad_fn is not None and out._base is None
+            and not any(out is t for t in (q, k, v))):
+        out.detach_()
     return _fast().attention_graph.apply(q, k, v, out, mask)
 
 

@@ -149,3 +149,23 @@ def test_masks_of_inference_mode(no_kernels):
     q, k, v = (t.requires_grad_() for t in _qkv())
     L.attention(q, k, v, mask).sum().backward()
     assert q.grad is not None
+
+
+def test_an_output_used_again_lets_go_of_what_was_saved(no_kernels):
+    """Calls into one tensor, one after the other: each overwrites what the one before gave, so
+    the graph holds the last one's inputs alone, and its gradients are the last one's."""
+    import gc
+    import weakref
+    w = torch.ones(1, 128, 128, dtype=BF, requires_grad=True)
+    k, v = _qkv()[1:]
+    buf, seen = torch.empty(1, 128, 128, dtype=BF), []
+    for call in (lambda q: L.dense_attention(q, k, v, out=buf),
+                 lambda q: L.attention(q, k, v, _masks()[0], out=buf)) * 3:
+        q = w * 2
+        seen.append(weakref.ref(q))
+        assert call(q) is buf
+        del q
+        gc.collect()
+    assert [s() is None for s in seen] == [True] * 5 + [False]
+    buf.sum().backward()
+    assert (w.grad == 2).all()
