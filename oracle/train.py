@@ -89,3 +89,128 @@ def after(r, kind, eps, of, scale=None, shift=None, weight=None, bias=None):
     h = h if weight is None else h * weight
     h = h if bias is None else h + bias
     return h if scale is None else h * (1 + scale[of]) + shift[of]
+
+
+# -------------------------------------- the residual step's gradients in whole numbers
+#
+# Rows of eight-column groups, each a whole number times one of the rows h_i of an 8 x 8
+# Hadamard matrix (h_i h_j = h_(i xor j), of sum 0 for i != j), so that with eps 0 every
+# quantity on the way is a whole number and fp32 holds it and every sum exactly:
+#   r = +-h_1 and, under a norm, y = +-h_2 are their own normalised rows;
+#   grad_h = t h_3, grad_r = u h_4, parameters constant over a group: the means over a row of
+#   grad_h M, of its product with r, of e G and of its product with y are 0.
+# t and u have no zeros: every row counts in every sum.
+
+def _hadamard(i):
+    return torch.tensor([(-1.0) ** bin(i & j).count("1") for j in range(8)], dtype=torch.double)
+
+
+def whole_step(n, dim, frame, post, names, with_y=True, seed=0):
+    """(tensors by name, grad_r, grad_h) in float64."""
+    g = torch.Generator().manual_seed(seed)
+
+    def rows(count, *values):
+        at = torch.randint(len(values), (count, dim // 8, 1), generator=g)
+        return torch.tensor(values, dtype=torch.double)[at]
+
+    def along(x, i=0):
+        return (x * _hadamard(i)).reshape(x.shape[0], dim)
+
+    t = {"x": along(rows(n, -1, 1), 1)}
+    if with_y:
+        t["y"] = along(rows(n, -1, 1) if post != "none" else rows(n, -2, -1, 1, 2), 2)
+    frames = -(-n // (frame or n))
+    for name in names:
+        if name in ("gate", "scale", "shift"):
+            t[name] = along(rows(frames, -1, 1, 2) - float(name == "scale"))
+        else:
+            t[name] = along(rows(1, -1, 1, 2))[0]
+    return t, along(rows(n, -2, -1, 1, 2), 4), along(rows(n, -2, -1, 1, 2), 3)
+
+
+def whole_gradients(t, gr, gh, kind, a, frame):
+    """Every gradient of that step by name, in float64, at r = t["x"]."""
+    n, dim = t["x"].shape
+    of = torch.arange(n, device=gr.device) // (frame or n)
+    frames = int(of[-1]) + 1
+
+    def param(name, none):
+        p = t.get(name)
+        return none if p is None else p[of] if name in ("gate", "scale", "shift") else p
+
+    def add(x):       # a frame's rows
+        return torch.zeros(frames, dim, dtype=torch.double, device=x.device).index_add_(0, of, x)
+
+    e, found = gr, {}
+    if kind != "none":
+        wide = 1 + param("scale", 0.0)
+        e = gr + gh * param("weight", 1.0) * wide
+        found["shift"] = add(gh)
+        found["scale"] = add(gh * (t["x"] * param("weight", 1.0) + param("bias", 0.0)))
+        found["weight"] = (gh * t["x"] * wide).sum(0)
+        found["bias"] = (gh * wide).sum(0)
+    found["x"] = a * e
+    if "y" in t:
+        found["gate"] = add(e * t["y"] * param("post_weight", 1.0))
+        found["post_weight"] = (e * t["y"] * param("gate", 1.0)).sum(0)
+        found["y"] = e * param("gate", 1.0) * param("post_weight", 1.0)
+    return {k: x for k, x in found.items() if k in t}
+
+
+# The 2-norm of what a row of r, h, dx or dy is off by in fp32, relative to its own, for rows
+# whose mean is below their deviations and terms that do not cancel, u = 2^-24.  A sum over a
+# row has at most 16 additions in a thread, 6 over a wave, 4 over waves: 26 u of the sizes added.
+# A mean is then off by 28 u of them, a factor by half of (26 + 3) u + 2 (28 + 1) u and 3 u,
+# 47 u, a normalised element by 28 u + 1 u and 47 u of itself: 76 u, with the parameters 80 u, of
+# sizes that together are no larger than twice the result; h behind a norm of y has both norms',
+# a gradient through a norm two more such means beside it, of terms that are off by those 80 u,
+# and dy twice that.
+ROW_NORM = {"r": 160 * 2.0 ** -24, "h": 240 * 2.0 ** -24, "x": 480 * 2.0 ** -24, "y": 960 * 2.0 ** -24}
+
+
+def row_case(dim, post, n=60, seed=0):
+    """Tensors by name, grad_r and grad_h, in float32, frames of 25 rows."""
+    g = torch.Generator().manual_seed(seed + dim)
+
+    def normal(rows, size, mean=0.0):
+        return torch.randn(rows, dim, generator=g) * size + mean
+
+    t = {"x": normal(n, 1.5, 0.3), "y": normal(n, 0.7, 0.2), "gate": normal(3, 0.1, 0.5),
+         "scale": normal(3, 0.1), "shift": normal(3, 0.4), "weight": normal(1, 0.1, 1.0)[0]}
+    if post != "none":
+        t["post_weight"] = normal(1, 0.1, 1.0)[0]
+    return t, normal(n, 0.5, 0.2), normal(n, 0.5, 0.2)
+
+
+def row_results(t, gr, gh, kind, post, eps, frame, left=None):
+    """r and h of the step, dx and dy at t["x"] in r's place, in float64; `left`: a column that
+    the rows' means leave out."""
+    dim = t["x"].shape[-1]
+    of = torch.arange(t["x"].shape[0], device=gr.device) // frame
+    keep = torch.ones(dim, dtype=torch.double, device=gr.device)
+    if left is not None:
+        keep[left] = 0.0
+
+    def mean(x):
+        return (x * keep).sum(-1, keepdim=True) / dim
+
+    def norm(x, kind):
+        if kind == "none":
+            return x, 1.0
+        x = x - mean(x) if kind == "layer" else x
+        f = 1 / torch.sqrt(mean(x * x) + eps)
+        return x * f, f
+
+    def back(g, u, f, kind):
+        if kind == "none":
+            return g
+        return f * (g - (mean(g) if kind == "layer" else 0.0) - u * mean(g * u))
+
+    v, fv = norm(t["y"], post)
+    scale = t["gate"][of] * t.get("post_weight", 1.0)
+    r = t["x"] + scale * v
+    m = t["weight"] * (1 + t["scale"][of])
+    u, f = norm(t["x"], kind)
+    e = gr + back(gh * m, u, f, kind)
+    return {"r": r, "h": norm(r, kind)[0] * m + t["shift"][of], "x": e,
+            "y": back(e * scale, v, fv, post)}

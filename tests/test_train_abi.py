@@ -8,6 +8,7 @@ import torch
 
 import paper_2605_31057_amd as L
 from oracle import train as OT
+from tests import whole_cases as WHOLE
 
 ref = ctypes.byref
 PTR = 0x100000
@@ -338,3 +339,83 @@ def test_more_heads_than_a_launch_holds(mask):
     t = [_tensor(heads=2 ** 23, n=1, data=(i + 1) * PTR) for i in range(8)]
     assert lib.lvsa_attention_backward(*map(ref, t[:5]), 20 * PTR, m, *map(ref, t[5:]), 30 * PTR,
                                        1 << 60, None) == L.EUNSUPPORTED
+
+
+# --------------------------------------- the residual step in whole numbers
+
+@pytest.mark.parametrize("kind", ["none", "layer", "rms"])
+@pytest.mark.parametrize("post", ["none", "layer", "rms"])
+@pytest.mark.parametrize("n,dim,frame", [(1, 8, 0), (7, 24, 3), (12, 16, 1), (9, 40, 0)])
+def test_whole_numbers_are_the_formulas(n, dim, frame, kind, post):
+    """whole_gradients against automatic differentiation of the step, eps 0."""
+    names = [k for k in WHOLE.ALL if (kind != "none" or k in ("gate", "post_weight")) and
+             (post != "none" or k != "post_weight")]
+    for with_y in (True, False) if kind != "none" and post == "none" else (True,):
+        use = [k for k in names if with_y or k not in ("gate", "post_weight")]
+        t, gr, gh = OT.whole_step(n, dim, frame, post, use, with_y, seed=n)
+        got = OT.whole_gradients(t, gr, gh, kind, 0.5, frame)
+        w = {k: x.clone().requires_grad_() for k, x in t.items()}
+        of = torch.arange(n) // (frame or n)
+        e = gr
+        if kind != "none":
+            h = OT.after(w["x"], kind, 0.0, of, *(w.get(k) for k in ("scale", "shift", "weight", "bias")))
+            later = [k for k in ("x", "scale", "shift", "weight", "bias") if k in w]
+            want = dict(zip(later, torch.autograd.grad(h, [w[k] for k in later], gh)))
+            e = gr + want["x"]
+        else:
+            want = {}
+        want["x"] = 0.5 * e
+        if with_y:
+            u = OT.unit(w["y"], post, 0.0) * w.get("post_weight", 1.0)
+            u = u * w["gate"][of] if "gate" in w else u
+            before = [k for k in ("y", "gate", "post_weight") if k in w]
+            want.update(zip(before, torch.autograd.grad(u, [w[k] for k in before], e)))
+        assert set(got) == set(want) == set(t)
+        for k in got:
+            assert (got[k] - want[k]).abs().max() <= 1e-9, k
+            assert (got[k] * 2 == (got[k] * 2).round()).all() and got[k].abs().max() < 2 ** 20, k
+
+
+@pytest.mark.parametrize("n,dim,frame", [s for s in WHOLE.SHAPES if s[0] * s[1] <= 2 ** 21])
+@pytest.mark.parametrize("names", WHOLE.NAMES)
+def test_whole_numbers_see_a_missing_row(n, dim, frame, names):
+    """A row left out, or a stretch of them, changes every gradient, whole numbers that fp32
+    holds: no bound hides it."""
+    post = "rms" if "post_weight" in names else "none"
+    t, gr, gh = OT.whole_step(n, dim, frame, post, names, seed=n)
+    want = OT.whole_gradients(t, gr, gh, "layer", 1.0, frame)
+    for first, more in ((0, 0), (n // 2, 0), (n - 1, 0), (n // 3, n // 32)):
+        left = slice(first, first + more + 1)
+        less = [x.clone() for x in (gr, gh)]
+        for x in less:
+            x[left] = 0.0
+        other = OT.whole_gradients(t, *less, "layer", 1.0, frame)
+        for k in want:
+            assert (other[k] - want[k]).abs().max() >= 1, (k, left)
+
+
+@pytest.mark.parametrize("dim", WHOLE.WIDTHS)
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("post", ["none", "layer", "rms"])
+def test_the_bound_of_a_row_sees_a_missing_column(dim, kind, post):
+    """A column that is left out of a row's means, of any row where its values are not near
+    zero, passes the bound on the row; and the plain results are the formula's."""
+    t, gr, gh = OT.row_case(dim, post)
+    t, gr, gh = {k: x.double() for k, x in t.items()}, gr.double(), gh.double()
+    want = OT.row_results(t, gr, gh, kind, post, 1e-5, 25)
+    plain = OT.residual_norm(t["x"], t["y"], kind, post, 1e-5, 1.0, 25,
+                             **{k: x for k, x in t.items() if k not in ("x", "y")})
+    w = {k: t[k].clone().requires_grad_() for k in ("x", "y")}
+    of = torch.arange(60) // 25
+    h = OT.after(w["x"], kind, 1e-5, of, t["scale"], t["shift"], t["weight"])
+    e = gr + torch.autograd.grad(h, w["x"], gh)[0]
+    u = OT.unit(w["y"], post, 1e-5) * t.get("post_weight", 1.0) * t["gate"][of]
+    for k, x in zip(("r", "h", "x", "y"), (*plain, e, torch.autograd.grad(u, w["y"], e)[0])):
+        assert (want[k] - x).abs().max() <= 1e-10, k
+    for left in (0, dim // 2 + 1, dim - 1):
+        other = OT.row_results(t, gr, gh, kind, post, 1e-5, 25, left)
+        for k in want:
+            if k == "r" and post == "none":
+                continue
+            off = (other[k] - want[k]).norm(dim=-1) / want[k].norm(dim=-1)
+            assert off.max() > OT.ROW_NORM[k], (k, left, float(off.max()))
