@@ -706,3 +706,37 @@ def test_heads_of_few_tokens_under_a_mask(H, n, block):
     for h in {0, H // 2, H - 1}:
         _check({k: t[h: h + 1] for k, t in got.items()}, *(t[h: h + 1] for t in x),
                OT.kept_tokens(kept, block, n))
+
+
+@pytest.mark.parametrize("block", [0, 64, 128])
+def test_against_differences_of_the_librarys_output(block):
+    """sum(out * grad) of the library's own forward pass, half a step of h to both sides of the
+    inputs along the signs of the gradients, against the gradients: inputs are multiples of h
+    below 4, so bf16 holds both ends.  What the difference has beyond the slope, h not being
+    small, is the formula's in 64 bits at the same ends."""
+    H, n, h = 2, 200, 2.0 ** -3
+    kept = _kept(n, block, 0.6, seed=4) | np.eye(-(-n // block), dtype=bool) if block else None
+    mask = _mask(kept, n, block) if block else None
+    pairs = (OT.kept_tokens(kept, block, n) if block else torch.ones(n, n, dtype=torch.bool)).cuda()
+    x = _inputs(H, n, seed=21)
+    x[:3] = [((t.float() / h).round() * h).clamp(-3.5, 3.5).to(BF) for t in x[:3]]
+    got = _pass(*x, mask)
+    names = ("dq", "dk", "dv")
+    step = [torch.where(got[k] > 0, 0.5, -0.5).float() * h for k in names]
+    ends = [[(t.float() + way * s) for t, s in zip(x, step)] for way in (1, -1)]
+    held = [[t.to(BF) for t in end] for end in ends]
+    assert all(torch.equal(a.float(), b) for e, f in zip(held, ends) for a, b in zip(e, f))
+    grad = x[3].double()
+    values, plain, room = [], [], 0.0
+    for end in held:
+        out = L.attention(*end, mask) if block else L.dense_attention(*end)
+        want = OT.attention(*(t.double() for t in end), grad, pairs)["out"]
+        values.append(float((out.double() * grad).sum()))
+        plain.append(float((want * grad).sum()))
+        room += OT.NORM * float(want.norm() * grad.norm())
+    want = OT.attention(*(t.double() for t in x), pairs)
+    along = sum(float((want[k] * s.double()).sum()) for k, s in zip(names, step)) * 2
+    mine = sum(float((got[k].double() * s.double()).sum()) for k, s in zip(names, step)) * 2
+    room += sum(OT.NORM * float(want[k].norm() * s.double().norm()) for k, s in zip(names, step)) * 2
+    off = values[0] - values[1] - (plain[0] - plain[1] - along) - mine
+    assert abs(off) <= room and room <= 0.2 * mine, (off, room, mine)
