@@ -466,7 +466,8 @@ def attention(q, k, v, mask, out=None, stream=None):
 
 def attention_noalloc(q, k, v, mask, out, stream=None):
     """lvsa_attention_noalloc: block-sparse attention that allocates nothing
-    (the caller passes `out`); calls overlapping on one device race."""
+    (the caller passes `out`); calls overlapping on one device race.  It has no
+    gradient."""
     tq, tk, tv, to = (_tensor(x) for x in (q, k, v, out))
     _check(lib().lvsa_attention_noalloc(ctypes.byref(tq), ctypes.byref(tk),
                                         ctypes.byref(tv), ctypes.byref(mask),
@@ -477,7 +478,8 @@ def attention_noalloc(q, k, v, mask, out, stream=None):
 
 
 def attention_exact(q, k, v, mask, out=None, stream=None):
-    """Token-exact attention (lvsa_attention_exact): Eq. 2 token for token."""
+    """Token-exact attention (lvsa_attention_exact): Eq. 2 token for token.  It has no
+    gradient: what it returns is no part of a graph."""
     import torch
     given = out is not None
     if not given:

@@ -132,7 +132,8 @@ hipError_t launch_norm_forward(const NormArgs& a, int32_t stream_type, int32_t b
 // what is worked at one time lies together in memory: 32,760 rows of 1,536 columns 79 us, with
 // 8 rows 84, 12 rows 87, all rows shared out evenly to what fits at once 86, and dealt out to
 // it in turn 94.  Back, where a team leaves a row of three sums, there are as many as fit at
-// once: 12 waves on each of 256 compute units (these rows 140 us; 24 waves 145; in turn 146).
+// once: 12 waves on each of 256 compute units, on any device, as the sums' order follows from
+// it (these rows 140 us; 24 waves 145; in turn 146).
 constexpr int64_t ROWS_FORWARD = 4;
 void norm_units(NormArgs& a, bool backward) {
   const NormTeam t = norm_team(a.dim);
