@@ -451,6 +451,9 @@ def attention(q, k, v, mask, out=None, stream=None):
     import torch
     _no_tangents(q, k, v, out)
     if _recording(q, k, v, out):
+        _byref(mask)       # refused as without a graph: no mask, a mask without rows
+        if not mask.row_ptr or not mask.col_idx:
+            raise LvsaError(EINVAL, "lvsa_attention")
         return _attend(q, k, v, mask, out, stream)
     given = out is not None
     if not given:

@@ -10,11 +10,12 @@ BF = torch.bfloat16
 
 class _Calls:
     def __getattr__(self, name):
-        return lambda *args: L.OK
+        return lambda *args: b"" if name == "lvsa_status_str" else L.OK
 
 
 @pytest.fixture
 def no_library(monkeypatch):
+    L._fast()          # what the calls keep of the library is of the real one
     monkeypatch.setattr(L, "lib", _Calls)
     monkeypatch.setattr(L, "_stream_ptr", lambda stream: None)
     monkeypatch.setattr(L, "_tensor", lambda t: L._Tensor(t.data_ptr(), *t.shape, *t.stride()[:2]))
@@ -169,3 +170,18 @@ def test_an_output_used_again_lets_go_of_what_was_saved(no_kernels):
     assert [s() is None for s in seen] == [True] * 5 + [False]
     buf.sum().backward()
     assert (w.grad == 2).all()
+
+
+@pytest.mark.parametrize("recorded", [False, True])
+def test_attention_takes_a_mask_with_rows_alone(no_kernels, no_library, recorded):
+    """No mask, or one without rows, is refused with gradients as without: every key is
+    dense_attention's (and attention_lse's) to take."""
+    q, k, v = (t.requires_grad_(recorded) for t in _qkv())
+    with pytest.raises(TypeError):
+        L.attention(q, k, v, None)
+    if recorded:       # without a graph the library itself refuses
+        for rows, cols in ((None, None), (None, 4096), (4096, None)):
+            with pytest.raises(L.LvsaError) as e:
+                L.attention(q, k, v, L.BlockMask(128, 128, 1, 1, rows, cols))
+            assert e.value.status == L.EINVAL
+    assert L.dense_attention(q, k, v).requires_grad == recorded
